@@ -292,6 +292,125 @@ int foe_group_attention(foe_dtype dt, int H, int S, int d, int nq, int hd, float
 size_t foe_group_attention_workspace_bytes(int H, int S, int d, int nq, int hd);
 
 /*
+ * The 8-bit key/value cache: what a layer's attention keeps between calls, for
+ * prompts in chunks and for decode steps (Section 3.1: each of the H groups has
+ * one key/value head, shared by its nq query heads).
+ *
+ * A cache is a pool of n_pages pages of FOE_CACHE_PAGE tokens, for all groups:
+ *   k_cache   [n_pages, H, 64, hd]     e4m3 codes (OCP fp8), a row per token; the keys
+ *                                      are held after their rotation
+ *   v_cache   [n_pages, H, 4, hd, 16]  e4m3 codes: per 16 tokens, each dim's 16 tokens
+ *                                      side by side
+ *   kv_scale  [n_pages, H, 2]          fp32, the page's key and value scale of a group:
+ *                                      powers of two, at least 2^-100; value = code * scale
+ *   mass      [n_pages, H, 64]         fp32, the attention weight that each token has
+ *                                      received (for foe_cache_evict; optional elsewhere)
+ * The scale of a group's 64 tokens is the smallest power of two s >= 2^-100 with
+ * |x| <= 448 s for all of them.  A power of two costs a floating format no
+ * precision, keeps the products' operands exact in bf16, and a scale that has to
+ * grow rescales earlier codes without a second rounding (but among the 2^-9 s
+ * steps of the smallest magnitudes).
+ * The caller owns the pool and hands out pages:
+ *   block_table [B, max_blocks] int32  pages of each sequence, in token order; token t of
+ *                                      sequence b is in slot t % 64 of page
+ *                                      block_table[b, t / 64]
+ * A call's sequences b = 0 .. B-1 must not share a page that the call writes.
+ * Entries outside [0, n_pages) are absent pages: nothing is stored there and
+ * their tokens are not seen.  Lengths are cut to [0, 64 * max_blocks], row
+ * ranges to [0, N].
+ *
+ * bf16 activations and hd = 96 or 128 only (else FOE_ERR_UNSUPPORTED).  Limits:
+ * 1 <= H <= 64, 1 <= nq <= 64, B <= 65535, n_pages >= 1, 1 <= max_blocks <= 2^24.
+ */
+#define FOE_CACHE_PAGE 64
+
+/*
+ * foe_cache_append - rotates new tokens and stores their keys and values.
+ * The batch packs the new rows of all sequences: sequence b has rows
+ * row_start[b] .. row_start[b+1]-1 of N (possibly none), which become its tokens
+ * ctx_len[b], ctx_len[b] + 1, ...
+ *
+ *   qkv       [H, N, nq+2, hd] dt   per group and row: nq query heads, the key, the value
+ *   row_start [B+1]      int32      non-decreasing
+ *   ctx_len   [B]        int32      tokens that each sequence holds before the call
+ *   pos       [B]        int32      rotary position of a sequence's first new row, or NULL:
+ *                                   ctx_len[b] (after an eviction positions run ahead)
+ *   theta, scale                    rotary base and scaling as in foe_group_attention:
+ *                                   dims i and i + hd/2 turn by (p/scale)*theta^(-2i/hd)
+ *   q_out     [H, N, nq, hd] dt out the rotated queries (not qkv itself)
+ *   k_cache, v_cache, kv_scale      updated: keys and values are quantised from fp32, a
+ *                                   page that held tokens keeps a scale of at least its old
+ *                                   one (its codes rescaled when it grows); slots past the
+ *                                   new tokens are left as they were
+ * A token whose key or value holds a non-finite element is stored as a key of
+ * NaN codes and a zero value, and has no part in the scales: every query that
+ * sees it gives NaN, and no other does.  Rows past the table's end give q_out
+ * alone.  Needs no workspace.
+ */
+int foe_cache_append(foe_dtype dt, int H, int B, int N, int nq, int hd, int n_pages,
+                     int max_blocks, float theta, float scale, const void* qkv,
+                     const int32_t* row_start, const int32_t* ctx_len, const int32_t* pos,
+                     const int32_t* block_table, void* q_out, void* k_cache, void* v_cache,
+                     float* kv_scale, void* stream);
+
+/*
+ * foe_cache_attention - causal attention of the new rows over the cache, after
+ * foe_cache_append has stored them (same row_start and ctx_len):
+ *   o[r,h,j] = sum_t p_t v_t,  p = softmax over t <= ctx_len[b] + i of q.k_t/sqrt(hd)
+ * for row r = row_start[b] + i, group h and query head j.  A row that sees no
+ * token (all its pages absent) gives zeros.
+ *
+ *   max_rows               upper bound (>= 1) of the rows of one sequence; it picks the
+ *                          kernels (a decode step passes 1).  A sequence's rows past it are
+ *                          left out
+ *   q         [H, N, nq, hd] dt   rotated queries
+ *   mass_in   [n_pages, H, 64] fp32, mass_out [n_pages, H, 64] fp32 out, or both NULL:
+ *                          mass_out[t] = (t < ctx_len[b] ? mass_in[t] : 0) + the sum of p_t
+ *                          over the call's rows and heads, for the tokens t of the
+ *                          sequences that have rows (0 <= t < ctx_len[b] + rows); other
+ *                          entries are not written.  mass_out may be mass_in itself
+ *   out       [N, H, nq, hd] dt out   the layout of w_o's columns in foe_group_attention
+ *   ws, ws_bytes           workspace of foe_cache_attention_workspace_bytes()
+ * bf16: products in bf16 MFMA with fp32 accumulation; softmax statistics, mass and
+ * sums in fp32, the probabilities are rounded to bf16 for the product with v.
+ */
+int foe_cache_attention(foe_dtype dt, int H, int B, int N, int nq, int hd, int n_pages,
+                        int max_blocks, int max_rows, const void* q, const int32_t* row_start,
+                        const int32_t* ctx_len, const int32_t* block_table, const void* k_cache,
+                        const void* v_cache, const float* kv_scale, const float* mass_in,
+                        float* mass_out, void* out, void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace bytes of foe_cache_attention (with_mass: mass_out is given; SIZE_MAX
+ * for invalid sizes). */
+size_t foe_cache_attention_workspace_bytes(int H, int B, int N, int nq, int hd, int max_blocks,
+                                           int max_rows, int with_mass);
+
+/*
+ * foe_cache_evict - keeps the tokens that received the most attention.  Of a
+ * sequence longer than `keep`, each group keeps the last `recent` tokens and,
+ * of those before, the keep - recent of largest mass (equal masses: the
+ * earlier token; NaN counts as the largest).  Groups choose for themselves.
+ * The kept tokens, in their order, become tokens 0, 1, ... of the pages of
+ * dst_table; shorter sequences are moved whole.  Each page's scales follow
+ * from the values that it then holds, and mass moves with its token.
+ *
+ *   keep, recent           0 <= recent <= keep, keep >= 1
+ *   length    [B]          int32  tokens of each sequence
+ *   k_cache, v_cache, kv_scale, mass   the pool: read at block_table's pages, written at
+ *                          dst_table's, which must be other pages
+ *   dst_table [B, dst_blocks] int32    64 * dst_blocks >= keep; slots past the kept tokens
+ *                          are left as they were
+ *   kept      [B, H, keep] int32 out   the kept tokens' former numbers, ascending; -1 past
+ *                          a shorter sequence's end
+ *   new_len   [B]          int32 out   min(length, keep)
+ * Needs no workspace.
+ */
+int foe_cache_evict(int H, int B, int hd, int n_pages, int max_blocks, int keep, int recent,
+                    const int32_t* length, const int32_t* block_table, const int32_t* dst_table,
+                    int dst_blocks, void* k_cache, void* v_cache, float* kv_scale, float* mass,
+                    int32_t* kept, int32_t* new_len, void* stream);
+
+/*
  * foe_workspace_bytes - workspace size in bytes for `op` (host string:
  * "route", "permute", "expert_ffn", "combine", "reduce", "cluster_block").
  * Arguments an op does not use are ignored (pass 0); for "expert_ffn" T is the

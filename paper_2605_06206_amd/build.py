@@ -19,7 +19,8 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(PKG_DIR, "libfoe.so")
 
-SOURCES = ["foe_api.hip", "route.hip", "permute.hip", "ffn.hip", "combine.hip", "attention.hip"]
+SOURCES = ["foe_api.hip", "route.hip", "permute.hip", "ffn.hip", "combine.hip", "attention.hip",
+           "kv_cache.hip", "kv_attention.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

@@ -581,6 +581,170 @@ int foe_group_attention(foe_dtype dt, int H, int S, int d, int nq, int hd, float
   return FOE_OK;
 }
 
+}  // extern "C"
+
+namespace foe {
+namespace {
+// ---- the 8-bit key/value cache --------------------------------------------------
+void check_cache(Check& c, int H, int B, int n_pages, int max_blocks) {
+  c.need(H >= 1 && H <= 64, "H must be in [1, 64]");
+  c.need(B >= 0 && B <= 65535, "B must be in [0, 65535]");
+  c.need(n_pages >= 1, "n_pages must be >= 1");
+  c.need(max_blocks >= 1 && max_blocks <= (1 << 24), "max_blocks must be in [1, 2^24]");
+}
+void check_rows(Check& c, int N, int nq) {
+  c.need(nq >= 1 && nq <= 64, "nq must be in [1, 64]");
+  c.need(N >= 0 && (long long)N * (nq < 1 ? 1 : nq) <= (1 << 26), "N*nq must be in [0, 2^26]");
+}
+bool cache_hd(int hd) { return hd == 96 || hd == 128; }
+
+// No exception leaves a C entry point: the only ones its host code can raise are
+// failed allocations of a message or of a timing record.
+template <typename F>
+int entry(F body) {
+  try {
+    return body();
+  } catch (...) {
+    return FOE_ERR_HIP;
+  }
+}
+}  // namespace
+}  // namespace foe
+
+extern "C" {
+
+int foe_cache_append(foe_dtype dt, int H, int B, int N, int nq, int hd, int n_pages,
+                     int max_blocks, float theta, float scale, const void* qkv,
+                     const int32_t* row_start, const int32_t* ctx_len, const int32_t* pos,
+                     const int32_t* block_table, void* q_out, void* k_cache, void* v_cache,
+                     float* kv_scale, void* stream) {
+  return entry([&]() -> int {
+    Check c;
+    check_dtype(c, dt);
+    check_cache(c, H, B, n_pages, max_blocks);
+    check_rows(c, N, nq);
+    c.need(theta > 0.f && scale > 0.f, "theta and scale must be > 0");
+    const bool any = N > 0 && B > 0;
+    c.tensor(qkv, any, "qkv");
+    c.small(row_start, any, "row_start");
+    c.small(ctx_len, any, "ctx_len");
+    c.small(pos, false, "pos");
+    c.small(block_table, any, "block_table");
+    c.tensor(q_out, any, "q_out");
+    c.tensor(k_cache, any, "k_cache");
+    c.tensor(v_cache, any, "v_cache");
+    c.tensor(kv_scale, any, "kv_scale");
+    c.need(!any || qkv != q_out, "q_out must not be qkv");
+    if (!c.err.empty()) return fail(FOE_ERR_INVALID, "foe_cache_append: " + c.err);
+    if (dt != FOE_BF16 || !cache_hd(hd))
+      return fail(FOE_ERR_UNSUPPORTED, "foe_cache_append: bf16 with hd = 96 or 128 only");
+    if (!any) return FOE_OK;
+    const CacheArgs a{H, hd, B, n_pages, max_blocks, static_cast<uint8_t*>(k_cache),
+                      static_cast<uint8_t*>(v_cache), kv_scale, block_table, ctx_len};
+    hipError_t e = launch_cache_append(a, nq, N, qkv, q_out, row_start, pos, theta, scale,
+                                       reinterpret_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "foe_cache_append");
+    return FOE_OK;
+  });
+}
+
+size_t foe_cache_attention_workspace_bytes(int H, int B, int N, int nq, int hd, int max_blocks,
+                                           int max_rows, int with_mass) {
+  try {
+    Check c;
+    check_cache(c, H, B, 1, max_blocks);
+    check_rows(c, N, nq);
+    c.need(cache_hd(hd), "hd must be 96 or 128");
+    c.need(max_rows >= 1, "max_rows must be >= 1");
+    if (!c.err.empty()) return (g_err = c.err, SIZE_MAX);
+    if (N == 0 || B == 0) return 0;
+    if (max_rows > N) max_rows = N;
+    return cache_attention_scratch_bytes(H, B, N, nq, hd, max_blocks, max_rows, with_mass != 0);
+  } catch (...) {
+    return SIZE_MAX;
+  }
+}
+
+int foe_cache_attention(foe_dtype dt, int H, int B, int N, int nq, int hd, int n_pages,
+                        int max_blocks, int max_rows, const void* q, const int32_t* row_start,
+                        const int32_t* ctx_len, const int32_t* block_table, const void* k_cache,
+                        const void* v_cache, const float* kv_scale, const float* mass_in,
+                        float* mass_out, void* out, void* ws, size_t ws_bytes, void* stream) {
+  return entry([&]() -> int {
+    Check c;
+    check_dtype(c, dt);
+    check_cache(c, H, B, n_pages, max_blocks);
+    check_rows(c, N, nq);
+    const bool any = N > 0 && B > 0;
+    c.need(max_rows >= 1, "max_rows must be >= 1");
+    if (max_rows > N) max_rows = N;
+    c.tensor(q, any, "q");
+    c.small(row_start, any, "row_start");
+    c.small(ctx_len, any, "ctx_len");
+    c.small(block_table, any, "block_table");
+    c.tensor(k_cache, any, "k_cache");
+    c.tensor(v_cache, any, "v_cache");
+    c.tensor(kv_scale, any, "kv_scale");
+    c.tensor(mass_in, false, "mass_in");
+    c.tensor(mass_out, false, "mass_out");
+    c.need((mass_in == nullptr) == (mass_out == nullptr), "mass_in and mass_out go together");
+    c.tensor(out, any, "out");
+    if (!c.err.empty()) return fail(FOE_ERR_INVALID, "foe_cache_attention: " + c.err);
+    if (dt != FOE_BF16 || !cache_hd(hd))
+      return fail(FOE_ERR_UNSUPPORTED, "foe_cache_attention: bf16 with hd = 96 or 128 only");
+    if (!any) return FOE_OK;
+    const size_t need = cache_attention_scratch_bytes(H, B, N, nq, hd, max_blocks, max_rows,
+                                                      mass_out != nullptr);
+    if (need > 0 && (ws == nullptr || !aligned16(ws)))
+      return fail(FOE_ERR_INVALID, "foe_cache_attention: ws is NULL or not 16-byte aligned");
+    if (ws_bytes < need)
+      return fail(FOE_ERR_WORKSPACE, "foe_cache_attention: workspace needs " +
+                                         std::to_string(need) + " bytes, got " +
+                                         std::to_string(ws_bytes));
+    const CacheArgs a{H, hd, B, n_pages, max_blocks,
+                      static_cast<uint8_t*>(const_cast<void*>(k_cache)),
+                      static_cast<uint8_t*>(const_cast<void*>(v_cache)),
+                      const_cast<float*>(kv_scale), block_table, ctx_len};
+    hipError_t e = launch_cache_attention(a, nq, N, max_rows, q, row_start, mass_in, mass_out, out,
+                                          ws, reinterpret_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "foe_cache_attention");
+    return FOE_OK;
+  });
+}
+
+int foe_cache_evict(int H, int B, int hd, int n_pages, int max_blocks, int keep, int recent,
+                    const int32_t* length, const int32_t* block_table, const int32_t* dst_table,
+                    int dst_blocks, void* k_cache, void* v_cache, float* kv_scale, float* mass,
+                    int32_t* kept, int32_t* new_len, void* stream) {
+  return entry([&]() -> int {
+    Check c;
+    check_cache(c, H, B, n_pages, max_blocks);
+    c.need(keep >= 1 && keep <= (1 << 30), "keep must be in [1, 2^30]");
+    c.need(recent >= 0 && recent <= keep, "recent must be in [0, keep]");
+    c.need(dst_blocks >= 1 && (long long)dst_blocks * FOE_CACHE_PAGE >= keep,
+           "64 * dst_blocks must be at least keep");
+    const bool any = B > 0;
+    c.small(length, any, "length");
+    c.small(block_table, any, "block_table");
+    c.small(dst_table, any, "dst_table");
+    c.tensor(k_cache, any, "k_cache");
+    c.tensor(v_cache, any, "v_cache");
+    c.tensor(kv_scale, any, "kv_scale");
+    c.tensor(mass, any, "mass");
+    c.small(kept, any, "kept");
+    c.small(new_len, any, "new_len");
+    if (!c.err.empty()) return fail(FOE_ERR_INVALID, "foe_cache_evict: " + c.err);
+    if (!cache_hd(hd)) return fail(FOE_ERR_UNSUPPORTED, "foe_cache_evict: hd = 96 or 128 only");
+    if (!any) return FOE_OK;
+    const CacheArgs a{H, hd, B, n_pages, max_blocks, static_cast<uint8_t*>(k_cache),
+                      static_cast<uint8_t*>(v_cache), kv_scale, block_table, length};
+    hipError_t e = launch_cache_evict(a, mass, keep, recent, dst_table, dst_blocks, kept, new_len,
+                                      reinterpret_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "foe_cache_evict");
+    return FOE_OK;
+  });
+}
+
 int foe_profile_enable(int on) {
   std::lock_guard<std::mutex> lock(g_prof_mu);
   g_prof_on = on != 0;

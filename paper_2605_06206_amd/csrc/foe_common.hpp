@@ -220,6 +220,26 @@ hipError_t launch_combine(foe_dtype dt, int T, int d, int k, const void* y_perm,
                           void* out, hipStream_t s);
 hipError_t launch_reduce(foe_dtype dt, int C, int T, int d, const void* partials,
                          const void* residual, float scale, void* out, hipStream_t s);
+
+// the 8-bit key/value cache (kv_cache.hip, kv_attention.hip): the arguments that
+// its entry points share; `length` = tokens of each sequence before the call
+struct CacheArgs {
+  int H, hd, B, n_pages, max_blocks;
+  uint8_t *k, *v;
+  float* kv_scale;
+  const int32_t *block_table, *length;
+};
+hipError_t launch_cache_append(const CacheArgs& a, int nq, int N, const void* qkv, void* q,
+                               const int32_t* row_start, const int32_t* pos, float theta,
+                               float scale, hipStream_t s);
+size_t cache_attention_scratch_bytes(int H, int B, int N, int nq, int hd, int max_blocks,
+                                     int max_rows, bool mass);
+hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_rows, const void* q,
+                                  const int32_t* row_start, const float* mass_in, float* mass_out,
+                                  void* out, void* scratch, hipStream_t s);
+hipError_t launch_cache_evict(const CacheArgs& a, float* mass, int keep, int recent,
+                              const int32_t* dst_table, int dst_blocks, int32_t* kept,
+                              int32_t* new_len, hipStream_t s);
 hipError_t launch_fill_i32(int32_t* p, int n, int32_t v, hipStream_t s);
 
 }  // namespace foe

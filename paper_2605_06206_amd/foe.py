@@ -52,6 +52,10 @@ _SIGNATURES = {
     "foe_group_attention": (_c_int, [_c_int, _c_int, _c_int, _c_int, _c_int, _c_int, _c_float,
                                      _c_float, _p, _p, _p, _p, _p, _c_size, _p]),
     "foe_group_attention_workspace_bytes": (_c_size, [_c_int, _c_int, _c_int, _c_int, _c_int]),
+    "foe_cache_append": (_c_int, [_c_int] * 8 + [_c_float] * 2 + [_p] * 10),
+    "foe_cache_attention": (_c_int, [_c_int] * 9 + [_p] * 10 + [_p, _c_size, _p]),
+    "foe_cache_attention_workspace_bytes": (_c_size, [_c_int] * 8),
+    "foe_cache_evict": (_c_int, [_c_int] * 7 + [_p] * 3 + [_c_int] + [_p] * 7),
     "foe_last_error": (ctypes.c_char_p, []),
     "foe_profile_enable": (_c_int, [_c_int]),
     "foe_profile_reset": (_c_int, []),
@@ -305,6 +309,152 @@ def group_attention(x, w_qkv, w_o, nq, theta, scale=1.0, out=None, ws=None, stre
                                    _dev(ws, "ws"), ws.numel(), _stream(stream))
     _check(rc, "foe_group_attention")
     return out
+
+
+# ---- the 8-bit key/value cache --------------------------------------------------
+
+CACHE_PAGE = 64  # tokens per page
+
+
+def cache_empty(n_pages, H, hd, device="cuda"):
+    """A pool of pages: dict(k, v, kv_scale, mass), with zero masses and scales
+    of the smallest value (the codes are not initialised)."""
+    f8 = torch.float8_e4m3fn
+    return {"k": torch.empty((n_pages, H, CACHE_PAGE, hd), dtype=f8, device=device),
+            "v": torch.empty((n_pages, H, CACHE_PAGE // 16, hd, 16), dtype=f8, device=device),
+            "kv_scale": torch.full((n_pages, H, 2), 2.0 ** -100, device=device),
+            "mass": torch.zeros((n_pages, H, CACHE_PAGE), device=device)}
+
+
+def _shape(t, shape, name):
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise FoeError(FOE_ERR_INVALID, f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def _same_device(first, *tensors):
+    for t in tensors:
+        if t is not None and t.device != first.device:
+            raise ValueError(f"tensors on {first.device} and {t.device}")
+
+
+def _on(device, stream):
+    """Context in which a call allocates and launches: the tensors' device, and
+    `stream` as the current one, so that what the call allocates for itself belongs
+    to the stream that uses it."""
+    if not device.type == "cuda":
+        raise TypeError("GPU tensors are needed")
+    if stream is None:
+        return torch.cuda.device(device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    return torch.cuda.stream(stream)
+
+
+def _cache_pool(k, v, kv_scale):
+    """(n_pages, H, hd) of a pool, its tensors checked against each other."""
+    n_pages, H, _, hd = k.shape
+    _shape(k, (n_pages, H, CACHE_PAGE, hd), "k")
+    _shape(v, (n_pages, H, CACHE_PAGE // 16, hd, 16), "v")
+    _shape(kv_scale, (n_pages, H, 2), "kv_scale")
+    return n_pages, H, hd
+
+
+def _pool_ptrs(k, v, kv_scale):
+    f8 = torch.float8_e4m3fn
+    return _dev(k, "k", f8), _dev(v, "v", f8), _dev(kv_scale, "kv_scale", torch.float32)
+
+
+def cache_append(qkv, k, v, kv_scale, block_table, ctx_len, row_start, theta, scale=1.0, pos=None,
+                 q=None, stream=None):
+    """foe_cache_append: qkv [H,N,nq+2,hd] into the pages of block_table
+    [B,max_blocks]; returns the rotated queries [H,N,nq,hd]."""
+    n_pages, H, hd = _cache_pool(k, v, kv_scale)
+    N, nq = qkv.shape[1], qkv.shape[2] - 2
+    B, max_blocks = block_table.shape
+    _shape(qkv, (H, N, nq + 2, hd), "qkv")
+    _shape(ctx_len, (B,), "ctx_len")
+    _shape(row_start, (B + 1,), "row_start")
+    _shape(pos, (B,), "pos")
+    _same_device(qkv, k, v, kv_scale, block_table, ctx_len, row_start, pos, q)
+    _shape(q, (H, N, nq, hd), "q")
+    i32 = torch.int32
+    with _on(qkv.device, stream):
+        if q is None:
+            q = torch.empty((H, N, nq, hd), dtype=qkv.dtype, device=qkv.device)
+        rc = lib().foe_cache_append(
+            _dt(qkv), H, B, N, nq, hd, n_pages, max_blocks, float(theta), float(scale),
+            _dev(qkv, "qkv"), _dev(row_start, "row_start", i32), _dev(ctx_len, "ctx_len", i32),
+            _dev(pos, "pos", i32), _dev(block_table, "block_table", i32),
+            _dev(q, "q", qkv.dtype), *_pool_ptrs(k, v, kv_scale), _stream(stream))
+    _check(rc, "foe_cache_append")
+    return q
+
+
+def cache_attention_workspace_bytes(q, block_table, max_rows, with_mass=False):
+    """Workspace bytes of cache_attention for these tensors."""
+    H, N, nq, hd = q.shape
+    B, max_blocks = block_table.shape
+    n = lib().foe_cache_attention_workspace_bytes(H, B, N, nq, hd, max_blocks, max_rows,
+                                                  1 if with_mass else 0)
+    if n == ctypes.c_size_t(-1).value:
+        raise FoeError(FOE_ERR_INVALID, f"foe_cache_attention_workspace_bytes: {last_error()}")
+    return n
+
+
+def cache_attention(q, k, v, kv_scale, block_table, ctx_len, row_start, max_rows, mass_in=None,
+                    mass_out=None, out=None, ws=None, stream=None):
+    """foe_cache_attention: q [H,N,nq,hd] over the pages of block_table; returns
+    out [N,H,nq,hd]."""
+    n_pages, H, hd = _cache_pool(k, v, kv_scale)
+    N, nq = q.shape[1], q.shape[2]
+    B, max_blocks = block_table.shape
+    _shape(q, (H, N, nq, hd), "q")
+    _shape(ctx_len, (B,), "ctx_len")
+    _shape(row_start, (B + 1,), "row_start")
+    _shape(mass_in, (n_pages, H, CACHE_PAGE), "mass_in")
+    _shape(mass_out, (n_pages, H, CACHE_PAGE), "mass_out")
+    _same_device(q, k, v, kv_scale, block_table, ctx_len, row_start, mass_in, mass_out, out, ws)
+    _shape(out, (N, H, nq, hd), "out")
+    need = cache_attention_workspace_bytes(q, block_table, max_rows, mass_out is not None)
+    i32, f32 = torch.int32, torch.float32
+    with _on(q.device, stream):
+        if out is None:
+            out = torch.empty((N, H, nq, hd), dtype=q.dtype, device=q.device)
+        ws = _workspace(ws, need, q.device)
+        rc = lib().foe_cache_attention(
+            _dt(q), H, B, N, nq, hd, n_pages, max_blocks, max_rows, _dev(q, "q"),
+            _dev(row_start, "row_start", i32), _dev(ctx_len, "ctx_len", i32),
+            _dev(block_table, "block_table", i32), *_pool_ptrs(k, v, kv_scale),
+            _dev(mass_in, "mass_in", f32), _dev(mass_out, "mass_out", f32),
+            _dev(out, "out", q.dtype), _dev(ws, "ws"), ws.numel(), _stream(stream))
+    _check(rc, "foe_cache_attention")
+    return out
+
+
+def cache_evict(k, v, kv_scale, mass, block_table, length, keep, recent, dst_table, kept=None,
+                new_len=None, stream=None):
+    """foe_cache_evict: returns (kept [B,H,keep], new_len [B])."""
+    n_pages, H, hd = _cache_pool(k, v, kv_scale)
+    B, max_blocks = block_table.shape
+    _shape(mass, (n_pages, H, CACHE_PAGE), "mass")
+    _shape(length, (B,), "length")
+    _shape(dst_table, (B, dst_table.shape[-1]), "dst_table")
+    _same_device(k, v, kv_scale, mass, block_table, length, dst_table, kept, new_len)
+    i32 = torch.int32
+    _shape(kept, (B, H, keep), "kept")
+    _shape(new_len, (B,), "new_len")
+    with _on(k.device, stream):
+        if kept is None:
+            kept = torch.empty((B, H, keep), dtype=i32, device=k.device)
+        if new_len is None:
+            new_len = torch.empty((B,), dtype=i32, device=k.device)
+        rc = lib().foe_cache_evict(
+            H, B, hd, n_pages, max_blocks, keep, recent, _dev(length, "length", i32),
+            _dev(block_table, "block_table", i32), _dev(dst_table, "dst_table", i32),
+            dst_table.shape[1], *_pool_ptrs(k, v, kv_scale), _dev(mass, "mass", torch.float32),
+            _dev(kept, "kept", i32), _dev(new_len, "new_len", i32), _stream(stream))
+    _check(rc, "foe_cache_evict")
+    return kept, new_len
 
 
 # ---- kernel timing -------------------------------------------------------------
