@@ -340,8 +340,9 @@ size_t foe_group_attention_workspace_bytes(int H, int S, int d, int nq, int hd);
  *   q_out     [H, N, nq, hd] dt out the rotated queries (not qkv itself)
  *   k_cache, v_cache, kv_scale      updated: keys and values are quantised from fp32, a
  *                                   page that held tokens keeps a scale of at least its old
- *                                   one (its codes rescaled when it grows); slots past the
- *                                   new tokens are left as they were
+ *                                   one (when it grows, the codes of all its other slots
+ *                                   are rescaled); else slots without a new token are left
+ *                                   as they were
  * A token whose key or value holds a non-finite element is stored as a key of
  * NaN codes and a zero value, and has no part in the scales: every query that
  * sees it gives NaN, and no other does.  Rows past the table's end give q_out

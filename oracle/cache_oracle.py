@@ -121,11 +121,9 @@ def append(pool, qkv, table, ctx, row_start, theta, scale, pos=None):
                         s = max(s, old)
                         if s != old:
                             if name == "k":
-                                cc = pool["k"][p, h, :t0]
-                                pool["k"][p, h, :t0] = encode(decode(cc) * (old / s))
+                                pool["k"][p, h] = encode(decode(pool["k"][p, h]) * (old / s))
                             else:
-                                cc = _v_rows(pool["v"][p, h])[:t0]
-                                _v_put(pool["v"][p, h], encode(decode(cc) * (old / s)), 0)
+                                pool["v"][p, h] = encode(decode(pool["v"][p, h]) * (old / s))
                     pool["kv_scale"][p, h, i] = s
                     codes = encode(np.where(ok[:, None], y, 0.0) / s)
                     if name == "k":

@@ -14,8 +14,8 @@ namespace {
 // double and reduced modulo 2 pi, as in the preparation pass of the prompt
 // attention; q goes out in bf16, the rotated key is quantised from its fp32
 // value.  (2) The page's scales from the largest new magnitudes and, if the
-// page held tokens, its old scales; a scale that grows rescales the tokens
-// before.  (3) Key rows are stored as they are held; values go through LDS into
+// page held tokens, its old scales; a scale that grows rescales the page's
+// other codes.  (3) Key rows are stored as they are held; values go through LDS into
 // 16-byte pieces of one dim and 16 tokens, the tokens around the new ones kept.
 constexpr int kAppThr = 256;
 
@@ -141,8 +141,9 @@ __global__ __launch_bounds__(kAppThr) void cache_append_kernel(
       vt[(8 * u + 4 + e) * kPage + t] = (uint8_t)(v1w >> (8 * e));
     }
   }
-  if (kratio != 1.f)  // the tokens before, in units of the new scale
-    for (int i = tid; i < lo * (HD / 16); i += kAppThr) {
+  if (kratio != 1.f)  // the page's other rows, in units of the new scale
+    for (int i = tid; i < kPage * (HD / 16); i += kAppThr) {
+      if (i >= lo * (HD / 16) && i < hi * (HD / 16)) continue;
       u32x4* w = reinterpret_cast<u32x4*>(kp + i * 16);
       u32x4 x = *w;
 #pragma unroll
@@ -154,7 +155,7 @@ __global__ __launch_bounds__(kAppThr) void cache_append_kernel(
   for (int i = tid; i < (kPage / kSub) * HD; i += kAppThr) {
     const int g = i / HD, d = i % HD;
     const int t0 = g * kSub;
-    if (t0 >= hi || (t0 + kSub <= lo && vratio == 1.f)) continue;
+    if ((t0 >= hi || t0 + kSub <= lo) && vratio == 1.f) continue;
     u32x4* w = reinterpret_cast<u32x4*>(vp + i * 16);
     const u32x4 x = *reinterpret_cast<const u32x4*>(vt + d * kPage + t0);
     if (t0 >= lo && t0 + kSub <= hi) {
@@ -164,15 +165,13 @@ __global__ __launch_bounds__(kAppThr) void cache_append_kernel(
     u32x4 old = *w;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      uint32_t before = 0, fresh = 0;  // bytes of tokens before lo, and new ones
+      uint32_t fresh = 0;  // bytes of the new tokens
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int t = t0 + 4 * e + k;
-        if (t < lo) before |= 0xffu << (8 * k);
-        else if (t < hi) fresh |= 0xffu << (8 * k);
+        if (t >= lo && t < hi) fresh |= 0xffu << (8 * k);
       }
-      uint32_t o = old[e];
-      if (vratio != 1.f) o = (rescale4(o, vratio) & before) | (o & ~before);
+      const uint32_t o = vratio != 1.f ? rescale4(old[e], vratio) : old[e];
       old[e] = (o & ~fresh) | (x[e] & fresh);
     }
     *w = old;

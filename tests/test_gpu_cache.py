@@ -341,6 +341,17 @@ def test_attention_random_batches(i):
     check_attention(*run_attention(rng, H, nq, hd, seqs, bool(i % 2)))
 
 
+@pytest.mark.parametrize("nq,top", [(1, 1), (2, 20)])
+def test_attention_many_sequences(nq, top):
+    """More sequences than a workgroup has threads, many of them without rows, one long."""
+    rng = np.random.default_rng([18, nq])
+    seqs = [(int(c), int(n)) for c, n in zip(rng.integers(0, 150, 1100),
+                                             rng.integers(0, top + 1, 1100))]
+    seqs[3], seqs[900], seqs[1099] = (2000, 1), (1000, top), (70, top)
+    say("many sequences", nq, top)
+    check_attention(*run_attention(rng, 1, nq, 96, seqs, True))
+
+
 @pytest.mark.parametrize("rows", [1, 150])
 def test_attention_sharp_and_rising_scores(rows):
     """Scores over hundreds of log2 units, rising along the keys, so that the running
