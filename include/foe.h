@@ -404,12 +404,16 @@ size_t foe_cache_attention_workspace_bytes(int H, int B, int N, int nq, int hd, 
  *   kept      [B, H, keep] int32 out   the kept tokens' former numbers, ascending; -1 past
  *                          a shorter sequence's end
  *   new_len   [B]          int32 out   min(length, keep)
- * Needs no workspace.
+ *   ws, ws_bytes           workspace of foe_cache_evict_workspace_bytes() (none for tables of
+ *                          up to 512 pages)
  */
 int foe_cache_evict(int H, int B, int hd, int n_pages, int max_blocks, int keep, int recent,
                     const int32_t* length, const int32_t* block_table, const int32_t* dst_table,
                     int dst_blocks, void* k_cache, void* v_cache, float* kv_scale, float* mass,
-                    int32_t* kept, int32_t* new_len, void* stream);
+                    int32_t* kept, int32_t* new_len, void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace bytes of foe_cache_evict (SIZE_MAX for invalid sizes). */
+size_t foe_cache_evict_workspace_bytes(int H, int B, int max_blocks);
 
 /*
  * foe_workspace_bytes - workspace size in bytes for `op` (host string:

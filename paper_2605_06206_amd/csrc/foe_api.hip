@@ -715,7 +715,7 @@ int foe_cache_attention(foe_dtype dt, int H, int B, int N, int nq, int hd, int n
 int foe_cache_evict(int H, int B, int hd, int n_pages, int max_blocks, int keep, int recent,
                     const int32_t* length, const int32_t* block_table, const int32_t* dst_table,
                     int dst_blocks, void* k_cache, void* v_cache, float* kv_scale, float* mass,
-                    int32_t* kept, int32_t* new_len, void* stream) {
+                    int32_t* kept, int32_t* new_len, void* ws, size_t ws_bytes, void* stream) {
   return entry([&]() -> int {
     Check c;
     check_cache(c, H, B, n_pages, max_blocks);
@@ -736,13 +736,30 @@ int foe_cache_evict(int H, int B, int hd, int n_pages, int max_blocks, int keep,
     if (!c.err.empty()) return fail(FOE_ERR_INVALID, "foe_cache_evict: " + c.err);
     if (!cache_hd(hd)) return fail(FOE_ERR_UNSUPPORTED, "foe_cache_evict: hd = 96 or 128 only");
     if (!any) return FOE_OK;
+    const size_t need = cache_evict_scratch_bytes(H, B, max_blocks);
+    if (need > 0 && (ws == nullptr || !aligned16(ws)))
+      return fail(FOE_ERR_INVALID, "foe_cache_evict: ws is NULL or not 16-byte aligned");
+    if (ws_bytes < need)
+      return fail(FOE_ERR_WORKSPACE, "foe_cache_evict: workspace needs " + std::to_string(need) +
+                                         " bytes, got " + std::to_string(ws_bytes));
     const CacheArgs a{H, hd, B, n_pages, max_blocks, static_cast<uint8_t*>(k_cache),
                       static_cast<uint8_t*>(v_cache), kv_scale, block_table, length};
     hipError_t e = launch_cache_evict(a, mass, keep, recent, dst_table, dst_blocks, kept, new_len,
-                                      reinterpret_cast<hipStream_t>(stream));
+                                      ws, reinterpret_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "foe_cache_evict");
     return FOE_OK;
   });
+}
+
+size_t foe_cache_evict_workspace_bytes(int H, int B, int max_blocks) {
+  try {
+    Check c;
+    check_cache(c, H, B, 1, max_blocks);
+    if (!c.err.empty()) return (g_err = c.err, SIZE_MAX);
+    return cache_evict_scratch_bytes(H, B, max_blocks);
+  } catch (...) {
+    return SIZE_MAX;
+  }
 }
 
 int foe_profile_enable(int on) {

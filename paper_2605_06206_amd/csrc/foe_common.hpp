@@ -239,7 +239,8 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
                                   void* out, void* scratch, hipStream_t s);
 hipError_t launch_cache_evict(const CacheArgs& a, float* mass, int keep, int recent,
                               const int32_t* dst_table, int dst_blocks, int32_t* kept,
-                              int32_t* new_len, hipStream_t s);
+                              int32_t* new_len, void* scratch, hipStream_t s);
+size_t cache_evict_scratch_bytes(int H, int B, int max_blocks);
 hipError_t launch_fill_i32(int32_t* p, int n, int32_t v, hipStream_t s);
 
 }  // namespace foe

@@ -179,12 +179,26 @@ __global__ __launch_bounds__(kAppThr) void cache_append_kernel(
 }
 
 // ---- eviction -------------------------------------------------------------------
-// Selection: one workgroup per (sequence, group).  The keep - recent largest
-// masses among the tokens before the recent ones: the masses are mapped to
-// unsigned keys of the same order, the smallest kept key is found digit by digit
-// (8 bits, counted in LDS), and the tokens above it, and the first ones equal to
-// it, are listed in token order by ballots.
+// Selection of the keep - recent largest masses among the tokens before the recent
+// ones, per (sequence, group).  The masses are mapped to unsigned keys of the same
+// order; the smallest kept key is found digit by digit, 11, 11 and 10 bits, counted in
+// LDS (the first digit ends inside the significand, so masses of similar size spread
+// over counters); the tokens above it, and the first ones equal to it, are listed in
+// token order from ballots.  A workgroup holds the keys of 32768 tokens in registers,
+// four neighbouring tokens to a register group.  Where the table has room for more, each
+// 32768 tokens have a workgroup, their counts are joined between launches, one for each
+// digit and one that lists.
+// us for two sequences of 131072 tokens, 8 groups: one workgroup a sequence and group
+// with 8-bit digits, each pass from memory 398, with these digits 113 (its compute unit's
+// vector instructions are the bound), spread 53; 24 of at most 16000 tokens: 76, 17.
 constexpr int kSelThr = 1024;
+constexpr int kSelWaves = kSelThr / kWave;
+constexpr int kSelRegs = 8;                          // 4-token pieces of a thread
+constexpr int kSelTokens = kSelThr * 4 * kSelRegs;   // tokens of a workgroup
+constexpr int kSelBins = 2048;
+
+__device__ __forceinline__ int digit_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
+__device__ __forceinline__ int digit_bits(int pass) { return pass == 2 ? 10 : 11; }
 
 __device__ __forceinline__ uint32_t mass_key(float m) {
   if (m != m) return 0xffffffffu;  // NaN ranks first
@@ -192,14 +206,158 @@ __device__ __forceinline__ uint32_t mass_key(float m) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// Keys of tokens base + (j * 1024 + thread) * 4 + e.  Tokens past the old ones, and of
+// absent pages, get the lowest key: they come after every other of the same key, and
+// fewer than `old` are kept.
+__device__ __forceinline__ void load_keys(const float* mass, const CacheBatch& bt, int b, int h,
+                                          int old, int base, u32x4* key) {
+  int page[kSelRegs];
+  f32x4 m[kSelRegs];
+#pragma unroll
+  for (int j = 0; j < kSelRegs; ++j)  // (a token's page is within the table)
+    page[j] = bt.table[(size_t)b * bt.max_blocks +
+                       min(base + (j * kSelThr + (int)threadIdx.x) * 4, old - 1) / kPage];
+#pragma unroll
+  for (int j = 0; j < kSelRegs; ++j) {
+    const int t = (base + (j * kSelThr + (int)threadIdx.x) * 4) % kPage;
+    const size_t p = page[j] >= 0 && page[j] < bt.n_pages ? page[j] : 0;
+    m[j] = *reinterpret_cast<const f32x4*>(mass + (p * bt.H + h) * kPage + t);
+  }
+#pragma unroll
+  for (int j = 0; j < kSelRegs; ++j) {
+    const int t = base + (j * kSelThr + (int)threadIdx.x) * 4;
+    const bool absent = page[j] < 0 || page[j] >= bt.n_pages;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) key[j][e] = absent || t + e >= old ? 0u : mass_key(m[j][e]);
+  }
+}
+
+// Counts the next digit of the keys that have the prefix; np pieces hold tokens.
+__device__ __forceinline__ void count_keys(const u32x4* key, int np, int pass, uint32_t prefix,
+                                           int* hist) {
+  const int shift = digit_shift(pass), bits = digit_bits(pass), lane = lane_id();
+  __syncthreads();
+  hist[threadIdx.x] = 0;
+  hist[threadIdx.x + kSelThr] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kSelRegs; ++j) {
+    if (j >= np) continue;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t k = key[j][e];
+      if (pass > 0 && (k >> (shift + bits)) != (prefix >> (shift + bits))) continue;
+      const int d = (k >> shift) & ((1 << bits) - 1);
+      // lanes with the first lane's digit count together (equal masses)
+      const int d0 = __builtin_amdgcn_readfirstlane(d);
+      const uint64_t same = __builtin_amdgcn_ballot_w64(d == d0);
+      if (d != d0) atomicAdd(&hist[d], 1);
+      else if ((same & (((uint64_t)1 << lane) - 1)) == 0) atomicAdd(&hist[d], __popcll(same));
+    }
+  }
+  __syncthreads();
+}
+
+// The digit of the want-th largest key, and how many keys have a larger one, from
+// count(d) (threads take the digits two by two, the largest first).
+template <typename Count>
+__device__ __forceinline__ void find_digit(int pass, Count count, uint32_t& prefix, int& want) {
+  __shared__ int wsum[kSelWaves];
+  __shared__ int sh[2];
+  const int lane = lane_id(), wave = threadIdx.x >> 6;
+  const int hi = (1 << digit_bits(pass)) - 1 - 2 * (int)threadIdx.x;
+  const int c1 = hi > 0 ? count(hi) : 0, c2 = hi > 0 ? count(hi - 1) : 0;
+  int incl = c1 + c2;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int up = __shfl_up(incl, o);
+    if (lane >= o) incl += up;
+  }
+  if (lane == kWave - 1) wsum[wave] = incl;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) incl += wsum[w];
+  const int above = incl - c1 - c2;
+  if (above < want && want <= incl) {
+    const bool first = want <= above + c1;
+    sh[0] = first ? hi : hi - 1;
+    sh[1] = first ? above : above + c1;
+  }
+  __syncthreads();
+  prefix |= (uint32_t)sh[0] << digit_shift(pass);
+  want -= sh[1];
+}
+
+// Lists the tokens above the prefix and the first `want` equal to it; gt and eq tokens
+// came before.
+__device__ __forceinline__ void list_keys(const u32x4* key, int np, int base, uint32_t prefix,
+                                          int want, int gt, int eq, int32_t* out) {
+  constexpr int NC = kSelRegs * kSelWaves;
+  __shared__ int2 cnt[NC];  // tokens (above, equal) of a wave's piece, then of those before
+  __shared__ int2 half;
+  const int lane = lane_id(), wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int j = 0; j < kSelRegs; ++j) {
+    int g = 0, q = 0;
+    if (j < np) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        g += __popcll(__builtin_amdgcn_ballot_w64(key[j][e] > prefix));
+        q += __popcll(__builtin_amdgcn_ballot_w64(key[j][e] == prefix));
+      }
+    }
+    if (lane == 0) cnt[j * kSelWaves + wave] = int2{g, q};
+  }
+  __syncthreads();
+  static_assert(NC == 2 * kWave, "two waves' scan");
+  int2 mine{0, 0}, incl{0, 0};
+  if (threadIdx.x < NC) {
+    mine = incl = cnt[threadIdx.x];
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+      const int ug = __shfl_up(incl.x, o), uq = __shfl_up(incl.y, o);
+      if (lane >= o) incl.x += ug, incl.y += uq;
+    }
+    if (threadIdx.x == kWave - 1) half = incl;
+  }
+  __syncthreads();
+  if (threadIdx.x < NC) {
+    if (wave == 1) incl.x += half.x, incl.y += half.y;
+    cnt[threadIdx.x] = int2{gt + incl.x - mine.x, eq + incl.y - mine.y};
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kSelRegs; ++j) {
+    if (j >= np) continue;
+    const int2 x = cnt[j * kSelWaves + wave];
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    int pg = x.x, pe = x.y;  // before this lane's first token
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      pg += __popcll(__builtin_amdgcn_ballot_w64(key[j][e] > prefix) & below);
+      pe += __popcll(__builtin_amdgcn_ballot_w64(key[j][e] == prefix) & below);
+    }
+    const int t = base + (j * kSelThr + (int)threadIdx.x) * 4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool g = key[j][e] > prefix, q = key[j][e] == prefix;
+      if (g || (q && pe < want)) out[pg + min(pe, want)] = t + e;
+      pg += g;
+      pe += q;
+    }
+  }
+}
+
+// pieces that hold tokens of a workgroup's
+__device__ __forceinline__ int key_pieces(int old, int base) {
+  return min(kSelRegs, (old - base + kSelThr * 4 - 1) / (kSelThr * 4));
+}
+
+// The whole of a sequence's old tokens in one workgroup.
 __global__ __launch_bounds__(kSelThr) void cache_select_kernel(
     const float* __restrict__ mass, CacheBatch bt, int keep, int recent, int32_t* __restrict__ kept,
     int32_t* __restrict__ new_len) {
-  __shared__ int hist[256];
-  __shared__ int sh[2];
-  __shared__ int wgt[kSelThr / kWave], weq[kSelThr / kWave];
+  __shared__ int hist[kSelBins];
   const int tid = threadIdx.x, h = blockIdx.x, b = blockIdx.y;
-  const int lane = lane_id(), wave = tid >> 6;
   const int n = bt.context(b);
   int32_t* out = kept + ((size_t)b * bt.H + h) * keep;
   if (h == 0 && tid == 0) new_len[b] = min(n, keep);
@@ -208,171 +366,219 @@ __global__ __launch_bounds__(kSelThr) void cache_select_kernel(
     return;
   }
   const int old = n - recent, need = keep - recent;  // 0 <= need < old
-  auto key = [&](int t) {
-    const int p = bt.page(b, t / kPage);
-    return p < 0 ? 0u : mass_key(mass[((size_t)p * bt.H + h) * kPage + t % kPage]);
-  };
+  for (int j = tid; j < recent; j += kSelThr) out[need + j] = old + j;
+  if (need == 0) return;
+  u32x4 key[kSelRegs];
+  load_keys(mass, bt, b, h, old, 0, key);
+  const int np = key_pieces(old, 0);
   uint32_t prefix = 0;
   int want = need;  // of the keys with this prefix, the largest `want` are kept
-  if (need > 0)
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
-      __syncthreads();
-      for (int t = tid; t < old; t += kSelThr) {
-        const uint32_t k = key(t);
-        if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8)))
-          atomicAdd(&hist[(k >> shift) & 255], 1);
-      }
-      __syncthreads();
-      if (tid == 0) {
-        int d = 255, above = 0;
-        while (d > 0 && above + hist[d] < want) above += hist[d--];
-        sh[0] = d;
-        sh[1] = above;
-      }
-      __syncthreads();
-      prefix |= (uint32_t)sh[0] << shift;
-      want -= sh[1];
-      __syncthreads();
-    }
-  int gt = 0, eq = 0;  // kept above the prefix, and equal to it, so far
-  if (need > 0)
-    for (int base = 0; base < old; base += kSelThr) {
-      const int t = base + tid;
-      const uint32_t k = t < old ? key(t) : 0u;
-      const bool g = t < old && k > prefix, e = t < old && k == prefix;
-      const uint64_t mg = __builtin_amdgcn_ballot_w64(g), me = __builtin_amdgcn_ballot_w64(e);
-      if (lane == 0) wgt[wave] = __popcll(mg), weq[wave] = __popcll(me);
-      __syncthreads();
-      int gb = gt, eb = eq;
-      for (int w = 0; w < kSelThr / kWave; ++w) {
-        if (w < wave) gb += wgt[w], eb += weq[w];
-        gt += wgt[w], eq += weq[w];
-      }
-      const uint64_t below = ((uint64_t)1 << lane) - 1;
-      gb += __popcll(mg & below);
-      eb += __popcll(me & below);
-      if (g || (e && eb < want)) out[gb + min(eb, want)] = t;
-      __syncthreads();
-    }
-  for (int j = tid; j < recent; j += kSelThr) out[need + j] = old + j;
+#pragma unroll
+  for (int pass = 0; pass < 3; ++pass) {
+    count_keys(key, np, pass, prefix, hist);
+    find_digit(pass, [&](int d) { return hist[d]; }, prefix, want);
+  }
+  list_keys(key, np, 0, prefix, want, 0, 0, out);
 }
 
-// Moving the kept tokens: one workgroup per (page of the result, group,
-// sequence).
-constexpr int kMoveThr = 256;
+// One workgroup per 32768 tokens: launch `pass` counts that digit into
+// counts[pass][b][h][slice], launch 3 lists.
+template <int PASS>
+__global__ __launch_bounds__(kSelThr) void cache_select_slice_kernel(
+    const float* __restrict__ mass, CacheBatch bt, int keep, int recent, int* __restrict__ counts,
+    int32_t* __restrict__ kept, int32_t* __restrict__ new_len) {
+  __shared__ int hist[kSelBins];
+  __shared__ int before[2];
+  const int tid = threadIdx.x, slice = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+  const int n = bt.context(b);
+  const int old = n - recent, need = keep - recent, base = slice * kSelTokens;
+  int32_t* out = kept + ((size_t)b * bt.H + h) * keep;
+  if (PASS == 3) {
+    if (h == 0 && slice == 0 && tid == 0) new_len[b] = min(n, keep);
+    const int at = slice * kSelThr + tid, step = gridDim.x * kSelThr;
+    if (n <= keep) {
+      for (int j = at; j < keep; j += step) out[j] = j < n ? j : -1;
+    } else {
+      for (int j = at; j < recent; j += step) out[need + j] = old + j;
+    }
+  }
+  if (n <= keep || need == 0 || base >= old) return;
+  u32x4 key[kSelRegs];
+  load_keys(mass, bt, b, h, old, base, key);
+  const int np = key_pieces(old, base), slices = (old + kSelTokens - 1) / kSelTokens;
+  auto counts_of = [&](int pass) {
+    return counts + (((size_t)pass * bt.B + b) * bt.H + h) * gridDim.x * kSelBins;
+  };
+  uint32_t prefix = 0;
+  int want = need, gt = 0, eq = 0;
+#pragma unroll
+  for (int pass = 0; pass < PASS; ++pass) {
+    const int* c = counts_of(pass);
+    find_digit(pass, [&](int d) {
+      int x = 0;
+      for (int s = 0; s < slices; ++s) x += c[(size_t)s * kSelBins + d];
+      return x;
+    }, prefix, want);
+    if (PASS == 3) {  // tokens of the slices before with a larger digit, or the same at last
+      const int d0 = (prefix >> digit_shift(pass)) & ((1 << digit_bits(pass)) - 1);
+      if (tid == 0) before[0] = before[1] = 0;
+      __syncthreads();
+      for (int d = tid; d < 1 << digit_bits(pass); d += kSelThr) {
+        if (d < d0 || (d == d0 && pass < 2)) continue;
+        int x = 0;
+        for (int s = 0; s < slice; ++s) x += c[(size_t)s * kSelBins + d];
+        if (x > 0) atomicAdd(&before[d == d0], x);
+      }
+      __syncthreads();
+      gt += before[0];
+      eq += before[1];
+    }
+  }
+  if constexpr (PASS == 3) {
+    list_keys(key, np, base, prefix, want, gt, eq, out);
+  } else {
+    count_keys(key, np, PASS, prefix, hist);
+    int* c = counts_of(PASS) + (size_t)slice * kSelBins;
+    for (int d = tid; d < 1 << digit_bits(PASS); d += kSelThr) c[d] = hist[d];
+  }
+}
+
+// Moving the kept tokens: one workgroup per (page of the result, group, sequence).
+// Keys: thread -> 16 bytes of a row.  Values: the 128 threads of group g = 0..3 (a thread
+// a dim) gather the 16 tokens 16 g .. +15 of the page; a token is the same for all of
+// them, so its address and its byte within the 4 bytes that a thread loads are scalars,
+// and a byte permutation puts it in its place; neighbouring tokens share cache lines.
+// A token's place is a chain of loads (its number, its page, the page's scales, the
+// codes), hidden by the four workgroups that a CU has room for at 50 registers.
+// us for two sequences of 131072 tokens cut to half, 8 groups (the sources' cache lines
+// and the results are 640 MB: 125): 180.  A load for each byte 249; the source's 16-byte
+// pieces in registers, bytes taken by scalar branches, the chain loaded ahead over
+// several pages a workgroup 383 (135 registers); that with permutations 193 (80
+// registers); a wave for each page's keys and one for its values, without barriers, 401.
+constexpr int kMoveThr = 512;
 
 template <int HD>
-__global__ __launch_bounds__(kMoveThr) void cache_move_kernel(
+__global__ __launch_bounds__(kMoveThr, 8) void cache_move_kernel(
     uint8_t* __restrict__ kc, uint8_t* __restrict__ vc, float* __restrict__ kv_scale,
     float* __restrict__ mass, CacheBatch bt, const int32_t* __restrict__ dst_table, int dst_blocks,
     int keep, const int32_t* __restrict__ kept) {
-  constexpr int NP = kPage * HD / 16;                       // 16-byte pieces of a page's keys or values
-  constexpr int NI = (NP + kMoveThr - 1) / kMoveThr;  // of a thread
-  __shared__ int spage[kPage], stok[kPage];
-  __shared__ float2 sscale[kPage];
+  constexpr int CPR = HD / 16;
+  __shared__ int sp[kPage], st[kPage];
+  __shared__ float2 ss[kPage];
   const int tid = threadIdx.x, blk = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+  const int lane = lane_id();
   const int cnt = min(min(bt.context(b), keep) - blk * kPage, kPage);
   if (cnt <= 0) return;
   const int dp = dst_table[(size_t)b * dst_blocks + blk];
-  if (dp < 0 || dp >= bt.n_pages) return;
-  const size_t dst = (size_t)dp * bt.H + h;
+  auto lane_f = [&](float x, int i) {
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i));
+  };
   if (tid < kPage) {
-    int p = -1, t = 0;
-    if (tid < cnt) {
-      t = kept[((size_t)b * bt.H + h) * keep + blk * kPage + tid];
-      p = t >= 0 ? bt.page(b, t / kPage) : -1;
-      t %= kPage;
-    }
-    spage[tid] = p;
-    stok[tid] = t;
-    float2 s{0.f, 0.f};
-    if (p >= 0) {
-      const size_t sp = (size_t)p * bt.H + h;
-      s = float2{kv_scale[sp * 2], kv_scale[sp * 2 + 1]};
-      mass[dst * kPage + tid] = mass[sp * kPage + t];
-    } else if (tid < cnt) {
-      mass[dst * kPage + tid] = 0.f;
-    }
-    sscale[tid] = s;
+    const int t = tid < cnt ? kept[((size_t)b * bt.H + h) * keep + blk * kPage + tid] : -1;
+    const int p = t >= 0 ? bt.page(b, t / kPage) : -1;
+    sp[tid] = p;
+    st[tid] = t >= 0 ? t % kPage : 0;
+    ss[tid] = p >= 0 ? *reinterpret_cast<const float2*>(kv_scale + ((size_t)p * bt.H + h) * 2)
+                     : float2{0.f, 0.f};
   }
   __syncthreads();
-  u32x4 kw[NI], vw[NI];
-  float2 amax{0.f, 0.f};
-  auto bigger = [](float a, uint32_t w, int i, float s) {
-    float x = 0.f;
-    switch (i) {
-      case 0: x = __builtin_amdgcn_cvt_f32_fp8(w, 0); break;
-      case 1: x = __builtin_amdgcn_cvt_f32_fp8(w, 1); break;
-      case 2: x = __builtin_amdgcn_cvt_f32_fp8(w, 2); break;
-      default: x = __builtin_amdgcn_cvt_f32_fp8(w, 3); break;
-    }
-    return fmaxf(a, fabsf(x) * s);  // (a NaN code counts for nothing)
+  const int kt = tid / CPR;            // key row
+  const int g = tid >> 7, d = tid & 127;
+  u32x4 kw = zero_u32x4();
+  const bool has_k = kt < cnt && sp[kt] >= 0;
+  if (has_k)
+    kw = *reinterpret_cast<const u32x4*>(kc + ((size_t)sp[kt] * bt.H + h) * (kPage * HD) +
+                                         st[kt] * HD + (tid % CPR) * 16);
+  float m = 0.f;
+  if (tid < cnt && sp[tid] >= 0) m = mass[((size_t)sp[tid] * bt.H + h) * kPage + st[tid]];
+  // values: token 16 g + i in lane i of every wave
+  const int my_page = sp[g * kSub + (lane & 15)], my_tok = st[g * kSub + (lane & 15)];
+  const float my_scale = ss[g * kSub + (lane & 15)].y;
+  // where its 4 bytes are in dim 0, and the permutation that puts its byte at i % 4
+  // (an absent token: a zero byte)
+  const int at = (lane & 3) * 8;
+  const uint32_t my_sel = (0x03020100u & ~(0xffu << at)) |
+                          ((my_page < 0 ? 0x0cu : 4u + (my_tok & 3)) << at);
+  const uint64_t my_off =
+      my_page < 0 ? 0
+                  : ((uint64_t)my_page * bt.H + h) * (kPage * HD) +
+                        (uint32_t)((my_tok / kSub) * (HD * kSub) + (my_tok % kSub & ~3));
+  const uint32_t dim = min(d, HD - 1) * kSub;
+  auto gather = [&](int i) {
+    const uint64_t off =
+        (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(my_off >> 32), i) << 32 |
+        (uint32_t)__builtin_amdgcn_readlane((uint32_t)my_off, i);
+    return *reinterpret_cast<const uint32_t*>(vc + off + dim);
+  };
+  uint32_t got[kSub / 2];  // (eight loads in flight)
+#pragma unroll
+  for (int i = 0; i < kSub / 2; ++i) got[i] = gather(i);
+  float2 amax{0.f, 0.f};  // (a NaN code counts for no scale)
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float x = fmaxf(fabsf(__builtin_amdgcn_cvt_f32_fp8(kw[e], 0)),
+                    fabsf(__builtin_amdgcn_cvt_f32_fp8(kw[e], 1)));
+    x = fmaxf(x, fmaxf(fabsf(__builtin_amdgcn_cvt_f32_fp8(kw[e], 2)),
+                       fabsf(__builtin_amdgcn_cvt_f32_fp8(kw[e], 3))));
+    if (has_k) amax.x = fmaxf(amax.x, x * ss[kt].x);
+  }
+  u32x4 vw = zero_u32x4();
+  auto place_byte = [&](int i, uint32_t x) {
+    vw[i / 4] = __builtin_amdgcn_perm(x, vw[i / 4], __builtin_amdgcn_readlane(my_sel, i));
   };
 #pragma unroll
-  for (int i = 0; i < NI; ++i) {
-    const int item = i * kMoveThr + tid, t = item / (HD / 16), c = item % (HD / 16);
-    kw[i] = zero_u32x4();
-    if (item >= NP) break;
-    if (spage[t] >= 0) {
-      kw[i] = *reinterpret_cast<const u32x4*>(
-          kc + ((size_t)spage[t] * bt.H + h) * (kPage * HD) + stok[t] * HD + c * 16);
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) amax.x = bigger(amax.x, kw[i][e], k, sscale[t].x);
-    }
+  for (int i = 0; i < kSub / 2; ++i) {
+    place_byte(i, got[i]);
+    got[i] = gather(kSub / 2 + i);
   }
 #pragma unroll
-  for (int i = 0; i < NI; ++i) {
-    const int item = i * kMoveThr + tid, g = item / HD, d = item % HD;
-    vw[i] = zero_u32x4();
-    if (item >= NP) break;
+  for (int i = 0; i < kSub / 2; ++i) place_byte(kSub / 2 + i, got[i]);
 #pragma unroll
-    for (int e = 0; e < kSub; ++e) {
-      const int t = g * kSub + e;
-      if (spage[t] < 0) continue;
-      const uint32_t c = vc[((size_t)spage[t] * bt.H + h) * (kPage * HD) +
-                            (stok[t] / kSub) * (HD * kSub) + d * kSub + stok[t] % kSub];
-      vw[i][e / 4] |= c << (8 * (e % 4));
-      amax.y = bigger(amax.y, c, 0, sscale[t].y);
-    }
+  for (int e = 0; e < 4; ++e) {
+    const float x0 = fabsf(__builtin_amdgcn_cvt_f32_fp8(vw[e], 0)) * lane_f(my_scale, 4 * e);
+    const float x1 = fabsf(__builtin_amdgcn_cvt_f32_fp8(vw[e], 1)) * lane_f(my_scale, 4 * e + 1);
+    const float x2 = fabsf(__builtin_amdgcn_cvt_f32_fp8(vw[e], 2)) * lane_f(my_scale, 4 * e + 2);
+    const float x3 = fabsf(__builtin_amdgcn_cvt_f32_fp8(vw[e], 3)) * lane_f(my_scale, 4 * e + 3);
+    amax.y = fmaxf(fmaxf(amax.y, x0), fmaxf(fmaxf(x1, x2), x3));
   }
   amax = block_max<kMoveThr>(amax);
   const float ks = block_scale(amax.x), vs = block_scale(amax.y);
   const float ki = pow2_inv(ks), vi = pow2_inv(vs);
-  if (tid == 0) kv_scale[dst * 2] = ks, kv_scale[dst * 2 + 1] = vs;
-  uint8_t* kp = kc + dst * (kPage * HD);
-  uint8_t* vp = vc + dst * (kPage * HD);
+  if (dp >= 0 && dp < bt.n_pages) {
+    const size_t dst = (size_t)dp * bt.H + h;
+    if (tid == 0) *reinterpret_cast<float2*>(kv_scale + dst * 2) = float2{ks, vs};
+    if (tid < cnt) mass[dst * kPage + tid] = m;
+    if (kt < cnt) {
+      const float r = ss[kt].x * ki;
+      if (r != 1.f) {
 #pragma unroll
-  for (int i = 0; i < NI; ++i) {
-    const int item = i * kMoveThr + tid, t = item / (HD / 16);
-    if (item >= NP || t >= cnt) continue;
-    const float r = sscale[t].x * ki;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) kw[i][e] = rescale4(kw[i][e], r);
-    *reinterpret_cast<u32x4*>(kp + item * 16) = kw[i];
-  }
-#pragma unroll
-  for (int i = 0; i < NI; ++i) {
-    const int item = i * kMoveThr + tid, t0 = item / HD * kSub;
-    if (item >= NP || t0 >= cnt) continue;
-    u32x4* w = reinterpret_cast<u32x4*>(vp + item * 16);
-    const u32x4 was = t0 + kSub > cnt ? *w : zero_u32x4();
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int t = t0 + 4 * e;
-      const uint32_t x = vw[i][e];
-      uint32_t y = to_codes4(__builtin_amdgcn_cvt_f32_fp8(x, 0) * (sscale[t].y * vi),
-                             __builtin_amdgcn_cvt_f32_fp8(x, 1) * (sscale[t + 1].y * vi),
-                             __builtin_amdgcn_cvt_f32_fp8(x, 2) * (sscale[t + 2].y * vi),
-                             __builtin_amdgcn_cvt_f32_fp8(x, 3) * (sscale[t + 3].y * vi));
-      // slots past the kept tokens stay as they were
-      const int left = cnt - t;
-      const uint32_t m = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1;
-      vw[i][e] = (y & m) | (was[e] & ~m);
+        for (int e = 0; e < 4; ++e) kw[e] = rescale4(kw[e], r);
+      }
+      *reinterpret_cast<u32x4*>(kc + dst * (kPage * HD) + tid * 16) = kw;
     }
-    *w = vw[i];
+    if (g * kSub < cnt && d < HD) {
+      u32x4* w = reinterpret_cast<u32x4*>(vc + dst * (kPage * HD) + (g * HD + d) * kSub);
+      const int left = cnt - g * kSub;  // slots past the kept tokens stay as they were
+      const u32x4 was = left < kSub ? *w : zero_u32x4();
+      const float r = my_scale * vi;
+      if (__builtin_amdgcn_ballot_w64(r != 1.f)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t x = vw[e];
+          vw[e] = to_codes4(__builtin_amdgcn_cvt_f32_fp8(x, 0) * lane_f(r, 4 * e),
+                            __builtin_amdgcn_cvt_f32_fp8(x, 1) * lane_f(r, 4 * e + 1),
+                            __builtin_amdgcn_cvt_f32_fp8(x, 2) * lane_f(r, 4 * e + 2),
+                            __builtin_amdgcn_cvt_f32_fp8(x, 3) * lane_f(r, 4 * e + 3));
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int in = left - 4 * e;
+        const uint32_t mk = in >= 4 ? 0xffffffffu : in <= 0 ? 0u : (1u << (8 * in)) - 1;
+        vw[e] = (vw[e] & mk) | (was[e] & ~mk);
+      }
+      *w = vw;
+    }
   }
 }
 
@@ -395,19 +601,41 @@ hipError_t launch_cache_append(const CacheArgs& a, int nq, int N, const void* qk
   return hipGetLastError();
 }
 
+// the table has room for more tokens than a workgroup holds
+static int select_slices(int max_blocks) {
+  return ceil_div((long long)max_blocks * kPage, kSelTokens);
+}
+
+size_t cache_evict_scratch_bytes(int H, int B, int max_blocks) {
+  const int slices = select_slices(max_blocks);
+  return slices > 1 ? (size_t)3 * B * H * slices * kSelBins * 4 : 0;
+}
+
 hipError_t launch_cache_evict(const CacheArgs& a, float* mass, int keep, int recent,
                               const int32_t* dst_table, int dst_blocks, int32_t* kept,
-                              int32_t* new_len, hipStream_t s) {
+                              int32_t* new_len, void* scratch, hipStream_t s) {
   const CacheBatch bt{a.H, a.B, 0, 0, a.n_pages, a.max_blocks, a.block_table, a.length, nullptr};
-  {
+  const int slices = select_slices(a.max_blocks);
+  if (slices == 1) {
     ProfileScope ps("cache_select", s);
     FOE_LAUNCH(cache_select_kernel, dim3(a.H, a.B), dim3(kSelThr), 0, s, mass, bt, keep, recent,
                kept, new_len);
+  } else {
+    auto go = [&](auto kern, const char* name) {
+      ProfileScope ps(name, s);
+      FOE_LAUNCH(kern, dim3(slices, a.H, a.B), dim3(kSelThr), 0, s, mass, bt, keep, recent,
+                 static_cast<int*>(scratch), kept, new_len);
+    };
+    go(cache_select_slice_kernel<0>, "cache_select_0");
+    go(cache_select_slice_kernel<1>, "cache_select_1");
+    go(cache_select_slice_kernel<2>, "cache_select_2");
+    go(cache_select_slice_kernel<3>, "cache_select_3");
   }
   {
     ProfileScope ps("cache_move", s);
+    const int blocks = std::min(ceil_div(keep, kPage), a.max_blocks);
     auto go = [&](auto kern) {
-      FOE_LAUNCH(kern, dim3(ceil_div(keep, kPage), a.H, a.B), dim3(kMoveThr), 0, s, a.k, a.v,
+      FOE_LAUNCH(kern, dim3(blocks, a.H, a.B), dim3(kMoveThr), 0, s, a.k, a.v,
                  a.kv_scale, mass, bt, dst_table, dst_blocks, keep, kept);
     };
     if (a.hd == 96) go(cache_move_kernel<96>);

@@ -55,7 +55,9 @@ _SIGNATURES = {
     "foe_cache_append": (_c_int, [_c_int] * 8 + [_c_float] * 2 + [_p] * 10),
     "foe_cache_attention": (_c_int, [_c_int] * 9 + [_p] * 10 + [_p, _c_size, _p]),
     "foe_cache_attention_workspace_bytes": (_c_size, [_c_int] * 8),
-    "foe_cache_evict": (_c_int, [_c_int] * 7 + [_p] * 3 + [_c_int] + [_p] * 7),
+    "foe_cache_evict": (_c_int, [_c_int] * 7 + [_p] * 3 + [_c_int] + [_p] * 7 +
+                        [_c_size, _p]),
+    "foe_cache_evict_workspace_bytes": (_c_size, [_c_int] * 3),
     "foe_last_error": (ctypes.c_char_p, []),
     "foe_profile_enable": (_c_int, [_c_int]),
     "foe_profile_reset": (_c_int, []),
@@ -432,15 +434,18 @@ def cache_attention(q, k, v, kv_scale, block_table, ctx_len, row_start, max_rows
 
 
 def cache_evict(k, v, kv_scale, mass, block_table, length, keep, recent, dst_table, kept=None,
-                new_len=None, stream=None):
+                new_len=None, ws=None, stream=None):
     """foe_cache_evict: returns (kept [B,H,keep], new_len [B])."""
     n_pages, H, hd = _cache_pool(k, v, kv_scale)
     B, max_blocks = block_table.shape
     _shape(mass, (n_pages, H, CACHE_PAGE), "mass")
     _shape(length, (B,), "length")
     _shape(dst_table, (B, dst_table.shape[-1]), "dst_table")
-    _same_device(k, v, kv_scale, mass, block_table, length, dst_table, kept, new_len)
+    _same_device(k, v, kv_scale, mass, block_table, length, dst_table, kept, new_len, ws)
     i32 = torch.int32
+    need = lib().foe_cache_evict_workspace_bytes(H, B, max_blocks)
+    if need == ctypes.c_size_t(-1).value:
+        raise FoeError(FOE_ERR_INVALID, f"foe_cache_evict_workspace_bytes: {last_error()}")
     _shape(kept, (B, H, keep), "kept")
     _shape(new_len, (B,), "new_len")
     with _on(k.device, stream):
@@ -448,11 +453,13 @@ def cache_evict(k, v, kv_scale, mass, block_table, length, keep, recent, dst_tab
             kept = torch.empty((B, H, keep), dtype=i32, device=k.device)
         if new_len is None:
             new_len = torch.empty((B,), dtype=i32, device=k.device)
+        ws = _workspace(ws, need, k.device)
         rc = lib().foe_cache_evict(
             H, B, hd, n_pages, max_blocks, keep, recent, _dev(length, "length", i32),
             _dev(block_table, "block_table", i32), _dev(dst_table, "dst_table", i32),
             dst_table.shape[1], *_pool_ptrs(k, v, kv_scale), _dev(mass, "mass", torch.float32),
-            _dev(kept, "kept", i32), _dev(new_len, "new_len", i32), _stream(stream))
+            _dev(kept, "kept", i32), _dev(new_len, "new_len", i32), _dev(ws, "ws"), ws.numel(),
+            _stream(stream))
     _check(rc, "foe_cache_evict")
     return kept, new_len
 

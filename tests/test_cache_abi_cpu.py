@@ -58,7 +58,21 @@ def test_attention_rejects(L, at, value, rc, msg):
     assert msg in foe.last_error()
 
 
-EVICT = [8, 4, 128, 100, 16, 128, 16, P, P, P, 2, P, P, P, P, P, P, None]
+EVICT = [8, 4, 128, 100, 16, 128, 16, P, P, P, 2, P, P, P, P, P, P, None, 0, None]
+
+
+LONG = 513  # pages: more tokens than a workgroup of the selection holds
+
+
+def test_evict_workspace(L):
+    assert L.foe_cache_evict_workspace_bytes(8, 4, 512) == 0
+    need = L.foe_cache_evict_workspace_bytes(8, 4, LONG)
+    assert 0 < need < SIZE_MAX
+    assert L.foe_cache_evict_workspace_bytes(8, -1, LONG) == SIZE_MAX
+    long = changed(EVICT, 4, LONG)
+    assert L.foe_cache_evict(*long) == INV and "ws is NULL" in foe.last_error()
+    long[17:19] = P2, need - 1
+    assert L.foe_cache_evict(*long) == WS and "workspace needs" in foe.last_error()
 
 
 @pytest.mark.parametrize("at,value,rc,msg", [
@@ -80,7 +94,7 @@ def test_empty_calls_are_noops(L):
     assert L.foe_cache_attention(BF16, 8, 4, 0, 2, 128, 1, 1, 1, *empty[:11], 0,
                                  None) == foe.FOE_OK
     assert L.foe_cache_evict(8, 0, 128, 1, 1, 1, 0, None, None, None, 1,
-                             *empty[:7]) == foe.FOE_OK
+                             *empty[:7], 0, None) == foe.FOE_OK
 
 
 def test_workspace_bytes(L):

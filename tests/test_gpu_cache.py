@@ -547,6 +547,21 @@ def test_evict_masses_near_each_other(what):
     check_evict(rng, 2, 96, [700, 100, 1500], 333, 20, mass=mass)
 
 
+@pytest.mark.parametrize("what", ["equal", "two", "spread"])
+def test_evict_long_sequences(what):
+    """Sequences of more tokens than a workgroup of the selection holds, beside shorter
+    ones of the same call, ties across the workgroups' borders included."""
+    rng = np.random.default_rng(25)
+
+    def mass(m):
+        if what == "equal":
+            return np.full_like(m, 0.5)
+        return (rng.random(m.shape) < 0.4) * 0.25 if what == "two" else m
+
+    say("evict long sequences", what)
+    check_evict(rng, 1, 96, [70001, 32768, 33000, 150, 65536], 20000, 300, mass=mass)
+
+
 def test_evict_spread_scales_and_nan_keys():
     """Tokens of pages with scales far apart in one new page (the small ones fall
     among its subnormals or to zero), keys of NaN codes, and absent pages."""
