@@ -2,11 +2,12 @@
 // each cached token receives.
 //
 // A column is one query: row i of a sequence and head j of a group, numbered
-// i * nq + j (the heads share the group's keys and values).  Two forms, by the
-// sequence's columns:
+// i * nq + j (the heads share the group's keys and values).  Two forms, by the most
+// columns that a sequence of the call can have:
 // - few (at most 16: decode steps): a tile of 16 columns walks the pages with
 //   16x16x32 MFMAs fed from registers; reading the pages is all the work;
-// - many (chunks): tiles of up to 256 columns share each page through LDS.
+// - many (chunks, and the decode steps that ride along): tiles of up to 256 columns
+//   share each page through LDS.
 // In both, S^T = K Q^T and O^T += V^T P^T with an online softmax in base 2, and the
 // work is dealt out alike: the (sequence, group, tile, page) units of the batch,
 // numbered in that order, are cut into equal ranges, one for each workgroup of a
@@ -32,8 +33,7 @@ constexpr float kMFloor = -1.0e30f;   // the running maximum's start: finite, be
 
 // ---- dealing out the work -------------------------------------------------------
 
-// The units of a batch in one of the two forms, numbered by sequence, group, tile
-// and page.  A tile of the many form has 2^log2r rows, tile t reaches page
+// The units of a batch in a form, numbered by sequence, group, tile and page.  A tile of the many form has 2^log2r rows, tile t reaches page
 // ceil((ctx + last row + 1) / 64), and the sums over tiles are closed forms.
 struct Units {
   CacheBatch bt;
@@ -42,11 +42,6 @@ struct Units {
   long long* prefix;  // [B + 1]: units before each sequence, and in all (written for the join)
 
   __device__ __forceinline__ int rows(int b) const { return min(bt.rows(b), max_rows); }
-  // rows of sequence b in this form
-  __device__ __forceinline__ int mine(int b) const {
-    const int n = rows(b);
-    return (n * bt.nq <= kFewCols) == (log2r < 0) ? n : 0;
-  }
   __device__ __forceinline__ int tiles(int n) const { return (n + (1 << log2r) - 1) >> log2r; }
   // pages of the tiles before tile t (t < tiles)
   __device__ __forceinline__ long long before(int ctx, int t) const {
@@ -67,7 +62,7 @@ struct Units {
   }
   // units of one group of sequence b
   __device__ __forceinline__ long long group(int b) const {
-    const int n = mine(b);
+    const int n = rows(b);
     if (n <= 0) return 0;
     const int ctx = bt.context(b), t = log2r < 0 ? 0 : tiles(n) - 1;
     return (log2r < 0 ? 0 : before(ctx, t)) + pages(ctx, n, t);
@@ -215,7 +210,8 @@ template <int HD>
 __global__ __launch_bounds__(kAttThr) void cache_attn_few_kernel(
     const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
     const float* __restrict__ kv_scale, Units w, int least, int part_cols, float c_log2,
-    bf16* __restrict__ out, float2* __restrict__ stat, float* __restrict__ part) {
+    bf16* __restrict__ out, float2* __restrict__ stat, float* __restrict__ part,
+    float* __restrict__ score) {
   using F = PageFrags<HD>;
   __shared__ float mm[kAttWaves][16], ll[kAttWaves][16];
   __shared__ __align__(16) float oo[kAttWaves][HD][16];
@@ -227,8 +223,9 @@ __global__ __launch_bounds__(kAttThr) void cache_attn_few_kernel(
   locate<kAttThr>(w, gridDim.x, blockIdx.x, least, total, b, off);
   if (b < 0) return;
   const int per = (int)range_units(total, gridDim.x, least);
-  int left = (int)min((long long)per, total - (long long)blockIdx.x * per);
-  int rows = w.mine(b), ctx = bt.context(b), np = w.pages(ctx, rows, 0);
+  long long unit = (long long)blockIdx.x * per;
+  int left = (int)min((long long)per, total - unit);
+  int rows = w.rows(b), ctx = bt.context(b), np = w.pages(ctx, rows, 0);
   int h = (int)(off / np), blk0 = (int)(off % np);
   bool first_tile = true;
   while (true) {
@@ -269,6 +266,11 @@ __global__ __launch_bounds__(kAttThr) void cache_attn_few_kernel(
 #pragma unroll
           for (int dt = 0; dt < F::NDT; ++dt) f.v[dt][e] &= m;
         }
+      }
+      if (score != nullptr && n < ncol) {
+        float* to = score + ((unit + blk - blk0) * part_cols + n) * kPage + 16 * g;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4*>(to + 4 * t) = s[t];
       }
       float mx = s[0][0];
 #pragma unroll
@@ -350,15 +352,16 @@ __global__ __launch_bounds__(kAttThr) void cache_attn_few_kernel(
       }
     }
     left -= blk1 - blk0;
+    unit += blk1 - blk0;
     if (left <= 0) return;
-    // the next group, or the next sequence with rows of this form
+    // the next group, or the next sequence with rows
     first_tile = false;
     blk0 = 0;
     if (++h == bt.H) {
       h = 0;
       do {
         if (++b >= bt.B) return;
-        rows = w.mine(b);
+        rows = w.rows(b);
       } while (rows <= 0);
       ctx = bt.context(b);
       np = w.pages(ctx, rows, 0);
@@ -401,7 +404,7 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
   if (b < 0) return;
   const int per = (int)range_units(total, gridDim.x, least);
   int left = (int)min((long long)per, total - (long long)range * per);
-  int rows = w.mine(b), ctx = bt.context(b), nt = w.tiles(rows), h, t, blk0;
+  int rows = w.rows(b), ctx = bt.context(b), nt = w.tiles(rows), h, t, blk0;
   {
     const long long each = w.group(b);
     h = (int)(off / each);
@@ -631,7 +634,7 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
     }
     left -= niter;
     if (left <= 0) return;
-    // the next tile, group, or sequence with rows of this form
+    // the next tile, group, or sequence with rows
     first_tile = false;
     blk0 = 0;
     if (++t == nt) {
@@ -640,7 +643,7 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
         h = 0;
         do {
           if (++b >= bt.B) return;
-          rows = w.mine(b);
+          rows = w.rows(b);
         } while (rows <= 0);
         ctx = bt.context(b);
         nt = w.tiles(rows);
@@ -650,138 +653,314 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
 }
 
 // ---- joining the parts ---------------------------------------------------------------
-// One workgroup per (32 columns of a tile, group, sequence), 8 groups of 32 lanes, a
-// lane taking 4 dims: a few columns have their parts dealt to the 8 groups (each sums
-// every eighth, then the groups are summed in order), many columns are dealt
-// themselves.  A tile that lies in one range has been written already.
-template <int HD, bool FEW>
-__global__ __launch_bounds__(256) void cache_join_kernel(Units w, int ranges, int least,
-                                                         int part_cols, const float* __restrict__ part,
-                                                         bf16* __restrict__ out,
-                                                         float2* __restrict__ stat) {
-  constexpr int TILE = FEW ? 1 : kTileCols / 32;  // workgroups of a tile
-  __shared__ f32x4 osum[FEW ? 8 : 1][32];
+// The parts of a tile: ranges r0 .. r1, the first in slot 2 r0 + 1 unless the tile starts
+// its range.
+struct Parts {
+  const float* part;
+  int cols, hd, r0, r1;
+  bool first_late;
+  __device__ __forceinline__ const float* at(int r) const {
+    return part + (2 * (size_t)r + (r == r0 && first_late)) * part_floats(cols, hd);
+  }
+  __device__ __forceinline__ const float2* stats(int r) const {  // (maximum, sum) by column
+    return reinterpret_cast<const float2*>(at(r) + (size_t)cols * hd);
+  }
+};
+// units u0 .. u0 + np - 1 of the tile; false where one range wrote it whole
+__device__ __forceinline__ bool find_parts(const Units& w, int ranges, int least, long long u0,
+                                           int np, Parts& p) {
+  const long long per = range_units(w.prefix[w.bt.B], ranges, least);
+  p.r0 = (int)(u0 / per);
+  p.r1 = (int)((u0 + np - 1) / per);
+  p.first_late = u0 % per != 0;
+  return p.r0 != p.r1;
+}
+
+// Few columns: one workgroup per (group, sequence).  8 groups of 32 lanes (a lane 4 dims)
+// each sum every eighth part, and are then summed in order.
+template <int HD>
+__global__ __launch_bounds__(256) void cache_join_few_kernel(Units w, int ranges, int least,
+                                                             int part_cols,
+                                                             const float* __restrict__ part,
+                                                             bf16* __restrict__ out,
+                                                             float2* __restrict__ stat) {
+  __shared__ f32x4 osum[8][32];
   const CacheBatch& bt = w.bt;
-  const int t = blockIdx.x / TILE, h = blockIdx.y, b = blockIdx.z;
-  const int c0 = (blockIdx.x % TILE) * 32;
-  const int rows = w.mine(b);
-  if (rows <= 0 || (!FEW && t >= w.tiles(rows))) return;
-  const int ctx = bt.context(b), row0 = FEW ? 0 : t << w.log2r;
-  const int ncol = ((FEW ? rows : min(rows, (t + 1) << w.log2r)) - row0) * bt.nq;
-  if (c0 >= ncol) return;
-  const long long total = w.prefix[bt.B], per = range_units(total, ranges, least);
-  const long long u0 = w.prefix[b] + (w.group(b) * h + (FEW ? 0 : w.before(ctx, t)));
-  const int np = w.pages(ctx, rows, t);
-  const int r0 = (int)(u0 / per), r1 = (int)((u0 + np - 1) / per);
-  if (r0 == r1) return;
-  const size_t pf = part_floats(part_cols, HD);
-  auto slot = [&](int r) { return part + (2 * (size_t)r + (r == r0 && u0 % per != 0)) * pf; };
-  const int grp = threadIdx.x >> 5, l5 = threadIdx.x & 31;
-  const int d = 4 * l5;
-  auto ml = [&](int r, int c) {
-    return reinterpret_cast<const float2*>(slot(r) + (size_t)part_cols * HD)[c];
-  };
-  for (int c = c0 + (FEW ? 0 : grp); c < min(ncol, c0 + 32); c += FEW ? 1 : 8) {
+  const int h = blockIdx.x, b = blockIdx.y;
+  const int rows = w.rows(b);
+  if (rows <= 0) return;
+  const int np = w.pages(bt.context(b), rows, 0), ncol = rows * bt.nq;
+  Parts p{part, part_cols, HD};
+  if (!find_parts(w, ranges, least, w.prefix[b] + (long long)np * h, np, p)) return;
+  const int grp = threadIdx.x >> 5, l5 = threadIdx.x & 31, d = 4 * l5;
+  for (int c = 0; c < ncol; ++c) {
     float m = kMFloor, l = 0.f;
-    for (int r = r0 + l5; r <= r1; r += 32) m = fmaxf(m, ml(r, c).x);
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
-    for (int r = r0 + l5; r <= r1; r += 32) {
-      const float2 x = ml(r, c);
-      l += x.y * __builtin_amdgcn_exp2f(x.x - m);
+    for (int r = p.r0 + l5; r <= p.r1; r += 32) {
+      const float2 x = p.stats(r)[c];
+      const float mn = fmaxf(m, x.x);
+      l = l * __builtin_amdgcn_exp2f(m - mn) + x.y * __builtin_amdgcn_exp2f(x.x - mn);
+      m = mn;
     }
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) l += __shfl_xor(l, o);
+    for (int o = 1; o < 32; o <<= 1) {
+      const float mo = __shfl_xor(m, o), lo = __shfl_xor(l, o), mn = fmaxf(m, mo);
+      l = l * __builtin_amdgcn_exp2f(m - mn) + lo * __builtin_amdgcn_exp2f(mo - mn);
+      m = mn;
+    }
     f32x4 x{0.f, 0.f, 0.f, 0.f};
-    if (d < HD)
-      for (int r = r0 + (FEW ? grp : 0); r <= r1; r += FEW ? 8 : 1) {
-        const float a = __builtin_amdgcn_exp2f(ml(r, c).x - m);
-        const f32x4 y = *reinterpret_cast<const f32x4*>(slot(r) + (size_t)c * HD + d);
+    if (d < HD) {
+#pragma unroll 4
+      for (int r = p.r0 + grp; r <= p.r1; r += 8) {
+        const float a = __builtin_amdgcn_exp2f(p.stats(r)[c].x - m);
+        const f32x4 y = *reinterpret_cast<const f32x4*>(p.at(r) + (size_t)c * HD + d);
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] += y[e] * a;
       }
-    if constexpr (FEW) {
-      __syncthreads();
-      osum[grp][l5] = x;
-      __syncthreads();
-      x = osum[0][l5];
-#pragma unroll
-      for (int k = 1; k < 8; ++k)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] += osum[k][l5][e];
-      if (grp != 0) continue;
     }
+    __syncthreads();
+    osum[grp][l5] = x;
+    __syncthreads();
+    if (grp != 0) continue;
+#pragma unroll
+    for (int k = 1; k < 8; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += osum[k][l5][e];
     const float inv = l == 0.f ? 0.f : 1.f / l;
     if (d < HD) {
-      const int row = bt.first_row(b) + row0 + c / bt.nq;
+      const int row = bt.first_row(b) + c / bt.nq;
       bf16* dst = out + (((size_t)row * bt.H + h) * bt.nq + c % bt.nq) * HD + d;
       *reinterpret_cast<bf16x4*>(dst) = bf16x4{(bf16)(x[0] * inv), (bf16)(x[1] * inv),
                                                (bf16)(x[2] * inv), (bf16)(x[3] * inv)};
     }
     if (stat != nullptr && l5 == 0)
-      stat[((size_t)h * bt.N + bt.first_row(b) + row0) * bt.nq + c] = float2{m, inv};
+      stat[((size_t)h * bt.N + bt.first_row(b)) * bt.nq + c] = float2{m, inv};
   }
 }
 
-// ---- mass ---------------------------------------------------------------------------
-// Mass: one workgroup per (page, group, sequence); the scores again, each
-// probability from its column's maximum and sum, summed over the columns.
+// Many columns: one workgroup per (32 columns of a tile, group, sequence), 8 threads a
+// column.
 template <int HD>
-__global__ __launch_bounds__(kAttThr) void cache_mass_kernel(
+__global__ __launch_bounds__(256) void cache_join_tile_kernel(Units w, int ranges, int least,
+                                                              const float* __restrict__ part,
+                                                              bf16* __restrict__ out,
+                                                              float2* __restrict__ stat) {
+  constexpr int NV = HD / 32;  // 4-dim pieces of a thread
+  const CacheBatch& bt = w.bt;
+  const int t = blockIdx.x / (kTileCols / 32), h = blockIdx.y, b = blockIdx.z;
+  const int c = blockIdx.x % (kTileCols / 32) * 32 + (threadIdx.x >> 3), l3 = threadIdx.x & 7;
+  const int rows = w.rows(b);
+  if (rows <= 0 || t >= w.tiles(rows)) return;
+  const int ctx = bt.context(b), row0 = t << w.log2r;
+  const int ncol = (min(rows, (t + 1) << w.log2r) - row0) * bt.nq;
+  const int np = w.pages(ctx, rows, t);
+  Parts p{part, kTileCols, HD};
+  if (!find_parts(w, ranges, least, w.prefix[b] + w.group(b) * h + w.before(ctx, t), np, p) ||
+      c >= ncol)
+    return;
+  float m = kMFloor, l = 0.f;
+#pragma unroll 4
+  for (int r = p.r0; r <= p.r1; ++r) m = fmaxf(m, p.stats(r)[c].x);
+  f32x4 x[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) x[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+  for (int r = p.r0; r <= p.r1; ++r) {
+    const float2 z = p.stats(r)[c];
+    const float a = __builtin_amdgcn_exp2f(z.x - m);
+    l += z.y * a;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const f32x4 y = *reinterpret_cast<const f32x4*>(p.at(r) + (size_t)c * HD + 4 * (l3 + 8 * k));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[k][e] += y[e] * a;
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const int row = bt.first_row(b) + row0 + c / bt.nq;
+  bf16* dst = out + (((size_t)row * bt.H + h) * bt.nq + c % bt.nq) * HD;
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+    *reinterpret_cast<bf16x4*>(dst + 4 * (l3 + 8 * k)) =
+        bf16x4{(bf16)(x[k][0] * inv), (bf16)(x[k][1] * inv), (bf16)(x[k][2] * inv),
+               (bf16)(x[k][3] * inv)};
+  if (stat != nullptr && l3 == 0)
+    stat[((size_t)h * bt.N + bt.first_row(b) + row0) * bt.nq + c] = float2{m, inv};
+}
+
+// ---- mass ---------------------------------------------------------------------------
+// A token's mass is the sum of its probabilities over the columns, each from its score
+// and its column's final maximum and sum, so it follows the joining.  With few columns the
+// scores were kept; else they are formed again.
+
+// Few columns: the ranges of the attention; a wave takes every fourth page, a lane a token.
+__global__ __launch_bounds__(kAttThr) void cache_mass_few_kernel(
+    const float* __restrict__ score, Units w, int least, int part_cols, float c_log2,
+    const float2* __restrict__ stat, const float* __restrict__ mass_in,
+    float* __restrict__ mass_out) {
+  __shared__ int found;
+  const CacheBatch& bt = w.bt;
+  const int lane = lane_id(), wave = threadIdx.x >> 6;
+  const long long total = w.prefix[bt.B], per = range_units(total, gridDim.x, least);
+  long long unit = blockIdx.x * per;
+  if (unit >= total) return;
+  for (int i = threadIdx.x; i < bt.B; i += kAttThr)
+    if (w.prefix[i] <= unit && unit < w.prefix[i + 1]) found = i;
+  __syncthreads();
+  int b = found;
+  int left = (int)min(per, total - unit);
+  int rows = w.rows(b), ctx = bt.context(b), np = w.pages(ctx, rows, 0);
+  const int off = (int)(unit - w.prefix[b]);
+  int h = off / np, blk0 = off % np;
+  while (true) {
+    const int blk1 = min(np, blk0 + left), ncol = rows * bt.nq;
+    float2 z{0.f, 0.f};  // of column `lane`
+    if (lane < ncol) z = stat[((size_t)h * bt.N + bt.first_row(b)) * bt.nq + lane];
+    for (int blk = blk0 + wave; blk < blk1; blk += kAttWaves) {
+      const int page = bt.page(b, blk), slot = blk * kPage + lane;
+      if (page < 0) continue;
+      const size_t at = ((size_t)page * bt.H + h) * kPage + lane;
+      float x = slot < ctx ? mass_in[at] : 0.f, y = 0.f;
+      const float* s = score + (unit + blk - blk0) * part_cols * kPage + lane;
+      for (int c = 0; c < ncol; ++c) {
+        const float m = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(z.x), c));
+        const float inv = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(z.y), c));
+        y += __builtin_amdgcn_exp2f(fmaf(s[c * kPage], c_log2, -m)) * inv;
+      }
+      if (slot < min(ctx + rows, bt.cap())) mass_out[at] = x + y;
+    }
+    left -= blk1 - blk0;
+    unit += blk1 - blk0;
+    if (left <= 0) return;
+    blk0 = 0;
+    if (++h == bt.H) {
+      h = 0;
+      do {
+        if (++b >= bt.B) return;
+        rows = w.rows(b);
+      } while (rows <= 0);
+      ctx = bt.context(b);
+      np = w.pages(ctx, rows, 0);
+    }
+  }
+}
+
+// Any columns: one workgroup per (two pages, group, sequence), a wave for 32 keys, held in
+// registers as A operand of v_mfma_f32_32x32x16_bf16; tiles of 64 columns go by through
+// LDS (256-byte rows, 16-byte chunk c in slot c ^ (column & 15)).  The exponentials are
+// the bound: they take longer than the scores' MFMAs.
+constexpr int kMassThr = 256, kMassCols = 64;
+
+template <int HD>
+__global__ __launch_bounds__(kMassThr) void cache_mass_kernel(
     const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const float* __restrict__ kv_scale,
     CacheBatch bt, int max_rows, float c_log2, const float2* __restrict__ stat,
     const float* __restrict__ mass_in, float* __restrict__ mass_out) {
-  using F = PageFrags<HD>;
-  __shared__ float sum[kAttWaves][kPage];
+  constexpr int NST = HD / 16, CPR = HD / 8;
+  constexpr int NQ = kMassCols * CPR / kMassThr;  // 16-byte pieces of a thread and tile
+  static_assert(kMassCols * CPR % kMassThr == 0, "whole pieces");
+  __shared__ __align__(16) unsigned char smem[2][kMassCols * 256];
+  __shared__ float sum[kMassThr / kWave][32];
   const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
-  const int blk = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
-  const int n = lane & 15, g = lane >> 4;
+  const int qi = lane & 31, hl = lane >> 5;
+  const int h = blockIdx.x % bt.H, b = blockIdx.y, blk0 = blockIdx.x / bt.H * 2;
   const int rows = min(bt.rows(b), max_rows), ctx = bt.context(b);
   const int len = min(ctx + rows, bt.cap());
-  if (rows == 0 || blk * kPage >= len) return;
-  const int page = bt.page(b, blk);
-  if (page < 0) return;
-  const size_t pg = (size_t)page * bt.H + h;
-  F f;
-  f.load_k(kc + pg * (kPage * HD), lane);
-  const float ks = kv_scale[pg * 2];
-  const int ncol = rows * bt.nq, k0 = blk * kPage + 16 * g;
+  if (rows == 0 || blk0 * kPage >= len) return;
+  const int key0 = blk0 * kPage + wave * 32;  // the wave's first key
+  const int page = bt.page(b, key0 / kPage);
+  const bool works = page >= 0 && key0 < len;  // (wave-uniform)
+  const size_t pg = (size_t)max(page, 0) * bt.H + h;
+  // key qi; in steps st, st + 1 the lane halves hold dims 32 (st / 2) + 16 hl + 8 (st % 2)
+  bf16x8 kf[NST];
+  {
+    const float ks = works ? kv_scale[pg * 2] : 0.f;
+    const uint8_t* row = kc + pg * (kPage * HD) + ((wave & 1) * 32 + qi) * HD + 16 * hl;
+#pragma unroll
+    for (int st = 0; st < NST; st += 2) {
+      u32x4 x = zero_u32x4();
+      if (works) x = *reinterpret_cast<const u32x4*>(row + 16 * st);
+      kf[st] = codes_to_bf16(x[0], x[1], ks);
+      kf[st + 1] = codes_to_bf16(x[2], x[3], ks);
+    }
+  }
+  const int ncol = rows * bt.nq;
   const size_t qrow = ((size_t)h * bt.N + bt.first_row(b)) * bt.nq;
   float acc[16];
 #pragma unroll
-  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-  // columns before the first that sees the page are left out
-  const int first = max(blk * kPage - ctx, 0) * bt.nq / 16;
-  for (int t0 = first + wave; t0 * 16 < ncol; t0 += kAttWaves) {
-    const int col = t0 * 16 + n;
-    bf16x8 qf[F::NST];
-    load_q<HD>(q + qrow * HD, col, ncol, g, qf);
-    const float2 z = col < ncol ? stat[qrow + col] : float2{0.f, 0.f};  // maximum, 1 / sum
-    const int seen = col < ncol ? min(ctx + col / bt.nq + 1, bt.cap()) : 0;
-    f32x4 s[4];
-    f.scores(qf, ks, s);
+  for (int v = 0; v < 16; ++v) acc[v] = 0.f;
+  // tiles before the first column that sees the pages are left out
+  const long long c_first = (long long)max(blk0 * kPage - ctx, 0) * bt.nq;
+  const int t0 = (int)(c_first / kMassCols), t1 = (ncol + kMassCols - 1) / kMassCols;
+  u32x4 qr[NQ];
+  float2 z[2], zn[2];
+  auto fetch = [&](int t) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int i = 0; i < NQ; ++i) {
+      const int p = i * kMassThr + tid, c = t * kMassCols + p / CPR;
+      qr[i] = zero_u32x4();
+      if (c < ncol) qr[i] = *reinterpret_cast<const u32x4*>(q + (qrow + c) * HD + p % CPR * 8);
+    }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x = __builtin_amdgcn_exp2f(fmaf(s[t][e], c_log2, -z.x)) * z.y;
-        acc[4 * t + e] += k0 + 4 * t + e < seen ? x : 0.f;
+    for (int i = 0; i < 2; ++i) {
+      const int c = t * kMassCols + i * 32 + qi;
+      zn[i] = c < ncol ? stat[qrow + c] : float2{0.f, 0.f};
+    }
+  };
+  auto stage = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      const int p = i * kMassThr + tid, c = p / CPR;
+      *reinterpret_cast<u32x4*>(&smem[t & 1][c * 256 + (((p % CPR) ^ (c & 15)) << 4)]) = qr[i];
+    }
+    z[0] = zn[0];
+    z[1] = zn[1];
+  };
+  if (t0 < t1) {
+    fetch(t0);
+    stage(t0);
+  }
+  for (int t = t0; t < t1; ++t) {
+    __syncthreads();
+    if (t + 1 < t1) fetch(t + 1);
+    if (works) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int c = i * 32 + qi, col = t * kMassCols + c;
+        f32x16 s;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) s[v] = 0.f;
+#pragma unroll
+        for (int st = 0; st < NST; ++st) {
+          const int ch = 4 * (st / 2) + 2 * hl + st % 2;
+          const bf16x8 qf =
+              *reinterpret_cast<const bf16x8*>(&smem[t & 1][c * 256 + ((ch ^ (c & 15)) << 4)]);
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[st], qf, s, 0, 0, 0);
+        }
+        // (the tile's first column sees the fewest)
+        if (ctx + t * kMassCols / bt.nq + 1 < min(key0 + 32, len + 1)) {
+          const int seen = col < ncol ? ctx + col / bt.nq + 1 : 0;
+#pragma unroll
+          for (int v = 0; v < 16; ++v)
+            if (key0 + 8 * (v >> 2) + 4 * hl + (v & 3) >= seen) s[v] = -__builtin_inff();
+        }
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          acc[v] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[v], c_log2, -z[i].x)), z[i].y, acc[v]);
       }
+    }
+    if (t + 1 < t1) stage(t + 1);
   }
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {
+  for (int v = 0; v < 16; ++v) {
 #pragma unroll
-    for (int o = 1; o < 16; o <<= 1) acc[e] += __shfl_xor(acc[e], o);
-    if (n == 0) sum[wave][16 * g + e] = acc[e];
+    for (int o = 1; o < 32; o <<= 1) acc[v] += __shfl_xor(acc[v], o);
+    if (qi == 0) sum[wave][8 * (v >> 2) + 4 * hl + (v & 3)] = acc[v];
   }
   __syncthreads();
-  const int slot = blk * kPage + tid;
-  if (tid < kPage && slot < len) {
-    float x = slot < ctx ? mass_in[pg * kPage + tid] : 0.f;
-    float y = 0.f;
-#pragma unroll
-    for (int w = 0; w < kAttWaves; ++w) y += sum[w][tid];
-    mass_out[pg * kPage + tid] = x + y;
+  const int slot = key0 + lane;
+  if (works && lane < 32 && slot < len) {
+    const size_t at = pg * kPage + (wave & 1) * 32 + lane;
+    mass_out[at] = (slot < ctx ? mass_in[at] : 0.f) + sum[wave][lane];
   }
 }
 
@@ -797,40 +976,45 @@ int device_cus() {
 }
 
 // Host side of the two forms: ranges (workgroups) and scratch.
-struct AttnPlan {
-  bool few, many;           // launches
-  int few_ranges, many_ranges, few_cols, log2r, max_tiles;
-  size_t few_prefix, many_prefix, few_part, many_part, stat, total;
-};
 constexpr int kFewLeast = 4;   // pages of a range at least: one for each wave
 constexpr int kManyLeast = 2;
+// the scores of few columns are kept for the mass up to this many bytes; beyond, they
+// are formed again
+constexpr size_t kScoreBytes = (size_t)256 << 20;
+
+struct AttnPlan {
+  bool few, scores;
+  int ranges, cols, log2r, tiles;
+  size_t prefix, part, stat, score, total;
+};
 
 AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_rows, bool mass,
                    int cus) {
   AttnPlan p{};
-  p.many = (long long)max_rows * nq > kFewCols;
-  p.few = nq <= kFewCols;
-  p.few_cols = std::min(kFewCols, max_rows * nq);
-  const long long most = (long long)B * H * max_blocks;  // few units at most
-  p.few_ranges = (int)std::min<long long>(4LL * cus, (most + kFewLeast - 1) / kFewLeast);
-  p.many_ranges = cus;
-  while ((2 << p.log2r) * nq <= kTileCols) ++p.log2r;
-  p.max_tiles = ceil_div(max_rows, 1 << p.log2r);
-  size_t off = 0;
-  auto take = [&](size_t& field, size_t bytes) {
-    field = off;
-    off = align_up(off + bytes, 256);
-  };
+  p.few = (long long)max_rows * nq <= kFewCols;
+  const long long pages = (long long)B * H * max_blocks;
   if (p.few) {
-    take(p.few_prefix, (size_t)(B + 1) * 8);
-    take(p.few_part, 2 * (size_t)p.few_ranges * part_floats(p.few_cols, hd) * 4);
+    p.cols = max_rows * nq;
+    p.ranges = (int)std::min<long long>(4LL * cus, (pages + kFewLeast - 1) / kFewLeast);
+    p.log2r = -1;
+  } else {
+    p.cols = kTileCols;
+    p.ranges = cus;
+    while ((2 << p.log2r) * nq <= kTileCols) ++p.log2r;
+    p.tiles = ceil_div(max_rows, 1 << p.log2r);
   }
-  if (p.many) {
-    take(p.many_prefix, (size_t)(B + 1) * 8);
-    take(p.many_part, 2 * (size_t)p.many_ranges * part_floats(kTileCols, hd) * 4);
+  auto take = [&](size_t& field, size_t bytes) {
+    field = p.total;
+    p.total = align_up(p.total + bytes, 256);
+  };
+  take(p.prefix, (size_t)(B + 1) * 8);
+  take(p.part, 2 * (size_t)p.ranges * part_floats(p.cols, hd) * 4);
+  if (mass) {
+    take(p.stat, (size_t)H * N * nq * sizeof(float2));
+    const size_t bytes = (size_t)pages * p.cols * kPage * 4;
+    p.scores = p.few && bytes <= kScoreBytes;
+    if (p.scores) take(p.score, bytes);
   }
-  if (mass) take(p.stat, (size_t)H * N * nq * sizeof(float2));
-  p.total = off;
   return p;
 }
 }  // namespace
@@ -844,43 +1028,46 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
                                   const int32_t* row_start, const float* mass_in, float* mass_out,
                                   void* out, void* scratch, hipStream_t s) {
   const CacheBatch bt{a.H, a.B, N, nq, a.n_pages, a.max_blocks, a.block_table, a.length, row_start};
+  static const int cus = std::min(device_cus(), kMaxCus);
   const AttnPlan p = attn_plan(a.H, a.B, N, nq, a.hd, a.max_blocks, max_rows, mass_out != nullptr,
-                               std::min(device_cus(), kMaxCus));
+                               cus);
   unsigned char* base = static_cast<unsigned char*>(scratch);
+  const Units w{bt, max_rows, p.log2r, reinterpret_cast<long long*>(base + p.prefix)};
+  float* part = reinterpret_cast<float*>(base + p.part);
   float2* stat = mass_out != nullptr ? reinterpret_cast<float2*>(base + p.stat) : nullptr;
+  float* score = p.scores ? reinterpret_cast<float*>(base + p.score) : nullptr;
   const float c_log2 = 1.4426950408889634f / sqrtf((float)a.hd);
   const bf16* qb = static_cast<const bf16*>(q);
   bf16* ob = static_cast<bf16*>(out);
   auto go = [&](auto hdv) {
     constexpr int HD = decltype(hdv)::value;
     if (p.few) {
-      const Units w{bt, max_rows, -1, reinterpret_cast<long long*>(base + p.few_prefix)};
-      float* part = reinterpret_cast<float*>(base + p.few_part);
       {
         ProfileScope ps("cache_attn_few", s);
-        FOE_LAUNCH(cache_attn_few_kernel<HD>, dim3(p.few_ranges), dim3(kAttThr), 0, s, qb, a.k, a.v,
-                   a.kv_scale, w, kFewLeast, p.few_cols, c_log2, ob, stat, part);
+        FOE_LAUNCH(cache_attn_few_kernel<HD>, dim3(p.ranges), dim3(kAttThr), 0, s, qb, a.k, a.v,
+                   a.kv_scale, w, kFewLeast, p.cols, c_log2, ob, stat, part, score);
       }
       ProfileScope ps("cache_join_few", s);
-      FOE_LAUNCH((cache_join_kernel<HD, true>), dim3(1, a.H, a.B), dim3(256), 0, s, w, p.few_ranges,
-                 kFewLeast, p.few_cols, part, ob, stat);
-    }
-    if (p.many) {
-      const Units w{bt, max_rows, p.log2r, reinterpret_cast<long long*>(base + p.many_prefix)};
-      float* part = reinterpret_cast<float*>(base + p.many_part);
+      FOE_LAUNCH(cache_join_few_kernel<HD>, dim3(a.H, a.B), dim3(256), 0, s, w, p.ranges, kFewLeast,
+                 p.cols, part, ob, stat);
+    } else {
       {
         ProfileScope ps("cache_attn_tile", s);
-        FOE_LAUNCH(cache_attn_tile_kernel<HD>, dim3(p.many_ranges), dim3(kTileThr), 0, s, qb, a.k,
-                   a.v, a.kv_scale, w, kManyLeast, c_log2, ob, stat, part);
+        FOE_LAUNCH(cache_attn_tile_kernel<HD>, dim3(p.ranges), dim3(kTileThr), 0, s, qb, a.k, a.v,
+                   a.kv_scale, w, kManyLeast, c_log2, ob, stat, part);
       }
       ProfileScope ps("cache_join_tile", s);
-      FOE_LAUNCH((cache_join_kernel<HD, false>), dim3(p.max_tiles * (kTileCols / 32), a.H, a.B),
-                 dim3(256), 0, s, w, p.many_ranges, kManyLeast, kTileCols, part, ob, stat);
+      FOE_LAUNCH(cache_join_tile_kernel<HD>, dim3(p.tiles * (kTileCols / 32), a.H, a.B), dim3(256),
+                 0, s, w, p.ranges, kManyLeast, part, ob, stat);
     }
-    if (mass_out != nullptr) {
+    if (score != nullptr) {
+      ProfileScope ps("cache_mass_few", s);
+      FOE_LAUNCH(cache_mass_few_kernel, dim3(p.ranges), dim3(kAttThr), 0, s, score, w, kFewLeast,
+                 p.cols, c_log2, stat, mass_in, mass_out);
+    } else if (mass_out != nullptr) {
       ProfileScope ps("cache_mass", s);
-      FOE_LAUNCH(cache_mass_kernel<HD>, dim3(a.max_blocks, a.H, a.B), dim3(kAttThr), 0, s, qb, a.k,
-                 a.kv_scale, bt, max_rows, c_log2, stat, mass_in, mass_out);
+      FOE_LAUNCH(cache_mass_kernel<HD>, dim3(ceil_div(a.max_blocks, 2) * a.H, a.B), dim3(kMassThr),
+                 0, s, qb, a.k, a.kv_scale, bt, max_rows, c_log2, stat, mass_in, mass_out);
     }
   };
   if (a.hd == 96) go(std::integral_constant<int, 96>{});

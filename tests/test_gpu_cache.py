@@ -402,6 +402,29 @@ def test_attention_absent_pages_and_garbage_behind_the_end(rows):
     assert (host(out)[rs[2]:] == 0).all()
 
 
+def test_attention_wide_table():
+    """A table with room for far more pages than there are (the scores of so many are not
+    kept for the mass): the same results as with a narrow one."""
+    rng = np.random.default_rng(19)
+    H, nq, hd, seqs = 2, 8, 128, [(300, 2), (0, 1), (700, 1)]
+    ctx, rs, table, pages = batch(rng, seqs)
+    dev = to_dev(random_pool(rng, pages, H, hd))
+    wide = np.full((3, 12000), -1, dtype=np.int32)
+    wide[:, :table.shape[1]] = table
+    q = bf16(rng.normal(size=(H, rs[-1], nq, hd)))
+    say("wide table")
+    outs = []
+    for t in (table, wide):
+        m = torch.full_like(dev["mass"], -7.0)
+        outs.append((foe.cache_attention(q, dev["k"], dev["v"], dev["kv_scale"], ints(t), ints(ctx),
+                                         ints(rs), 2, mass_in=dev["mass"], mass_out=m), m))
+    torch.cuda.synchronize()
+    pool = to_host(dev)
+    for o, m in outs:
+        check_attention(pool, table, ctx, rs, q, o, m)
+    assert torch.equal(outs[0][0], outs[1][0])
+
+
 def test_attention_rows_past_max_rows_are_left():
     rng = np.random.default_rng(15)
     pool, table, ctx, rs, q, out, mass = run_attention(rng, 1, 2, 128, [(100, 3), (50, 1)], True,
