@@ -14,7 +14,7 @@
 // grid that fills the chip, whatever the lengths are.  A workgroup walks the tiles in
 // its range; a tile that lies in one range is written at once, the others leave their
 // unnormalised parts, which a second launch joins in page order.  (One workgroup per
-// tile of 16 columns: 1151 us instead of 200 for four sequences of 131072 tokens, 8 groups.)
+// tile of 16 columns: 1151 us instead of 195 for four sequences of 131072 tokens, 8 groups.)
 #include <algorithm>
 #include <type_traits>
 
@@ -206,18 +206,172 @@ __device__ __forceinline__ void load_q(const bf16* q, int col, int ncol, int g, 
 // (slot 2 r), and of its last one if another (2 r + 1).
 __host__ __device__ inline size_t part_floats(int cols, int hd) { return (size_t)cols * (hd + 2); }
 
-template <int HD>
-__global__ __launch_bounds__(kAttThr) void cache_attn_few_kernel(
+struct AttnOut {
+  bf16* out;
+  float2* stat;      // (maximum, 1 / sum) of each column, or null
+  float* part;
+  int part_cols;
+};
+
+template <int HD, int NW>
+struct FewLds {
+  float mm[NW][16], ll[NW][16];
+  float oo[NW][16][HD + 4];  // (rows of other bank groups)
+};
+
+// Pages blk0 .. blk1-1 of at most 16 columns (rows row0 .. of sequence b, group h), dealt to
+// the NW waves of the workgroup; `slot` is where a part goes, `score` the scores of page
+// blk0 or null.
+template <int HD, int NW>
+__device__ __forceinline__ void few_columns(
     const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
-    const float* __restrict__ kv_scale, Units w, int least, int part_cols, float c_log2,
-    bf16* __restrict__ out, float2* __restrict__ stat, float* __restrict__ part,
-    float* __restrict__ score) {
+    const float* __restrict__ kv_scale, const CacheBatch& bt, int b, int h, int rows, int row0,
+    int ctx, int np, int blk0, int blk1, float c_log2, const AttnOut& o, size_t slot,
+    float* __restrict__ score, FewLds<HD, NW>& lds) {
   using F = PageFrags<HD>;
-  __shared__ float mm[kAttWaves][16], ll[kAttWaves][16];
-  __shared__ __align__(16) float oo[kAttWaves][HD][16];
-  const CacheBatch& bt = w.bt;
   const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
   const int n = lane & 15, g = lane >> 4;
+  const int ncol = (rows - row0) * bt.nq;
+  const size_t qrow = ((size_t)h * bt.N + bt.first_row(b) + row0) * bt.nq;
+  bf16x8 qf[F::NST];
+  load_q<HD>(q + qrow * HD, n, ncol, g, qf);
+  const int len = min(ctx + rows, bt.cap());  // tokens the cache holds now
+  const int seen = n < ncol ? min(ctx + row0 + n / bt.nq + 1, bt.cap()) : 0;
+  const int fewest = min(ctx + row0 + 1, bt.cap());  // that a column sees
+  f32x4 oacc[F::NDT];
+#pragma unroll
+  for (int dt = 0; dt < F::NDT; ++dt) oacc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m_run = kMFloor, l_run = 0.f;
+  // page numbers and scales of the wave's next 64 pages, one a lane
+  int pid = -1;
+  float2 psc{0.f, 0.f};
+  F fn;
+  auto fetch = [&](int i) {  // the wave's i-th page; an absent one loads page 0
+    if ((i & 63) == 0) {
+      const int blk = blk0 + wave + NW * (i + lane);
+      pid = blk < blk1 ? bt.page(b, blk) : -1;
+      if (pid >= 0)
+        psc = *reinterpret_cast<const float2*>(kv_scale + ((size_t)pid * bt.H + h) * 2);
+    }
+    const int page = __builtin_amdgcn_readlane(pid, i & 63);
+    const size_t pg = ((size_t)max(page, 0) * bt.H + h) * (kPage * HD);
+    fn.load_k(kc + pg, lane);
+    fn.load_v(vc + pg, lane);
+  };
+  const int mine = (blk1 - blk0 - wave + NW - 1) / NW;  // pages of this wave
+  if (mine > 0) fetch(0);
+  for (int i = 0; i < mine; ++i) {
+    const int blk = blk0 + wave + NW * i;
+    const int page = __builtin_amdgcn_readlane(pid, i & 63);
+    const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(psc.x), i & 63));
+    const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(psc.y), i & 63));
+    F f = fn;
+    if (i + 1 < mine) fetch(i + 1);
+    if (page < 0) continue;
+    f32x4 s[4];
+    f.scores(qf, ks, s);
+    const int k0 = blk * kPage + 16 * g;
+    if ((blk + 1) * kPage > fewest) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (k0 + 4 * t + e >= seen) s[t][e] = -__builtin_inff();
+      // slots past the last token hold anything: 0 * NaN is NaN
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int in = len - (k0 + 4 * e);
+        const uint32_t m = in >= 4 ? 0xffffffffu : in <= 0 ? 0u : (1u << (8 * in)) - 1;
+#pragma unroll
+        for (int dt = 0; dt < F::NDT; ++dt) f.v[dt][e] &= m;
+      }
+    }
+    if (score != nullptr && n < ncol) {
+      float* to = score + ((size_t)(blk - blk0) * o.part_cols + n) * kPage + 16 * g;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4*>(to + 4 * t) = s[t];
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[t][e]);
+    mx = fmaxf(mx, __shfl_xor(mx, 16));
+    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    // the maximum moves only when a page exceeds it by 2^8: probabilities stay below
+    // that, and the sums are rescaled on those pages alone
+    const float mxs = mx * c_log2;
+    const bool need = mxs > m_run + 8.f;
+    if (__builtin_amdgcn_ballot_w64(need)) {
+      const float m_new = need ? mxs : m_run;
+      const float a = __builtin_amdgcn_exp2f(m_run - m_new);
+      m_run = m_new;
+      l_run *= a;
+#pragma unroll
+      for (int dt = 0; dt < F::NDT; ++dt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) oacc[dt][e] *= a;
+    }
+    bf16x8 p[2];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[t][e], c_log2, -m_run));
+        l_run += x;
+        p[t >> 1][4 * (t & 1) + e] = (bf16)x;
+      }
+#pragma unroll
+    for (int dt = 0; dt < F::NDT; ++dt)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        oacc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            codes_to_bf16(f.v[dt][2 * u], f.v[dt][2 * u + 1], vs), p[u], oacc[dt], 0, 0, 0);
+  }
+  // the waves' states, merged in wave order
+  l_run += __shfl_xor(l_run, 16);
+  l_run += __shfl_xor(l_run, 32);
+  __syncthreads();  // what was in LDS before has been read
+  if (g == 0) lds.mm[wave][n] = m_run, lds.ll[wave][n] = l_run;
+  if (n < ncol) {
+#pragma unroll
+    for (int dt = 0; dt < F::NDT; ++dt)
+      *reinterpret_cast<f32x4*>(&lds.oo[wave][n][16 * dt + 4 * g]) = oacc[dt];
+  }
+  __syncthreads();
+  const bool whole = blk0 == 0 && blk1 == np;
+  float* pt = o.part + slot * part_floats(o.part_cols, HD);
+  for (int i = tid; i < ncol * HD; i += NW * kWave) {
+    const int c = i / HD, d = i % HD;
+    float m = lds.mm[0][c], l = 0.f, x = 0.f;
+#pragma unroll
+    for (int v = 1; v < NW; ++v) m = fmaxf(m, lds.mm[v][c]);
+#pragma unroll
+    for (int v = 0; v < NW; ++v) {
+      const float a = __builtin_amdgcn_exp2f(lds.mm[v][c] - m);
+      l += lds.ll[v][c] * a;
+      x += lds.oo[v][c][d] * a;
+    }
+    if (whole) {
+      // a column that sees no token gives zeros
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const int row = bt.first_row(b) + row0 + c / bt.nq;
+      o.out[(((size_t)row * bt.H + h) * bt.nq + c % bt.nq) * HD + d] = (bf16)(x * inv);
+      if (d == 0 && o.stat != nullptr) o.stat[qrow + c] = float2{m, inv};
+    } else {
+      pt[i] = x;
+      if (d == 0) reinterpret_cast<float2*>(pt + o.part_cols * HD)[c] = float2{m, l};
+    }
+  }
+}
+
+template <int HD>
+__global__ __launch_bounds__(kAttThr, 2) void cache_attn_few_kernel(
+    const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
+    const float* __restrict__ kv_scale, Units w, int least, float c_log2, AttnOut o,
+    float* __restrict__ score) {
+  __shared__ FewLds<HD, kAttWaves> lds;
+  const CacheBatch& bt = w.bt;
   long long total, off;
   int b;
   locate<kAttThr>(w, gridDim.x, blockIdx.x, least, total, b, off);
@@ -227,135 +381,17 @@ __global__ __launch_bounds__(kAttThr) void cache_attn_few_kernel(
   int left = (int)min((long long)per, total - unit);
   int rows = w.rows(b), ctx = bt.context(b), np = w.pages(ctx, rows, 0);
   int h = (int)(off / np), blk0 = (int)(off % np);
-  bool first_tile = true;
+  size_t slot = 2 * (size_t)blockIdx.x;
   while (true) {
     const int blk1 = min(np, blk0 + left);
-    const int ncol = rows * bt.nq;
-    const size_t qrow = ((size_t)h * bt.N + bt.first_row(b)) * bt.nq;
-    bf16x8 qf[F::NST];
-    load_q<HD>(q + qrow * HD, n, ncol, g, qf);
-    const int len = min(ctx + rows, bt.cap());  // tokens the cache holds now
-    const int seen = n < ncol ? min(ctx + n / bt.nq + 1, bt.cap()) : 0;
-    const int fewest = min(ctx + 1, bt.cap());  // that a column sees
-    f32x4 oacc[F::NDT];
-#pragma unroll
-    for (int dt = 0; dt < F::NDT; ++dt) oacc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m_run = kMFloor, l_run = 0.f;
-    for (int blk = blk0 + wave; blk < blk1; blk += kAttWaves) {
-      const int page = bt.page(b, blk);
-      if (page < 0) continue;
-      const size_t pg = (size_t)page * bt.H + h;
-      const float ks = kv_scale[pg * 2], vs = kv_scale[pg * 2 + 1];
-      F f;
-      f.load_k(kc + pg * (kPage * HD), lane);
-      f.load_v(vc + pg * (kPage * HD), lane);
-      f32x4 s[4];
-      f.scores(qf, ks, s);
-      const int k0 = blk * kPage + 16 * g;
-      if ((blk + 1) * kPage > fewest) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (k0 + 4 * t + e >= seen) s[t][e] = -__builtin_inff();
-        // slots past the last token hold anything: 0 * NaN is NaN
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int in = len - (k0 + 4 * e);
-          const uint32_t m = in >= 4 ? 0xffffffffu : in <= 0 ? 0u : (1u << (8 * in)) - 1;
-#pragma unroll
-          for (int dt = 0; dt < F::NDT; ++dt) f.v[dt][e] &= m;
-        }
-      }
-      if (score != nullptr && n < ncol) {
-        float* to = score + ((unit + blk - blk0) * part_cols + n) * kPage + 16 * g;
-#pragma unroll
-        for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4*>(to + 4 * t) = s[t];
-      }
-      float mx = s[0][0];
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[t][e]);
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
-      // the maximum moves only when a page exceeds it by 2^8: probabilities stay below
-      // that, and the sums are rescaled on those pages alone
-      const float mxs = mx * c_log2;
-      const bool need = mxs > m_run + 8.f;
-      if (__builtin_amdgcn_ballot_w64(need)) {
-        const float m_new = need ? mxs : m_run;
-        const float a = __builtin_amdgcn_exp2f(m_run - m_new);
-        m_run = m_new;
-        l_run *= a;
-#pragma unroll
-        for (int dt = 0; dt < F::NDT; ++dt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) oacc[dt][e] *= a;
-      }
-      bf16x8 p[2];
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float x = __builtin_amdgcn_exp2f(fmaf(s[t][e], c_log2, -m_run));
-          l_run += x;
-          p[t >> 1][4 * (t & 1) + e] = (bf16)x;
-        }
-#pragma unroll
-      for (int dt = 0; dt < F::NDT; ++dt)
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-          oacc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-              codes_to_bf16(f.v[dt][2 * u], f.v[dt][2 * u + 1], vs), p[u], oacc[dt], 0, 0, 0);
-    }
-    // the four waves' states, merged in wave order
-    l_run += __shfl_xor(l_run, 16);
-    l_run += __shfl_xor(l_run, 32);
-    __syncthreads();  // the previous tile's merge has been read
-    if (g == 0) mm[wave][n] = m_run, ll[wave][n] = l_run;
-    if (n < ncol) {
-#pragma unroll
-      for (int dt = 0; dt < F::NDT; ++dt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) oo[wave][16 * dt + 4 * g + e][n] = oacc[dt][e];
-    }
-    __syncthreads();
-    const int c = tid >> 4;  // column; its 16 threads take every 16th dim
-    if (c < ncol) {
-      float m = mm[0][c], l = 0.f, a[kAttWaves];
-#pragma unroll
-      for (int v = 1; v < kAttWaves; ++v) m = fmaxf(m, mm[v][c]);
-#pragma unroll
-      for (int v = 0; v < kAttWaves; ++v) {
-        a[v] = __builtin_amdgcn_exp2f(mm[v][c] - m);
-        l += ll[v][c] * a[v];
-      }
-      const bool whole = blk0 == 0 && blk1 == np;
-      // a column that sees no token gives zeros
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      const int row = bt.first_row(b) + c / bt.nq;
-      bf16* dst = out + (((size_t)row * bt.H + h) * bt.nq + c % bt.nq) * HD;
-      float* pt = part + (2 * (size_t)blockIdx.x + (first_tile ? 0 : 1)) * part_floats(part_cols, HD);
-#pragma unroll
-      for (int i = 0; i < HD / 16; ++i) {
-        const int d = i * 16 + (tid & 15);
-        float x = 0.f;
-#pragma unroll
-        for (int v = 0; v < kAttWaves; ++v) x += oo[v][d][c] * a[v];
-        if (whole) dst[d] = (bf16)(x * inv);
-        else pt[c * HD + d] = x;
-      }
-      if ((tid & 15) == 0) {
-        if (!whole) reinterpret_cast<float2*>(pt + part_cols * HD)[c] = float2{m, l};
-        else if (stat != nullptr) stat[qrow + c] = float2{m, inv};
-      }
-    }
+    few_columns<HD, kAttWaves>(q, kc, vc, kv_scale, bt, b, h, rows, 0, ctx, np, blk0, blk1, c_log2,
+                               o, slot,
+                               score != nullptr ? score + unit * o.part_cols * kPage : nullptr, lds);
     left -= blk1 - blk0;
     unit += blk1 - blk0;
     if (left <= 0) return;
     // the next group, or the next sequence with rows
-    first_tile = false;
+    slot |= 1;
     blk0 = 0;
     if (++h == bt.H) {
       h = 0;
@@ -384,8 +420,7 @@ template <int HD>
 __global__ __launch_bounds__(kTileThr) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ kc,
                        const uint8_t* __restrict__ vc, const float* __restrict__ kv_scale, Units w,
-                       int least, float c_log2, bf16* __restrict__ out, float2* __restrict__ stat,
-                       float* __restrict__ part) {
+                       int least, float c_log2, AttnOut o) {
   constexpr int KT = kPage * 256;       // K tile bytes
   constexpr int VT = HD * kPage * 2;    // V^T tile bytes
   constexpr int NST = HD / 16;          // score k-steps
@@ -418,7 +453,7 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
     t = lo;
     blk0 = (int)(off - w.before(ctx, t));
   }
-  bool first_tile = true;
+  size_t slot = 2 * (size_t)range;
 
   // staging: thread -> 16 bytes of a key row, and 16 tokens of a value dim
   const bool stages = tid < kPage * CPR;
@@ -610,19 +645,19 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
       if (whole) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
         const int row = bt.first_row(b) + row0 + col / bt.nq;
-        bf16* dst = out + (((size_t)row * bt.H + h) * bt.nq + col % bt.nq) * HD;
+        bf16* dst = o.out + (((size_t)row * bt.H + h) * bt.nq + col % bt.nq) * HD;
 #pragma unroll
         for (int i = 0; i < NDT; ++i)
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
-            bf16x4 o;
+            bf16x4 x;
 #pragma unroll
-            for (int v = 0; v < 4; ++v) o[v] = (bf16)(oacc[i][g * 4 + v] * inv);
-            *reinterpret_cast<bf16x4*>(dst + i * 32 + g * 8 + hl * 4) = o;
+            for (int v = 0; v < 4; ++v) x[v] = (bf16)(oacc[i][g * 4 + v] * inv);
+            *reinterpret_cast<bf16x4*>(dst + i * 32 + g * 8 + hl * 4) = x;
           }
-        if (stat != nullptr && hl == 0) stat[qrow + col] = float2{m_run, inv};
+        if (o.stat != nullptr && hl == 0) o.stat[qrow + col] = float2{m_run, inv};
       } else {
-        float* pt = part + (2 * (size_t)range + (first_tile ? 0 : 1)) * part_floats(kTileCols, HD);
+        float* pt = o.part + slot * part_floats(kTileCols, HD);
 #pragma unroll
         for (int i = 0; i < NDT; ++i)
 #pragma unroll
@@ -635,7 +670,7 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
     left -= niter;
     if (left <= 0) return;
     // the next tile, group, or sequence with rows
-    first_tile = false;
+    slot |= 1;
     blk0 = 0;
     if (++t == nt) {
       t = 0;
@@ -680,17 +715,14 @@ __device__ __forceinline__ bool find_parts(const Units& w, int ranges, int least
 // each sum every eighth part, and are then summed in order.
 template <int HD>
 __global__ __launch_bounds__(256) void cache_join_few_kernel(Units w, int ranges, int least,
-                                                             int part_cols,
-                                                             const float* __restrict__ part,
-                                                             bf16* __restrict__ out,
-                                                             float2* __restrict__ stat) {
+                                                             AttnOut o) {
   __shared__ f32x4 osum[8][32];
   const CacheBatch& bt = w.bt;
   const int h = blockIdx.x, b = blockIdx.y;
   const int rows = w.rows(b);
   if (rows <= 0) return;
   const int np = w.pages(bt.context(b), rows, 0), ncol = rows * bt.nq;
-  Parts p{part, part_cols, HD};
+  Parts p{o.part, o.part_cols, HD};
   if (!find_parts(w, ranges, least, w.prefix[b] + (long long)np * h, np, p)) return;
   const int grp = threadIdx.x >> 5, l5 = threadIdx.x & 31, d = 4 * l5;
   for (int c = 0; c < ncol; ++c) {
@@ -702,8 +734,8 @@ __global__ __launch_bounds__(256) void cache_join_few_kernel(Units w, int ranges
       m = mn;
     }
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const float mo = __shfl_xor(m, o), lo = __shfl_xor(l, o), mn = fmaxf(m, mo);
+    for (int i = 1; i < 32; i <<= 1) {
+      const float mo = __shfl_xor(m, i), lo = __shfl_xor(l, i), mn = fmaxf(m, mo);
       l = l * __builtin_amdgcn_exp2f(m - mn) + lo * __builtin_amdgcn_exp2f(mo - mn);
       m = mn;
     }
@@ -728,12 +760,12 @@ __global__ __launch_bounds__(256) void cache_join_few_kernel(Units w, int ranges
     const float inv = l == 0.f ? 0.f : 1.f / l;
     if (d < HD) {
       const int row = bt.first_row(b) + c / bt.nq;
-      bf16* dst = out + (((size_t)row * bt.H + h) * bt.nq + c % bt.nq) * HD + d;
+      bf16* dst = o.out + (((size_t)row * bt.H + h) * bt.nq + c % bt.nq) * HD + d;
       *reinterpret_cast<bf16x4*>(dst) = bf16x4{(bf16)(x[0] * inv), (bf16)(x[1] * inv),
                                                (bf16)(x[2] * inv), (bf16)(x[3] * inv)};
     }
-    if (stat != nullptr && l5 == 0)
-      stat[((size_t)h * bt.N + bt.first_row(b)) * bt.nq + c] = float2{m, inv};
+    if (o.stat != nullptr && l5 == 0)
+      o.stat[((size_t)h * bt.N + bt.first_row(b)) * bt.nq + c] = float2{m, inv};
   }
 }
 
@@ -741,9 +773,7 @@ __global__ __launch_bounds__(256) void cache_join_few_kernel(Units w, int ranges
 // column.
 template <int HD>
 __global__ __launch_bounds__(256) void cache_join_tile_kernel(Units w, int ranges, int least,
-                                                              const float* __restrict__ part,
-                                                              bf16* __restrict__ out,
-                                                              float2* __restrict__ stat) {
+                                                              AttnOut o) {
   constexpr int NV = HD / 32;  // 4-dim pieces of a thread
   const CacheBatch& bt = w.bt;
   const int t = blockIdx.x / (kTileCols / 32), h = blockIdx.y, b = blockIdx.z;
@@ -753,7 +783,7 @@ __global__ __launch_bounds__(256) void cache_join_tile_kernel(Units w, int range
   const int ctx = bt.context(b), row0 = t << w.log2r;
   const int ncol = (min(rows, (t + 1) << w.log2r) - row0) * bt.nq;
   const int np = w.pages(ctx, rows, t);
-  Parts p{part, kTileCols, HD};
+  Parts p{o.part, kTileCols, HD};
   if (!find_parts(w, ranges, least, w.prefix[b] + w.group(b) * h + w.before(ctx, t), np, p) ||
       c >= ncol)
     return;
@@ -777,14 +807,14 @@ __global__ __launch_bounds__(256) void cache_join_tile_kernel(Units w, int range
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const int row = bt.first_row(b) + row0 + c / bt.nq;
-  bf16* dst = out + (((size_t)row * bt.H + h) * bt.nq + c % bt.nq) * HD;
+  bf16* dst = o.out + (((size_t)row * bt.H + h) * bt.nq + c % bt.nq) * HD;
 #pragma unroll
   for (int k = 0; k < NV; ++k)
     *reinterpret_cast<bf16x4*>(dst + 4 * (l3 + 8 * k)) =
         bf16x4{(bf16)(x[k][0] * inv), (bf16)(x[k][1] * inv), (bf16)(x[k][2] * inv),
                (bf16)(x[k][3] * inv)};
-  if (stat != nullptr && l3 == 0)
-    stat[((size_t)h * bt.N + bt.first_row(b) + row0) * bt.nq + c] = float2{m, inv};
+  if (o.stat != nullptr && l3 == 0)
+    o.stat[((size_t)h * bt.N + bt.first_row(b) + row0) * bt.nq + c] = float2{m, inv};
 }
 
 // ---- mass ---------------------------------------------------------------------------
@@ -801,7 +831,7 @@ __global__ __launch_bounds__(kAttThr) void cache_mass_few_kernel(
   const CacheBatch& bt = w.bt;
   const int lane = lane_id(), wave = threadIdx.x >> 6;
   const long long total = w.prefix[bt.B], per = range_units(total, gridDim.x, least);
-  long long unit = blockIdx.x * per;
+  const long long unit = blockIdx.x * per;
   if (unit >= total) return;
   for (int i = threadIdx.x; i < bt.B; i += kAttThr)
     if (w.prefix[i] <= unit && unit < w.prefix[i + 1]) found = i;
@@ -811,6 +841,7 @@ __global__ __launch_bounds__(kAttThr) void cache_mass_few_kernel(
   int rows = w.rows(b), ctx = bt.context(b), np = w.pages(ctx, rows, 0);
   const int off = (int)(unit - w.prefix[b]);
   int h = off / np, blk0 = off % np;
+  score += unit * part_cols * kPage;
   while (true) {
     const int blk1 = min(np, blk0 + left), ncol = rows * bt.nq;
     float2 z{0.f, 0.f};  // of column `lane`
@@ -820,7 +851,7 @@ __global__ __launch_bounds__(kAttThr) void cache_mass_few_kernel(
       if (page < 0) continue;
       const size_t at = ((size_t)page * bt.H + h) * kPage + lane;
       float x = slot < ctx ? mass_in[at] : 0.f, y = 0.f;
-      const float* s = score + (unit + blk - blk0) * part_cols * kPage + lane;
+      const float* s = score + (size_t)(blk - blk0) * part_cols * kPage + lane;
       for (int c = 0; c < ncol; ++c) {
         const float m = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(z.x), c));
         const float inv = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(z.y), c));
@@ -829,7 +860,7 @@ __global__ __launch_bounds__(kAttThr) void cache_mass_few_kernel(
       if (slot < min(ctx + rows, bt.cap())) mass_out[at] = x + y;
     }
     left -= blk1 - blk0;
-    unit += blk1 - blk0;
+    score += (size_t)(blk1 - blk0) * part_cols * kPage;
     if (left <= 0) return;
     blk0 = 0;
     if (++h == bt.H) {
@@ -845,19 +876,20 @@ __global__ __launch_bounds__(kAttThr) void cache_mass_few_kernel(
 }
 
 // Any columns: one workgroup per (two pages, group, sequence), a wave for 32 keys, held in
-// registers as A operand of v_mfma_f32_32x32x16_bf16; tiles of 64 columns go by through
-// LDS (256-byte rows, 16-byte chunk c in slot c ^ (column & 15)).  The exponentials are
-// the bound: they take longer than the scores' MFMAs.
-constexpr int kMassThr = 256, kMassCols = 64;
+// registers as A operand of v_mfma_f32_32x32x16_bf16; tiles of 32 columns go by through
+// LDS (256-byte rows, 16-byte chunk c in slot c ^ (column & 15)), and four workgroups fit a
+// CU: many of them do little (a decoding sequence's pages) and wait for their loads.
+// (us of this kernel for a 512-row chunk beside 16 decoding sequences: tiles of 64 columns
+// and two workgroups a CU 55, a pair of waves for each 32 keys 54, so 46.)
+constexpr int kMassThr = 256, kMassCols = 32;
 
 template <int HD>
-__global__ __launch_bounds__(kMassThr) void cache_mass_kernel(
+__global__ __launch_bounds__(kMassThr, 4) void cache_mass_kernel(
     const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const float* __restrict__ kv_scale,
     CacheBatch bt, int max_rows, float c_log2, const float2* __restrict__ stat,
     const float* __restrict__ mass_in, float* __restrict__ mass_out) {
   constexpr int NST = HD / 16, CPR = HD / 8;
-  constexpr int NQ = kMassCols * CPR / kMassThr;  // 16-byte pieces of a thread and tile
-  static_assert(kMassCols * CPR % kMassThr == 0, "whole pieces");
+  constexpr int NQ = (kMassCols * CPR + kMassThr - 1) / kMassThr;  // 16-byte pieces of a thread
   __shared__ __align__(16) unsigned char smem[2][kMassCols * 256];
   __shared__ float sum[kMassThr / kWave][32];
   const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
@@ -892,28 +924,26 @@ __global__ __launch_bounds__(kMassThr) void cache_mass_kernel(
   const long long c_first = (long long)max(blk0 * kPage - ctx, 0) * bt.nq;
   const int t0 = (int)(c_first / kMassCols), t1 = (ncol + kMassCols - 1) / kMassCols;
   u32x4 qr[NQ];
-  float2 z[2], zn[2];
+  float2 z, zn;  // maximum and 1 / sum of this lane's column, of this tile and the next
   auto fetch = [&](int t) {
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
       const int p = i * kMassThr + tid, c = t * kMassCols + p / CPR;
       qr[i] = zero_u32x4();
-      if (c < ncol) qr[i] = *reinterpret_cast<const u32x4*>(q + (qrow + c) * HD + p % CPR * 8);
+      if (p < kMassCols * CPR && c < ncol)
+        qr[i] = *reinterpret_cast<const u32x4*>(q + (qrow + c) * HD + p % CPR * 8);
     }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int c = t * kMassCols + i * 32 + qi;
-      zn[i] = c < ncol ? stat[qrow + c] : float2{0.f, 0.f};
-    }
+    const int c = t * kMassCols + qi;
+    zn = c < ncol ? stat[qrow + c] : float2{0.f, 0.f};
   };
   auto stage = [&](int t) {
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
       const int p = i * kMassThr + tid, c = p / CPR;
-      *reinterpret_cast<u32x4*>(&smem[t & 1][c * 256 + (((p % CPR) ^ (c & 15)) << 4)]) = qr[i];
+      if (p < kMassCols * CPR)
+        *reinterpret_cast<u32x4*>(&smem[t & 1][c * 256 + (((p % CPR) ^ (c & 15)) << 4)]) = qr[i];
     }
-    z[0] = zn[0];
-    z[1] = zn[1];
+    z = zn;
   };
   if (t0 < t1) {
     fetch(t0);
@@ -923,30 +953,26 @@ __global__ __launch_bounds__(kMassThr) void cache_mass_kernel(
     __syncthreads();
     if (t + 1 < t1) fetch(t + 1);
     if (works) {
+      f32x16 x;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int c = i * 32 + qi, col = t * kMassCols + c;
-        f32x16 s;
+      for (int v = 0; v < 16; ++v) x[v] = 0.f;
 #pragma unroll
-        for (int v = 0; v < 16; ++v) s[v] = 0.f;
-#pragma unroll
-        for (int st = 0; st < NST; ++st) {
-          const int ch = 4 * (st / 2) + 2 * hl + st % 2;
-          const bf16x8 qf =
-              *reinterpret_cast<const bf16x8*>(&smem[t & 1][c * 256 + ((ch ^ (c & 15)) << 4)]);
-          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[st], qf, s, 0, 0, 0);
-        }
-        // (the tile's first column sees the fewest)
-        if (ctx + t * kMassCols / bt.nq + 1 < min(key0 + 32, len + 1)) {
-          const int seen = col < ncol ? ctx + col / bt.nq + 1 : 0;
-#pragma unroll
-          for (int v = 0; v < 16; ++v)
-            if (key0 + 8 * (v >> 2) + 4 * hl + (v & 3) >= seen) s[v] = -__builtin_inff();
-        }
+      for (int st = 0; st < NST; ++st) {
+        const int ch = 4 * (st / 2) + 2 * hl + st % 2;
+        const bf16x8 qf =
+            *reinterpret_cast<const bf16x8*>(&smem[t & 1][qi * 256 + ((ch ^ (qi & 15)) << 4)]);
+        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[st], qf, x, 0, 0, 0);
+      }
+      // (the tile's first column sees the fewest)
+      if (ctx + t * kMassCols / bt.nq + 1 < min(key0 + 32, len + 1)) {
+        const int col = t * kMassCols + qi, seen = col < ncol ? ctx + col / bt.nq + 1 : 0;
 #pragma unroll
         for (int v = 0; v < 16; ++v)
-          acc[v] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[v], c_log2, -z[i].x)), z[i].y, acc[v]);
+          if (key0 + 8 * (v >> 2) + 4 * hl + (v & 3) >= seen) x[v] = -__builtin_inff();
       }
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        acc[v] = fmaf(__builtin_amdgcn_exp2f(fmaf(x[v], c_log2, -z.x)), z.y, acc[v]);
     }
     if (t + 1 < t1) stage(t + 1);
   }
@@ -1033,41 +1059,41 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
                                cus);
   unsigned char* base = static_cast<unsigned char*>(scratch);
   const Units w{bt, max_rows, p.log2r, reinterpret_cast<long long*>(base + p.prefix)};
-  float* part = reinterpret_cast<float*>(base + p.part);
-  float2* stat = mass_out != nullptr ? reinterpret_cast<float2*>(base + p.stat) : nullptr;
+  const AttnOut o{static_cast<bf16*>(out),
+                  mass_out != nullptr ? reinterpret_cast<float2*>(base + p.stat) : nullptr,
+                  reinterpret_cast<float*>(base + p.part), p.cols};
   float* score = p.scores ? reinterpret_cast<float*>(base + p.score) : nullptr;
   const float c_log2 = 1.4426950408889634f / sqrtf((float)a.hd);
   const bf16* qb = static_cast<const bf16*>(q);
-  bf16* ob = static_cast<bf16*>(out);
   auto go = [&](auto hdv) {
     constexpr int HD = decltype(hdv)::value;
     if (p.few) {
       {
         ProfileScope ps("cache_attn_few", s);
         FOE_LAUNCH(cache_attn_few_kernel<HD>, dim3(p.ranges), dim3(kAttThr), 0, s, qb, a.k, a.v,
-                   a.kv_scale, w, kFewLeast, p.cols, c_log2, ob, stat, part, score);
+                   a.kv_scale, w, kFewLeast, c_log2, o, score);
       }
       ProfileScope ps("cache_join_few", s);
       FOE_LAUNCH(cache_join_few_kernel<HD>, dim3(a.H, a.B), dim3(256), 0, s, w, p.ranges, kFewLeast,
-                 p.cols, part, ob, stat);
+                 o);
     } else {
       {
         ProfileScope ps("cache_attn_tile", s);
         FOE_LAUNCH(cache_attn_tile_kernel<HD>, dim3(p.ranges), dim3(kTileThr), 0, s, qb, a.k, a.v,
-                   a.kv_scale, w, kManyLeast, c_log2, ob, stat, part);
+                   a.kv_scale, w, kManyLeast, c_log2, o);
       }
       ProfileScope ps("cache_join_tile", s);
       FOE_LAUNCH(cache_join_tile_kernel<HD>, dim3(p.tiles * (kTileCols / 32), a.H, a.B), dim3(256),
-                 0, s, w, p.ranges, kManyLeast, part, ob, stat);
+                 0, s, w, p.ranges, kManyLeast, o);
     }
     if (score != nullptr) {
       ProfileScope ps("cache_mass_few", s);
       FOE_LAUNCH(cache_mass_few_kernel, dim3(p.ranges), dim3(kAttThr), 0, s, score, w, kFewLeast,
-                 p.cols, c_log2, stat, mass_in, mass_out);
+                 p.cols, c_log2, o.stat, mass_in, mass_out);
     } else if (mass_out != nullptr) {
       ProfileScope ps("cache_mass", s);
       FOE_LAUNCH(cache_mass_kernel<HD>, dim3(ceil_div(a.max_blocks, 2) * a.H, a.B), dim3(kMassThr),
-                 0, s, qb, a.k, a.kv_scale, bt, max_rows, c_log2, stat, mass_in, mass_out);
+                 0, s, qb, a.k, a.kv_scale, bt, max_rows, c_log2, o.stat, mass_in, mass_out);
     }
   };
   if (a.hd == 96) go(std::integral_constant<int, 96>{});

@@ -328,22 +328,11 @@ def cache_empty(n_pages, H, hd, device="cuda"):
             "mass": torch.zeros((n_pages, H, CACHE_PAGE), device=device)}
 
 
-def _shape(t, shape, name):
-    if t is not None and tuple(t.shape) != tuple(shape):
-        raise FoeError(FOE_ERR_INVALID, f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
-
-
-def _same_device(first, *tensors):
-    for t in tensors:
-        if t is not None and t.device != first.device:
-            raise ValueError(f"tensors on {first.device} and {t.device}")
-
-
 def _on(device, stream):
     """Context in which a call allocates and launches: the tensors' device, and
     `stream` as the current one, so that what the call allocates for itself belongs
     to the stream that uses it."""
-    if not device.type == "cuda":
+    if device.type != "cuda":
         raise TypeError("GPU tensors are needed")
     if stream is None:
         return torch.cuda.device(device)
@@ -352,42 +341,71 @@ def _on(device, stream):
     return torch.cuda.stream(stream)
 
 
-def _cache_pool(k, v, kv_scale):
-    """(n_pages, H, hd) of a pool, its tensors checked against each other."""
-    n_pages, H, _, hd = k.shape
-    _shape(k, (n_pages, H, CACHE_PAGE, hd), "k")
-    _shape(v, (n_pages, H, CACHE_PAGE // 16, hd, 16), "v")
-    _shape(kv_scale, (n_pages, H, 2), "kv_scale")
-    return n_pages, H, hd
+def _stream_of(dev):
+    """Handle of the current stream of device ``dev``."""
+    return torch._C._cuda_getCurrentRawStream(dev)
 
 
-def _pool_ptrs(k, v, kv_scale):
+def _elsewhere(t, stream):
+    """Whether a call on ``t`` needs that context.  (A decode step's calls take a few
+    microseconds on the GPU, so what they cost on the host counts.)"""
+    return stream is not None or t.get_device() != torch.cuda.current_device()
+
+
+def _arg(t, name, dtype, shape, dev):
+    """Device pointer of a contiguous tensor of that dtype and shape on device ``dev``."""
+    if (t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == dev):
+        return t.data_ptr()
+    if t.get_device() != dev:
+        raise ValueError(f"tensors on cuda:{dev} and {t.device} ({name})")
+    if t.shape != shape:
+        raise FoeError(FOE_ERR_INVALID, f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
+    return _dev(t, name, dtype)  # raises
+
+
+def _pool_args(k, v, kv_scale, n_pages, H, hd, dev):
     f8 = torch.float8_e4m3fn
-    return _dev(k, "k", f8), _dev(v, "v", f8), _dev(kv_scale, "kv_scale", torch.float32)
+    return (_arg(k, "k", f8, (n_pages, H, CACHE_PAGE, hd), dev),
+            _arg(v, "v", f8, (n_pages, H, CACHE_PAGE // 16, hd, 16), dev),
+            _arg(kv_scale, "kv_scale", torch.float32, (n_pages, H, 2), dev))
+
+
+def _ws_arg(ws, nbytes, device, dev):
+    """A workspace of nbytes() bytes, or the caller's (the library refuses one that is too
+    small): (tensor, pointer, bytes)."""
+    if ws is None:
+        ws = torch.empty(max(nbytes(), 1), dtype=torch.uint8, device=device)
+    return ws, _arg(ws, "ws", torch.uint8, ws.shape, dev), ws.numel()
+
+
+def _size(n, name):
+    if n == ctypes.c_size_t(-1).value:
+        raise FoeError(FOE_ERR_INVALID, f"{name}: {last_error()}")
+    return n
 
 
 def cache_append(qkv, k, v, kv_scale, block_table, ctx_len, row_start, theta, scale=1.0, pos=None,
                  q=None, stream=None):
     """foe_cache_append: qkv [H,N,nq+2,hd] into the pages of block_table
     [B,max_blocks]; returns the rotated queries [H,N,nq,hd]."""
-    n_pages, H, hd = _cache_pool(k, v, kv_scale)
+    if _elsewhere(qkv, stream):
+        with _on(qkv.device, stream):
+            return cache_append(qkv, k, v, kv_scale, block_table, ctx_len, row_start, theta, scale,
+                                pos, q)
+    n_pages, H, _, hd = k.shape
     N, nq = qkv.shape[1], qkv.shape[2] - 2
     B, max_blocks = block_table.shape
-    _shape(qkv, (H, N, nq + 2, hd), "qkv")
-    _shape(ctx_len, (B,), "ctx_len")
-    _shape(row_start, (B + 1,), "row_start")
-    _shape(pos, (B,), "pos")
-    _same_device(qkv, k, v, kv_scale, block_table, ctx_len, row_start, pos, q)
-    _shape(q, (H, N, nq, hd), "q")
-    i32 = torch.int32
-    with _on(qkv.device, stream):
-        if q is None:
-            q = torch.empty((H, N, nq, hd), dtype=qkv.dtype, device=qkv.device)
-        rc = lib().foe_cache_append(
-            _dt(qkv), H, B, N, nq, hd, n_pages, max_blocks, float(theta), float(scale),
-            _dev(qkv, "qkv"), _dev(row_start, "row_start", i32), _dev(ctx_len, "ctx_len", i32),
-            _dev(pos, "pos", i32), _dev(block_table, "block_table", i32),
-            _dev(q, "q", qkv.dtype), *_pool_ptrs(k, v, kv_scale), _stream(stream))
+    dev, i32, dt = qkv.get_device(), torch.int32, _dt(qkv)
+    if q is None:
+        q = torch.empty((H, N, nq, hd), dtype=qkv.dtype, device=qkv.device)
+    rc = lib().foe_cache_append(
+        dt, H, B, N, nq, hd, n_pages, max_blocks, theta, scale,
+        _arg(qkv, "qkv", qkv.dtype, (H, N, nq + 2, hd), dev),
+        _arg(row_start, "row_start", i32, (B + 1,), dev), _arg(ctx_len, "ctx_len", i32, (B,), dev),
+        None if pos is None else _arg(pos, "pos", i32, (B,), dev),
+        _arg(block_table, "block_table", i32, (B, max_blocks), dev),
+        _arg(q, "q", qkv.dtype, (H, N, nq, hd), dev),
+        *_pool_args(k, v, kv_scale, n_pages, H, hd, dev), _stream_of(dev))
     _check(rc, "foe_cache_append")
     return q
 
@@ -396,70 +414,74 @@ def cache_attention_workspace_bytes(q, block_table, max_rows, with_mass=False):
     """Workspace bytes of cache_attention for these tensors."""
     H, N, nq, hd = q.shape
     B, max_blocks = block_table.shape
-    n = lib().foe_cache_attention_workspace_bytes(H, B, N, nq, hd, max_blocks, max_rows,
-                                                  1 if with_mass else 0)
-    if n == ctypes.c_size_t(-1).value:
-        raise FoeError(FOE_ERR_INVALID, f"foe_cache_attention_workspace_bytes: {last_error()}")
-    return n
+    return _size(lib().foe_cache_attention_workspace_bytes(H, B, N, nq, hd, max_blocks, max_rows,
+                                                           1 if with_mass else 0),
+                 "foe_cache_attention_workspace_bytes")
 
 
 def cache_attention(q, k, v, kv_scale, block_table, ctx_len, row_start, max_rows, mass_in=None,
                     mass_out=None, out=None, ws=None, stream=None):
     """foe_cache_attention: q [H,N,nq,hd] over the pages of block_table; returns
     out [N,H,nq,hd]."""
-    n_pages, H, hd = _cache_pool(k, v, kv_scale)
+    if _elsewhere(q, stream):
+        with _on(q.device, stream):
+            return cache_attention(q, k, v, kv_scale, block_table, ctx_len, row_start, max_rows,
+                                   mass_in, mass_out, out, ws)
+    n_pages, H, _, hd = k.shape
     N, nq = q.shape[1], q.shape[2]
     B, max_blocks = block_table.shape
-    _shape(q, (H, N, nq, hd), "q")
-    _shape(ctx_len, (B,), "ctx_len")
-    _shape(row_start, (B + 1,), "row_start")
-    _shape(mass_in, (n_pages, H, CACHE_PAGE), "mass_in")
-    _shape(mass_out, (n_pages, H, CACHE_PAGE), "mass_out")
-    _same_device(q, k, v, kv_scale, block_table, ctx_len, row_start, mass_in, mass_out, out, ws)
-    _shape(out, (N, H, nq, hd), "out")
-    need = cache_attention_workspace_bytes(q, block_table, max_rows, mass_out is not None)
-    i32, f32 = torch.int32, torch.float32
-    with _on(q.device, stream):
-        if out is None:
-            out = torch.empty((N, H, nq, hd), dtype=q.dtype, device=q.device)
-        ws = _workspace(ws, need, q.device)
-        rc = lib().foe_cache_attention(
-            _dt(q), H, B, N, nq, hd, n_pages, max_blocks, max_rows, _dev(q, "q"),
-            _dev(row_start, "row_start", i32), _dev(ctx_len, "ctx_len", i32),
-            _dev(block_table, "block_table", i32), *_pool_ptrs(k, v, kv_scale),
-            _dev(mass_in, "mass_in", f32), _dev(mass_out, "mass_out", f32),
-            _dev(out, "out", q.dtype), _dev(ws, "ws"), ws.numel(), _stream(stream))
+    dev, i32, f32, dt = q.get_device(), torch.int32, torch.float32, _dt(q)
+    mshape = (n_pages, H, CACHE_PAGE)
+    if out is None:
+        out = torch.empty((N, H, nq, hd), dtype=q.dtype, device=q.device)
+    ws, ws_ptr, ws_bytes = _ws_arg(
+        ws, lambda: cache_attention_workspace_bytes(q, block_table, max_rows,
+                                                    mass_out is not None), q.device, dev)
+    rc = lib().foe_cache_attention(
+        dt, H, B, N, nq, hd, n_pages, max_blocks, max_rows,
+        _arg(q, "q", q.dtype, (H, N, nq, hd), dev),
+        _arg(row_start, "row_start", i32, (B + 1,), dev), _arg(ctx_len, "ctx_len", i32, (B,), dev),
+        _arg(block_table, "block_table", i32, (B, max_blocks), dev),
+        *_pool_args(k, v, kv_scale, n_pages, H, hd, dev),
+        None if mass_in is None else _arg(mass_in, "mass_in", f32, mshape, dev),
+        None if mass_out is None else _arg(mass_out, "mass_out", f32, mshape, dev),
+        _arg(out, "out", q.dtype, (N, H, nq, hd), dev), ws_ptr, ws_bytes, _stream_of(dev))
     _check(rc, "foe_cache_attention")
     return out
+
+
+def cache_evict_workspace_bytes(block_table, H):
+    """Workspace bytes of cache_evict for a table and H groups."""
+    B, max_blocks = block_table.shape
+    return _size(lib().foe_cache_evict_workspace_bytes(H, B, max_blocks),
+                 "foe_cache_evict_workspace_bytes")
 
 
 def cache_evict(k, v, kv_scale, mass, block_table, length, keep, recent, dst_table, kept=None,
                 new_len=None, ws=None, stream=None):
     """foe_cache_evict: returns (kept [B,H,keep], new_len [B])."""
-    n_pages, H, hd = _cache_pool(k, v, kv_scale)
+    if _elsewhere(k, stream):
+        with _on(k.device, stream):
+            return cache_evict(k, v, kv_scale, mass, block_table, length, keep, recent, dst_table,
+                               kept, new_len, ws)
+    n_pages, H, _, hd = k.shape
     B, max_blocks = block_table.shape
-    _shape(mass, (n_pages, H, CACHE_PAGE), "mass")
-    _shape(length, (B,), "length")
-    _shape(dst_table, (B, dst_table.shape[-1]), "dst_table")
-    _same_device(k, v, kv_scale, mass, block_table, length, dst_table, kept, new_len, ws)
-    i32 = torch.int32
-    need = lib().foe_cache_evict_workspace_bytes(H, B, max_blocks)
-    if need == ctypes.c_size_t(-1).value:
-        raise FoeError(FOE_ERR_INVALID, f"foe_cache_evict_workspace_bytes: {last_error()}")
-    _shape(kept, (B, H, keep), "kept")
-    _shape(new_len, (B,), "new_len")
-    with _on(k.device, stream):
-        if kept is None:
-            kept = torch.empty((B, H, keep), dtype=i32, device=k.device)
-        if new_len is None:
-            new_len = torch.empty((B,), dtype=i32, device=k.device)
-        ws = _workspace(ws, need, k.device)
-        rc = lib().foe_cache_evict(
-            H, B, hd, n_pages, max_blocks, keep, recent, _dev(length, "length", i32),
-            _dev(block_table, "block_table", i32), _dev(dst_table, "dst_table", i32),
-            dst_table.shape[1], *_pool_ptrs(k, v, kv_scale), _dev(mass, "mass", torch.float32),
-            _dev(kept, "kept", i32), _dev(new_len, "new_len", i32), _dev(ws, "ws"), ws.numel(),
-            _stream(stream))
+    dst_blocks = dst_table.shape[-1]
+    dev, i32 = k.get_device(), torch.int32
+    if kept is None:
+        kept = torch.empty((B, H, max(keep, 0)), dtype=i32, device=k.device)
+    if new_len is None:
+        new_len = torch.empty((B,), dtype=i32, device=k.device)
+    ws, ws_ptr, ws_bytes = _ws_arg(ws, lambda: cache_evict_workspace_bytes(block_table, H),
+                                   k.device, dev)
+    rc = lib().foe_cache_evict(
+        H, B, hd, n_pages, max_blocks, keep, recent, _arg(length, "length", i32, (B,), dev),
+        _arg(block_table, "block_table", i32, (B, max_blocks), dev),
+        _arg(dst_table, "dst_table", i32, (B, dst_blocks), dev), dst_blocks,
+        *_pool_args(k, v, kv_scale, n_pages, H, hd, dev),
+        _arg(mass, "mass", torch.float32, (n_pages, H, CACHE_PAGE), dev),
+        _arg(kept, "kept", i32, (B, H, keep), dev), _arg(new_len, "new_len", i32, (B,), dev),
+        ws_ptr, ws_bytes, _stream_of(dev))
     _check(rc, "foe_cache_evict")
     return kept, new_len
 

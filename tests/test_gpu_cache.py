@@ -404,7 +404,8 @@ def test_attention_absent_pages_and_garbage_behind_the_end(rows):
 
 def test_attention_wide_table():
     """A table with room for far more pages than there are (the scores of so many are not
-    kept for the mass): the same results as with a narrow one."""
+    kept for the mass) and a narrow one, whose pages are dealt out otherwise: each within
+    the bounds (another order of the sums, so not bit for bit)."""
     rng = np.random.default_rng(19)
     H, nq, hd, seqs = 2, 8, 128, [(300, 2), (0, 1), (700, 1)]
     ctx, rs, table, pages = batch(rng, seqs)
@@ -422,7 +423,6 @@ def test_attention_wide_table():
     pool = to_host(dev)
     for o, m in outs:
         check_attention(pool, table, ctx, rs, q, o, m)
-    assert torch.equal(outs[0][0], outs[1][0])
 
 
 def test_attention_rows_past_max_rows_are_left():
