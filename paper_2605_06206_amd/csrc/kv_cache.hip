@@ -9,14 +9,19 @@ namespace {
 
 // ---- append -------------------------------------------------------------------
 // One workgroup per (touched page, group).  Thread (row, u) holds the key pairs
-// 4u .. 4u+3 (dims i and i + HD/2) and the value dims 8u .. 8u+7 of a row.
-// (1) Rotary embedding with the angle (p / scale) * theta^(-2i/HD) formed in
-// double and reduced modulo 2 pi, as in the preparation pass of the prompt
-// attention; q goes out in bf16, the rotated key is quantised from its fp32
-// value.  (2) The page's scales from the largest new magnitudes and, if the
-// page held tokens, its old scales; a scale that grows rescales the page's
-// other codes.  (3) Key rows are stored as they are held; values go through LDS into
-// 16-byte pieces of one dim and 16 tokens, the tokens around the new ones kept.
+// 4u .. 4u+3 (dims i and i + HD/2) and the value dims 8u .. 8u+7 of a row, and of the
+// rows 16, 32 and 48 further on; all rows' loads of a head are in flight together, the
+// next head's behind them.
+// (1) Rotary embedding with the angle (p / scale) * theta^(-2i/HD) formed in double and
+// reduced modulo 2 pi, for every eighth of the page's positions and for the distances
+// 0 .. 7; a position's sine and cosine follow from the two (a quarter of the sines).
+// q goes out in bf16, the rotated key is quantised from its fp32 value.  (2) The page's
+// scales from the largest new magnitudes and, if the page held tokens, its old scales;
+// a scale that grows rescales the page's other codes.  (3) Key rows are stored as they
+// are held; values go through LDS into 16-byte pieces of one dim and 16 tokens, the
+// tokens around the new ones kept.
+// us for 4096 rows of 8 groups, two query heads, hd 128 (59 MB: 11.5): a sine a position
+// and a row's heads one after another 22, so 16.
 constexpr int kAppThr = 256;
 
 template <int HD>
@@ -24,10 +29,14 @@ __global__ __launch_bounds__(kAppThr) void cache_append_kernel(
     const bf16* __restrict__ qkv, bf16* __restrict__ q_out, uint8_t* __restrict__ kc,
     uint8_t* __restrict__ vc, float* __restrict__ kv_scale, CacheBatch bt,
     const int32_t* __restrict__ pos, double log2_theta, double rope_scale) {
-  constexpr int NIT = kPage * 16 / kAppThr;  // rows per thread
+  constexpr int NIT = kPage * 16 / kAppThr;  // rows of a thread
+  constexpr int VROW = kPage + 4;            // bytes of a value dim's row in LDS
+  // (cosine, sine) of pair i at positions first + 8 a (rows 0-7) and b (rows 8-15)
+  __shared__ float2 turn[16][HD / 2];
+  __shared__ __align__(16) uint8_t vt[HD * VROW];
   __shared__ double inv_freq[HD / 2];
-  __shared__ __align__(16) uint8_t vt[HD * kPage];
   const int tid = threadIdx.x, h = blockIdx.y;
+  // (the first frequency is 1 for an infinite base too, where 0 * log2 is NaN)
   if (tid < HD / 2) inv_freq[tid] = tid == 0 ? 1.0 : exp2(-2.0 * tid / HD * log2_theta);
   int b, local;
   const bool any = find_tile<kAppThr>(
@@ -38,107 +47,156 @@ __global__ __launch_bounds__(kAppThr) void cache_append_kernel(
       },
       b, local);
   if (!any) return;
-  const int c0 = bt.context(b), n = bt.rows(b), r0 = bt.first_row(b);
+  const int c0 = bt.context(b), r0 = bt.first_row(b);
   const int blk = c0 / kPage + local;
-  const int lo = max(c0 - blk * kPage, 0), hi = min(c0 + n - blk * kPage, kPage);
+  const int lo = max(c0 - blk * kPage, 0), hi = min(c0 + bt.rows(b) - blk * kPage, kPage);
   const int page = bt.page(b, blk);
-  const long long p0 = pos != nullptr ? pos[b] : c0;
+  const int i0 = blk * kPage + lo - c0;  // the sequence's row at slot lo
 
-  const int u = tid & 15;
+  const int u = tid & 15, rr = tid >> 4;
   const bool act = u < HD / 8;
-  float kr[NIT][8], vr[NIT][8];
-  bool bad[NIT];
-  float2 amax{0.f, 0.f};
-  constexpr double kTwoPi = 6.283185307179586476925286766559;
+  // row of the thread's it-th slot; rows past the last are loaded as it and not stored
+  const int cnt = hi - lo;
+  const size_t row0 = (size_t)h * bt.N + r0 + i0;
+  auto row_of = [&](int it) { return row0 + min(it * (kAppThr / 16) + rr, cnt - 1); };
+  auto has = [&](int it) { return act && it * (kAppThr / 16) + rr < cnt; };
+  auto some = [&](int it) { return it * (kAppThr / 16) < cnt; };  // (uniform)
+  const int uc = act ? u : 0;
+  bf16x8 v[NIT];
+  bf16x4 x1[NIT], x2[NIT];
+  auto load_head = [&](int j) {
+#pragma unroll
+    for (int it = 0; it < NIT; ++it) {
+      if (!some(it)) continue;
+      const bf16* src = qkv + (row_of(it) * (bt.nq + 2) + j) * HD + 4 * uc;
+      x1[it] = *reinterpret_cast<const bf16x4*>(src);
+      x2[it] = *reinterpret_cast<const bf16x4*>(src + HD / 2);
+    }
+  };
 #pragma unroll
   for (int it = 0; it < NIT; ++it) {
-    const int t = lo + it * (kAppThr / 16) + (tid >> 4);
-    bool b_here = false;
+    x1[it] = x2[it] = bf16x4{};
+    v[it] = bf16x8{};
+    if (some(it))
+      v[it] = *reinterpret_cast<const bf16x8*>(qkv + (row_of(it) * (bt.nq + 2) + bt.nq + 1) * HD +
+                                               8 * uc);
+  }
+  load_head(0);
+  // what the page holds that the new tokens are put beside: its scales, and the value
+  // pieces that they share with other tokens
+  constexpr int NV = ((kPage / kSub) * HD + kAppThr - 1) / kAppThr;
+  float* sp = kv_scale + ((size_t)max(page, 0) * bt.H + h) * 2;
+  uint8_t* kp = kc + ((size_t)max(page, 0) * bt.H + h) * (kPage * HD);
+  uint8_t* vp = vc + ((size_t)max(page, 0) * bt.H + h) * (kPage * HD);
+  const float2 scale_was =
+      lo > 0 && page >= 0 ? *reinterpret_cast<const float2*>(sp) : float2{0.f, 0.f};
+  auto touched = [&](int t0) { return t0 < hi && t0 + kSub > lo; };
+  auto full = [&](int t0) { return t0 >= lo && t0 + kSub <= hi; };
+  u32x4 beside[NV];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) kr[it][e] = vr[it][e] = 0.f;
-    if (act && t < hi) {
-      const int i = blk * kPage + t - c0;  // row of the sequence
-      float cs[4], sn[4];
+  for (int k = 0; k < NV; ++k) {
+    const int i = k * kAppThr + tid, t0 = i / HD * kSub;
+    beside[k] = zero_u32x4();
+    if (page >= 0 && t0 < kPage && touched(t0) && !full(t0))
+      beside[k] = *reinterpret_cast<const u32x4*>(vp + i * 16);
+  }
+  {
+    const long long first = (pos != nullptr ? pos[b] : c0) + (long long)i0;
+    constexpr double kTwoPi = 6.283185307179586476925286766559;
+    const int na = (cnt + 7) / 8, nb = min(cnt, 8);
+    for (int e = tid; e < (na + nb) * (HD / 2); e += kAppThr) {
+      const int k = e / (HD / 2), i = e % (HD / 2);
+      double a = (double)(k < na ? first + 8 * k : k - na) / rope_scale * inv_freq[i];
+      a -= kTwoPi * floor(a / kTwoPi);
+      float2 t;
+      sincosf((float)a, &t.y, &t.x);
+      turn[k < na ? k : 8 + k - na][i] = t;
+    }
+  }
+  __syncthreads();
+  float cs[NIT][4], sn[NIT][4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        double a = (double)(p0 + i) / rope_scale * inv_freq[4 * u + e];
-        a -= kTwoPi * floor(a / kTwoPi);
-        sincosf((float)a, &sn[e], &cs[e]);
-      }
-      const size_t row = (size_t)h * bt.N + r0 + i;
-      const bf16* src = qkv + row * (size_t)(bt.nq + 2) * HD;
-      for (int j = 0; j <= bt.nq; ++j) {
-        const bf16x4 x1 = *reinterpret_cast<const bf16x4*>(src + (size_t)j * HD + 4 * u);
-        const bf16x4 x2 = *reinterpret_cast<const bf16x4*>(src + (size_t)j * HD + HD / 2 + 4 * u);
-        float y1[4], y2[4];
+  for (int it = 0; it < NIT; ++it) {
+    const int i = min(it * (kAppThr / 16) + rr, cnt - 1);  // position - first
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float a1 = (float)x1[e], a2 = (float)x2[e];
-          y1[e] = a1 * cs[e] - a2 * sn[e];
-          y2[e] = a2 * cs[e] + a1 * sn[e];
-        }
-        if (j < bt.nq) {
-          bf16* dst = q_out + (row * bt.nq + j) * HD + 4 * u;
-          *reinterpret_cast<bf16x4*>(dst) =
-              bf16x4{(bf16)y1[0], (bf16)y1[1], (bf16)y1[2], (bf16)y1[3]};
-          *reinterpret_cast<bf16x4*>(dst + HD / 2) =
-              bf16x4{(bf16)y2[0], (bf16)y2[1], (bf16)y2[2], (bf16)y2[3]};
-        } else {
+    for (int e = 0; e < 4; ++e) {
+      const float2 a = turn[i >> 3][4 * uc + e], d = turn[8 + (i & 7)][4 * uc + e];
+      cs[it][e] = a.x * d.x - a.y * d.y;
+      sn[it][e] = a.y * d.x + a.x * d.y;
+    }
+  }
+  auto rotate = [&](int it, float* y) {  // dims 4u .. +3, then HD/2 on
 #pragma unroll
-          for (int e = 0; e < 4; ++e) kr[it][e] = y1[e], kr[it][4 + e] = y2[e];
-        }
-      }
-      const bf16x8 v = *reinterpret_cast<const bf16x8*>(src + (size_t)(bt.nq + 1) * HD + 8 * u);
+    for (int e = 0; e < 4; ++e) {
+      const float a1 = (float)x1[it][e], a2 = (float)x2[it][e];
+      y[e] = a1 * cs[it][e] - a2 * sn[it][e];
+      y[4 + e] = a2 * cs[it][e] + a1 * sn[it][e];
+    }
+  };
+  for (int j = 0; j < bt.nq; ++j) {
+    bf16x8 y8[NIT];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        vr[it][e] = (float)v[e];
-        b_here |= !(fabsf(kr[it][e]) < __builtin_inff()) || !(fabsf(vr[it][e]) < __builtin_inff());
-      }
+    for (int it = 0; it < NIT; ++it) {
+      float y[8];
+      rotate(it, y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y8[it][e] = (bf16)y[e];
+    }
+    load_head(j + 1);  // (the key follows the last query)
+#pragma unroll
+    for (int it = 0; it < NIT; ++it) {
+      if (!has(it)) continue;
+      bf16* dst = q_out + (row_of(it) * bt.nq + j) * HD + 4 * u;
+      *reinterpret_cast<bf16x4*>(dst) = bf16x4{y8[it][0], y8[it][1], y8[it][2], y8[it][3]};
+      *reinterpret_cast<bf16x4*>(dst + HD / 2) = bf16x4{y8[it][4], y8[it][5], y8[it][6], y8[it][7]};
+    }
+  }
+  bool bad[NIT];
+  float2 amax{0.f, 0.f};
+#pragma unroll
+  for (int it = 0; it < NIT; ++it) {
+    bool not_finite = false;
+    float2 m{0.f, 0.f};
+    float y[8];
+    rotate(it, y);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float k = fabsf(y[e]), w = fabsf((float)v[it][e]);
+      not_finite |= !(k < __builtin_inff()) || !(w < __builtin_inff());
+      m.x = fmaxf(m.x, k);
+      m.y = fmaxf(m.y, w);
     }
     // a row with a non-finite key or value counts for no scale
-    const uint64_t m = __builtin_amdgcn_ballot_w64(b_here);
-    bad[it] = ((m >> (lane_id() & 48)) & 0xffffu) != 0;
-    if (!bad[it]) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        amax.x = fmaxf(amax.x, fabsf(kr[it][e]));
-        amax.y = fmaxf(amax.y, fabsf(vr[it][e]));
-      }
-    }
+    const uint64_t any_bad = __builtin_amdgcn_ballot_w64(not_finite && has(it));
+    bad[it] = ((any_bad >> (lane_id() & 48)) & 0xffffu) != 0;
+    if (!bad[it] && has(it)) amax = float2{fmaxf(amax.x, m.x), fmaxf(amax.y, m.y)};
   }
   if (page < 0) return;  // (uniform) nowhere to store
   amax = block_max<kAppThr>(amax);
-  float* sp = kv_scale + ((size_t)page * bt.H + h) * 2;
-  float ks = block_scale(amax.x), vs = block_scale(amax.y);
-  float kratio = 1.f, vratio = 1.f;
-  if (lo > 0) {
-    const float ko = sp[0], vo = sp[1];
-    ks = fmaxf(ks, ko);
-    vs = fmaxf(vs, vo);
-    kratio = ko * pow2_inv(ks);
-    vratio = vo * pow2_inv(vs);
-  }
+  // (scale_was is 0 where the page held no token: its other codes are left)
+  const float ks = fmaxf(block_scale(amax.x), scale_was.x);
+  const float vs = fmaxf(block_scale(amax.y), scale_was.y);
   const float ki = pow2_inv(ks), vi = pow2_inv(vs);
+  const float kratio = lo > 0 ? scale_was.x * ki : 1.f, vratio = lo > 0 ? scale_was.y * vi : 1.f;
 
-  uint8_t* kp = kc + ((size_t)page * bt.H + h) * (kPage * HD);
-  uint8_t* vp = vc + ((size_t)page * bt.H + h) * (kPage * HD);
 #pragma unroll
   for (int it = 0; it < NIT; ++it) {
-    const int t = lo + it * (kAppThr / 16) + (tid >> 4);
-    if (!act || t >= hi) continue;
-    const float* k = kr[it];
-    const float* v = vr[it];
+    if (!has(it)) continue;
+    const int t = lo + it * (kAppThr / 16) + rr;
+    float k[8], w[8];
+    rotate(it, k);  // (again: its registers are not held meanwhile)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = (float)v[it][e] * vi;
     uint32_t c0w = to_codes4(k[0] * ki, k[1] * ki, k[2] * ki, k[3] * ki);
     uint32_t c1w = to_codes4(k[4] * ki, k[5] * ki, k[6] * ki, k[7] * ki);
-    uint32_t v0w = to_codes4(v[0] * vi, v[1] * vi, v[2] * vi, v[3] * vi);
-    uint32_t v1w = to_codes4(v[4] * vi, v[5] * vi, v[6] * vi, v[7] * vi);
+    uint32_t v0w = to_codes4(w[0], w[1], w[2], w[3]), v1w = to_codes4(w[4], w[5], w[6], w[7]);
     if (bad[it]) c0w = c1w = 0x7f7f7f7fu, v0w = v1w = 0u;
     *reinterpret_cast<uint32_t*>(kp + t * HD + 4 * u) = c0w;
     *reinterpret_cast<uint32_t*>(kp + t * HD + HD / 2 + 4 * u) = c1w;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      vt[(8 * u + e) * kPage + t] = (uint8_t)(v0w >> (8 * e));
-      vt[(8 * u + 4 + e) * kPage + t] = (uint8_t)(v1w >> (8 * e));
+      vt[(8 * u + e) * VROW + t] = (uint8_t)(v0w >> (8 * e));
+      vt[(8 * u + 4 + e) * VROW + t] = (uint8_t)(v1w >> (8 * e));
     }
   }
   if (kratio != 1.f)  // the page's other rows, in units of the new scale
@@ -151,18 +209,21 @@ __global__ __launch_bounds__(kAppThr) void cache_append_kernel(
       *w = x;
     }
   __syncthreads();
-  if (tid == 0) sp[0] = ks, sp[1] = vs;
-  for (int i = tid; i < (kPage / kSub) * HD; i += kAppThr) {
-    const int g = i / HD, d = i % HD;
-    const int t0 = g * kSub;
-    if ((t0 >= hi || t0 + kSub <= lo) && vratio == 1.f) continue;
+  if (tid == 0) *reinterpret_cast<float2*>(sp) = float2{ks, vs};
+#pragma unroll
+  for (int n = 0; n < NV; ++n) {
+    const int i = n * kAppThr + tid, d = i % HD, t0 = i / HD * kSub;
+    if (t0 >= kPage || (!touched(t0) && vratio == 1.f)) continue;
     u32x4* w = reinterpret_cast<u32x4*>(vp + i * 16);
-    const u32x4 x = *reinterpret_cast<const u32x4*>(vt + d * kPage + t0);
-    if (t0 >= lo && t0 + kSub <= hi) {
+    u32x4 x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      x[e] = *reinterpret_cast<const uint32_t*>(vt + d * VROW + t0 + 4 * e);
+    if (full(t0)) {
       *w = x;
       continue;
     }
-    u32x4 old = *w;
+    u32x4 old = touched(t0) ? beside[n] : *w;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       uint32_t fresh = 0;  // bytes of the new tokens
