@@ -594,7 +594,7 @@ void check_cache(Check& c, int H, int B, int n_pages, int max_blocks) {
 }
 void check_rows(Check& c, int N, int nq) {
   c.need(nq >= 1 && nq <= 64, "nq must be in [1, 64]");
-  c.need(N >= 0 && (long long)N * (nq < 1 ? 1 : nq) <= (1 << 26), "N*nq must be in [0, 2^26]");
+  c.need(N >= 0 && (long long)N * (nq < 1 ? 1 : nq) <= (1 << 22), "N*nq must be in [0, 2^22]");
 }
 bool cache_hd(int hd) { return hd == 96 || hd == 128; }
 

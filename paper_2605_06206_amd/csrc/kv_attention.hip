@@ -2,12 +2,13 @@
 // each cached token receives.
 //
 // A column is one query: row i of a sequence and head j of a group, numbered
-// i * nq + j (the heads share the group's keys and values).  Two forms, by the most
-// columns that a sequence of the call can have:
-// - few (at most 16: decode steps): a tile of 16 columns walks the pages with
-//   16x16x32 MFMAs fed from registers; reading the pages is all the work;
-// - many (chunks, and the decode steps that ride along): tiles of up to 256 columns
-//   share each page through LDS.
+// i * nq + j (the heads share the group's keys and values).  Two forms:
+// - few columns (at most 16: decode steps): a tile of 16 walks the pages with 16x16x32
+//   MFMAs fed from registers; reading the pages is all the work;
+// - many (chunks): tiles of up to 256 columns share each page through LDS.
+// A call whose sequences may have more than 16 columns takes the second form, for short
+// sequences too, unless most of them look short (see attn_plan): then each form takes
+// its sequences.
 // In both, S^T = K Q^T and O^T += V^T P^T with an online softmax in base 2, and the
 // work is dealt out alike: the (sequence, group, tile, page) units of the batch,
 // numbered in that order, are cut into equal ranges, one for each workgroup of a
@@ -15,10 +16,13 @@
 // its range; a tile that lies in one range is written at once, the others leave their
 // unnormalised parts, which a second launch joins in page order.  (One workgroup per
 // tile of 16 columns: 1151 us instead of 195 for four sequences of 131072 tokens, 8 groups.)
+#include <limits.h>
+
 #include <algorithm>
 #include <type_traits>
 
 #include "kv_cache.hpp"
+#include "lds_dma.hpp"
 
 namespace foe {
 namespace {
@@ -39,9 +43,14 @@ struct Units {
   CacheBatch bt;
   int max_rows;
   int log2r;  // few: -1
+  int lo, hi;  // columns that a sequence of this form has: lo < columns <= hi
   long long* prefix;  // [B + 1]: units before each sequence, and in all (written for the join)
 
-  __device__ __forceinline__ int rows(int b) const { return min(bt.rows(b), max_rows); }
+  // rows of sequence b in this form
+  __device__ __forceinline__ int rows(int b) const {
+    const int n = min(bt.rows(b), max_rows);
+    return n * bt.nq > lo && n * bt.nq <= hi ? n : 0;
+  }
   __device__ __forceinline__ int tiles(int n) const { return (n + (1 << log2r) - 1) >> log2r; }
   // pages of the tiles before tile t (t < tiles)
   __device__ __forceinline__ long long before(int ctx, int t) const {
@@ -201,7 +210,8 @@ __device__ __forceinline__ void load_q(const bf16* q, int col, int ncol, int g, 
   }
 }
 
-// A part of a tile that several workgroups share: [columns][HD] unnormalised sums,
+// A part of a tile that several workgroups share: unnormalised sums ([columns][HD] with
+// few columns; [HD / 4][columns][4] with many, as the lanes hold them, a column each),
 // then [columns] (maximum, sum).  Workgroup r leaves at most two: of its first tile
 // (slot 2 r), and of its last one if another (2 r + 1).
 __host__ __device__ inline size_t part_floats(int cols, int hd) { return (size_t)cols * (hd + 2); }
@@ -662,7 +672,7 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
         for (int i = 0; i < NDT; ++i)
 #pragma unroll
           for (int g = 0; g < 4; ++g)
-            *reinterpret_cast<f32x4*>(pt + col * HD + i * 32 + g * 8 + hl * 4) =
+            *reinterpret_cast<f32x4*>(pt + ((i * 8 + g * 2 + hl) * kTileCols + col) * 4) =
                 f32x4{oacc[i][g * 4], oacc[i][g * 4 + 1], oacc[i][g * 4 + 2], oacc[i][g * 4 + 3]};
         if (hl == 0) reinterpret_cast<float2*>(pt + kTileCols * HD)[col] = float2{m_run, l};
       }
@@ -769,15 +779,16 @@ __global__ __launch_bounds__(256) void cache_join_few_kernel(Units w, int ranges
   }
 }
 
-// Many columns: one workgroup per (32 columns of a tile, group, sequence), 8 threads a
-// column.
+// Many columns: one workgroup per (32 columns and 32 dims of a tile, group, sequence); a
+// thread has 4 dims of a column and loads eight parts at a time.
 template <int HD>
 __global__ __launch_bounds__(256) void cache_join_tile_kernel(Units w, int ranges, int least,
                                                               AttnOut o) {
-  constexpr int NV = HD / 32;  // 4-dim pieces of a thread
+  constexpr int CB = kTileCols / 32, DB = HD / 32, AT_ONCE = 8;
   const CacheBatch& bt = w.bt;
-  const int t = blockIdx.x / (kTileCols / 32), h = blockIdx.y, b = blockIdx.z;
-  const int c = blockIdx.x % (kTileCols / 32) * 32 + (threadIdx.x >> 3), l3 = threadIdx.x & 7;
+  const int t = blockIdx.x / (CB * DB), h = blockIdx.y, b = blockIdx.z;
+  const int c = blockIdx.x % CB * 32 + (threadIdx.x & 31);
+  const int d4 = blockIdx.x / CB % DB * 8 + (threadIdx.x >> 5);
   const int rows = w.rows(b);
   if (rows <= 0 || t >= w.tiles(rows)) return;
   const int ctx = bt.context(b), row0 = t << w.log2r;
@@ -788,32 +799,40 @@ __global__ __launch_bounds__(256) void cache_join_tile_kernel(Units w, int range
       c >= ncol)
     return;
   float m = kMFloor, l = 0.f;
-#pragma unroll 4
-  for (int r = p.r0; r <= p.r1; ++r) m = fmaxf(m, p.stats(r)[c].x);
-  f32x4 x[NV];
+  f32x4 x{0.f, 0.f, 0.f, 0.f};
+  for (int r0 = p.r0; r0 <= p.r1; r0 += AT_ONCE) {
+    float2 z[AT_ONCE];
+    f32x4 y[AT_ONCE];
 #pragma unroll
-  for (int k = 0; k < NV; ++k) x[k] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 2
-  for (int r = p.r0; r <= p.r1; ++r) {
-    const float2 z = p.stats(r)[c];
-    const float a = __builtin_amdgcn_exp2f(z.x - m);
-    l += z.y * a;
+    for (int i = 0; i < AT_ONCE; ++i) {
+      z[i] = float2{kMFloor, 0.f};
+      y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (r0 + i > p.r1) continue;
+      z[i] = p.stats(r0 + i)[c];
+      y[i] = *reinterpret_cast<const f32x4*>(p.at(r0 + i) + ((size_t)d4 * kTileCols + c) * 4);
+    }
+    float mn = m;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const f32x4 y = *reinterpret_cast<const f32x4*>(p.at(r) + (size_t)c * HD + 4 * (l3 + 8 * k));
+    for (int i = 0; i < AT_ONCE; ++i) mn = fmaxf(mn, z[i].x);
+    const float a0 = __builtin_amdgcn_exp2f(m - mn);
+    m = mn;
+    l *= a0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[k][e] += y[e] * a;
+    for (int e = 0; e < 4; ++e) x[e] *= a0;
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const float a = __builtin_amdgcn_exp2f(z[i].x - m);
+      l += z[i].y * a;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += y[i][e] * a;
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const int row = bt.first_row(b) + row0 + c / bt.nq;
   bf16* dst = o.out + (((size_t)row * bt.H + h) * bt.nq + c % bt.nq) * HD;
-#pragma unroll
-  for (int k = 0; k < NV; ++k)
-    *reinterpret_cast<bf16x4*>(dst + 4 * (l3 + 8 * k)) =
-        bf16x4{(bf16)(x[k][0] * inv), (bf16)(x[k][1] * inv), (bf16)(x[k][2] * inv),
-               (bf16)(x[k][3] * inv)};
-  if (o.stat != nullptr && l3 == 0)
+  *reinterpret_cast<bf16x4*>(dst + 4 * d4) =
+      bf16x4{(bf16)(x[0] * inv), (bf16)(x[1] * inv), (bf16)(x[2] * inv), (bf16)(x[3] * inv)};
+  if (o.stat != nullptr && d4 == 0)
     o.stat[((size_t)h * bt.N + bt.first_row(b) + row0) * bt.nq + c] = float2{m, inv};
 }
 
@@ -876,26 +895,32 @@ __global__ __launch_bounds__(kAttThr) void cache_mass_few_kernel(
 }
 
 // Any columns: one workgroup per (two pages, group, sequence), a wave for 32 keys, held in
-// registers as A operand of v_mfma_f32_32x32x16_bf16; tiles of 32 columns go by through
-// LDS (256-byte rows, 16-byte chunk c in slot c ^ (column & 15)), and four workgroups fit a
-// CU: many of them do little (a decoding sequence's pages) and wait for their loads.
-// (us of this kernel for a 512-row chunk beside 16 decoding sequences: tiles of 64 columns
-// and two workgroups a CU 55, a pair of waves for each 32 keys 54, so 46.)
+// registers as A operand of v_mfma_f32_32x32x16_bf16.  Tiles of 32 columns go by through a
+// ring of four in LDS, filled by LDS-DMA three tiles ahead (256-byte rows, 16-byte chunk
+// c in slot c ^ (column & 15); the columns' maxima and sums behind them), since a tile
+// takes less time than a load.  Four workgroups fit a CU: many of them do little (a
+// decoding sequence's pages) and wait for their first loads.
+// us of this kernel for 4096 rows over 4096 tokens, 8 groups of two heads, and for a 512-row
+// chunk beside 16 decoding sequences: tiles through registers, one ahead 224 and 46; so XX.
 constexpr int kMassThr = 256, kMassCols = 32;
+constexpr int kMassStages = 4;
 
 template <int HD>
 __global__ __launch_bounds__(kMassThr, 4) void cache_mass_kernel(
     const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const float* __restrict__ kv_scale,
-    CacheBatch bt, int max_rows, float c_log2, const float2* __restrict__ stat,
-    const float* __restrict__ mass_in, float* __restrict__ mass_out) {
-  constexpr int NST = HD / 16, CPR = HD / 8;
-  constexpr int NQ = (kMassCols * CPR + kMassThr - 1) / kMassThr;  // 16-byte pieces of a thread
-  __shared__ __align__(16) unsigned char smem[2][kMassCols * 256];
+    Units w, float c_log2, const float2* __restrict__ stat, const float* __restrict__ mass_in,
+    float* __restrict__ mass_out) {
+  constexpr int NST = HD / 16;
+  constexpr int QT = kMassCols * 256, STAGE = QT + 256;  // bytes of a tile, and with its statistics
+  constexpr int QI = QT / 1024 / (kMassThr / kWave);     // 1 KB DMA instructions of a wave
+  __shared__ __align__(1024) unsigned char smem[kMassStages * STAGE];
   __shared__ float sum[kMassThr / kWave][32];
   const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
+  const int wave_u = __builtin_amdgcn_readfirstlane(wave);
   const int qi = lane & 31, hl = lane >> 5;
+  const CacheBatch& bt = w.bt;
   const int h = blockIdx.x % bt.H, b = blockIdx.y, blk0 = blockIdx.x / bt.H * 2;
-  const int rows = min(bt.rows(b), max_rows), ctx = bt.context(b);
+  const int rows = w.rows(b), ctx = bt.context(b);
   const int len = min(ctx + rows, bt.cap());
   if (rows == 0 || blk0 * kPage >= len) return;
   const int key0 = blk0 * kPage + wave * 32;  // the wave's first key
@@ -915,6 +940,9 @@ __global__ __launch_bounds__(kMassThr, 4) void cache_mass_kernel(
       kf[st + 1] = codes_to_bf16(x[2], x[3], ks);
     }
   }
+  // arrived before the loop, whose loads are counted
+#pragma unroll
+  for (int st = 0; st < NST; ++st) asm volatile("" ::"v"(kf[st]));
   const int ncol = rows * bt.nq;
   const size_t qrow = ((size_t)h * bt.N + bt.first_row(b)) * bt.nq;
   float acc[16];
@@ -923,36 +951,38 @@ __global__ __launch_bounds__(kMassThr, 4) void cache_mass_kernel(
   // tiles before the first column that sees the pages are left out
   const long long c_first = (long long)max(blk0 * kPage - ctx, 0) * bt.nq;
   const int t0 = (int)(c_first / kMassCols), t1 = (ncol + kMassCols - 1) / kMassCols;
-  u32x4 qr[NQ];
-  float2 z, zn;  // maximum and 1 / sum of this lane's column, of this tile and the next
-  auto fetch = [&](int t) {
+  // columns past the last read zeros: no query, maximum 0 and 1 / sum 0
+  const __amdgpu_buffer_rsrc_t rq = make_rsrc_u(q + qrow * HD, (uint32_t)ncol * (HD * 2));
+  const __amdgpu_buffer_rsrc_t rz = make_rsrc_u(stat + qrow, (uint32_t)ncol * 8u);
+  rsrc_settle(rq, rz);
+  uint32_t qoff[QI];
 #pragma unroll
-    for (int i = 0; i < NQ; ++i) {
-      const int p = i * kMassThr + tid, c = t * kMassCols + p / CPR;
-      qr[i] = zero_u32x4();
-      if (p < kMassCols * CPR && c < ncol)
-        qr[i] = *reinterpret_cast<const u32x4*>(q + (qrow + c) * HD + p % CPR * 8);
-    }
-    const int c = t * kMassCols + qi;
-    zn = c < ncol ? stat[qrow + c] : float2{0.f, 0.f};
-  };
-  auto stage = [&](int t) {
-#pragma unroll
-    for (int i = 0; i < NQ; ++i) {
-      const int p = i * kMassThr + tid, c = p / CPR;
-      if (p < kMassCols * CPR)
-        *reinterpret_cast<u32x4*>(&smem[t & 1][c * 256 + (((p % CPR) ^ (c & 15)) << 4)]) = qr[i];
-    }
-    z = zn;
-  };
-  if (t0 < t1) {
-    fetch(t0);
-    stage(t0);
+  for (int i = 0; i < QI; ++i) {
+    const int c = 4 * (wave * QI + i) + (lane >> 4), ch = (lane & 15) ^ (c & 15);
+    qoff[i] = ch < HD / 8 ? (uint32_t)(c * (HD * 2) + ch * 16) : kOob;
   }
+  const uint32_t lds = lds_addr(smem);
+  auto issue = [&](int t) {
+    const uint32_t to = lds + (uint32_t)((t & (kMassStages - 1)) * STAGE);
+    const uint32_t step = (uint32_t)t * (kMassCols * HD * 2);
+#pragma unroll
+    for (int i = 0; i < QI; ++i) dma16(rq, qoff[i] + step, to + (uint32_t)wave_u * (QI * 1024), i * 1024);
+    // (every wave loads the statistics, so that all count the same)
+    dma4(rz, (uint32_t)t * (kMassCols * 8) + lane * 4u, to, QT);
+  };
+  constexpr int OPS = QI + 1;  // DMA instructions of a wave and tile
+#pragma unroll
+  for (int i = 0; i < kMassStages - 1; ++i)
+    if (t0 + i < t1) issue(t0 + i);
   for (int t = t0; t < t1; ++t) {
-    __syncthreads();
-    if (t + 1 < t1) fetch(t + 1);
+    // this tile has landed for every wave, and the one before is done with
+    if (t + 2 < t1) vm_barrier<2 * OPS>();
+    else if (t + 1 < t1) vm_barrier<OPS>();
+    else vm_barrier<0>();
+    if (t + kMassStages - 1 < t1) issue(t + kMassStages - 1);
+    const unsigned char* tile = smem + (t & (kMassStages - 1)) * STAGE;
     if (works) {
+      const float2 z = *reinterpret_cast<const float2*>(tile + QT + qi * 8);
       f32x16 x;
 #pragma unroll
       for (int v = 0; v < 16; ++v) x[v] = 0.f;
@@ -960,7 +990,7 @@ __global__ __launch_bounds__(kMassThr, 4) void cache_mass_kernel(
       for (int st = 0; st < NST; ++st) {
         const int ch = 4 * (st / 2) + 2 * hl + st % 2;
         const bf16x8 qf =
-            *reinterpret_cast<const bf16x8*>(&smem[t & 1][qi * 256 + ((ch ^ (qi & 15)) << 4)]);
+            *reinterpret_cast<const bf16x8*>(tile + qi * 256 + ((ch ^ (qi & 15)) << 4));
         x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[st], qf, x, 0, 0, 0);
       }
       // (the tile's first column sees the fewest)
@@ -974,7 +1004,6 @@ __global__ __launch_bounds__(kMassThr, 4) void cache_mass_kernel(
       for (int v = 0; v < 16; ++v)
         acc[v] = fmaf(__builtin_amdgcn_exp2f(fmaf(x[v], c_log2, -z.x)), z.y, acc[v]);
     }
-    if (t + 1 < t1) stage(t + 1);
   }
 #pragma unroll
   for (int v = 0; v < 16; ++v) {
@@ -1008,37 +1037,54 @@ constexpr int kManyLeast = 2;
 // are formed again
 constexpr size_t kScoreBytes = (size_t)256 << 20;
 
-struct AttnPlan {
-  bool few, scores;
+// One form of a call: what it launches and where its scratch is.
+struct FormPlan {
+  bool on;
+  int lo, hi;                 // columns of its sequences
   int ranges, cols, log2r, tiles;
-  size_t prefix, part, stat, score, total;
+  size_t prefix, part;
+};
+struct AttnPlan {
+  FormPlan few, many;
+  bool scores;
+  size_t stat, score, total;
 };
 
 AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_rows, bool mass,
                    int cus) {
   AttnPlan p{};
-  p.few = (long long)max_rows * nq <= kFewCols;
-  const long long pages = (long long)B * H * max_blocks;
-  if (p.few) {
-    p.cols = max_rows * nq;
-    p.ranges = (int)std::min<long long>(4LL * cus, (pages + kFewLeast - 1) / kFewLeast);
-    p.log2r = -1;
-  } else {
-    p.cols = kTileCols;
-    p.ranges = cus;
-    while ((2 << p.log2r) * nq <= kTileCols) ++p.log2r;
-    p.tiles = ceil_div(max_rows, 1 << p.log2r);
-  }
+  const long long most = (long long)max_rows * nq;
+  // Both forms where the sequences beside the longest have few columns on average: each
+  // form's launches cost some 10 us where it has no sequence (us for a 512-row chunk beside
+  // 16 decoding sequences, with mass: XX, and 117 in the second form alone).
+  p.few.on = most <= kFewCols || (B > 1 && (long long)(N - max_rows) * nq <= kFewCols * (B - 1LL));
+  p.many.on = most > kFewCols;
+  p.few.hi = kFewCols;
+  p.many.lo = p.few.on ? kFewCols : 0;
+  p.many.hi = INT_MAX;
   auto take = [&](size_t& field, size_t bytes) {
     field = p.total;
     p.total = align_up(p.total + bytes, 256);
   };
-  take(p.prefix, (size_t)(B + 1) * 8);
-  take(p.part, 2 * (size_t)p.ranges * part_floats(p.cols, hd) * 4);
+  auto scratch = [&](FormPlan& f) {
+    if (!f.on) return;
+    take(f.prefix, (size_t)(B + 1) * 8);
+    take(f.part, 2 * (size_t)f.ranges * part_floats(f.cols, hd) * 4);
+  };
+  const long long pages = (long long)B * H * max_blocks;
+  p.few.cols = (int)std::min<long long>(kFewCols, most);
+  p.few.ranges = (int)std::min<long long>(4LL * cus, (pages + kFewLeast - 1) / kFewLeast);
+  p.few.log2r = -1;
+  p.many.cols = kTileCols;
+  p.many.ranges = cus;
+  while ((2 << p.many.log2r) * nq <= kTileCols) ++p.many.log2r;
+  p.many.tiles = ceil_div(max_rows, 1 << p.many.log2r);
+  scratch(p.few);
+  scratch(p.many);
   if (mass) {
     take(p.stat, (size_t)H * N * nq * sizeof(float2));
-    const size_t bytes = (size_t)pages * p.cols * kPage * 4;
-    p.scores = p.few && bytes <= kScoreBytes;
+    const size_t bytes = (size_t)pages * p.few.cols * kPage * 4;
+    p.scores = p.few.on && bytes <= kScoreBytes;
     if (p.scores) take(p.score, bytes);
   }
   return p;
@@ -1058,42 +1104,59 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
   const AttnPlan p = attn_plan(a.H, a.B, N, nq, a.hd, a.max_blocks, max_rows, mass_out != nullptr,
                                cus);
   unsigned char* base = static_cast<unsigned char*>(scratch);
-  const Units w{bt, max_rows, p.log2r, reinterpret_cast<long long*>(base + p.prefix)};
-  const AttnOut o{static_cast<bf16*>(out),
-                  mass_out != nullptr ? reinterpret_cast<float2*>(base + p.stat) : nullptr,
-                  reinterpret_cast<float*>(base + p.part), p.cols};
-  float* score = p.scores ? reinterpret_cast<float*>(base + p.score) : nullptr;
   const float c_log2 = 1.4426950408889634f / sqrtf((float)a.hd);
   const bf16* qb = static_cast<const bf16*>(q);
+  float2* stat = mass_out != nullptr ? reinterpret_cast<float2*>(base + p.stat) : nullptr;
+  float* score = p.scores ? reinterpret_cast<float*>(base + p.score) : nullptr;
+  auto units = [&](const FormPlan& f) {
+    return Units{bt, max_rows, f.log2r, f.lo, f.hi, reinterpret_cast<long long*>(base + f.prefix)};
+  };
+  auto result = [&](const FormPlan& f) {
+    return AttnOut{static_cast<bf16*>(out), stat, reinterpret_cast<float*>(base + f.part), f.cols};
+  };
   auto go = [&](auto hdv) {
     constexpr int HD = decltype(hdv)::value;
-    if (p.few) {
-      {
-        ProfileScope ps("cache_attn_few", s);
-        FOE_LAUNCH(cache_attn_few_kernel<HD>, dim3(p.ranges), dim3(kAttThr), 0, s, qb, a.k, a.v,
-                   a.kv_scale, w, kFewLeast, c_log2, o, score);
-      }
-      ProfileScope ps("cache_join_few", s);
-      FOE_LAUNCH(cache_join_few_kernel<HD>, dim3(a.H, a.B), dim3(256), 0, s, w, p.ranges, kFewLeast,
-                 o);
-    } else {
-      {
-        ProfileScope ps("cache_attn_tile", s);
-        FOE_LAUNCH(cache_attn_tile_kernel<HD>, dim3(p.ranges), dim3(kTileThr), 0, s, qb, a.k, a.v,
-                   a.kv_scale, w, kManyLeast, c_log2, o);
-      }
-      ProfileScope ps("cache_join_tile", s);
-      FOE_LAUNCH(cache_join_tile_kernel<HD>, dim3(p.tiles * (kTileCols / 32), a.H, a.B), dim3(256),
-                 0, s, w, p.ranges, kManyLeast, o);
-    }
-    if (score != nullptr) {
-      ProfileScope ps("cache_mass_few", s);
-      FOE_LAUNCH(cache_mass_few_kernel, dim3(p.ranges), dim3(kAttThr), 0, s, score, w, kFewLeast,
-                 p.cols, c_log2, o.stat, mass_in, mass_out);
-    } else if (mass_out != nullptr) {
+    auto mass = [&](const Units& w) {
       ProfileScope ps("cache_mass", s);
       FOE_LAUNCH(cache_mass_kernel<HD>, dim3(ceil_div(a.max_blocks, 2) * a.H, a.B), dim3(kMassThr),
-                 0, s, qb, a.k, a.kv_scale, bt, max_rows, c_log2, o.stat, mass_in, mass_out);
+                 0, s, qb, a.k, a.kv_scale, w, c_log2, stat, mass_in, mass_out);
+    };
+    if (p.few.on) {
+      const Units w = units(p.few);
+      const AttnOut o = result(p.few);
+      {
+        ProfileScope ps("cache_attn_few", s);
+        FOE_LAUNCH(cache_attn_few_kernel<HD>, dim3(p.few.ranges), dim3(kAttThr), 0, s, qb, a.k,
+                   a.v, a.kv_scale, w, kFewLeast, c_log2, o, score);
+      }
+      {
+        ProfileScope ps("cache_join_few", s);
+        FOE_LAUNCH(cache_join_few_kernel<HD>, dim3(a.H, a.B), dim3(256), 0, s, w, p.few.ranges,
+                   kFewLeast, o);
+      }
+      if (score != nullptr) {
+        ProfileScope ps("cache_mass_few", s);
+        FOE_LAUNCH(cache_mass_few_kernel, dim3(p.few.ranges), dim3(kAttThr), 0, s, score, w,
+                   kFewLeast, p.few.cols, c_log2, stat, mass_in, mass_out);
+      } else if (mass_out != nullptr) {
+        mass(w);
+      }
+    }
+    if (p.many.on) {
+      const Units w = units(p.many);
+      const AttnOut o = result(p.many);
+      {
+        ProfileScope ps("cache_attn_tile", s);
+        FOE_LAUNCH(cache_attn_tile_kernel<HD>, dim3(p.many.ranges), dim3(kTileThr), 0, s, qb, a.k,
+                   a.v, a.kv_scale, w, kManyLeast, c_log2, o);
+      }
+      {
+        ProfileScope ps("cache_join_tile", s);
+        FOE_LAUNCH(cache_join_tile_kernel<HD>,
+                   dim3(p.many.tiles * (kTileCols / 32) * (HD / 32), a.H, a.B), dim3(256), 0, s, w,
+                   p.many.ranges, kManyLeast, o);
+      }
+      if (mass_out != nullptr) mass(w);
     }
   };
   if (a.hd == 96) go(std::integral_constant<int, 96>{});

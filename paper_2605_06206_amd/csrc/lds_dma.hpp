@@ -60,6 +60,13 @@ __device__ __forceinline__ void dma16(__amdgpu_buffer_rsrc_t r, uint32_t voff, u
                "s"(r), "s"(lds), "i"(imm)
                : "memory", "scc");
 }
+// the same with 4 bytes a lane (256 bytes of LDS)
+__device__ __forceinline__ void dma4(__amdgpu_buffer_rsrc_t r, uint32_t voff, uint32_t lds,
+                                     int imm) {
+  asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(voff),
+               "s"(r), "s"(lds), "i"(imm)
+               : "memory", "scc");
+}
 // wait until at most N of this wave's vector memory operations are
 // outstanding and its LDS operations are done, then meet the other waves
 template <int N>
