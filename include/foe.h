@@ -321,7 +321,7 @@ size_t foe_group_attention_workspace_bytes(int H, int S, int d, int nq, int hd);
  *
  * bf16 activations and hd = 96 or 128 only (else FOE_ERR_UNSUPPORTED).  Limits:
  * 1 <= H <= 64, 1 <= nq <= 64, B <= 65535, N*nq <= 2^22, n_pages >= 1,
- * 1 <= max_blocks <= 2^24.
+ * 1 <= max_blocks <= 2^18.
  */
 #define FOE_CACHE_PAGE 64
 

@@ -37,14 +37,16 @@ constexpr float kMFloor = -1.0e30f;   // the running maximum's start: finite, be
 
 // ---- dealing out the work -------------------------------------------------------
 
-// The units of a batch in a form, numbered by sequence, group, tile and page.  A tile of the many form has 2^log2r rows, tile t reaches page
-// ceil((ctx + last row + 1) / 64), and the sums over tiles are closed forms.
+// The units of a batch in a form, numbered by sequence, group, tile and page.  A tile of
+// many columns has 2^log2r rows, tile t reaches page ceil((ctx + last row + 1) / 64), and
+// the sums over tiles are closed forms (which count pages past the table's end too).
+template <bool FEW>
 struct Units {
   CacheBatch bt;
   int max_rows;
-  int log2r;  // few: -1
+  int log2r;   // (many)
   int lo, hi;  // columns that a sequence of this form has: lo < columns <= hi
-  long long* prefix;  // [B + 1]: units before each sequence, and in all (written for the join)
+  long long* prefix;  // [B + 1]: units before each sequence, and in all (for the launches after)
 
   // rows of sequence b in this form
   __device__ __forceinline__ int rows(int b) const {
@@ -66,15 +68,15 @@ struct Units {
   }
   // pages of tile t of a sequence with n rows
   __device__ __forceinline__ int pages(int ctx, int n, int t) const {
-    const int last = log2r < 0 ? n : min((t + 1) << log2r, n);
-    return (ctx + last + kPage - 1) / kPage;
+    if (FEW) return min((ctx + n + kPage - 1) / kPage, bt.max_blocks);
+    return (ctx + min((t + 1) << log2r, n) + kPage - 1) / kPage;
   }
   // units of one group of sequence b
   __device__ __forceinline__ long long group(int b) const {
     const int n = rows(b);
     if (n <= 0) return 0;
-    const int ctx = bt.context(b), t = log2r < 0 ? 0 : tiles(n) - 1;
-    return (log2r < 0 ? 0 : before(ctx, t)) + pages(ctx, n, t);
+    const int ctx = bt.context(b), t = FEW ? 0 : tiles(n) - 1;
+    return (FEW ? 0 : before(ctx, t)) + pages(ctx, n, t);
   }
 };
 
@@ -84,16 +86,17 @@ __device__ __forceinline__ long long range_units(long long total, int ranges, in
   return per < least ? least : per;
 }
 
-// Total of the units, and the sequence that unit range * per falls in (b, or -1 past the
-// end) with its offset there.  Every thread of the workgroup calls it; range 0 writes
-// the prefix.
-template <int NT>
-__device__ __forceinline__ void locate(const Units& w, int ranges, int range, int least,
-                                       long long& total, int& b, long long& off) {
+// Total of the units, count(b) of sequence b, and the sequence that unit range * per falls
+// in (b, or -1 past the end) with its offset there.  Every thread of the workgroup calls
+// it; range 0 writes the prefix, if any: the units before each sequence, and in all.
+template <int NT, typename Count>
+__device__ __forceinline__ void locate(int B, Count count, int ranges, int range, int least,
+                                       long long* prefix, long long& total, int& b,
+                                       long long& off) {
   constexpr int NW = NT / kWave;
   __shared__ long long wave_sum[NW];
   __shared__ long long found[2];
-  const int B = w.bt.B, lane = lane_id(), wave = threadIdx.x >> 6;
+  const int lane = lane_id(), wave = threadIdx.x >> 6;
   auto scan = [&](long long c, long long& all) {  // inclusive sum over the threads
     long long incl = c;
 #pragma unroll
@@ -112,29 +115,30 @@ __device__ __forceinline__ void locate(const Units& w, int ranges, int range, in
     }
     return incl;
   };
-  const long long first = (int)threadIdx.x < B ? w.group(threadIdx.x) * w.bt.H : 0;
+  const long long first = (int)threadIdx.x < B ? count(threadIdx.x) : 0;
   long long mine = first;
-  for (int i = threadIdx.x + NT; i < B; i += NT) mine += w.group(i) * w.bt.H;
+  for (int i = threadIdx.x + NT; i < B; i += NT) mine += count(i);
   long long incl = scan(mine, total);
   const long long u0 = range * range_units(total, ranges, least);
+  const bool writes = prefix != nullptr && range == 0;
   if (threadIdx.x == 0) found[0] = -1;
-  if (B > NT && (u0 < total || range == 0)) {  // (uniform) again, a row of threads at a time
+  if (B > NT && (u0 < total || writes)) {  // (uniform) again, a row of threads at a time
     long long run = 0, all;
     for (int base = 0; base < B; base += NT) {
       const int i = base + (int)threadIdx.x;
-      const long long c = base == 0 ? first : i < B ? w.group(i) * w.bt.H : 0;
+      const long long c = base == 0 ? first : i < B ? count(i) : 0;
       incl = run + scan(c, all);
       if (u0 >= incl - c && u0 < incl) found[0] = i, found[1] = u0 - (incl - c);
-      if (range == 0 && i < B) w.prefix[i] = incl - c;
+      if (writes && i < B) prefix[i] = incl - c;
       run += all;
     }
   } else if (B <= NT) {
     __syncthreads();
     const int i = threadIdx.x;
     if (u0 >= incl - first && u0 < incl) found[0] = i, found[1] = u0 - (incl - first);
-    if (range == 0 && i < B) w.prefix[i] = incl - first;
+    if (writes && i < B) prefix[i] = incl - first;
   }
-  if (range == 0 && threadIdx.x == 0) w.prefix[B] = total;
+  if (writes && threadIdx.x == 0) prefix[B] = total;
   __syncthreads();
   b = (int)found[0];
   off = found[1];
@@ -378,13 +382,15 @@ __device__ __forceinline__ void few_columns(
 template <int HD>
 __global__ __launch_bounds__(kAttThr, 2) void cache_attn_few_kernel(
     const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
-    const float* __restrict__ kv_scale, Units w, int least, float c_log2, AttnOut o,
+    const float* __restrict__ kv_scale, Units<true> w, int least, float c_log2, AttnOut o,
     float* __restrict__ score) {
   __shared__ FewLds<HD, kAttWaves> lds;
   const CacheBatch& bt = w.bt;
   long long total, off;
   int b;
-  locate<kAttThr>(w, gridDim.x, blockIdx.x, least, total, b, off);
+  locate<kAttThr>(
+      bt.B, [&](int i) { return w.group(i) * bt.H; }, gridDim.x, blockIdx.x, least, w.prefix, total,
+      b, off);
   if (b < 0) return;
   const int per = (int)range_units(total, gridDim.x, least);
   long long unit = (long long)blockIdx.x * per;
@@ -429,8 +435,8 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_few_kernel(
 template <int HD>
 __global__ __launch_bounds__(kTileThr) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ kc,
-                       const uint8_t* __restrict__ vc, const float* __restrict__ kv_scale, Units w,
-                       int least, float c_log2, AttnOut o) {
+                       const uint8_t* __restrict__ vc, const float* __restrict__ kv_scale,
+                       Units<false> w, int least, float c_log2, AttnOut o) {
   constexpr int KT = kPage * 256;       // K tile bytes
   constexpr int VT = HD * kPage * 2;    // V^T tile bytes
   constexpr int NST = HD / 16;          // score k-steps
@@ -445,7 +451,9 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
   const int range = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
   long long total, off;
   int b;
-  locate<kTileThr>(w, gridDim.x, range, least, total, b, off);
+  locate<kTileThr>(
+      bt.B, [&](int i) { return w.group(i) * bt.H; }, gridDim.x, range, least, w.prefix, total, b,
+      off);
   if (b < 0) return;
   const int per = (int)range_units(total, gridDim.x, least);
   int left = (int)min((long long)per, total - (long long)range * per);
@@ -712,7 +720,8 @@ struct Parts {
   }
 };
 // units u0 .. u0 + np - 1 of the tile; false where one range wrote it whole
-__device__ __forceinline__ bool find_parts(const Units& w, int ranges, int least, long long u0,
+template <bool FEW>
+__device__ __forceinline__ bool find_parts(const Units<FEW>& w, int ranges, int least, long long u0,
                                            int np, Parts& p) {
   const long long per = range_units(w.prefix[w.bt.B], ranges, least);
   p.r0 = (int)(u0 / per);
@@ -724,7 +733,7 @@ __device__ __forceinline__ bool find_parts(const Units& w, int ranges, int least
 // Few columns: one workgroup per (group, sequence).  8 groups of 32 lanes (a lane 4 dims)
 // each sum every eighth part, and are then summed in order.
 template <int HD>
-__global__ __launch_bounds__(256) void cache_join_few_kernel(Units w, int ranges, int least,
+__global__ __launch_bounds__(256) void cache_join_few_kernel(Units<true> w, int ranges, int least,
                                                              AttnOut o) {
   __shared__ f32x4 osum[8][32];
   const CacheBatch& bt = w.bt;
@@ -779,19 +788,19 @@ __global__ __launch_bounds__(256) void cache_join_few_kernel(Units w, int ranges
   }
 }
 
-// Many columns: one workgroup per (32 columns and 32 dims of a tile, group, sequence); a
-// thread has 4 dims of a column and loads eight parts at a time.
+// Many columns: one workgroup per (32 columns of a tile, group), 8 threads a column; a
+// thread loads its dims of four parts at a time.
 template <int HD>
-__global__ __launch_bounds__(256) void cache_join_tile_kernel(Units w, int ranges, int least,
+__global__ __launch_bounds__(256) void cache_join_tile_kernel(Units<false> w, int ranges, int least,
                                                               AttnOut o) {
-  constexpr int CB = kTileCols / 32, DB = HD / 32, AT_ONCE = 8;
+  constexpr int CB = kTileCols / 32, NV = HD / 32, AT_ONCE = 4;
   const CacheBatch& bt = w.bt;
-  const int t = blockIdx.x / (CB * DB), h = blockIdx.y, b = blockIdx.z;
-  const int c = blockIdx.x % CB * 32 + (threadIdx.x & 31);
-  const int d4 = blockIdx.x / CB % DB * 8 + (threadIdx.x >> 5);
-  const int rows = w.rows(b);
-  if (rows <= 0 || t >= w.tiles(rows)) return;
-  const int ctx = bt.context(b), row0 = t << w.log2r;
+  const int h = blockIdx.y;
+  int b, t;
+  if (!find_tile<256>(bt.B, blockIdx.x / CB, [&](int i) { return w.tiles(w.rows(i)); }, b, t))
+    return;
+  const int c = blockIdx.x % CB * 32 + (threadIdx.x & 31), l3 = threadIdx.x >> 5;
+  const int rows = w.rows(b), ctx = bt.context(b), row0 = t << w.log2r;
   const int ncol = (min(rows, (t + 1) << w.log2r) - row0) * bt.nq;
   const int np = w.pages(ctx, rows, t);
   Parts p{o.part, kTileCols, HD};
@@ -799,17 +808,23 @@ __global__ __launch_bounds__(256) void cache_join_tile_kernel(Units w, int range
       c >= ncol)
     return;
   float m = kMFloor, l = 0.f;
-  f32x4 x{0.f, 0.f, 0.f, 0.f};
+  f32x4 x[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) x[k] = f32x4{0.f, 0.f, 0.f, 0.f};
   for (int r0 = p.r0; r0 <= p.r1; r0 += AT_ONCE) {
     float2 z[AT_ONCE];
-    f32x4 y[AT_ONCE];
+    f32x4 y[AT_ONCE][NV];
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i) {
       z[i] = float2{kMFloor, 0.f};
-      y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < NV; ++k) y[i][k] = f32x4{0.f, 0.f, 0.f, 0.f};
       if (r0 + i > p.r1) continue;
       z[i] = p.stats(r0 + i)[c];
-      y[i] = *reinterpret_cast<const f32x4*>(p.at(r0 + i) + ((size_t)d4 * kTileCols + c) * 4);
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        y[i][k] = *reinterpret_cast<const f32x4*>(p.at(r0 + i) +
+                                                  ((size_t)(l3 + 8 * k) * kTileCols + c) * 4);
     }
     float mn = m;
 #pragma unroll
@@ -818,21 +833,28 @@ __global__ __launch_bounds__(256) void cache_join_tile_kernel(Units w, int range
     m = mn;
     l *= a0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] *= a0;
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[k][e] *= a0;
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i) {
       const float a = __builtin_amdgcn_exp2f(z[i].x - m);
       l += z[i].y * a;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] += y[i][e] * a;
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[k][e] += y[i][k][e] * a;
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const int row = bt.first_row(b) + row0 + c / bt.nq;
   bf16* dst = o.out + (((size_t)row * bt.H + h) * bt.nq + c % bt.nq) * HD;
-  *reinterpret_cast<bf16x4*>(dst + 4 * d4) =
-      bf16x4{(bf16)(x[0] * inv), (bf16)(x[1] * inv), (bf16)(x[2] * inv), (bf16)(x[3] * inv)};
-  if (o.stat != nullptr && d4 == 0)
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+    *reinterpret_cast<bf16x4*>(dst + 4 * (l3 + 8 * k)) =
+        bf16x4{(bf16)(x[k][0] * inv), (bf16)(x[k][1] * inv), (bf16)(x[k][2] * inv),
+               (bf16)(x[k][3] * inv)};
+  if (o.stat != nullptr && l3 == 0)
     o.stat[((size_t)h * bt.N + bt.first_row(b) + row0) * bt.nq + c] = float2{m, inv};
 }
 
@@ -843,7 +865,7 @@ __global__ __launch_bounds__(256) void cache_join_tile_kernel(Units w, int range
 
 // Few columns: the ranges of the attention; a wave takes every fourth page, a lane a token.
 __global__ __launch_bounds__(kAttThr) void cache_mass_few_kernel(
-    const float* __restrict__ score, Units w, int least, int part_cols, float c_log2,
+    const float* __restrict__ score, Units<true> w, int least, int part_cols, float c_log2,
     const float2* __restrict__ stat, const float* __restrict__ mass_in,
     float* __restrict__ mass_out) {
   __shared__ int found;
@@ -894,21 +916,22 @@ __global__ __launch_bounds__(kAttThr) void cache_mass_few_kernel(
   }
 }
 
-// Any columns: one workgroup per (two pages, group, sequence), a wave for 32 keys, held in
+// Any columns: a workgroup takes pairs of pages, a wave 32 of their keys, held in
 // registers as A operand of v_mfma_f32_32x32x16_bf16.  Tiles of 32 columns go by through a
 // ring of four in LDS, filled by LDS-DMA three tiles ahead (256-byte rows, 16-byte chunk
 // c in slot c ^ (column & 15); the columns' maxima and sums behind them), since a tile
 // takes less time than a load.  Four workgroups fit a CU: many of them do little (a
 // decoding sequence's pages) and wait for their first loads.
 // us of this kernel for 4096 rows over 4096 tokens, 8 groups of two heads, and for a 512-row
-// chunk beside 16 decoding sequences: tiles through registers, one ahead 224 and 46; so XX.
+// chunk beside 16 decoding sequences: tiles through registers, one ahead 224 and 46; so 176
+// and 40 (two tiles at a time 170, with registers for three workgroups).
 constexpr int kMassThr = 256, kMassCols = 32;
 constexpr int kMassStages = 4;
 
 template <int HD>
 __global__ __launch_bounds__(kMassThr, 4) void cache_mass_kernel(
     const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const float* __restrict__ kv_scale,
-    Units w, float c_log2, const float2* __restrict__ stat, const float* __restrict__ mass_in,
+    Units<false> w, float c_log2, const float2* __restrict__ stat, const float* __restrict__ mass_in,
     float* __restrict__ mass_out) {
   constexpr int NST = HD / 16;
   constexpr int QT = kMassCols * 256, STAGE = QT + 256;  // bytes of a tile, and with its statistics
@@ -919,103 +942,124 @@ __global__ __launch_bounds__(kMassThr, 4) void cache_mass_kernel(
   const int wave_u = __builtin_amdgcn_readfirstlane(wave);
   const int qi = lane & 31, hl = lane >> 5;
   const CacheBatch& bt = w.bt;
-  const int h = blockIdx.x % bt.H, b = blockIdx.y, blk0 = blockIdx.x / bt.H * 2;
-  const int rows = w.rows(b), ctx = bt.context(b);
-  const int len = min(ctx + rows, bt.cap());
-  if (rows == 0 || blk0 * kPage >= len) return;
-  const int key0 = blk0 * kPage + wave * 32;  // the wave's first key
-  const int page = bt.page(b, key0 / kPage);
-  const bool works = page >= 0 && key0 < len;  // (wave-uniform)
-  const size_t pg = (size_t)max(page, 0) * bt.H + h;
-  // key qi; in steps st, st + 1 the lane halves hold dims 32 (st / 2) + 16 hl + 8 (st % 2)
-  bf16x8 kf[NST];
-  {
-    const float ks = works ? kv_scale[pg * 2] : 0.f;
-    const uint8_t* row = kc + pg * (kPage * HD) + ((wave & 1) * 32 + qi) * HD + 16 * hl;
-#pragma unroll
-    for (int st = 0; st < NST; st += 2) {
-      u32x4 x = zero_u32x4();
-      if (works) x = *reinterpret_cast<const u32x4*>(row + 16 * st);
-      kf[st] = codes_to_bf16(x[0], x[1], ks);
-      kf[st + 1] = codes_to_bf16(x[2], x[3], ks);
-    }
-  }
-  // arrived before the loop, whose loads are counted
-#pragma unroll
-  for (int st = 0; st < NST; ++st) asm volatile("" ::"v"(kf[st]));
-  const int ncol = rows * bt.nq;
-  const size_t qrow = ((size_t)h * bt.N + bt.first_row(b)) * bt.nq;
-  float acc[16];
-#pragma unroll
-  for (int v = 0; v < 16; ++v) acc[v] = 0.f;
-  // tiles before the first column that sees the pages are left out
-  const long long c_first = (long long)max(blk0 * kPage - ctx, 0) * bt.nq;
-  const int t0 = (int)(c_first / kMassCols), t1 = (ncol + kMassCols - 1) / kMassCols;
-  // columns past the last read zeros: no query, maximum 0 and 1 / sum 0
-  const __amdgpu_buffer_rsrc_t rq = make_rsrc_u(q + qrow * HD, (uint32_t)ncol * (HD * 2));
-  const __amdgpu_buffer_rsrc_t rz = make_rsrc_u(stat + qrow, (uint32_t)ncol * 8u);
-  rsrc_settle(rq, rz);
-  uint32_t qoff[QI];
-#pragma unroll
-  for (int i = 0; i < QI; ++i) {
-    const int c = 4 * (wave * QI + i) + (lane >> 4), ch = (lane & 15) ^ (c & 15);
-    qoff[i] = ch < HD / 8 ? (uint32_t)(c * (HD * 2) + ch * 16) : kOob;
-  }
-  const uint32_t lds = lds_addr(smem);
-  auto issue = [&](int t) {
-    const uint32_t to = lds + (uint32_t)((t & (kMassStages - 1)) * STAGE);
-    const uint32_t step = (uint32_t)t * (kMassCols * HD * 2);
-#pragma unroll
-    for (int i = 0; i < QI; ++i) dma16(rq, qoff[i] + step, to + (uint32_t)wave_u * (QI * 1024), i * 1024);
-    // (every wave loads the statistics, so that all count the same)
-    dma4(rz, (uint32_t)t * (kMassCols * 8) + lane * 4u, to, QT);
+  // pairs of a sequence, all groups; numbered by sequence, pair and group
+  auto pairs = [&](int i) -> long long {
+    const int n = w.rows(i);
+    const int len = min(bt.context(i) + n, bt.cap());
+    return n > 0 ? (long long)((len + 2 * kPage - 1) / (2 * kPage)) * bt.H : 0;
   };
-  constexpr int OPS = QI + 1;  // DMA instructions of a wave and tile
+  long long total, off;
+  int b;
+  locate<kMassThr>(bt.B, pairs, gridDim.x, blockIdx.x, 1, nullptr, total, b, off);
+  if (b < 0) return;
+  const long long per = range_units(total, gridDim.x, 1);
+  long long left = min(per, total - blockIdx.x * per);
+  while (true) {
+    const int h = (int)(off % bt.H), blk0 = (int)(off / bt.H) * 2;
+    const int rows = w.rows(b), ctx = bt.context(b);
+    const int len = min(ctx + rows, bt.cap());
+    const int key0 = blk0 * kPage + wave * 32;  // the wave's first key
+    const int page = bt.page(b, key0 / kPage);
+    const bool works = page >= 0 && key0 < len;  // (wave-uniform)
+    const size_t pg = (size_t)max(page, 0) * bt.H + h;
+    // key qi; in steps st, st + 1 the lane halves hold dims 32 (st / 2) + 16 hl + 8 (st % 2)
+    bf16x8 kf[NST];
+    {
+      const float ks = works ? kv_scale[pg * 2] : 0.f;
+      const uint8_t* row = kc + pg * (kPage * HD) + ((wave & 1) * 32 + qi) * HD + 16 * hl;
 #pragma unroll
-  for (int i = 0; i < kMassStages - 1; ++i)
-    if (t0 + i < t1) issue(t0 + i);
-  for (int t = t0; t < t1; ++t) {
-    // this tile has landed for every wave, and the one before is done with
-    if (t + 2 < t1) vm_barrier<2 * OPS>();
-    else if (t + 1 < t1) vm_barrier<OPS>();
-    else vm_barrier<0>();
-    if (t + kMassStages - 1 < t1) issue(t + kMassStages - 1);
-    const unsigned char* tile = smem + (t & (kMassStages - 1)) * STAGE;
-    if (works) {
-      const float2 z = *reinterpret_cast<const float2*>(tile + QT + qi * 8);
-      f32x16 x;
-#pragma unroll
-      for (int v = 0; v < 16; ++v) x[v] = 0.f;
-#pragma unroll
-      for (int st = 0; st < NST; ++st) {
-        const int ch = 4 * (st / 2) + 2 * hl + st % 2;
-        const bf16x8 qf =
-            *reinterpret_cast<const bf16x8*>(tile + qi * 256 + ((ch ^ (qi & 15)) << 4));
-        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[st], qf, x, 0, 0, 0);
+      for (int st = 0; st < NST; st += 2) {
+        u32x4 x = zero_u32x4();
+        if (works) x = *reinterpret_cast<const u32x4*>(row + 16 * st);
+        kf[st] = codes_to_bf16(x[0], x[1], ks);
+        kf[st + 1] = codes_to_bf16(x[2], x[3], ks);
       }
-      // (the tile's first column sees the fewest)
-      if (ctx + t * kMassCols / bt.nq + 1 < min(key0 + 32, len + 1)) {
-        const int col = t * kMassCols + qi, seen = col < ncol ? ctx + col / bt.nq + 1 : 0;
+    }
+    // arrived before the loop, whose loads are counted
+#pragma unroll
+    for (int st = 0; st < NST; ++st) asm volatile("" ::"v"(kf[st]));
+    const int ncol = rows * bt.nq;
+    const size_t qrow = ((size_t)h * bt.N + bt.first_row(b)) * bt.nq;
+    float acc[16];
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[v] = 0.f;
+    // tiles before the first column that sees the pages are left out
+    const long long c_first = (long long)max(blk0 * kPage - ctx, 0) * bt.nq;
+    const int t0 = (int)(c_first / kMassCols), t1 = (ncol + kMassCols - 1) / kMassCols;
+    // columns past the last read zeros: no query, maximum 0 and 1 / sum 0
+    const __amdgpu_buffer_rsrc_t rq = make_rsrc_u(q + qrow * HD, (uint32_t)ncol * (HD * 2));
+    const __amdgpu_buffer_rsrc_t rz = make_rsrc_u(stat + qrow, (uint32_t)ncol * 8u);
+    rsrc_settle(rq, rz);
+    uint32_t qoff[QI];
+#pragma unroll
+    for (int i = 0; i < QI; ++i) {
+      const int c = 4 * (wave * QI + i) + (lane >> 4), ch = (lane & 15) ^ (c & 15);
+      qoff[i] = ch < HD / 8 ? (uint32_t)(c * (HD * 2) + ch * 16) : kOob;
+    }
+    const uint32_t lds = lds_addr(smem);
+    auto issue = [&](int t) {
+      const uint32_t to = lds + (uint32_t)((t & (kMassStages - 1)) * STAGE);
+      const uint32_t step = (uint32_t)t * (kMassCols * HD * 2);
+#pragma unroll
+      for (int i = 0; i < QI; ++i) dma16(rq, qoff[i] + step, to + (uint32_t)wave_u * (QI * 1024), i * 1024);
+      // (every wave loads the statistics, so that all count the same)
+      dma4(rz, (uint32_t)t * (kMassCols * 8) + lane * 4u, to, QT);
+    };
+    constexpr int OPS = QI + 1;  // DMA instructions of a wave and tile
+#pragma unroll
+    for (int i = 0; i < kMassStages - 1; ++i)
+      if (t0 + i < t1) issue(t0 + i);
+    for (int t = t0; t < t1; ++t) {
+      // this tile has landed for every wave, and the one before is done with
+      if (t + 2 < t1) vm_barrier<2 * OPS>();
+      else if (t + 1 < t1) vm_barrier<OPS>();
+      else vm_barrier<0>();
+      if (t + kMassStages - 1 < t1) issue(t + kMassStages - 1);
+      const unsigned char* tile = smem + (t & (kMassStages - 1)) * STAGE;
+      if (works) {
+        const float2 z = *reinterpret_cast<const float2*>(tile + QT + qi * 8);
+        f32x16 x;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) x[v] = 0.f;
+#pragma unroll
+        for (int st = 0; st < NST; ++st) {
+          const int ch = 4 * (st / 2) + 2 * hl + st % 2;
+          const bf16x8 qf =
+              *reinterpret_cast<const bf16x8*>(tile + qi * 256 + ((ch ^ (qi & 15)) << 4));
+          x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[st], qf, x, 0, 0, 0);
+        }
+        // (the tile's first column sees the fewest)
+        if (ctx + t * kMassCols / bt.nq + 1 < min(key0 + 32, len + 1)) {
+          const int col = t * kMassCols + qi, seen = col < ncol ? ctx + col / bt.nq + 1 : 0;
+#pragma unroll
+          for (int v = 0; v < 16; ++v)
+            if (key0 + 8 * (v >> 2) + 4 * hl + (v & 3) >= seen) x[v] = -__builtin_inff();
+        }
 #pragma unroll
         for (int v = 0; v < 16; ++v)
-          if (key0 + 8 * (v >> 2) + 4 * hl + (v & 3) >= seen) x[v] = -__builtin_inff();
+          acc[v] = fmaf(__builtin_amdgcn_exp2f(fmaf(x[v], c_log2, -z.x)), z.y, acc[v]);
       }
-#pragma unroll
-      for (int v = 0; v < 16; ++v)
-        acc[v] = fmaf(__builtin_amdgcn_exp2f(fmaf(x[v], c_log2, -z.x)), z.y, acc[v]);
     }
-  }
 #pragma unroll
-  for (int v = 0; v < 16; ++v) {
+    for (int v = 0; v < 16; ++v) {
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) acc[v] += __shfl_xor(acc[v], o);
-    if (qi == 0) sum[wave][8 * (v >> 2) + 4 * hl + (v & 3)] = acc[v];
-  }
-  __syncthreads();
-  const int slot = key0 + lane;
-  if (works && lane < 32 && slot < len) {
-    const size_t at = pg * kPage + (wave & 1) * 32 + lane;
-    mass_out[at] = (slot < ctx ? mass_in[at] : 0.f) + sum[wave][lane];
+      for (int o = 1; o < 32; o <<= 1) acc[v] += __shfl_xor(acc[v], o);
+      if (qi == 0) sum[wave][8 * (v >> 2) + 4 * hl + (v & 3)] = acc[v];
+    }
+    __syncthreads();
+    const int slot = key0 + lane;
+    if (works && lane < 32 && slot < len) {
+      const size_t at = pg * kPage + (wave & 1) * 32 + lane;
+      mass_out[at] = (slot < ctx ? mass_in[at] : 0.f) + sum[wave][lane];
+    }
+    if (--left == 0) return;
+    __syncthreads();  // the ring and the sums have been read
+    if (++off == pairs(b)) {
+      off = 0;
+      do {
+        if (++b >= bt.B) return;
+      } while (w.rows(b) <= 0);
+    }
   }
 }
 
@@ -1056,7 +1100,7 @@ AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_
   const long long most = (long long)max_rows * nq;
   // Both forms where the sequences beside the longest have few columns on average: each
   // form's launches cost some 10 us where it has no sequence (us for a 512-row chunk beside
-  // 16 decoding sequences, with mass: XX, and 117 in the second form alone).
+  // 16 decoding sequences, with mass: 92, and 117 in the second form alone).
   p.few.on = most <= kFewCols || (B > 1 && (long long)(N - max_rows) * nq <= kFewCols * (B - 1LL));
   p.many.on = most > kFewCols;
   p.few.hi = kFewCols;
@@ -1074,11 +1118,11 @@ AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_
   const long long pages = (long long)B * H * max_blocks;
   p.few.cols = (int)std::min<long long>(kFewCols, most);
   p.few.ranges = (int)std::min<long long>(4LL * cus, (pages + kFewLeast - 1) / kFewLeast);
-  p.few.log2r = -1;
   p.many.cols = kTileCols;
   p.many.ranges = cus;
   while ((2 << p.many.log2r) * nq <= kTileCols) ++p.many.log2r;
-  p.many.tiles = ceil_div(max_rows, 1 << p.many.log2r);
+  // tiles of the batch: at most n / 2^log2r, rounded up, of each sequence
+  p.many.tiles = (int)std::min<long long>(N, ((long long)N >> p.many.log2r) + B);
   scratch(p.few);
   scratch(p.many);
   if (mass) {
@@ -1108,21 +1152,26 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
   const bf16* qb = static_cast<const bf16*>(q);
   float2* stat = mass_out != nullptr ? reinterpret_cast<float2*>(base + p.stat) : nullptr;
   float* score = p.scores ? reinterpret_cast<float*>(base + p.score) : nullptr;
-  auto units = [&](const FormPlan& f) {
-    return Units{bt, max_rows, f.log2r, f.lo, f.hi, reinterpret_cast<long long*>(base + f.prefix)};
+  auto units = [&](const FormPlan& f, auto few) {
+    return Units<decltype(few)::value>{bt, max_rows, f.log2r, f.lo, f.hi,
+                                       reinterpret_cast<long long*>(base + f.prefix)};
   };
   auto result = [&](const FormPlan& f) {
     return AttnOut{static_cast<bf16*>(out), stat, reinterpret_cast<float*>(base + f.part), f.cols};
   };
   auto go = [&](auto hdv) {
     constexpr int HD = decltype(hdv)::value;
-    auto mass = [&](const Units& w) {
+    auto mass = [&](const FormPlan& f) {
       ProfileScope ps("cache_mass", s);
-      FOE_LAUNCH(cache_mass_kernel<HD>, dim3(ceil_div(a.max_blocks, 2) * a.H, a.B), dim3(kMassThr),
-                 0, s, qb, a.k, a.kv_scale, w, c_log2, stat, mass_in, mass_out);
+      // (16 workgroups a CU at most: four rounds, which evens out what pages near a chunk's
+      // end have less to do)
+      const long long pairs = (long long)ceil_div(a.max_blocks, 2) * a.H * a.B;
+      FOE_LAUNCH(cache_mass_kernel<HD>, dim3((unsigned)std::min(16LL * cus, pairs)), dim3(kMassThr),
+                 0, s, qb, a.k, a.kv_scale, units(f, std::false_type{}), c_log2, stat, mass_in,
+                 mass_out);
     };
     if (p.few.on) {
-      const Units w = units(p.few);
+      const Units<true> w = units(p.few, std::true_type{});
       const AttnOut o = result(p.few);
       {
         ProfileScope ps("cache_attn_few", s);
@@ -1139,11 +1188,11 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
         FOE_LAUNCH(cache_mass_few_kernel, dim3(p.few.ranges), dim3(kAttThr), 0, s, score, w,
                    kFewLeast, p.few.cols, c_log2, stat, mass_in, mass_out);
       } else if (mass_out != nullptr) {
-        mass(w);
+        mass(p.few);
       }
     }
     if (p.many.on) {
-      const Units w = units(p.many);
+      const Units<false> w = units(p.many, std::false_type{});
       const AttnOut o = result(p.many);
       {
         ProfileScope ps("cache_attn_tile", s);
@@ -1153,10 +1202,10 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
       {
         ProfileScope ps("cache_join_tile", s);
         FOE_LAUNCH(cache_join_tile_kernel<HD>,
-                   dim3(p.many.tiles * (kTileCols / 32) * (HD / 32), a.H, a.B), dim3(256), 0, s, w,
-                   p.many.ranges, kManyLeast, o);
+                   dim3(p.many.tiles * (kTileCols / 32), a.H), dim3(256), 0, s, w, p.many.ranges,
+                   kManyLeast, o);
       }
-      if (mass_out != nullptr) mass(w);
+      if (mass_out != nullptr) mass(p.many);
     }
   };
   if (a.hd == 96) go(std::integral_constant<int, 96>{});

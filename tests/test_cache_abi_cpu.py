@@ -30,7 +30,7 @@ APPEND = [BF16, 8, 4, 6, 2, 128, 100, 16, 5e5, 16.0, P, P, P, None, P, P2, P, P,
     (2, -1, INV, "B must"), (2, 65536, INV, "B must"), (3, -1, INV, "N*nq"),
     (3, 1 << 26, INV, "N*nq"), (4, 0, INV, "nq must"), (4, 65, INV, "nq must"),
     (5, 64, UNS, "hd = 96"), (6, 0, INV, "n_pages"), (7, 0, INV, "max_blocks"),
-    (7, (1 << 24) + 1, INV, "max_blocks"), (8, 0.0, INV, "theta"), (8, float("nan"), INV, "theta"),
+    (7, (1 << 18) + 1, INV, "max_blocks"), (8, 0.0, INV, "theta"), (8, float("nan"), INV, "theta"),
     (9, -1.0, INV, "scale"), (10, None, INV, "qkv is NULL"), (10, P + 8, INV, "qkv is not"),
     (10, P2, INV, "q_out must not"), (11, None, INV, "row_start"), (12, P + 2, INV, "ctx_len"),
     (13, P + 1, INV, "pos"), (14, None, INV, "block_table"), (15, None, INV, "q_out"),

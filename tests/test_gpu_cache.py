@@ -454,6 +454,27 @@ def test_attention_past_the_tables_end():
     check_attention(pool, table, [120], np.array([0, 12]), q, out, mass)
 
 
+def test_attention_full_tables():
+    """Sequences that fill their tables, or would pass them, beside one another: what is
+    kept for the mass stays within the workspace."""
+    rng = np.random.default_rng(20)
+    H, nq, hd, B = 2, 4, 96, 5
+    pool = random_pool(rng, 12, H, hd)
+    dev, table = to_dev(pool), rng.permutation(12)[:10].reshape(5, 2).astype(np.int32)
+    ctx, rs = [128, 127, 128, 300, 126], np.array([0, 1, 3, 4, 6, 9])
+    q = bf16(rng.normal(size=(H, 9, nq, hd)))
+    n = foe.cache_attention_workspace_bytes(q, ints(table), 3, True)
+    ws = torch.zeros(n + (1 << 20), dtype=torch.uint8, device=DEV)
+    ws[n:] = 0xA5
+    say("full tables")
+    mass = torch.full_like(dev["mass"], -7.0)
+    out = foe.cache_attention(q, dev["k"], dev["v"], dev["kv_scale"], ints(table), ints(ctx),
+                              ints(rs), 3, mass_in=dev["mass"], mass_out=mass, ws=ws)
+    torch.cuda.synchronize()
+    assert (ws[n:] == 0xA5).all()
+    check_attention(pool, table, [min(c, 128) for c in ctx], rs, q, out, mass)
+
+
 @pytest.mark.parametrize("H,nq,hd,ctx,rows,picked", [
     (1, 2, 128, 131071, 1, [0]),
     (1, 1, 96, 40000, 300, [0, 1, 63, 64, 255, 256, 299]),
