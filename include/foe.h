@@ -321,7 +321,7 @@ size_t foe_group_attention_workspace_bytes(int H, int S, int d, int nq, int hd);
  *
  * bf16 activations and hd = 96 or 128 only (else FOE_ERR_UNSUPPORTED).  Limits:
  * 1 <= H <= 64, 1 <= nq <= 64, B <= 65535, N*nq <= 2^22, n_pages >= 1,
- * 1 <= max_blocks <= 2^18.
+ * 1 <= max_blocks <= 2^18, B*max_blocks <= 2^31.
  */
 #define FOE_CACHE_PAGE 64
 
@@ -396,7 +396,7 @@ size_t foe_cache_attention_workspace_bytes(int H, int B, int N, int nq, int hd, 
  * dst_table; shorter sequences are moved whole.  Each page's scales follow
  * from the values that it then holds, and mass moves with its token.
  *
- *   keep, recent           0 <= recent <= keep, keep >= 1
+ *   keep, recent           0 <= recent <= keep, 1 <= keep <= 2^30
  *   length    [B]          int32  tokens of each sequence
  *   k_cache, v_cache, kv_scale, mass   the pool: read at block_table's pages, written at
  *                          dst_table's, which must be other pages

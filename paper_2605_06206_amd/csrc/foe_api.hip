@@ -591,6 +591,7 @@ void check_cache(Check& c, int H, int B, int n_pages, int max_blocks) {
   c.need(B >= 0 && B <= 65535, "B must be in [0, 65535]");
   c.need(n_pages >= 1, "n_pages must be >= 1");
   c.need(max_blocks >= 1 && max_blocks <= (1 << 18), "max_blocks must be in [1, 2^18]");
+  c.need((long long)B * max_blocks <= 1LL << 31, "B*max_blocks must be at most 2^31");
 }
 void check_rows(Check& c, int N, int nq) {
   c.need(nq >= 1 && nq <= 64, "nq must be in [1, 64]");

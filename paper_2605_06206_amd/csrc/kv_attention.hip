@@ -32,7 +32,7 @@ constexpr int kAttWaves = kAttThr / kWave;
 constexpr int kFewCols = 16;
 constexpr int kTileThr = 512;         // many columns: eight waves of 32 columns
 constexpr int kTileCols = 256;
-constexpr int kMaxCus = 256;          // the workspace holds the parts of this many units
+constexpr int kCus = 256;             // compute units of the card; a multiple of the XCDs
 constexpr float kMFloor = -1.0e30f;   // the running maximum's start: finite, below any score
 
 // ---- dealing out the work -------------------------------------------------------
@@ -80,7 +80,8 @@ struct Units {
   }
 };
 
-// units of a workgroup's range
+// units of a workgroup's range (a batch's are below 2^39, of tables of up to 2^31 entries, 64
+// groups and 2^22 columns: a range of the launches here has fewer than 2^31)
 __device__ __forceinline__ long long range_units(long long total, int ranges, int least) {
   const long long per = (total + ranges - 1) / ranges;
   return per < least ? least : per;
@@ -227,31 +228,32 @@ struct AttnOut {
   int part_cols;
 };
 
-template <int HD, int NW>
+template <int HD>
 struct FewLds {
-  float mm[NW][16], ll[NW][16];
-  float oo[NW][16][HD + 4];  // (rows of other bank groups)
+  float mm[kAttWaves][16], ll[kAttWaves][16];
+  float oo[kAttWaves][16][HD + 4];  // (rows of other bank groups)
 };
 
-// Pages blk0 .. blk1-1 of at most 16 columns (rows row0 .. of sequence b, group h), dealt to
-// the NW waves of the workgroup; `slot` is where a part goes, `score` the scores of page
-// blk0 or null.
-template <int HD, int NW>
+// Pages blk0 .. blk1-1 of the columns (at most 16) of sequence b, group h, dealt to the
+// waves of the workgroup; `slot` is where a part goes, `score` the scores of page blk0 or
+// null.
+template <int HD>
 __device__ __forceinline__ void few_columns(
     const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
-    const float* __restrict__ kv_scale, const CacheBatch& bt, int b, int h, int rows, int row0,
-    int ctx, int np, int blk0, int blk1, float c_log2, const AttnOut& o, size_t slot,
-    float* __restrict__ score, FewLds<HD, NW>& lds) {
+    const float* __restrict__ kv_scale, const CacheBatch& bt, int b, int h, int rows, int ctx,
+    int np, int blk0, int blk1, float c_log2, const AttnOut& o, size_t slot,
+    float* __restrict__ score, FewLds<HD>& lds) {
   using F = PageFrags<HD>;
+  constexpr int NW = kAttWaves;
   const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
   const int n = lane & 15, g = lane >> 4;
-  const int ncol = (rows - row0) * bt.nq;
-  const size_t qrow = ((size_t)h * bt.N + bt.first_row(b) + row0) * bt.nq;
+  const int ncol = rows * bt.nq;
+  const size_t qrow = ((size_t)h * bt.N + bt.first_row(b)) * bt.nq;
   bf16x8 qf[F::NST];
   load_q<HD>(q + qrow * HD, n, ncol, g, qf);
   const int len = min(ctx + rows, bt.cap());  // tokens the cache holds now
-  const int seen = n < ncol ? min(ctx + row0 + n / bt.nq + 1, bt.cap()) : 0;
-  const int fewest = min(ctx + row0 + 1, bt.cap());  // that a column sees
+  const int seen = n < ncol ? min(ctx + n / bt.nq + 1, bt.cap()) : 0;
+  const int fewest = min(ctx + 1, bt.cap());  // that a column sees
   f32x4 oacc[F::NDT];
 #pragma unroll
   for (int dt = 0; dt < F::NDT; ++dt) oacc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -369,7 +371,7 @@ __device__ __forceinline__ void few_columns(
     if (whole) {
       // a column that sees no token gives zeros
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      const int row = bt.first_row(b) + row0 + c / bt.nq;
+      const int row = bt.first_row(b) + c / bt.nq;
       o.out[(((size_t)row * bt.H + h) * bt.nq + c % bt.nq) * HD + d] = (bf16)(x * inv);
       if (d == 0 && o.stat != nullptr) o.stat[qrow + c] = float2{m, inv};
     } else {
@@ -384,7 +386,7 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_few_kernel(
     const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
     const float* __restrict__ kv_scale, Units<true> w, int least, float c_log2, AttnOut o,
     float* __restrict__ score) {
-  __shared__ FewLds<HD, kAttWaves> lds;
+  __shared__ FewLds<HD> lds;
   const CacheBatch& bt = w.bt;
   long long total, off;
   int b;
@@ -400,9 +402,8 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_few_kernel(
   size_t slot = 2 * (size_t)blockIdx.x;
   while (true) {
     const int blk1 = min(np, blk0 + left);
-    few_columns<HD, kAttWaves>(q, kc, vc, kv_scale, bt, b, h, rows, 0, ctx, np, blk0, blk1, c_log2,
-                               o, slot,
-                               score != nullptr ? score + unit * o.part_cols * kPage : nullptr, lds);
+    few_columns<HD>(q, kc, vc, kv_scale, bt, b, h, rows, ctx, np, blk0, blk1, c_log2, o, slot,
+                    score != nullptr ? score + unit * o.part_cols * kPage : nullptr, lds);
     left -= blk1 - blk0;
     unit += blk1 - blk0;
     if (left <= 0) return;
@@ -923,8 +924,9 @@ __global__ __launch_bounds__(kAttThr) void cache_mass_few_kernel(
 // takes less time than a load.  Four workgroups fit a CU: many of them do little (a
 // decoding sequence's pages) and wait for their first loads.
 // us of this kernel for 4096 rows over 4096 tokens, 8 groups of two heads, and for a 512-row
-// chunk beside 16 decoding sequences: tiles through registers, one ahead 224 and 46; so 176
-// and 40 (two tiles at a time 170, with registers for three workgroups).
+// chunk beside 16 decoding sequences: tiles through registers, one ahead 224 and 46; the
+// ring 176 and 40 (two tiles at a time 170, with registers for three workgroups); equal
+// ranges of the pairs that exist, so that no launch follows the tables' width, 183 and 25.
 constexpr int kMassThr = 256, kMassCols = 32;
 constexpr int kMassStages = 4;
 
@@ -1063,17 +1065,6 @@ __global__ __launch_bounds__(kMassThr, 4) void cache_mass_kernel(
   }
 }
 
-}  // namespace
-
-namespace {
-int device_cus() {
-  int dev = 0, n = 0;
-  if (hipGetDevice(&dev) != hipSuccess ||
-      hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 8)
-    return 256;
-  return n / 8 * 8;
-}
-
 // Host side of the two forms: ranges (workgroups) and scratch.
 constexpr int kFewLeast = 4;   // pages of a range at least: one for each wave
 constexpr int kManyLeast = 2;
@@ -1094,13 +1085,12 @@ struct AttnPlan {
   size_t stat, score, total;
 };
 
-AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_rows, bool mass,
-                   int cus) {
+AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_rows, bool mass) {
   AttnPlan p{};
   const long long most = (long long)max_rows * nq;
   // Both forms where the sequences beside the longest have few columns on average: each
   // form's launches cost some 10 us where it has no sequence (us for a 512-row chunk beside
-  // 16 decoding sequences, with mass: 92, and 117 in the second form alone).
+  // 16 decoding sequences, with mass: 94, and 114 in the second form alone).
   p.few.on = most <= kFewCols || (B > 1 && (long long)(N - max_rows) * nq <= kFewCols * (B - 1LL));
   p.many.on = most > kFewCols;
   p.few.hi = kFewCols;
@@ -1117,9 +1107,9 @@ AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_
   };
   const long long pages = (long long)B * H * max_blocks;
   p.few.cols = (int)std::min<long long>(kFewCols, most);
-  p.few.ranges = (int)std::min<long long>(4LL * cus, (pages + kFewLeast - 1) / kFewLeast);
+  p.few.ranges = (int)std::min<long long>(4LL * kCus, (pages + kFewLeast - 1) / kFewLeast);
   p.many.cols = kTileCols;
-  p.many.ranges = cus;
+  p.many.ranges = kCus;
   while ((2 << p.many.log2r) * nq <= kTileCols) ++p.many.log2r;
   // tiles of the batch: at most n / 2^log2r, rounded up, of each sequence
   p.many.tiles = (int)std::min<long long>(N, ((long long)N >> p.many.log2r) + B);
@@ -1137,16 +1127,14 @@ AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_
 
 size_t cache_attention_scratch_bytes(int H, int B, int N, int nq, int hd, int max_blocks,
                                      int max_rows, bool mass) {
-  return attn_plan(H, B, N, nq, hd, max_blocks, max_rows, mass, kMaxCus).total;
+  return attn_plan(H, B, N, nq, hd, max_blocks, max_rows, mass).total;
 }
 
 hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_rows, const void* q,
                                   const int32_t* row_start, const float* mass_in, float* mass_out,
                                   void* out, void* scratch, hipStream_t s) {
   const CacheBatch bt{a.H, a.B, N, nq, a.n_pages, a.max_blocks, a.block_table, a.length, row_start};
-  static const int cus = std::min(device_cus(), kMaxCus);
-  const AttnPlan p = attn_plan(a.H, a.B, N, nq, a.hd, a.max_blocks, max_rows, mass_out != nullptr,
-                               cus);
+  const AttnPlan p = attn_plan(a.H, a.B, N, nq, a.hd, a.max_blocks, max_rows, mass_out != nullptr);
   unsigned char* base = static_cast<unsigned char*>(scratch);
   const float c_log2 = 1.4426950408889634f / sqrtf((float)a.hd);
   const bf16* qb = static_cast<const bf16*>(q);
@@ -1166,7 +1154,7 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
       // (16 workgroups a CU at most: four rounds, which evens out what pages near a chunk's
       // end have less to do)
       const long long pairs = (long long)ceil_div(a.max_blocks, 2) * a.H * a.B;
-      FOE_LAUNCH(cache_mass_kernel<HD>, dim3((unsigned)std::min(16LL * cus, pairs)), dim3(kMassThr),
+      FOE_LAUNCH(cache_mass_kernel<HD>, dim3((unsigned)std::min(16LL * kCus, pairs)), dim3(kMassThr),
                  0, s, qb, a.k, a.kv_scale, units(f, std::false_type{}), c_log2, stat, mass_in,
                  mass_out);
     };

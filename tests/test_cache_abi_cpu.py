@@ -88,6 +88,16 @@ def test_evict_rejects(L, at, value, rc, msg):
     assert msg in foe.last_error()
 
 
+def test_tables_past_the_limit(L):
+    for call, ok, at_b, at_blocks in ((L.foe_cache_append, APPEND, 2, 7),
+                                      (L.foe_cache_attention, ATTEND, 2, 7),
+                                      (L.foe_cache_evict, EVICT, 1, 4)):
+        args = changed(changed(ok, at_b, (1 << 13) + 1), at_blocks, 1 << 18)
+        assert call(*args) == INV and "B*max_blocks" in foe.last_error()
+    assert L.foe_cache_attention_workspace_bytes(8, (1 << 13) + 1, 4, 2, 128, 1 << 18, 1,
+                                                 0) == SIZE_MAX
+
+
 def test_empty_calls_are_noops(L):
     empty = [None] * 20
     assert L.foe_cache_append(BF16, 8, 4, 0, 2, 128, 1, 1, 5e5, 1.0, *empty[:10]) == foe.FOE_OK
