@@ -3,6 +3,7 @@
 #include <algorithm>
 
 #include "kv_cache.hpp"
+#include "lds_dma.hpp"
 
 namespace foe {
 namespace {
@@ -319,15 +320,17 @@ __device__ __forceinline__ void count_keys(const u32x4* key, int np, int pass, u
   __syncthreads();
 }
 
-// The digit of the want-th largest key, and how many keys have a larger one, from
-// count(d) (threads take the digits two by two, the largest first).
-template <typename Count>
-__device__ __forceinline__ void find_digit(int pass, Count count, uint32_t& prefix, int& want) {
+// A thread's digits, two by two from the largest: first_digit and the one below (negative:
+// none).
+__device__ __forceinline__ int first_digit(int pass) {
+  return (1 << digit_bits(pass)) - 1 - 2 * (int)threadIdx.x;
+}
+// The digit of the want-th largest key, and how many keys have a larger one, from the counts
+// of the thread's digits.
+__device__ __forceinline__ void find_digit(int pass, int c1, int c2, uint32_t& prefix, int& want) {
   __shared__ int wsum[kSelWaves];
   __shared__ int sh[2];
-  const int lane = lane_id(), wave = threadIdx.x >> 6;
-  const int hi = (1 << digit_bits(pass)) - 1 - 2 * (int)threadIdx.x;
-  const int c1 = hi > 0 ? count(hi) : 0, c2 = hi > 0 ? count(hi - 1) : 0;
+  const int lane = lane_id(), wave = threadIdx.x >> 6, hi = first_digit(pass);
   int incl = c1 + c2;
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) {
@@ -437,17 +440,20 @@ __global__ __launch_bounds__(kSelThr) void cache_select_kernel(
 #pragma unroll
   for (int pass = 0; pass < 3; ++pass) {
     count_keys(key, np, pass, prefix, hist);
-    find_digit(pass, [&](int d) { return hist[d]; }, prefix, want);
+    const int d = first_digit(pass);
+    find_digit(pass, d > 0 ? hist[d] : 0, d > 0 ? hist[d - 1] : 0, prefix, want);
   }
   list_keys(key, np, 0, prefix, want, 0, 0, out);
 }
 
 // One workgroup per 32768 tokens: launch `pass` counts that digit into
-// counts[pass][b][h][slice], launch 3 lists.
+// counts[pass][b][h][slice], launch 3 lists.  Each launch finds the digit counted before it;
+// what the earlier ones are is in state[b][h][slice]: (prefix, want, tokens of the slices
+// before that are above the prefix).
 template <int PASS>
 __global__ __launch_bounds__(kSelThr) void cache_select_slice_kernel(
     const float* __restrict__ mass, CacheBatch bt, int keep, int recent, int* __restrict__ counts,
-    int32_t* __restrict__ kept, int32_t* __restrict__ new_len) {
+    int4* __restrict__ state, int32_t* __restrict__ kept, int32_t* __restrict__ new_len) {
   __shared__ int hist[kSelBins];
   __shared__ int before[2];
   const int tid = threadIdx.x, slice = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
@@ -470,30 +476,37 @@ __global__ __launch_bounds__(kSelThr) void cache_select_slice_kernel(
   auto counts_of = [&](int pass) {
     return counts + (((size_t)pass * bt.B + b) * bt.H + h) * gridDim.x * kSelBins;
   };
+  state += ((size_t)b * bt.H + h) * gridDim.x + slice;
   uint32_t prefix = 0;
   int want = need, gt = 0, eq = 0;
-#pragma unroll
-  for (int pass = 0; pass < PASS; ++pass) {
-    const int* c = counts_of(pass);
-    find_digit(pass, [&](int d) {
-      int x = 0;
-      for (int s = 0; s < slices; ++s) x += c[(size_t)s * kSelBins + d];
-      return x;
-    }, prefix, want);
-    if (PASS == 3) {  // tokens of the slices before with a larger digit, or the same at last
-      const int d0 = (prefix >> digit_shift(pass)) & ((1 << digit_bits(pass)) - 1);
-      if (tid == 0) before[0] = before[1] = 0;
-      __syncthreads();
-      for (int d = tid; d < 1 << digit_bits(pass); d += kSelThr) {
-        if (d < d0 || (d == d0 && pass < 2)) continue;
-        int x = 0;
-        for (int s = 0; s < slice; ++s) x += c[(size_t)s * kSelBins + d];
-        if (x > 0) atomicAdd(&before[d == d0], x);
+  if constexpr (PASS > 1) {
+    const int4 x = *state;
+    prefix = (uint32_t)x.x, want = x.y, gt = x.z;
+  }
+  if constexpr (PASS > 0) {
+    const int d = first_digit(PASS - 1);
+    const int* c = counts_of(PASS - 1) + d - 1;
+    int2 all{0, 0}, ahead{0, 0};  // digits (d - 1, d), of all slices and of those before
+    if (d > 0) {
+#pragma unroll 4
+      for (int s = 0; s < slices; ++s) {
+        const int2 x = *reinterpret_cast<const int2*>(c + (size_t)s * kSelBins);
+        all.x += x.x, all.y += x.y;
+        if (s < slice) ahead.x += x.x, ahead.y += x.y;
       }
-      __syncthreads();
-      gt += before[0];
-      eq += before[1];
     }
+    if (tid == 0) before[0] = before[1] = 0;
+    find_digit(PASS - 1, all.y, all.x, prefix, want);
+    // tokens of the slices before with a larger digit, and at last with the same
+    const int at = (prefix >> digit_shift(PASS - 1)) & ((1 << digit_bits(PASS - 1)) - 1);
+    const int larger = (d > at ? ahead.y : 0) + (d - 1 > at ? ahead.x : 0);
+    const int same = d == at ? ahead.y : d - 1 == at ? ahead.x : 0;
+    if (larger > 0) atomicAdd(&before[0], larger);
+    if (PASS == 3 && same > 0) atomicAdd(&before[1], same);
+    __syncthreads();
+    gt += before[0];
+    eq = before[1];
+    if (PASS < 3 && tid == 0) *state = int4{(int)prefix, want, gt, 0};
   }
   if constexpr (PASS == 3) {
     list_keys(key, np, base, prefix, want, gt, eq, out);
@@ -517,6 +530,7 @@ __global__ __launch_bounds__(kSelThr) void cache_select_slice_kernel(
 // several pages a workgroup 383 (135 registers); that with permutations 193 (80
 // registers); a wave for each page's keys and one for its values, without barriers, 401.
 constexpr int kMoveThr = 512;
+constexpr int kMovePieces = 4;
 
 template <int HD>
 __global__ __launch_bounds__(kMoveThr, 8) void cache_move_kernel(
@@ -524,10 +538,11 @@ __global__ __launch_bounds__(kMoveThr, 8) void cache_move_kernel(
     float* __restrict__ mass, CacheBatch bt, const int32_t* __restrict__ dst_table, int dst_blocks,
     int keep, const int32_t* __restrict__ kept) {
   constexpr int CPR = HD / 16;
+  __shared__ __align__(16) uint8_t vstage[kMoveThr / kWave * kMovePieces * 1024];
   __shared__ int sp[kPage], st[kPage];
   __shared__ float2 ss[kPage];
   const int tid = threadIdx.x, blk = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
-  const int lane = lane_id();
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int cnt = min(min(bt.context(b), keep) - blk * kPage, kPage);
   if (cnt <= 0) return;
   const int dp = dst_table[(size_t)b * dst_blocks + blk];
@@ -565,15 +580,35 @@ __global__ __launch_bounds__(kMoveThr, 8) void cache_move_kernel(
                   : ((uint64_t)my_page * bt.H + h) * (kPage * HD) +
                         (uint32_t)((my_tok / kSub) * (HD * kSub) + (my_tok % kSub & ~3));
   const uint32_t dim = min(d, HD - 1) * kSub;
-  auto gather = [&](int i) {
-    const uint64_t off =
-        (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(my_off >> 32), i) << 32 |
-        (uint32_t)__builtin_amdgcn_readlane((uint32_t)my_off, i);
-    return *reinterpret_cast<const uint32_t*>(vc + off + dim);
+  auto place_of = [&](int i) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(my_off >> 32), i) << 32 |
+           (uint32_t)__builtin_amdgcn_readlane((uint32_t)my_off, i);
   };
-  uint32_t got[kSub / 2];  // (eight loads in flight)
+  // tokens whose 16-byte pieces differ from the previous token's
+  const uint32_t piece_lo = (uint32_t)my_off & ~15u, piece_hi = (uint32_t)(my_off >> 32);
+  const bool turns =
+      lane == 0 || piece_lo != __shfl_up(piece_lo, 1) || piece_hi != __shfl_up(piece_hi, 1);
+  const uint32_t turn = (uint32_t)__builtin_amdgcn_ballot_w64(turns) & 0xffffu;
+  const int my_piece = __popc(turn & ((2u << (lane & 15)) - 1)) - 1;
+  const bool staged = __popc(turn) <= kMovePieces;  // (uniform)
+  const uint32_t mine = lds_addr(vstage) + wave * (kMovePieces * 1024);
+  uint32_t got[kSub / 2];
+  if (staged) {
+    uint32_t rest = turn;
 #pragma unroll
-  for (int i = 0; i < kSub / 2; ++i) got[i] = gather(i);
+    for (int k = 0; k < kMovePieces; ++k) {
+      if (rest == 0) continue;
+      const uint64_t off = place_of(__builtin_ctz(rest)) & ~(uint64_t)15;
+      rest &= rest - 1;
+      const __amdgpu_buffer_rsrc_t piece = make_rsrc_u(vc + off, HD * kSub);
+      rsrc_settle(piece);
+      dma16(piece, dim, mine, k * 1024);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kSub / 2; ++i)
+      got[i] = *reinterpret_cast<const uint32_t*>(vc + place_of(i) + dim);
+  }
   float2 amax{0.f, 0.f};  // (a NaN code counts for no scale)
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -587,13 +622,23 @@ __global__ __launch_bounds__(kMoveThr, 8) void cache_move_kernel(
   auto place_byte = [&](int i, uint32_t x) {
     vw[i / 4] = __builtin_amdgcn_perm(x, vw[i / 4], __builtin_amdgcn_readlane(my_sel, i));
   };
+  if (staged) {
+    vm_wait<0>();
+    const uint32_t from = my_piece * 1024 + (my_tok % kSub & ~3);
 #pragma unroll
-  for (int i = 0; i < kSub / 2; ++i) {
-    place_byte(i, got[i]);
-    got[i] = gather(kSub / 2 + i);
+    for (int i = 0; i < kSub; ++i)
+      place_byte(i, *reinterpret_cast<const uint32_t*>(
+                        vstage + wave * (kMovePieces * 1024) + lane * 16 +
+                        __builtin_amdgcn_readlane(from, i)));
+  } else {
+#pragma unroll
+    for (int i = 0; i < kSub / 2; ++i) {
+      place_byte(i, got[i]);
+      got[i] = *reinterpret_cast<const uint32_t*>(vc + place_of(kSub / 2 + i) + dim);
+    }
+#pragma unroll
+    for (int i = 0; i < kSub / 2; ++i) place_byte(kSub / 2 + i, got[i]);
   }
-#pragma unroll
-  for (int i = 0; i < kSub / 2; ++i) place_byte(kSub / 2 + i, got[i]);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const float x0 = fabsf(__builtin_amdgcn_cvt_f32_fp8(vw[e], 0)) * lane_f(my_scale, 4 * e);
@@ -667,9 +712,11 @@ static int select_slices(int max_blocks) {
   return ceil_div((long long)max_blocks * kPage, kSelTokens);
 }
 
+static size_t select_counts(int H, int B, int slices) { return (size_t)3 * B * H * slices * kSelBins; }
+
 size_t cache_evict_scratch_bytes(int H, int B, int max_blocks) {
   const int slices = select_slices(max_blocks);
-  return slices > 1 ? (size_t)3 * B * H * slices * kSelBins * 4 : 0;
+  return slices > 1 ? select_counts(H, B, slices) * 4 + (size_t)B * H * slices * sizeof(int4) : 0;
 }
 
 hipError_t launch_cache_evict(const CacheArgs& a, float* mass, int keep, int recent,
@@ -682,10 +729,12 @@ hipError_t launch_cache_evict(const CacheArgs& a, float* mass, int keep, int rec
     FOE_LAUNCH(cache_select_kernel, dim3(a.H, a.B), dim3(kSelThr), 0, s, mass, bt, keep, recent,
                kept, new_len);
   } else {
+    int* counts = static_cast<int*>(scratch);
+    int4* state = reinterpret_cast<int4*>(counts + select_counts(a.H, a.B, slices));
     auto go = [&](auto kern, const char* name) {
       ProfileScope ps(name, s);
       FOE_LAUNCH(kern, dim3(slices, a.H, a.B), dim3(kSelThr), 0, s, mass, bt, keep, recent,
-                 static_cast<int*>(scratch), kept, new_len);
+                 counts, state, kept, new_len);
     };
     go(cache_select_slice_kernel<0>, "cache_select_0");
     go(cache_select_slice_kernel<1>, "cache_select_1");
