@@ -252,7 +252,8 @@ __global__ __launch_bounds__(kAppThr) void cache_append_kernel(
 // digit and one that lists.
 // us for two sequences of 131072 tokens, 8 groups: one workgroup a sequence and group
 // with 8-bit digits, each pass from memory 398, with these digits 113 (its compute unit's
-// vector instructions are the bound), spread 53; 24 of at most 16000 tokens: 76, 17.
+// vector instructions are the bound), spread 53, of which the last launch 22 as it found all
+// three digits again; with the state handed on 45.  24 of at most 16000 tokens: 76, 17.
 constexpr int kSelThr = 1024;
 constexpr int kSelWaves = kSelThr / kWave;
 constexpr int kSelRegs = 8;                          // 4-token pieces of a thread
@@ -520,17 +521,20 @@ __global__ __launch_bounds__(kSelThr) void cache_select_slice_kernel(
 // Moving the kept tokens: one workgroup per (page of the result, group, sequence).
 // Keys: thread -> 16 bytes of a row.  Values: the 128 threads of group g = 0..3 (a thread
 // a dim) gather the 16 tokens 16 g .. +15 of the page; a token is the same for all of
-// them, so its address and its byte within the 4 bytes that a thread loads are scalars,
-// and a byte permutation puts it in its place; neighbouring tokens share cache lines.
-// A token's place is a chain of loads (its number, its page, the page's scales, the
-// codes), hidden by the four workgroups that a CU has room for at 50 registers.
-// us for two sequences of 131072 tokens cut to half, 8 groups (the sources' cache lines
-// and the results are 640 MB: 125): 180.  A load for each byte 249; the source's 16-byte
-// pieces in registers, bytes taken by scalar branches, the chain loaded ahead over
-// several pages a workgroup 383 (135 registers); that with permutations 193 (80
-// registers); a wave for each page's keys and one for its values, without barriers, 401.
+// them, so its address and its byte within 4 bytes are scalars, and a byte permutation puts
+// it in its place.  Where the 16 tokens come out of at most four 16-byte pieces of the
+// source (tokens kept thickly), a wave loads the pieces into its own LDS and takes the
+// bytes from there; else it loads 4 bytes of each token, which touch the same cache lines
+// once a token.  A token's place is a chain of loads (its number, its page, the page's
+// scales, the codes), hidden by the four workgroups that a CU has room for.
+// us for 16 sequences of 16000 tokens, 8 groups, cut to 12000, 8000, 5300, 4000, 2000:
+// always 4 bytes 272 176 124 102 64; so 210 144 116 100 65; pieces alone, four at a time,
+// 222 148 116 100 67.  For two of 131072 cut to half (the sources' cache lines and the
+// results are 640 MB: 125) 147; a load for each byte 249; bytes taken out of pieces in
+// registers 193 to 383; a wave for each page's keys and one for its values 401; each
+// wave finding its tokens for itself, without barriers, 197.
 constexpr int kMoveThr = 512;
-constexpr int kMovePieces = 4;
+constexpr int kMovePieces = 4;  // (32 KB of LDS)
 
 template <int HD>
 __global__ __launch_bounds__(kMoveThr, 8) void cache_move_kernel(
