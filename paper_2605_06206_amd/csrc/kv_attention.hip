@@ -731,14 +731,13 @@ __device__ __forceinline__ bool find_parts(const Units<FEW>& w, int ranges, int 
   return p.r0 != p.r1;
 }
 
-// Few columns: one workgroup per (group, sequence).  8 groups of 32 lanes (a lane 4 dims)
-// each sum every eighth part, and are then summed in order.
+// Few columns: one workgroup per (group h, sequence b).  8 groups of 32 lanes (a lane 4
+// dims) each sum every eighth part, and are then summed in order.
 template <int HD>
-__global__ __launch_bounds__(256) void cache_join_few_kernel(Units<true> w, int ranges, int least,
-                                                             AttnOut o) {
+__device__ __forceinline__ void join_few(const Units<true>& w, int ranges, int least,
+                                         const AttnOut& o, int h, int b) {
   __shared__ f32x4 osum[8][32];
   const CacheBatch& bt = w.bt;
-  const int h = blockIdx.x, b = blockIdx.y;
   const int rows = w.rows(b);
   if (rows <= 0) return;
   const int np = w.pages(bt.context(b), rows, 0), ncol = rows * bt.nq;
@@ -789,18 +788,18 @@ __global__ __launch_bounds__(256) void cache_join_few_kernel(Units<true> w, int 
   }
 }
 
-// Many columns: one workgroup per (32 columns of a tile, group), 8 threads a column; a
+// Many columns: one workgroup per (32 columns of a tile, group h), 8 threads a column; a
 // thread loads its dims of four parts at a time.
+constexpr int kJoinCols = 32;
+
 template <int HD>
-__global__ __launch_bounds__(256) void cache_join_tile_kernel(Units<false> w, int ranges, int least,
-                                                              AttnOut o) {
-  constexpr int CB = kTileCols / 32, NV = HD / 32, AT_ONCE = 4;
+__device__ __forceinline__ void join_tile(const Units<false>& w, int ranges, int least,
+                                          const AttnOut& o, int h, int x32) {
+  constexpr int CB = kTileCols / kJoinCols, NV = HD / 32, AT_ONCE = 4;
   const CacheBatch& bt = w.bt;
-  const int h = blockIdx.y;
   int b, t;
-  if (!find_tile<256>(bt.B, blockIdx.x / CB, [&](int i) { return w.tiles(w.rows(i)); }, b, t))
-    return;
-  const int c = blockIdx.x % CB * 32 + (threadIdx.x & 31), l3 = threadIdx.x >> 5;
+  if (!find_tile<256>(bt.B, x32 / CB, [&](int i) { return w.tiles(w.rows(i)); }, b, t)) return;
+  const int c = x32 % CB * kJoinCols + (threadIdx.x & 31), l3 = threadIdx.x >> 5;
   const int rows = w.rows(b), ctx = bt.context(b), row0 = t << w.log2r;
   const int ncol = (min(rows, (t + 1) << w.log2r) - row0) * bt.nq;
   const int np = w.pages(ctx, rows, t);
@@ -859,21 +858,41 @@ __global__ __launch_bounds__(256) void cache_join_tile_kernel(Units<false> w, in
     o.stat[((size_t)h * bt.N + bt.first_row(b) + row0) * bt.nq + c] = float2{m, inv};
 }
 
+// What a form's launches share: its units, its workgroups and their least work, and where
+// it writes.
+template <bool FEW>
+struct Form {
+  Units<FEW> w;
+  int ranges, least;
+  AttnOut o;
+};
+
+// One launch joins both forms' parts: `many_blocks` workgroups the tiles', the rest the
+// sequences' of few columns.
+template <int HD>
+__global__ __launch_bounds__(256) void cache_join_kernel(Form<true> few, Form<false> many,
+                                                         int many_blocks) {
+  const int x = blockIdx.x, h = blockIdx.y;
+  if (x < many_blocks) join_tile<HD>(many.w, many.ranges, many.least, many.o, h, x);
+  else join_few<HD>(few.w, few.ranges, few.least, few.o, h, x - many_blocks);
+}
+
 // ---- mass ---------------------------------------------------------------------------
 // A token's mass is the sum of its probabilities over the columns, each from its score
 // and its column's final maximum and sum, so it follows the joining.  With few columns the
 // scores were kept; else they are formed again.
 
 // Few columns: the ranges of the attention; a wave takes every fourth page, a lane a token.
-__global__ __launch_bounds__(kAttThr) void cache_mass_few_kernel(
-    const float* __restrict__ score, Units<true> w, int least, int part_cols, float c_log2,
-    const float2* __restrict__ stat, const float* __restrict__ mass_in,
-    float* __restrict__ mass_out) {
+__device__ __forceinline__ void mass_few(const float* __restrict__ score, const Units<true>& w,
+                                         int ranges, int range, int least, int part_cols,
+                                         float c_log2, const float2* __restrict__ stat,
+                                         const float* __restrict__ mass_in,
+                                         float* __restrict__ mass_out) {
   __shared__ int found;
   const CacheBatch& bt = w.bt;
   const int lane = lane_id(), wave = threadIdx.x >> 6;
-  const long long total = w.prefix[bt.B], per = range_units(total, gridDim.x, least);
-  const long long unit = blockIdx.x * per;
+  const long long total = w.prefix[bt.B], per = range_units(total, ranges, least);
+  const long long unit = range * per;
   if (unit >= total) return;
   for (int i = threadIdx.x; i < bt.B; i += kAttThr)
     if (w.prefix[i] <= unit && unit < w.prefix[i + 1]) found = i;
@@ -931,10 +950,12 @@ constexpr int kMassThr = 256, kMassCols = 32;
 constexpr int kMassStages = 4;
 
 template <int HD>
-__global__ __launch_bounds__(kMassThr, 4) void cache_mass_kernel(
-    const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const float* __restrict__ kv_scale,
-    Units<false> w, float c_log2, const float2* __restrict__ stat, const float* __restrict__ mass_in,
-    float* __restrict__ mass_out) {
+__device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8_t* __restrict__ kc,
+                                         const float* __restrict__ kv_scale, const Units<false>& w,
+                                         int ranges, int range, float c_log2,
+                                         const float2* __restrict__ stat,
+                                         const float* __restrict__ mass_in,
+                                         float* __restrict__ mass_out) {
   constexpr int NST = HD / 16;
   constexpr int QT = kMassCols * 256, STAGE = QT + 256;  // bytes of a tile, and with its statistics
   constexpr int QI = QT / 1024 / (kMassThr / kWave);     // 1 KB DMA instructions of a wave
@@ -950,14 +971,17 @@ __global__ __launch_bounds__(kMassThr, 4) void cache_mass_kernel(
     const int len = min(bt.context(i) + n, bt.cap());
     return n > 0 ? (long long)((len + 2 * kPage - 1) / (2 * kPage)) * bt.H : 0;
   };
-  long long total, off;
+  long long total, first;
   int b;
-  locate<kMassThr>(bt.B, pairs, gridDim.x, blockIdx.x, 1, nullptr, total, b, off);
+  locate<kMassThr>(bt.B, pairs, ranges, range, 1, nullptr, total, b, first);
   if (b < 0) return;
-  const long long per = range_units(total, gridDim.x, 1);
-  long long left = min(per, total - blockIdx.x * per);
+  const long long per = range_units(total, ranges, 1);
+  // (in scalar registers: the keys and sums fill the others)
+  b = __builtin_amdgcn_readfirstlane(b);
+  int off = __builtin_amdgcn_readfirstlane((int)first);  // (of 2^17 pairs in 64 groups)
+  int left = __builtin_amdgcn_readfirstlane((int)min(per, total - range * per));
   while (true) {
-    const int h = (int)(off % bt.H), blk0 = (int)(off / bt.H) * 2;
+    const int h = off % bt.H, blk0 = off / bt.H * 2;
     const int rows = w.rows(b), ctx = bt.context(b);
     const int len = min(ctx + rows, bt.cap());
     const int key0 = blk0 * kPage + wave * 32;  // the wave's first key
@@ -1065,6 +1089,24 @@ __global__ __launch_bounds__(kMassThr, 4) void cache_mass_kernel(
   }
 }
 
+// One launch for both: `any_ranges` workgroups for the sequences of `any`, the rest for
+// those of few columns, from their scores.
+template <int HD>
+__global__ __launch_bounds__(kMassThr, 4) void cache_mass_kernel(
+    const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const float* __restrict__ kv_scale,
+    Units<false> any, int any_ranges, Form<true> few, const float* __restrict__ score, float c_log2,
+    const float2* __restrict__ stat, const float* __restrict__ mass_in,
+    float* __restrict__ mass_out) {
+  static_assert(kMassThr == kAttThr, "one workgroup size");
+  const int x = blockIdx.x;
+  if (x >= any_ranges) {
+    mass_few(score, few.w, few.ranges, x - any_ranges, few.least, few.o.part_cols, c_log2, stat,
+             mass_in, mass_out);
+    return;
+  }
+  mass_any<HD>(q, kc, kv_scale, any, any_ranges, x, c_log2, stat, mass_in, mass_out);
+}
+
 // Host side of the two forms: ranges (workgroups) and scratch.
 constexpr int kFewLeast = 4;   // pages of a range at least: one for each wave
 constexpr int kManyLeast = 2;
@@ -1088,9 +1130,9 @@ struct AttnPlan {
 AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_rows, bool mass) {
   AttnPlan p{};
   const long long most = (long long)max_rows * nq;
-  // Both forms where the sequences beside the longest have few columns on average: each
-  // form's launches cost some 10 us where it has no sequence (us for a 512-row chunk beside
-  // 16 decoding sequences, with mass: 94, and 114 in the second form alone).
+  // Both forms where the sequences beside the longest have few columns on average (us for a
+  // 512-row chunk beside 16 decoding sequences, with mass: 85, and 114 in the second form
+  // alone); where they are all chunks the first would be a launch for nothing.
   p.few.on = most <= kFewCols || (B > 1 && (long long)(N - max_rows) * nq <= kFewCols * (B - 1LL));
   p.many.on = most > kFewCols;
   p.few.hi = kFewCols;
@@ -1140,60 +1182,44 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
   const bf16* qb = static_cast<const bf16*>(q);
   float2* stat = mass_out != nullptr ? reinterpret_cast<float2*>(base + p.stat) : nullptr;
   float* score = p.scores ? reinterpret_cast<float*>(base + p.score) : nullptr;
-  auto units = [&](const FormPlan& f, auto few) {
-    return Units<decltype(few)::value>{bt, max_rows, f.log2r, f.lo, f.hi,
-                                       reinterpret_cast<long long*>(base + f.prefix)};
+  auto form = [&](const FormPlan& f, int least, auto few) {
+    return Form<decltype(few)::value>{
+        {bt, max_rows, f.log2r, f.lo, f.hi, reinterpret_cast<long long*>(base + f.prefix)},
+        f.ranges, least,
+        {static_cast<bf16*>(out), stat, reinterpret_cast<float*>(base + f.part), f.cols}};
   };
-  auto result = [&](const FormPlan& f) {
-    return AttnOut{static_cast<bf16*>(out), stat, reinterpret_cast<float*>(base + f.part), f.cols};
-  };
+  const Form<true> few = form(p.few, kFewLeast, std::true_type{});
+  const Form<false> many = form(p.many, kManyLeast, std::false_type{});
   auto go = [&](auto hdv) {
     constexpr int HD = decltype(hdv)::value;
-    auto mass = [&](const FormPlan& f) {
-      ProfileScope ps("cache_mass", s);
-      // (16 workgroups a CU at most: four rounds, which evens out what pages near a chunk's
-      // end have less to do)
-      const long long pairs = (long long)ceil_div(a.max_blocks, 2) * a.H * a.B;
-      FOE_LAUNCH(cache_mass_kernel<HD>, dim3((unsigned)std::min(16LL * kCus, pairs)), dim3(kMassThr),
-                 0, s, qb, a.k, a.kv_scale, units(f, std::false_type{}), c_log2, stat, mass_in,
-                 mass_out);
-    };
     if (p.few.on) {
-      const Units<true> w = units(p.few, std::true_type{});
-      const AttnOut o = result(p.few);
-      {
-        ProfileScope ps("cache_attn_few", s);
-        FOE_LAUNCH(cache_attn_few_kernel<HD>, dim3(p.few.ranges), dim3(kAttThr), 0, s, qb, a.k,
-                   a.v, a.kv_scale, w, kFewLeast, c_log2, o, score);
-      }
-      {
-        ProfileScope ps("cache_join_few", s);
-        FOE_LAUNCH(cache_join_few_kernel<HD>, dim3(a.H, a.B), dim3(256), 0, s, w, p.few.ranges,
-                   kFewLeast, o);
-      }
-      if (score != nullptr) {
-        ProfileScope ps("cache_mass_few", s);
-        FOE_LAUNCH(cache_mass_few_kernel, dim3(p.few.ranges), dim3(kAttThr), 0, s, score, w,
-                   kFewLeast, p.few.cols, c_log2, stat, mass_in, mass_out);
-      } else if (mass_out != nullptr) {
-        mass(p.few);
-      }
+      ProfileScope ps("cache_attn_few", s);
+      FOE_LAUNCH(cache_attn_few_kernel<HD>, dim3(few.ranges), dim3(kAttThr), 0, s, qb, a.k, a.v,
+                 a.kv_scale, few.w, few.least, c_log2, few.o, score);
     }
     if (p.many.on) {
-      const Units<false> w = units(p.many, std::false_type{});
-      const AttnOut o = result(p.many);
-      {
-        ProfileScope ps("cache_attn_tile", s);
-        FOE_LAUNCH(cache_attn_tile_kernel<HD>, dim3(p.many.ranges), dim3(kTileThr), 0, s, qb, a.k,
-                   a.v, a.kv_scale, w, kManyLeast, c_log2, o);
-      }
-      {
-        ProfileScope ps("cache_join_tile", s);
-        FOE_LAUNCH(cache_join_tile_kernel<HD>,
-                   dim3(p.many.tiles * (kTileCols / 32), a.H), dim3(256), 0, s, w, p.many.ranges,
-                   kManyLeast, o);
-      }
-      if (mass_out != nullptr) mass(p.many);
+      ProfileScope ps("cache_attn_tile", s);
+      FOE_LAUNCH(cache_attn_tile_kernel<HD>, dim3(many.ranges), dim3(kTileThr), 0, s, qb, a.k, a.v,
+                 a.kv_scale, many.w, many.least, c_log2, many.o);
+    }
+    {
+      ProfileScope ps("cache_join", s);
+      const int many_blocks = p.many.on ? p.many.tiles * (kTileCols / kJoinCols) : 0;
+      FOE_LAUNCH(cache_join_kernel<HD>, dim3(many_blocks + (p.few.on ? a.B : 0), a.H), dim3(256), 0,
+                 s, few, many, many_blocks);
+    }
+    if (mass_out != nullptr) {
+      ProfileScope ps("cache_mass", s);
+      // without scores the sequences of both forms; at most 16 workgroups a CU: four rounds,
+      // which evens out what pages near a chunk's end have less to do
+      Units<false> any = many.w;
+      if (score == nullptr) any.lo = 0;
+      const long long pairs = (long long)ceil_div(a.max_blocks, 2) * a.H * a.B;
+      const int any_ranges =
+          p.many.on || score == nullptr ? (int)std::min(16LL * kCus, pairs) : 0;
+      FOE_LAUNCH(cache_mass_kernel<HD>, dim3(any_ranges + (score != nullptr ? few.ranges : 0)),
+                 dim3(kMassThr), 0, s, qb, a.k, a.kv_scale, any, any_ranges, few, score, c_log2,
+                 stat, mass_in, mass_out);
     }
   };
   if (a.hd == 96) go(std::integral_constant<int, 96>{});
