@@ -80,18 +80,31 @@ struct Units {
   }
 };
 
-// units of a workgroup's range (a batch's are below 2^39, of tables of up to 2^31 entries, 64
-// groups and 2^22 columns: a range of the launches here has fewer than 2^31)
-__device__ __forceinline__ long long range_units(long long total, int ranges, int least) {
-  const long long per = (total + ranges - 1) / ranges;
-  return per < least ? least : per;
+// How a batch's units are dealt out: to `ranges` workgroups, at least `least` units each;
+// where `round` workgroups would have few enough (see kOneRound), to those.
+struct Deal {
+  int ranges, least, round;
+  // units of a range (a batch's are below 2^39, of tables of up to 2^31 entries, 64 groups
+  // and 2^22 columns: a range of the launches here has fewer than 2^31)
+  __device__ __forceinline__ long long per(long long total) const;
+};
+// Few columns: 1024 ranges are two rounds of the workgroups that fit the chip at a time, the
+// second filling the gaps that the first one's ends leave; while a range has few pages, one
+// round saves more in starting.  us with 1024 and with 512 ranges, 8 groups of two heads,
+// sequences of 1000 to 4000 tokens: 8 of them 23.5 20.5, 16 33.5 27, 32 (20 pages a range
+// of 512) 46.5 42.5; 48 of 100 to 4096, hd 96 (25 pages) 61 65; 64 of 256 to 8192 (66) 113 121.
+constexpr int kOneRound = 22;
+__device__ __forceinline__ long long Deal::per(long long total) const {
+  long long n = (total + ranges - 1) / ranges;
+  if (round > 0 && total <= (long long)kOneRound * round) n = (total + round - 1) / round;
+  return n < least ? least : n;
 }
 
 // Total of the units, count(b) of sequence b, and the sequence that unit range * per falls
 // in (b, or -1 past the end) with its offset there.  Every thread of the workgroup calls
 // it; range 0 writes the prefix, if any: the units before each sequence, and in all.
 template <int NT, typename Count>
-__device__ __forceinline__ void locate(int B, Count count, int ranges, int range, int least,
+__device__ __forceinline__ void locate(int B, Count count, const Deal& deal, int range,
                                        long long* prefix, long long& total, int& b,
                                        long long& off) {
   constexpr int NW = NT / kWave;
@@ -120,7 +133,7 @@ __device__ __forceinline__ void locate(int B, Count count, int ranges, int range
   long long mine = first;
   for (int i = threadIdx.x + NT; i < B; i += NT) mine += count(i);
   long long incl = scan(mine, total);
-  const long long u0 = range * range_units(total, ranges, least);
+  const long long u0 = range * deal.per(total);
   const bool writes = prefix != nullptr && range == 0;
   if (threadIdx.x == 0) found[0] = -1;
   if (B > NT && (u0 < total || writes)) {  // (uniform) again, a row of threads at a time
@@ -384,17 +397,16 @@ __device__ __forceinline__ void few_columns(
 template <int HD>
 __global__ __launch_bounds__(kAttThr, 2) void cache_attn_few_kernel(
     const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
-    const float* __restrict__ kv_scale, Units<true> w, int least, float c_log2, AttnOut o,
+    const float* __restrict__ kv_scale, Units<true> w, Deal deal, float c_log2, AttnOut o,
     float* __restrict__ score) {
   __shared__ FewLds<HD> lds;
   const CacheBatch& bt = w.bt;
   long long total, off;
   int b;
   locate<kAttThr>(
-      bt.B, [&](int i) { return w.group(i) * bt.H; }, gridDim.x, blockIdx.x, least, w.prefix, total,
-      b, off);
+      bt.B, [&](int i) { return w.group(i) * bt.H; }, deal, blockIdx.x, w.prefix, total, b, off);
   if (b < 0) return;
-  const int per = (int)range_units(total, gridDim.x, least);
+  const int per = (int)deal.per(total);
   long long unit = (long long)blockIdx.x * per;
   int left = (int)min((long long)per, total - unit);
   int rows = w.rows(b), ctx = bt.context(b), np = w.pages(ctx, rows, 0);
@@ -437,7 +449,7 @@ template <int HD>
 __global__ __launch_bounds__(kTileThr) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ kc,
                        const uint8_t* __restrict__ vc, const float* __restrict__ kv_scale,
-                       Units<false> w, int least, float c_log2, AttnOut o) {
+                       Units<false> w, Deal deal, float c_log2, AttnOut o) {
   constexpr int KT = kPage * 256;       // K tile bytes
   constexpr int VT = HD * kPage * 2;    // V^T tile bytes
   constexpr int NST = HD / 16;          // score k-steps
@@ -453,10 +465,9 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
   long long total, off;
   int b;
   locate<kTileThr>(
-      bt.B, [&](int i) { return w.group(i) * bt.H; }, gridDim.x, range, least, w.prefix, total, b,
-      off);
+      bt.B, [&](int i) { return w.group(i) * bt.H; }, deal, range, w.prefix, total, b, off);
   if (b < 0) return;
-  const int per = (int)range_units(total, gridDim.x, least);
+  const int per = (int)deal.per(total);
   int left = (int)min((long long)per, total - (long long)range * per);
   int rows = w.rows(b), ctx = bt.context(b), nt = w.tiles(rows), h, t, blk0;
   {
@@ -722,9 +733,9 @@ struct Parts {
 };
 // units u0 .. u0 + np - 1 of the tile; false where one range wrote it whole
 template <bool FEW>
-__device__ __forceinline__ bool find_parts(const Units<FEW>& w, int ranges, int least, long long u0,
+__device__ __forceinline__ bool find_parts(const Units<FEW>& w, const Deal& deal, long long u0,
                                            int np, Parts& p) {
-  const long long per = range_units(w.prefix[w.bt.B], ranges, least);
+  const long long per = deal.per(w.prefix[w.bt.B]);
   p.r0 = (int)(u0 / per);
   p.r1 = (int)((u0 + np - 1) / per);
   p.first_late = u0 % per != 0;
@@ -734,7 +745,7 @@ __device__ __forceinline__ bool find_parts(const Units<FEW>& w, int ranges, int 
 // Few columns: one workgroup per (group h, sequence b).  8 groups of 32 lanes (a lane 4
 // dims) each sum every eighth part, and are then summed in order.
 template <int HD>
-__device__ __forceinline__ void join_few(const Units<true>& w, int ranges, int least,
+__device__ __forceinline__ void join_few(const Units<true>& w, const Deal& deal,
                                          const AttnOut& o, int h, int b) {
   __shared__ f32x4 osum[8][32];
   const CacheBatch& bt = w.bt;
@@ -742,7 +753,7 @@ __device__ __forceinline__ void join_few(const Units<true>& w, int ranges, int l
   if (rows <= 0) return;
   const int np = w.pages(bt.context(b), rows, 0), ncol = rows * bt.nq;
   Parts p{o.part, o.part_cols, HD};
-  if (!find_parts(w, ranges, least, w.prefix[b] + (long long)np * h, np, p)) return;
+  if (!find_parts(w, deal, w.prefix[b] + (long long)np * h, np, p)) return;
   const int grp = threadIdx.x >> 5, l5 = threadIdx.x & 31, d = 4 * l5;
   for (int c = 0; c < ncol; ++c) {
     float m = kMFloor, l = 0.f;
@@ -793,7 +804,7 @@ __device__ __forceinline__ void join_few(const Units<true>& w, int ranges, int l
 constexpr int kJoinCols = 32;
 
 template <int HD>
-__device__ __forceinline__ void join_tile(const Units<false>& w, int ranges, int least,
+__device__ __forceinline__ void join_tile(const Units<false>& w, const Deal& deal,
                                           const AttnOut& o, int h, int x32) {
   constexpr int CB = kTileCols / kJoinCols, NV = HD / 32, AT_ONCE = 4;
   const CacheBatch& bt = w.bt;
@@ -804,7 +815,7 @@ __device__ __forceinline__ void join_tile(const Units<false>& w, int ranges, int
   const int ncol = (min(rows, (t + 1) << w.log2r) - row0) * bt.nq;
   const int np = w.pages(ctx, rows, t);
   Parts p{o.part, kTileCols, HD};
-  if (!find_parts(w, ranges, least, w.prefix[b] + w.group(b) * h + w.before(ctx, t), np, p) ||
+  if (!find_parts(w, deal, w.prefix[b] + w.group(b) * h + w.before(ctx, t), np, p) ||
       c >= ncol)
     return;
   float m = kMFloor, l = 0.f;
@@ -858,12 +869,11 @@ __device__ __forceinline__ void join_tile(const Units<false>& w, int ranges, int
     o.stat[((size_t)h * bt.N + bt.first_row(b) + row0) * bt.nq + c] = float2{m, inv};
 }
 
-// What a form's launches share: its units, its workgroups and their least work, and where
-// it writes.
+// What a form's launches share: its units, how they are dealt out, and where it writes.
 template <bool FEW>
 struct Form {
   Units<FEW> w;
-  int ranges, least;
+  Deal deal;
   AttnOut o;
 };
 
@@ -873,8 +883,8 @@ template <int HD>
 __global__ __launch_bounds__(256) void cache_join_kernel(Form<true> few, Form<false> many,
                                                          int many_blocks) {
   const int x = blockIdx.x, h = blockIdx.y;
-  if (x < many_blocks) join_tile<HD>(many.w, many.ranges, many.least, many.o, h, x);
-  else join_few<HD>(few.w, few.ranges, few.least, few.o, h, x - many_blocks);
+  if (x < many_blocks) join_tile<HD>(many.w, many.deal, many.o, h, x);
+  else join_few<HD>(few.w, few.deal, few.o, h, x - many_blocks);
 }
 
 // ---- mass ---------------------------------------------------------------------------
@@ -882,16 +892,17 @@ __global__ __launch_bounds__(256) void cache_join_kernel(Form<true> few, Form<fa
 // and its column's final maximum and sum, so it follows the joining.  With few columns the
 // scores were kept; else they are formed again.
 
-// Few columns: the ranges of the attention; a wave takes every fourth page, a lane a token.
+// Few columns: equal ranges of the units again; a wave takes every fourth page, a lane a
+// token.
 __device__ __forceinline__ void mass_few(const float* __restrict__ score, const Units<true>& w,
-                                         int ranges, int range, int least, int part_cols,
+                                         const Deal& deal, int range, int part_cols,
                                          float c_log2, const float2* __restrict__ stat,
                                          const float* __restrict__ mass_in,
                                          float* __restrict__ mass_out) {
   __shared__ int found;
   const CacheBatch& bt = w.bt;
   const int lane = lane_id(), wave = threadIdx.x >> 6;
-  const long long total = w.prefix[bt.B], per = range_units(total, ranges, least);
+  const long long total = w.prefix[bt.B], per = deal.per(total);
   const long long unit = range * per;
   if (unit >= total) return;
   for (int i = threadIdx.x; i < bt.B; i += kAttThr)
@@ -952,7 +963,7 @@ constexpr int kMassStages = 4;
 template <int HD>
 __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8_t* __restrict__ kc,
                                          const float* __restrict__ kv_scale, const Units<false>& w,
-                                         int ranges, int range, float c_log2,
+                                         const Deal& deal, int range, float c_log2,
                                          const float2* __restrict__ stat,
                                          const float* __restrict__ mass_in,
                                          float* __restrict__ mass_out) {
@@ -973,9 +984,9 @@ __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8
   };
   long long total, first;
   int b;
-  locate<kMassThr>(bt.B, pairs, ranges, range, 1, nullptr, total, b, first);
+  locate<kMassThr>(bt.B, pairs, deal, range, nullptr, total, b, first);
   if (b < 0) return;
-  const long long per = range_units(total, ranges, 1);
+  const long long per = deal.per(total);
   // (in scalar registers: the keys and sums fill the others)
   b = __builtin_amdgcn_readfirstlane(b);
   int off = __builtin_amdgcn_readfirstlane((int)first);  // (of 2^17 pairs in 64 groups)
@@ -1100,11 +1111,11 @@ __global__ __launch_bounds__(kMassThr, 4) void cache_mass_kernel(
   static_assert(kMassThr == kAttThr, "one workgroup size");
   const int x = blockIdx.x;
   if (x >= any_ranges) {
-    mass_few(score, few.w, few.ranges, x - any_ranges, few.least, few.o.part_cols, c_log2, stat,
-             mass_in, mass_out);
+    mass_few(score, few.w, Deal{few.deal.ranges, few.deal.least, 0}, x - any_ranges,
+             few.o.part_cols, c_log2, stat, mass_in, mass_out);
     return;
   }
-  mass_any<HD>(q, kc, kv_scale, any, any_ranges, x, c_log2, stat, mass_in, mass_out);
+  mass_any<HD>(q, kc, kv_scale, any, Deal{any_ranges, 1, 0}, x, c_log2, stat, mass_in, mass_out);
 }
 
 // Host side of the two forms: ranges (workgroups) and scratch.
@@ -1182,25 +1193,25 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
   const bf16* qb = static_cast<const bf16*>(q);
   float2* stat = mass_out != nullptr ? reinterpret_cast<float2*>(base + p.stat) : nullptr;
   float* score = p.scores ? reinterpret_cast<float*>(base + p.score) : nullptr;
-  auto form = [&](const FormPlan& f, int least, auto few) {
+  auto form = [&](const FormPlan& f, int least, int round, auto few) {
     return Form<decltype(few)::value>{
         {bt, max_rows, f.log2r, f.lo, f.hi, reinterpret_cast<long long*>(base + f.prefix)},
-        f.ranges, least,
+        {f.ranges, least, round},
         {static_cast<bf16*>(out), stat, reinterpret_cast<float*>(base + f.part), f.cols}};
   };
-  const Form<true> few = form(p.few, kFewLeast, std::true_type{});
-  const Form<false> many = form(p.many, kManyLeast, std::false_type{});
+  const Form<true> few = form(p.few, kFewLeast, std::min(p.few.ranges, 2 * kCus), std::true_type{});
+  const Form<false> many = form(p.many, kManyLeast, 0, std::false_type{});
   auto go = [&](auto hdv) {
     constexpr int HD = decltype(hdv)::value;
     if (p.few.on) {
       ProfileScope ps("cache_attn_few", s);
-      FOE_LAUNCH(cache_attn_few_kernel<HD>, dim3(few.ranges), dim3(kAttThr), 0, s, qb, a.k, a.v,
-                 a.kv_scale, few.w, few.least, c_log2, few.o, score);
+      FOE_LAUNCH(cache_attn_few_kernel<HD>, dim3(few.deal.ranges), dim3(kAttThr), 0, s, qb, a.k, a.v,
+                 a.kv_scale, few.w, few.deal, c_log2, few.o, score);
     }
     if (p.many.on) {
       ProfileScope ps("cache_attn_tile", s);
-      FOE_LAUNCH(cache_attn_tile_kernel<HD>, dim3(many.ranges), dim3(kTileThr), 0, s, qb, a.k, a.v,
-                 a.kv_scale, many.w, many.least, c_log2, many.o);
+      FOE_LAUNCH(cache_attn_tile_kernel<HD>, dim3(many.deal.ranges), dim3(kTileThr), 0, s, qb, a.k, a.v,
+                 a.kv_scale, many.w, many.deal, c_log2, many.o);
     }
     {
       ProfileScope ps("cache_join", s);
@@ -1217,7 +1228,7 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
       const long long pairs = (long long)ceil_div(a.max_blocks, 2) * a.H * a.B;
       const int any_ranges =
           p.many.on || score == nullptr ? (int)std::min(16LL * kCus, pairs) : 0;
-      FOE_LAUNCH(cache_mass_kernel<HD>, dim3(any_ranges + (score != nullptr ? few.ranges : 0)),
+      FOE_LAUNCH(cache_mass_kernel<HD>, dim3(any_ranges + (score != nullptr ? few.deal.ranges : 0)),
                  dim3(kMassThr), 0, s, qb, a.k, a.kv_scale, any, any_ranges, few, score, c_log2,
                  stat, mass_in, mass_out);
     }
