@@ -590,8 +590,9 @@ __global__ __launch_bounds__(kMoveThr, 8) void cache_move_kernel(
   };
   // tokens whose 16-byte pieces differ from the previous token's
   const uint32_t piece_lo = (uint32_t)my_off & ~15u, piece_hi = (uint32_t)(my_off >> 32);
-  const bool turns =
-      lane == 0 || piece_lo != __shfl_up(piece_lo, 1) || piece_hi != __shfl_up(piece_hi, 1);
+  // (all lanes take part in the shuffles)
+  const uint32_t last_lo = __shfl_up(piece_lo, 1), last_hi = __shfl_up(piece_hi, 1);
+  const bool turns = lane == 0 || piece_lo != last_lo || piece_hi != last_hi;
   const uint32_t turn = (uint32_t)__builtin_amdgcn_ballot_w64(turns) & 0xffffu;
   const int my_piece = __popc(turn & ((2u << (lane & 15)) - 1)) - 1;
   const bool staged = __popc(turn) <= kMovePieces;  // (uniform)

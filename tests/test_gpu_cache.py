@@ -475,6 +475,33 @@ def test_attention_full_tables():
     check_attention(pool, table, [min(c, 128) for c in ctx], rs, q, out, mass)
 
 
+def test_attention_large_decode_batch():
+    """A batch whose pages are dealt to more workgroups than the card holds at a time, with
+    the mass; three of its sequences against the oracle, in a pool of their pages."""
+    H, nq, hd, B, blocks = 2, 2, 96, 72, 110
+    rng = np.random.default_rng(19)
+    g = torch.Generator(DEV).manual_seed(19)
+    dev = foe.cache_empty(B * blocks, H, hd, DEV)
+    for n in ("k", "v"):
+        dev[n].copy_(torch.randn(dev[n].shape, generator=g, device=DEV))
+    dev["kv_scale"].copy_(2.0 ** torch.randint(-2, 2, dev["kv_scale"].shape, generator=g, device=DEV))
+    dev["mass"].uniform_(generator=g)
+    table = rng.permutation(B * blocks).astype(np.int32).reshape(B, blocks)
+    ctx = rng.integers(5500, 64 * blocks, B)
+    q = bf16(rng.normal(size=(H, B, nq, hd)))
+    mass = torch.full_like(dev["mass"], -7.0)
+    say("large decode batch")
+    out = foe.cache_attention(q, dev["k"], dev["v"], dev["kv_scale"], ints(table), ints(ctx),
+                              ints(range(B + 1)), 1, mass_in=dev["mass"], mass_out=mass)
+    torch.cuda.synchronize()
+    picked = [0, 41, B - 1]
+    pages = torch.from_numpy(table[picked].reshape(-1)).long().to(DEV)
+    pool = to_host({n: t.view(torch.uint8)[pages].view(t.dtype) if n in "kv" else t[pages]
+                    for n, t in dev.items()})
+    check_attention(pool, np.arange(len(pages), dtype=np.int32).reshape(3, blocks), ctx[picked],
+                    np.arange(4), q[:, picked].contiguous(), out[picked], mass[pages])
+
+
 @pytest.mark.parametrize("H,nq,hd,ctx,rows,picked", [
     (1, 2, 128, 131071, 1, [0]),
     (1, 1, 96, 40000, 300, [0, 1, 63, 64, 255, 256, 299]),
@@ -528,14 +555,17 @@ def test_pool_past_four_gib():
 
 # ---- eviction -----------------------------------------------------------------------
 
-def check_evict(rng, H, hd, lengths, keep, recent, blocks=None, mass=None, table=None, pool=None):
+def check_evict(rng, H, hd, lengths, keep, recent, blocks=None, mass=None, table=None, pool=None,
+                absent=(), dst=None):
     B = len(lengths)
     blocks = blocks or max(1, max((n + 63) // 64 for n in lengths))
     D = (keep + 63) // 64
     pages = B * (blocks + D) + 2
     order = rng.permutation(pages).astype(np.int32)
     table = order[:B * blocks].reshape(B, blocks) if table is None else table
-    dst = order[B * blocks:B * (blocks + D)].reshape(B, D)
+    for at in absent:
+        table[at] = -1
+    dst = order[B * blocks:B * (blocks + D)].reshape(B, D) if dst is None else dst
     pool = pool or random_pool(rng, pages, H, hd)
     if mass is not None:
         pool["mass"] = mass(pool["mass"]).astype(np.float32)
@@ -568,7 +598,33 @@ def test_evict_parity(H, hd, lengths, keep, recent):
     check_evict(np.random.default_rng([21, H, hd, keep]), H, hd, lengths, keep, recent)
 
 
-@pytest.mark.parametrize("what", ["equal", "two", "neighbours", "special", "negative"])
+@pytest.mark.parametrize("hd", [96, 128])
+@pytest.mark.parametrize("keep", [1900, 1000, 500, 250, 60])
+def test_evict_thick_and_sparse(hd, keep):
+    """16 kept tokens out of two to more than four of the source's 16-token groups, absent
+    pages among them."""
+    rng = np.random.default_rng([27, hd, keep])
+    say("evict thick and sparse", hd, keep)
+    check_evict(rng, 2, hd, [1984, 1951], keep, 20, absent=[(0, 3), (1, 0), (1, 17)])
+
+
+@pytest.mark.parametrize("first", [48, 57, 63])
+def test_evict_into_the_pools_first_page(first):
+    """Kept tokens that pass from the end of another page into page 0."""
+    rng = np.random.default_rng([28, first])
+    n, keep = 128, 128 - first
+
+    def mass(m):
+        m[1], m[0] = np.arange(64) >= first, 1.0
+        return m
+
+    say("evict into page 0", first)
+    check_evict(rng, 1, 128, [n], keep, 0, mass=mass, table=np.array([[1, 0]], dtype=np.int32),
+                dst=np.array([[3, 2]], dtype=np.int32))
+
+
+@pytest.mark.parametrize("what", ["equal", "two", "neighbours", "special", "infinite",
+                                  "negative"])
 def test_evict_masses_near_each_other(what):
     rng = np.random.default_rng(22)
 
@@ -579,6 +635,8 @@ def test_evict_masses_near_each_other(what):
             return (rng.random(m.shape) < 0.3) * 0.25
         if what == "neighbours":  # within four steps of each other
             return np.float32(1.0) + rng.integers(0, 4, m.shape) * np.float32(2.0 ** -23)
+        if what == "infinite":  # NaN ranks above infinity
+            return rng.choice(np.float32([np.nan, -np.nan, np.inf, -np.inf, 0.5]), m.shape)
         if what == "special":
             m = m.copy()
             m[rng.random(m.shape) < 0.05] = np.nan
