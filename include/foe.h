@@ -391,7 +391,7 @@ size_t foe_cache_attention_workspace_bytes(int H, int B, int N, int nq, int hd, 
  * foe_cache_evict - keeps the tokens that received the most attention.  Of a
  * sequence longer than `keep`, each group keeps the last `recent` tokens and,
  * of those before, the keep - recent of largest mass (equal masses: the
- * earlier token; NaN counts as the largest).  Groups choose for themselves.
+ * earlier token; NaN ranks above infinity).  Groups choose for themselves.
  * The kept tokens, in their order, become tokens 0, 1, ... of the pages of
  * dst_table; shorter sequences are moved whole.  Each page's scales follow
  * from the values that it then holds, and mass moves with its token.

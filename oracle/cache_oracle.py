@@ -203,8 +203,8 @@ def evict(pool, table, length, keep, recent, dst):
                 w = np.array([-np.inf if _page(pool, table, b, t // PAGE) < 0 else
                               pool["mass"][_page(pool, table, b, t // PAGE), h, t % PAGE]
                               for t in range(n - recent)], dtype=np.float64)
-                w[np.isnan(w)] = np.inf  # (with an infinite mass: the earlier first)
-                top = np.argsort(-w, kind="stable")[:keep - recent]
+                nan = np.isnan(w)  # (above infinity; the earlier of equals first)
+                top = np.lexsort((np.where(nan, 0.0, -w), ~nan))[:keep - recent]
                 ids = np.concatenate([np.sort(top), np.arange(n - recent, n)])
             kept[b, h, :len(ids)] = ids
             k, v, there = tokens(pool, table, b, h, n)
