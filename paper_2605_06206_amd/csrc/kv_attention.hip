@@ -742,61 +742,60 @@ __device__ __forceinline__ bool find_parts(const Units<FEW>& w, const Deal& deal
   return p.r0 != p.r1;
 }
 
-// Few columns: one workgroup per (group h, sequence b).  8 groups of 32 lanes (a lane 4
-// dims) each sum every eighth part, and are then summed in order.
+// Few columns: one workgroup per (group h, column c of sequence b).  8 groups of 32 lanes (a
+// lane 4 dims) each sum every eighth part, and are then summed in order.  (A sequence's
+// columns one after another in a workgroup: 13.7 us instead of 4.3 for 16 sequences of 1000 to
+// 4000 tokens, 4 groups of 8 heads.)
 template <int HD>
 __device__ __forceinline__ void join_few(const Units<true>& w, const Deal& deal,
-                                         const AttnOut& o, int h, int b) {
+                                         const AttnOut& o, int h, int b, int c) {
   __shared__ f32x4 osum[8][32];
   const CacheBatch& bt = w.bt;
   const int rows = w.rows(b);
-  if (rows <= 0) return;
-  const int np = w.pages(bt.context(b), rows, 0), ncol = rows * bt.nq;
+  if (c >= rows * bt.nq) return;
+  const int np = w.pages(bt.context(b), rows, 0);
   Parts p{o.part, o.part_cols, HD};
   if (!find_parts(w, deal, w.prefix[b] + (long long)np * h, np, p)) return;
   const int grp = threadIdx.x >> 5, l5 = threadIdx.x & 31, d = 4 * l5;
-  for (int c = 0; c < ncol; ++c) {
-    float m = kMFloor, l = 0.f;
-    for (int r = p.r0 + l5; r <= p.r1; r += 32) {
-      const float2 x = p.stats(r)[c];
-      const float mn = fmaxf(m, x.x);
-      l = l * __builtin_amdgcn_exp2f(m - mn) + x.y * __builtin_amdgcn_exp2f(x.x - mn);
-      m = mn;
-    }
-#pragma unroll
-    for (int i = 1; i < 32; i <<= 1) {
-      const float mo = __shfl_xor(m, i), lo = __shfl_xor(l, i), mn = fmaxf(m, mo);
-      l = l * __builtin_amdgcn_exp2f(m - mn) + lo * __builtin_amdgcn_exp2f(mo - mn);
-      m = mn;
-    }
-    f32x4 x{0.f, 0.f, 0.f, 0.f};
-    if (d < HD) {
-#pragma unroll 4
-      for (int r = p.r0 + grp; r <= p.r1; r += 8) {
-        const float a = __builtin_amdgcn_exp2f(p.stats(r)[c].x - m);
-        const f32x4 y = *reinterpret_cast<const f32x4*>(p.at(r) + (size_t)c * HD + d);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] += y[e] * a;
-      }
-    }
-    __syncthreads();
-    osum[grp][l5] = x;
-    __syncthreads();
-    if (grp != 0) continue;
-#pragma unroll
-    for (int k = 1; k < 8; ++k)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] += osum[k][l5][e];
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    if (d < HD) {
-      const int row = bt.first_row(b) + c / bt.nq;
-      bf16* dst = o.out + (((size_t)row * bt.H + h) * bt.nq + c % bt.nq) * HD + d;
-      *reinterpret_cast<bf16x4*>(dst) = bf16x4{(bf16)(x[0] * inv), (bf16)(x[1] * inv),
-                                               (bf16)(x[2] * inv), (bf16)(x[3] * inv)};
-    }
-    if (o.stat != nullptr && l5 == 0)
-      o.stat[((size_t)h * bt.N + bt.first_row(b)) * bt.nq + c] = float2{m, inv};
+  float m = kMFloor, l = 0.f;
+  for (int r = p.r0 + l5; r <= p.r1; r += 32) {
+    const float2 x = p.stats(r)[c];
+    const float mn = fmaxf(m, x.x);
+    l = l * __builtin_amdgcn_exp2f(m - mn) + x.y * __builtin_amdgcn_exp2f(x.x - mn);
+    m = mn;
   }
+#pragma unroll
+  for (int i = 1; i < 32; i <<= 1) {
+    const float mo = __shfl_xor(m, i), lo = __shfl_xor(l, i), mn = fmaxf(m, mo);
+    l = l * __builtin_amdgcn_exp2f(m - mn) + lo * __builtin_amdgcn_exp2f(mo - mn);
+    m = mn;
+  }
+  f32x4 x{0.f, 0.f, 0.f, 0.f};
+  if (d < HD) {
+#pragma unroll 4
+    for (int r = p.r0 + grp; r <= p.r1; r += 8) {
+      const float a = __builtin_amdgcn_exp2f(p.stats(r)[c].x - m);
+      const f32x4 y = *reinterpret_cast<const f32x4*>(p.at(r) + (size_t)c * HD + d);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += y[e] * a;
+    }
+  }
+  osum[grp][l5] = x;
+  __syncthreads();
+  if (grp != 0) return;
+#pragma unroll
+  for (int k = 1; k < 8; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] += osum[k][l5][e];
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if (d < HD) {
+    const int row = bt.first_row(b) + c / bt.nq;
+    bf16* dst = o.out + (((size_t)row * bt.H + h) * bt.nq + c % bt.nq) * HD + d;
+    *reinterpret_cast<bf16x4*>(dst) = bf16x4{(bf16)(x[0] * inv), (bf16)(x[1] * inv),
+                                             (bf16)(x[2] * inv), (bf16)(x[3] * inv)};
+  }
+  if (o.stat != nullptr && l5 == 0)
+    o.stat[((size_t)h * bt.N + bt.first_row(b)) * bt.nq + c] = float2{m, inv};
 }
 
 // Many columns: one workgroup per (32 columns of a tile, group h), 8 threads a column; a
@@ -877,14 +876,15 @@ struct Form {
   AttnOut o;
 };
 
-// One launch joins both forms' parts: `many_blocks` workgroups the tiles', the rest the
-// sequences' of few columns.
+// One launch joins both forms' parts: `many_blocks` by H workgroups those of tiles, the rest
+// those of few columns.
 template <int HD>
 __global__ __launch_bounds__(256) void cache_join_kernel(Form<true> few, Form<false> many,
                                                          int many_blocks) {
   const int x = blockIdx.x, h = blockIdx.y;
   if (x < many_blocks) join_tile<HD>(many.w, many.deal, many.o, h, x);
-  else join_few<HD>(few.w, few.deal, few.o, h, x - many_blocks);
+  else join_few<HD>(few.w, few.deal, few.o, h, (x - many_blocks) / few.o.part_cols,
+                    (x - many_blocks) % few.o.part_cols);
 }
 
 // ---- mass ---------------------------------------------------------------------------
@@ -1216,7 +1216,7 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
     {
       ProfileScope ps("cache_join", s);
       const int many_blocks = p.many.on ? p.many.tiles * (kTileCols / kJoinCols) : 0;
-      FOE_LAUNCH(cache_join_kernel<HD>, dim3(many_blocks + (p.few.on ? a.B : 0), a.H), dim3(256), 0,
+      FOE_LAUNCH(cache_join_kernel<HD>, dim3(many_blocks + (p.few.on ? a.B * few.o.part_cols : 0), a.H), dim3(256), 0,
                  s, few, many, many_blocks);
     }
     if (mass_out != nullptr) {
