@@ -1121,9 +1121,11 @@ __global__ __launch_bounds__(kMassThr, 4) void cache_mass_kernel(
 // Host side of the two forms: ranges (workgroups) and scratch.
 constexpr int kFewLeast = 4;   // pages of a range at least: one for each wave
 constexpr int kManyLeast = 2;
-// the scores of few columns are kept for the mass up to this many bytes; beyond, they
-// are formed again
-constexpr size_t kScoreBytes = (size_t)256 << 20;
+// The scores of few columns are kept for the mass where the tables' room for them is up to
+// this many bytes of workspace; beyond, they are formed again.  us kept and formed again, 8
+// groups of two heads: 16 sequences of 1000 to 4000 tokens 35 53, 64 of 1000 to 8000 155 264,
+// one of 100000 68 112.
+constexpr size_t kScoreBytes = (size_t)1 << 30;
 
 // One form of a call: what it launches and where its scratch is.
 struct FormPlan {

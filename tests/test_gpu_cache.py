@@ -410,7 +410,7 @@ def test_attention_wide_table():
     H, nq, hd, seqs = 2, 8, 128, [(300, 2), (0, 1), (700, 1)]
     ctx, rs, table, pages = batch(rng, seqs)
     dev = to_dev(random_pool(rng, pages, H, hd))
-    wide = np.full((3, 12000), -1, dtype=np.int32)
+    wide = np.full((3, 50000), -1, dtype=np.int32)
     wide[:, :table.shape[1]] = table
     q = bf16(rng.normal(size=(H, rs[-1], nq, hd)))
     say("wide table")
