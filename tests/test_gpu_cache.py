@@ -852,6 +852,54 @@ def test_graph_replay(seqs):
             assert torch.equal(a, b), rep
 
 
+def test_calls_on_two_streams_at_once():
+    """Two batches on streams of their own, in flight together, give what each gives alone."""
+    batches = [_decode_inputs(seed, seqs=seqs) for seed, seqs in (
+        (50, ((700, 1), (3000, 1), (64, 1))), (51, ((900, 60), (5, 1), (64, 90))))]
+
+    for x in batches:
+        x[0]["mass_out"] = torch.zeros_like(x[0]["mass"])
+
+    def call(x, stream=None):
+        dev, table, ctx, rs, qkv, dst = x
+        rows = 1 if qkv.shape[1] == table.shape[0] else 90
+        q = foe.cache_append(qkv, dev["k"], dev["v"], dev["kv_scale"], table, ctx, rs, THETA,
+                             stream=stream)
+        out = foe.cache_attention(q, dev["k"], dev["v"], dev["kv_scale"], table, ctx, rs, rows,
+                                  mass_in=dev["mass"], mass_out=dev["mass_out"], stream=stream)
+        kept, n = foe.cache_evict(dev["k"], dev["v"], dev["kv_scale"], dev["mass"], table, ctx,
+                                  150, 30, dst, stream=stream)
+        return out.view(torch.int16), dev["mass_out"], kept, n
+
+    say("two streams")
+    want = [[t.clone() for t in call(x)] for x in batches]
+    streams = [torch.cuda.Stream() for _ in batches]
+    torch.cuda.synchronize()
+    for _ in range(8):
+        got = [call(x, s) for x, s in zip(batches, streams)]
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_shared_prefix_pages():
+    """Sequences that read the same pages: a common prefix, and one table twice."""
+    rng = np.random.default_rng(52)
+    pool = random_pool(rng, 24, 2, 96)
+    table = rng.permutation(12).astype(np.int32).reshape(3, 4)
+    table[1, :3] = table[0, :3]
+    table[2] = table[0]
+    ctx, rs = [200, 230, 200], np.array([0, 1, 41, 42])
+    dev, q = to_dev(pool), bf16(rng.normal(size=(2, 42, 2, 96)))
+    say("shared prefix")
+    out = foe.cache_attention(q, dev["k"], dev["v"], dev["kv_scale"], ints(table), ints(ctx),
+                              ints(rs), 40)
+    torch.cuda.synchronize()
+    check_attention(pool, table, ctx, rs, q, out, None)
+    check_evict(rng, 2, 96, [200, 230, 200], 90, 10, table=table, pool=pool,
+                dst=np.arange(12, 18, dtype=np.int32).reshape(3, 2))
+
+
 def test_empty_batches():
     dev = foe.cache_empty(2, 1, 96, DEV)
     table, none = ints([[0, 1]]), ints([0])
