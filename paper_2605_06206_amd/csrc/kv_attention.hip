@@ -14,8 +14,8 @@
 // numbered in that order, are cut into equal ranges, one for each workgroup of a
 // grid that fills the chip, whatever the lengths are.  A workgroup walks the tiles in
 // its range; a tile that lies in one range is written at once, the others leave their
-// unnormalised parts, which a second launch joins in page order.  (One workgroup per
-// tile of 16 columns: 1151 us instead of 195 for four sequences of 131072 tokens, 8 groups.)
+// unnormalised parts, which the next launch joins in page order.  (One workgroup per
+// tile of 16 columns: 1151 us instead of 188 for four sequences of 131072 tokens, 8 groups.)
 #include <limits.h>
 
 #include <algorithm>
@@ -172,7 +172,8 @@ template <int HD>
 struct PageFrags {
   static constexpr int NST = HD / 32;  // score k-steps
   static constexpr int NDT = HD / 16;  // output tiles
-  u32x4 k[4][(HD + 63) / 64];          // tile t: 16 bytes at 64 h + 16 g (8 at 64 + 8 g for HD = 96)
+  // tile t: 16 bytes at 64 h + 16 g (8 at 64 + 8 g for HD = 96)
+  u32x4 k[4][(HD + 63) / 64];
   u32x4 v[NDT];                        // dims 16 dt + n, tokens 16 g .. +15
 
   __device__ __forceinline__ void load_k(const uint8_t* kp, int lane) {
@@ -1038,7 +1039,8 @@ __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8
       const uint32_t to = lds + (uint32_t)((t & (kMassStages - 1)) * STAGE);
       const uint32_t step = (uint32_t)t * (kMassCols * HD * 2);
 #pragma unroll
-      for (int i = 0; i < QI; ++i) dma16(rq, qoff[i] + step, to + (uint32_t)wave_u * (QI * 1024), i * 1024);
+      for (int i = 0; i < QI; ++i)
+        dma16(rq, qoff[i] + step, to + (uint32_t)wave_u * (QI * 1024), i * 1024);
       // (every wave loads the statistics, so that all count the same)
       dma4(rz, (uint32_t)t * (kMassCols * 8) + lane * 4u, to, QT);
     };
@@ -1207,19 +1209,20 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
     constexpr int HD = decltype(hdv)::value;
     if (p.few.on) {
       ProfileScope ps("cache_attn_few", s);
-      FOE_LAUNCH(cache_attn_few_kernel<HD>, dim3(few.deal.ranges), dim3(kAttThr), 0, s, qb, a.k, a.v,
-                 a.kv_scale, few.w, few.deal, c_log2, few.o, score);
+      FOE_LAUNCH(cache_attn_few_kernel<HD>, dim3(few.deal.ranges), dim3(kAttThr), 0, s, qb, a.k,
+                 a.v, a.kv_scale, few.w, few.deal, c_log2, few.o, score);
     }
     if (p.many.on) {
       ProfileScope ps("cache_attn_tile", s);
-      FOE_LAUNCH(cache_attn_tile_kernel<HD>, dim3(many.deal.ranges), dim3(kTileThr), 0, s, qb, a.k, a.v,
-                 a.kv_scale, many.w, many.deal, c_log2, many.o);
+      FOE_LAUNCH(cache_attn_tile_kernel<HD>, dim3(many.deal.ranges), dim3(kTileThr), 0, s, qb, a.k,
+                 a.v, a.kv_scale, many.w, many.deal, c_log2, many.o);
     }
     {
       ProfileScope ps("cache_join", s);
       const int many_blocks = p.many.on ? p.many.tiles * (kTileCols / kJoinCols) : 0;
-      FOE_LAUNCH(cache_join_kernel<HD>, dim3(many_blocks + (p.few.on ? a.B * few.o.part_cols : 0), a.H), dim3(256), 0,
-                 s, few, many, many_blocks);
+      const int few_blocks = p.few.on ? a.B * few.o.part_cols : 0;
+      FOE_LAUNCH(cache_join_kernel<HD>, dim3(many_blocks + few_blocks, a.H), dim3(256), 0, s, few,
+                 many, many_blocks);
     }
     if (mass_out != nullptr) {
       ProfileScope ps("cache_mass", s);

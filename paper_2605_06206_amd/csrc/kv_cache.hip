@@ -717,7 +717,9 @@ static int select_slices(int max_blocks) {
   return ceil_div((long long)max_blocks * kPage, kSelTokens);
 }
 
-static size_t select_counts(int H, int B, int slices) { return (size_t)3 * B * H * slices * kSelBins; }
+static size_t select_counts(int H, int B, int slices) {
+  return (size_t)3 * B * H * slices * kSelBins;
+}
 
 size_t cache_evict_scratch_bytes(int H, int B, int max_blocks) {
   const int slices = select_slices(max_blocks);

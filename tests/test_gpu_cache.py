@@ -484,7 +484,8 @@ def test_attention_large_decode_batch():
     dev = foe.cache_empty(B * blocks, H, hd, DEV)
     for n in ("k", "v"):
         dev[n].copy_(torch.randn(dev[n].shape, generator=g, device=DEV))
-    dev["kv_scale"].copy_(2.0 ** torch.randint(-2, 2, dev["kv_scale"].shape, generator=g, device=DEV))
+    dev["kv_scale"].copy_(2.0 ** torch.randint(-2, 2, dev["kv_scale"].shape, generator=g,
+                                               device=DEV))
     dev["mass"].uniform_(generator=g)
     table = rng.permutation(B * blocks).astype(np.int32).reshape(B, blocks)
     ctx = rng.integers(5500, 64 * blocks, B)
