@@ -660,7 +660,7 @@ __global__ __launch_bounds__(kMoveThr, 8) void cache_move_kernel(
     if (tid == 0) *reinterpret_cast<float2*>(kv_scale + dst * 2) = float2{ks, vs};
     if (tid < cnt) mass[dst * kPage + tid] = m;
     if (kt < cnt) {
-      const float r = ss[kt].x * ki;
+      const float r = scale_ratio(ss[kt].x, ki);
       if (r != 1.f) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) kw[e] = rescale4(kw[e], r);
@@ -671,7 +671,7 @@ __global__ __launch_bounds__(kMoveThr, 8) void cache_move_kernel(
       u32x4* w = reinterpret_cast<u32x4*>(vc + dst * (kPage * HD) + (g * HD + d) * kSub);
       const int left = cnt - g * kSub;  // slots past the kept tokens stay as they were
       const u32x4 was = left < kSub ? *w : zero_u32x4();
-      const float r = my_scale * vi;
+      const float r = scale_ratio(my_scale, vi);
       if (__builtin_amdgcn_ballot_w64(r != 1.f)) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {

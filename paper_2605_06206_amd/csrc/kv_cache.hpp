@@ -51,6 +51,11 @@ __device__ __forceinline__ float block_scale(float amax) {
 __device__ __forceinline__ float pow2_inv(float s) {
   return __uint_as_float((254u << 23) - __float_as_uint(s));
 }
+// old / new scale.  Where it passes fp32, the codes that it multiplies are zeros or NaN
+// (others, at least 2^-9, would have made the new scale larger), and 0 * inf is NaN.
+__device__ __forceinline__ float scale_ratio(float old, float inv_new) {
+  return fminf(old * inv_new, 0x1p127f);
+}
 
 // A call's sequences.  Lengths and tables are the caller's device data and are
 // not trusted: rows are cut to the batch, lengths to the table, and pages

@@ -1,0 +1,96 @@
+"""The 8-bit key/value cache at the ends of its range."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache_oracle as co
+from paper_2605_06206_amd import foe
+from test_gpu_cache import (DEV, SCALE, THETA, bf16, check_evict, ints, random_pool, say, to_host)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True, scope="module")
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    foe.lib()
+
+
+# ---- eviction ---------------------------------------------------------------------
+
+def zero_tokens(pool, table, which, what):
+    """Codes 0 (either sign) for the tokens `which` of the first sequence."""
+    for t in which:
+        p, s = table[0, t // 64], t % 64
+        if what != "v":
+            pool["k"][p, :, s] &= 0x80
+        if what != "k":
+            pool["v"][p, :, s // 16, :, s % 16] &= 0x80
+        pool["mass"][p, :, s] = 2.0
+
+
+@pytest.mark.parametrize("hd", [96, 128])
+@pytest.mark.parametrize("what", ["k", "v", "both"])
+@pytest.mark.parametrize("which", ["thick", "sparse"])
+def test_evict_zero_tokens_of_large_scales(hd, what, which):
+    """The kept tokens of a new page are all zero, in pages whose scale passes the smallest
+    one by more than fp32 holds: they stay zero."""
+    rng = np.random.default_rng([61, hd])
+    pool = random_pool(rng, 12, 2, hd)
+    pool["mass"][...] = 1.0
+    pool["kv_scale"][:6] = 2.0 ** np.array([27, 28, 30, 60, 100, 120])[:, None, None]
+    table = np.arange(6, dtype=np.int32)[None]
+    tokens = range(10, 384, 5) if which == "sparse" else [t for t in range(384) if t % 64 >= 20]
+    zero_tokens(pool, table, tokens, what)
+    say("evict zero tokens", hd, what, which)
+    check_evict(rng, 2, hd, [384], len(tokens), 0, pool=pool, table=table,
+                dst=np.arange(6, 6 + (len(tokens) + 63) // 64, dtype=np.int32)[None])
+
+
+@pytest.mark.parametrize("hd", [96, 128])
+def test_evict_zero_tokens_beside_small_ones(hd):
+    """Zero tokens of a page of large scale, and NaN keys there, beside tokens of a page of
+    small scale: the ratio of the scales passes fp32."""
+    rng = np.random.default_rng([62, hd])
+    pool = random_pool(rng, 4, 1, hd)
+    pool["mass"][...] = 1.0
+    pool["kv_scale"][:2] = 2.0 ** np.array([60, -90])[:, None, None]
+    pool["kv_scale"][0, 0] = 2.0 ** 60, 2.0 ** 100
+    pool["k"][0, :, 8] = 0x7F
+    table = np.array([[0, 1]], dtype=np.int32)
+    zero_tokens(pool, table, [t for t in range(0, 64, 3) if t != 8], "both")
+    pool["v"][0, :, 0, :, 8] = 0
+    pool["mass"][0, :, 8] = pool["mass"][1, :, 5:20] = 2.0
+    say("evict zero tokens beside small ones", hd)
+    check_evict(rng, 1, hd, [128], 22 + 1 + 15, 0, pool=pool, table=table,
+                dst=np.array([[3]], dtype=np.int32))
+
+
+def test_evict_the_neighbours_of_an_outlier():
+    """A token of 1e12 makes its page's ordinary tokens zero codes; it is evicted, and what
+    sees the others afterwards is finite."""
+    rng = np.random.default_rng(63)
+    H, nq, hd = 2, 2, 128
+    dev = foe.cache_empty(4, H, hd, DEV)
+    x = rng.normal(size=(H, 40, nq + 2, hd))
+    x[:, 3, nq:] = 1e12
+    table, rs = ints([[0]]), ints([0, 40])
+    pool = (dev["k"], dev["v"], dev["kv_scale"])
+    say("evict an outlier")
+    foe.cache_append(bf16(x), *pool, table, ints([0]), rs, THETA, SCALE)
+    dev["mass"].fill_(1.0)
+    dev["mass"][:, :, 3] = 0.5
+    before = to_host(dev)
+    kept, n = foe.cache_evict(*pool, dev["mass"], table, ints([40]), 30, 4, ints([[2]]))
+    q = foe.cache_append(bf16(rng.normal(size=(H, 1, nq + 2, hd))), *pool, ints([[2]]), n,
+                         ints([0, 1]), THETA, SCALE, pos=ints([40]))
+    o = foe.cache_attention(q, *pool, ints([[2]]), n, ints([0, 1]), 1)
+    torch.cuda.synchronize()
+    assert not (kept == 3).any()
+    k_ref, _ = co.evict(before, np.array([[0]]), [40], 30, 4, np.array([[2]]))
+    assert np.array_equal(kept.cpu().numpy(), k_ref)
+    assert (before["kv_scale"][2] == 2.0 ** -100).all()
+    assert (to_host(dev)["k"][2, :, :30] & 0x7F == 0).all()
+    assert torch.isfinite(o).all()
