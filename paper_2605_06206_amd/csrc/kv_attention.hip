@@ -925,10 +925,14 @@ __device__ __forceinline__ void mass_few(const float* __restrict__ score, const 
       const size_t at = ((size_t)page * bt.H + h) * kPage + lane;
       float x = slot < ctx ? mass_in[at] : 0.f, y = 0.f;
       const float* s = score + (size_t)(blk - blk0) * part_cols * kPage + lane;
+      int last = ctx, head = 0;  // the last token that column c sees
       for (int c = 0; c < ncol; ++c) {
         const float m = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(z.x), c));
         const float inv = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(z.y), c));
-        y += __builtin_amdgcn_exp2f(fmaf(s[c * kPage], c_log2, -m)) * inv;
+        // (the sum of a NaN row is NaN: 0 * inv would be NaN for the tokens behind it too)
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[c * kPage], c_log2, -m)) * inv;
+        y += slot <= last ? p : 0.f;
+        if (++head == bt.nq) head = 0, ++last;
       }
       if (slot < min(ctx + rows, bt.cap())) mass_out[at] = x + y;
     }
@@ -1056,7 +1060,7 @@ __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8
       if (t + kMassStages - 1 < t1) issue(t + kMassStages - 1);
       const unsigned char* tile = smem + (t & (kMassStages - 1)) * STAGE;
       if (works) {
-        const float2 z = *reinterpret_cast<const float2*>(tile + QT + qi * 8);
+        float2 z = *reinterpret_cast<const float2*>(tile + QT + qi * 8);
         f32x16 x;
 #pragma unroll
         for (int v = 0; v < 16; ++v) x[v] = 0.f;
@@ -1073,6 +1077,13 @@ __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8
 #pragma unroll
           for (int v = 0; v < 16; ++v)
             if (key0 + 8 * (v >> 2) + 4 * hl + (v & 3) >= seen) x[v] = -__builtin_inff();
+          // a NaN row counts, as NaN, for the tokens that it sees alone (0 * NaN is NaN)
+          if (__builtin_amdgcn_ballot_w64(z.y != z.y) && z.y != z.y) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+              if (key0 + 8 * (v >> 2) + 4 * hl + (v & 3) < seen) acc[v] = z.y;
+            z.y = 0.f;
+          }
         }
 #pragma unroll
         for (int v = 0; v < 16; ++v)

@@ -6,7 +6,8 @@ import torch
 
 from oracle import cache_oracle as co
 from paper_2605_06206_amd import foe
-from test_gpu_cache import (DEV, SCALE, THETA, bf16, check_evict, ints, random_pool, say, to_host)
+from test_gpu_cache import (DEV, SCALE, THETA, batch, bf16, check_evict, host, ints, mass_bound,
+                            random_pool, say, to_dev, to_host)
 
 pytestmark = pytest.mark.gpu
 
@@ -94,3 +95,70 @@ def test_evict_the_neighbours_of_an_outlier():
     assert (before["kv_scale"][2] == 2.0 ** -100).all()
     assert (to_host(dev)["k"][2, :, :30] & 0x7F == 0).all()
     assert torch.isfinite(o).all()
+
+
+# ---- mass beside rows that are not finite ----------------------------------------------
+
+def check_mass(pool, table, ctx, rs, q, mass_out, far=False):
+    """Masses against the oracle's, NaN where it has NaN.  (far: the probabilities are 0 or
+    equal, of scores that are exact)"""
+    m = host(mass_out)
+    nq, hd = q.shape[2:]
+    ref = co.attend(pool, host(q), table, ctx, rs, mass=True)
+    finite = np.nan_to_num(host(q), nan=0.0, posinf=0.0, neginf=0.0)
+    big = 0.0 if far else co.attend(pool, finite, table, ctx, rs)[2]
+    for (b, h), w in ref[3].items():
+        slot = np.arange(len(w))
+        p = table[b, slot // 64]
+        there = (p >= 0) & (p < len(m))
+        slot, p, w = slot[there], p[there], w[there]
+        got = m[p, h, slot % 64]
+        before = np.where(slot < ctx[b], pool["mass"][p, h, slot % 64], 0.0).astype(np.float64)
+        assert np.array_equal(np.isnan(got), np.isnan(w)), (b, h, np.isnan(got) ^ np.isnan(w))
+        lim = mass_bound(w, before, big, hd, (rs[b + 1] - rs[b]) * nq)
+        ok = np.isnan(w) | (np.abs(got - before - w) <= lim)
+        assert ok.all(), (b, h, slot[~ok][:8], got[~ok][:8], w[~ok][:8])
+    return ref
+
+
+NAN_ROWS = [
+    # nq, hd, [(ctx, rows)], row with a NaN query, width of the table (0: what is needed)
+    (2, 128, [(10, 8), (61, 6), (3, 1)], 3, 0),           # few columns, scores kept
+    (1, 96, [(62, 12), (0, 5)], 4, 0),
+    (2, 96, [(10, 8), (0, 3)], 5, 70000),                 # few columns, scores formed again
+    (2, 128, [(0, 40), (0, 1)], 20, 0),                   # chunks
+    (1, 96, [(100, 300), (5, 70)], 150, 0),
+    (3, 128, [(30, 100), (7, 2), (300, 1), (64, 1)], 33, 0),  # both
+]
+
+
+@pytest.mark.parametrize("nq,hd,seqs,bad,width", NAN_ROWS)
+@pytest.mark.parametrize("what", ["nan", "inf", "key"])
+def test_mass_beside_rows_that_are_not_finite(nq, hd, seqs, bad, width, what):
+    """A row of NaN (by its query, or a key that it sees) makes the masses of the tokens
+    that it sees NaN, and no other's."""
+    rng = np.random.default_rng([64, nq, hd, bad])
+    H = 2
+    ctx, rs, table, pages = batch(rng, seqs)
+    pool = random_pool(rng, pages, H, hd)
+    qx = rng.normal(size=(H, rs[-1], nq, hd))
+    if what == "key":  # of the last row: the rows before do not see it
+        t = ctx[0] + seqs[0][1] - 1
+        pool["k"][table[0, t // 64], 1, t % 64] = 0x7F
+    elif what == "nan":
+        qx[1, bad, nq - 1, 5] = np.nan
+    else:
+        qx[0, bad, 0, :] = -np.inf
+    dev, q = to_dev(pool), bf16(qx)
+    wide = table
+    if width:
+        wide = np.full((len(seqs), width), -1, dtype=np.int32)
+        wide[:, :table.shape[1]] = table
+    mass = torch.full_like(dev["mass"], -7.0)
+    say("mass beside rows that are not finite", nq, hd, seqs, bad, width, what)
+    o = foe.cache_attention(q, dev["k"], dev["v"], dev["kv_scale"], ints(wide), ints(ctx),
+                            ints(rs), max(n for _, n in seqs), mass_in=dev["mass"],
+                            mass_out=mass)
+    torch.cuda.synchronize()
+    ref = check_mass(pool, table, ctx, rs, q, mass)
+    assert np.array_equal(np.isnan(host(o)), np.isnan(ref[0]))
