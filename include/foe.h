@@ -375,6 +375,10 @@ int foe_cache_append(foe_dtype dt, int H, int B, int N, int nq, int hd, int n_pa
  *   ws, ws_bytes           workspace of foe_cache_attention_workspace_bytes()
  * bf16: products in bf16 MFMA with fp32 accumulation; softmax statistics, mass and
  * sums in fp32, the probabilities are rounded to bf16 for the product with v.
+ * Scores may lie anywhere in fp32's range.  A row with a score of NaN or +inf, or
+ * whose scores are all -inf (past fp32), gives NaN, and so do the masses of the
+ * tokens that it sees.  The sums with v are normalised at the end: values up to
+ * 2^94 in magnitude cannot take them past fp32.
  */
 int foe_cache_attention(foe_dtype dt, int H, int B, int N, int nq, int hd, int n_pages,
                         int max_blocks, int max_rows, const void* q, const int32_t* row_start,

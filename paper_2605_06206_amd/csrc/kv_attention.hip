@@ -33,7 +33,32 @@ constexpr int kFewCols = 16;
 constexpr int kTileThr = 512;         // many columns: eight waves of 32 columns
 constexpr int kTileCols = 256;
 constexpr int kCus = 256;             // compute units of the card; a multiple of the XCDs
-constexpr float kMFloor = -1.0e30f;   // the running maximum's start: finite, below any score
+// The running maximum starts below any finite score (times log2 e / sqrt(hd) < 0.15), and is
+// at least the next value once the column has seen a token: where the sum stays 0, that
+// tells a row whose scores are all -inf (NaN) from one that sees no token (zeros).
+constexpr float kMFloor = -0x1.000002p126f;
+constexpr float kMSeen = -0x1p126f;
+
+// 1 / sum
+__device__ __forceinline__ float inv_sum(float m, float l) {
+  return l == 0.f ? (m > kMFloor ? __builtin_nanf("") : 0.f) : 1.f / l;
+}
+// A probability is 2^(s c - m), s c not rounded before the subtraction, where m is a rounded
+// product: its rounding is a factor of all of a column's probabilities, and of their sum.
+// From 2^24 on that factor leaves [1/2, 2] and would soon leave fp32, so there s c is rounded
+// too, which makes the largest probability 1 again.
+__device__ __forceinline__ bool far_max(float m) {
+  return fabsf(m) >= 0x1p24f && fabsf(m) < 0x1p126f;
+}
+__device__ __forceinline__ float far_exponent(float s, float c, float m) {
+#pragma clang fp contract(off)
+  const float t = s * c;
+  return t - m;
+}
+// What the mass needs of a column: its maximum and 1 / sum, negative for a far maximum.
+__device__ __forceinline__ float2 column_stat(float m, float inv) {
+  return float2{m, far_max(m) ? -inv : inv};
+}
 
 // ---- dealing out the work -------------------------------------------------------
 
@@ -237,7 +262,7 @@ __host__ __device__ inline size_t part_floats(int cols, int hd) { return (size_t
 
 struct AttnOut {
   bf16* out;
-  float2* stat;      // (maximum, 1 / sum) of each column, or null
+  float2* stat;      // of each column (see column_stat), or null
   float* part;
   int part_cols;
 };
@@ -289,6 +314,8 @@ __device__ __forceinline__ void few_columns(
     fn.load_v(vc + pg, lane);
   };
   const int mine = (blk1 - blk0 - wave + NW - 1) / NW;  // pages of this wave
+  int first = -1;    // the first that is there
+  bool far = false;  // (uniform) a column's maximum is far from 0
   if (mine > 0) fetch(0);
   for (int i = 0; i < mine; ++i) {
     const int blk = blk0 + wave + NW * i;
@@ -298,6 +325,7 @@ __device__ __forceinline__ void few_columns(
     F f = fn;
     if (i + 1 < mine) fetch(i + 1);
     if (page < 0) continue;
+    if (first < 0) first = blk;
     f32x4 s[4];
     f.scores(qf, ks, s);
     const int k0 = blk * kPage + 16 * g;
@@ -336,18 +364,28 @@ __device__ __forceinline__ void few_columns(
       const float m_new = need ? mxs : m_run;
       const float a = __builtin_amdgcn_exp2f(m_run - m_new);
       m_run = m_new;
+      far = __builtin_amdgcn_ballot_w64(far_max(m_run)) != 0;
       l_run *= a;
 #pragma unroll
       for (int dt = 0; dt < F::NDT; ++dt)
 #pragma unroll
         for (int e = 0; e < 4; ++e) oacc[dt][e] *= a;
     }
+    float c_page = c_log2, m_page = m_run;
+    if (far) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[t][e] = far_exponent(s[t][e], c_log2, m_run);
+      c_page = 1.f;
+      m_page = 0.f;
+    }
     bf16x8 p[2];
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float x = __builtin_amdgcn_exp2f(fmaf(s[t][e], c_log2, -m_run));
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[t][e], c_page, -m_page));
         l_run += x;
         p[t >> 1][4 * (t & 1) + e] = (bf16)x;
       }
@@ -358,6 +396,7 @@ __device__ __forceinline__ void few_columns(
         oacc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
             codes_to_bf16(f.v[dt][2 * u], f.v[dt][2 * u + 1], vs), p[u], oacc[dt], 0, 0, 0);
   }
+  if (first >= 0 && first * kPage < seen) m_run = fmaxf(m_run, kMSeen);
   // the waves' states, merged in wave order
   l_run += __shfl_xor(l_run, 16);
   l_run += __shfl_xor(l_run, 32);
@@ -383,11 +422,10 @@ __device__ __forceinline__ void few_columns(
       x += lds.oo[v][c][d] * a;
     }
     if (whole) {
-      // a column that sees no token gives zeros
-      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const float inv = inv_sum(m, l);
       const int row = bt.first_row(b) + c / bt.nq;
       o.out[(((size_t)row * bt.H + h) * bt.nq + c % bt.nq) * HD + d] = (bf16)(x * inv);
-      if (d == 0 && o.stat != nullptr) o.stat[qrow + c] = float2{m, inv};
+      if (d == 0 && o.stat != nullptr) o.stat[qrow + c] = column_stat(m, inv);
     } else {
       pt[i] = x;
       if (d == 0) reinterpret_cast<float2*>(pt + o.part_cols * HD)[c] = float2{m, l};
@@ -642,8 +680,19 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
         }
         const float mxs = mx * c_log2;
         const bool need = mxs > m_run + 8.f;
-        const float m_new = need ? mxs : m_run;
+        float m_new = need ? mxs : m_run;
         const float a_new = need ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.f;
+        if (blk * kPage < seen) m_new = fmaxf(m_new, kMSeen);
+        m_run = m_new;
+        float c_page = c_log2;
+        if (__builtin_amdgcn_ballot_w64(far_max(m_new))) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) sacc[i][v] = far_exponent(sacc[i][v], c_log2, m_new);
+          c_page = 1.f;
+          m_new = 0.f;
+        }
         if (it > 0) pv(vb);
         float ps = 0.f;
 #pragma unroll
@@ -652,7 +701,7 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             const float x = __builtin_amdgcn_exp2f(
-                fmaf(sacc[u >> 1][(u & 1) * 8 + e], c_log2, -m_new));
+                fmaf(sacc[u >> 1][(u & 1) * 8 + e], c_page, -m_new));
             ps += x;
             p8[e] = (bf16)x;
           }
@@ -660,7 +709,6 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
         }
         resc = __builtin_amdgcn_ballot_w64(need) != 0;
         alpha = a_new;
-        m_run = m_new;
         l_run = l_run * a_new + ps;
       }
       if (it + 1 < niter)
@@ -674,7 +722,7 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
     if (col < ncol) {
       // lane holds dims 32 i + 8 g + 4 hl + [0, 4)
       if (whole) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const float inv = inv_sum(m_run, l);
         const int row = bt.first_row(b) + row0 + col / bt.nq;
         bf16* dst = o.out + (((size_t)row * bt.H + h) * bt.nq + col % bt.nq) * HD;
 #pragma unroll
@@ -686,7 +734,7 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
             for (int v = 0; v < 4; ++v) x[v] = (bf16)(oacc[i][g * 4 + v] * inv);
             *reinterpret_cast<bf16x4*>(dst + i * 32 + g * 8 + hl * 4) = x;
           }
-        if (o.stat != nullptr && hl == 0) o.stat[qrow + col] = float2{m_run, inv};
+        if (o.stat != nullptr && hl == 0) o.stat[qrow + col] = column_stat(m_run, inv);
       } else {
         float* pt = o.part + slot * part_floats(kTileCols, HD);
 #pragma unroll
@@ -788,7 +836,7 @@ __device__ __forceinline__ void join_few(const Units<true>& w, const Deal& deal,
   for (int k = 1; k < 8; ++k)
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] += osum[k][l5][e];
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float inv = inv_sum(m, l);
   if (d < HD) {
     const int row = bt.first_row(b) + c / bt.nq;
     bf16* dst = o.out + (((size_t)row * bt.H + h) * bt.nq + c % bt.nq) * HD + d;
@@ -796,7 +844,7 @@ __device__ __forceinline__ void join_few(const Units<true>& w, const Deal& deal,
                                              (bf16)(x[2] * inv), (bf16)(x[3] * inv)};
   }
   if (o.stat != nullptr && l5 == 0)
-    o.stat[((size_t)h * bt.N + bt.first_row(b)) * bt.nq + c] = float2{m, inv};
+    o.stat[((size_t)h * bt.N + bt.first_row(b)) * bt.nq + c] = column_stat(m, inv);
 }
 
 // Many columns: one workgroup per (32 columns of a tile, group h), 8 threads a column; a
@@ -857,7 +905,7 @@ __device__ __forceinline__ void join_tile(const Units<false>& w, const Deal& dea
         for (int e = 0; e < 4; ++e) x[k][e] += y[i][k][e] * a;
     }
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float inv = inv_sum(m, l);
   const int row = bt.first_row(b) + row0 + c / bt.nq;
   bf16* dst = o.out + (((size_t)row * bt.H + h) * bt.nq + c % bt.nq) * HD;
 #pragma unroll
@@ -866,7 +914,7 @@ __device__ __forceinline__ void join_tile(const Units<false>& w, const Deal& dea
         bf16x4{(bf16)(x[k][0] * inv), (bf16)(x[k][1] * inv), (bf16)(x[k][2] * inv),
                (bf16)(x[k][3] * inv)};
   if (o.stat != nullptr && l3 == 0)
-    o.stat[((size_t)h * bt.N + bt.first_row(b) + row0) * bt.nq + c] = float2{m, inv};
+    o.stat[((size_t)h * bt.N + bt.first_row(b) + row0) * bt.nq + c] = column_stat(m, inv);
 }
 
 // What a form's launches share: its units, how they are dealt out, and where it writes.
@@ -923,18 +971,21 @@ __device__ __forceinline__ void mass_few(const float* __restrict__ score, const 
       const int page = bt.page(b, blk), slot = blk * kPage + lane;
       if (page < 0) continue;
       const size_t at = ((size_t)page * bt.H + h) * kPage + lane;
-      float x = slot < ctx ? mass_in[at] : 0.f, y = 0.f;
+      const float before = slot < ctx ? mass_in[at] : 0.f;
+      float y = 0.f;
       const float* s = score + (size_t)(blk - blk0) * part_cols * kPage + lane;
       int last = ctx, head = 0;  // the last token that column c sees
       for (int c = 0; c < ncol; ++c) {
         const float m = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(z.x), c));
         const float inv = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(z.y), c));
         // (the sum of a NaN row is NaN: 0 * inv would be NaN for the tokens behind it too)
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[c * kPage], c_log2, -m)) * inv;
+        const float x = s[c * kPage];
+        const float p = __builtin_amdgcn_exp2f(inv < 0.f ? far_exponent(x, c_log2, m)
+                                                         : fmaf(x, c_log2, -m)) * fabsf(inv);
         y += slot <= last ? p : 0.f;
         if (++head == bt.nq) head = 0, ++last;
       }
-      if (slot < min(ctx + rows, bt.cap())) mass_out[at] = x + y;
+      if (slot < min(ctx + rows, bt.cap())) mass_out[at] = before + y;
     }
     left -= blk1 - blk0;
     score += (size_t)(blk1 - blk0) * part_cols * kPage;
@@ -1061,14 +1112,19 @@ __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8
       const unsigned char* tile = smem + (t & (kMassStages - 1)) * STAGE;
       if (works) {
         float2 z = *reinterpret_cast<const float2*>(tile + QT + qi * 8);
+        const uint32_t qat = (uint32_t)((t & (kMassStages - 1)) * STAGE + qi * 256 +
+                                        (((2 * hl) ^ (qi & 15)) << 4));
+        // (formed before the products, so that nothing waits for it behind them)
+        uint64_t special = __builtin_amdgcn_ballot_w64(!(z.y >= 0.f));
+        asm volatile("" : "+s"(special));
         f32x16 x;
 #pragma unroll
         for (int v = 0; v < 16; ++v) x[v] = 0.f;
 #pragma unroll
         for (int st = 0; st < NST; ++st) {
-          const int ch = 4 * (st / 2) + 2 * hl + st % 2;
-          const bf16x8 qf =
-              *reinterpret_cast<const bf16x8*>(tile + qi * 256 + ((ch ^ (qi & 15)) << 4));
+          // chunk 4 (st / 2) + 2 hl + st % 2; in bits 4 to 7 of the address, for all stages
+          const bf16x8 qf = *reinterpret_cast<const bf16x8*>(
+              smem + (qat ^ (uint32_t)((4 * (st / 2) + st % 2) << 4)));
           x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[st], qf, x, 0, 0, 0);
         }
         // (the tile's first column sees the fewest)
@@ -1077,17 +1133,25 @@ __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8
 #pragma unroll
           for (int v = 0; v < 16; ++v)
             if (key0 + 8 * (v >> 2) + 4 * hl + (v & 3) >= seen) x[v] = -__builtin_inff();
+        }
+        float c_tile = c_log2;
+        if (special) {
           // a NaN row counts, as NaN, for the tokens that it sees alone (0 * NaN is NaN)
-          if (__builtin_amdgcn_ballot_w64(z.y != z.y) && z.y != z.y) {
+          if (z.y != z.y) {
+            const int seen = ctx + (t * kMassCols + qi) / bt.nq + 1;
 #pragma unroll
             for (int v = 0; v < 16; ++v)
               if (key0 + 8 * (v >> 2) + 4 * hl + (v & 3) < seen) acc[v] = z.y;
             z.y = 0.f;
           }
+#pragma unroll
+          for (int v = 0; v < 16; ++v) x[v] = far_exponent(x[v], c_log2, z.x);
+          c_tile = 1.f;
+          z = float2{0.f, fabsf(z.y)};
         }
 #pragma unroll
         for (int v = 0; v < 16; ++v)
-          acc[v] = fmaf(__builtin_amdgcn_exp2f(fmaf(x[v], c_log2, -z.x)), z.y, acc[v]);
+          acc[v] = fmaf(__builtin_amdgcn_exp2f(fmaf(x[v], c_tile, -z.x)), z.y, acc[v]);
       }
     }
 #pragma unroll

@@ -6,8 +6,8 @@ import torch
 
 from oracle import cache_oracle as co
 from paper_2605_06206_amd import foe
-from test_gpu_cache import (DEV, SCALE, THETA, batch, bf16, check_evict, host, ints, mass_bound,
-                            random_pool, say, to_dev, to_host)
+from test_gpu_cache import (DEV, SCALE, THETA, attention_bound, batch, bf16, check_evict, host,
+                            ints, mass_bound, random_pool, say, to_dev, to_host)
 
 pytestmark = pytest.mark.gpu
 
@@ -162,3 +162,81 @@ def test_mass_beside_rows_that_are_not_finite(nq, hd, seqs, bad, width, what):
     torch.cuda.synchronize()
     ref = check_mass(pool, table, ctx, rs, q, mass)
     assert np.array_equal(np.isnan(host(o)), np.isnan(ref[0]))
+
+
+# ---- scores near the ends of fp32 ----------------------------------------------------
+
+FAR = [(1, [(0, 1), (300, 1), (700, 1), (64, 1)]),          # few columns
+       (2, [(90, 8), (5, 3)]),
+       (2, [(0, 70), (300, 200)]),                          # chunks
+       (1, [(1500, 100), (200, 1), (0, 1), (129, 1), (0, 16)])]  # both
+
+
+@pytest.mark.parametrize("hd", [96, 128])
+@pytest.mark.parametrize("nq,seqs", FAR)
+@pytest.mark.parametrize("sign,level", [(1, 2), (-1, 2), (1, 32), (-1, 32), (-1, 60), (1, 100),
+                                        (-1, 100), (1, 112), (-1, 112)])
+def test_attention_scores_far_from_zero(hd, nq, seqs, sign, level):
+    """Scores of some 2^level of either sign: the tokens whose score is the largest share
+    the weight alike (their scores are equal and exact), the others, a quarter of it below,
+    get none."""
+    rng = np.random.default_rng([65, hd, nq, level])
+    H = 2
+    ctx, rs, table, pages = batch(rng, seqs)
+    pool = random_pool(rng, pages, H, hd)
+    # keys of ones and of 1.25, in units of 2^(level - 60): pages and tokens of both
+    big = (rng.random((pages, H, 64)) < 0.3) | (rng.random((pages, 1, 1)) < 0.3)
+    pool["k"][...] = co.encode(np.where(big, 1.25, 1.0))[..., None]
+    s = level - 60
+    pool["kv_scale"][..., 0] = 2.0 ** s
+    qx = np.full((H, rs[-1], nq, hd), sign * 2.0 ** 60)
+    dev, q = to_dev(pool), bf16(qx)
+    mass = torch.full_like(dev["mass"], -7.0)
+    say("far scores", hd, nq, seqs, sign, level)
+    o = foe.cache_attention(q, dev["k"], dev["v"], dev["kv_scale"], ints(table), ints(ctx),
+                            ints(rs), max(n for _, n in seqs), mass_in=dev["mass"],
+                            mass_out=mass)
+    torch.cuda.synchronize()
+    ref = check_mass(pool, table, ctx, rs, q, mass, far=level > 2)
+    err, lim = np.abs(host(o) - ref[0]), attention_bound(ref[0], ref[1])
+    assert (err <= lim).all(), (np.argwhere(err > lim)[:8], err.max())
+
+
+@pytest.mark.parametrize("rows", [1, 6, 90])
+@pytest.mark.parametrize("what", ["query", "overflow", "mixed"])
+def test_attention_scores_of_minus_infinity(rows, what):
+    """A row whose scores are all -inf (an infinite query, or products past fp32) is NaN, as
+    its softmax is; one that sees no token gives zeros."""
+    rng = np.random.default_rng([66, rows])
+    H, nq, hd = 1, 2, 96
+    seqs = [(300, rows), (0, 2), (700, 1)]
+    ctx, rs, table, pages = batch(rng, seqs)
+    pool = random_pool(rng, pages, H, hd)
+    pool["k"][...] = co.encode(1.0)
+    pool["kv_scale"][..., 0] = 2.0 ** 60
+    table[2] = -1
+    qx = rng.normal(size=(H, rs[-1], nq, hd))
+    bad = np.zeros((rs[-1], H, nq), dtype=bool)
+    bad[rows // 2, 0, 1] = bad[rs[1], 0, 0] = bad[rs[2], 0, 1] = True
+    qx[np.swapaxes(bad, 0, 1)] = {"query": -np.inf, "overflow": -2.0 ** 100,
+                                  "mixed": -2.0 ** 100}[what]
+    if what == "mixed":  # one page in reach: the others lose nothing by it
+        pool["kv_scale"][table[0, 0], :, 0] = 2.0 ** 10
+    dev, q = to_dev(pool), bf16(qx)
+    mass = torch.full_like(dev["mass"], -7.0)
+    say("scores of -inf", rows, what)
+    o = host(foe.cache_attention(q, dev["k"], dev["v"], dev["kv_scale"], ints(table), ints(ctx),
+                                 ints(rs), rows, mass_in=dev["mass"], mass_out=mass))
+    want = bad.copy()
+    want[rs[2]] = False                       # sees no token
+    if what == "mixed":
+        want[rows // 2] = False               # the scores of one page are finite
+        ref = co.attend(pool, host(q), table, ctx, rs)
+        assert (np.abs(o - ref[0]) <= attention_bound(ref[0], ref[1]))[rows // 2].all()
+    assert np.array_equal(np.isnan(o).all(-1), want)
+    assert np.isfinite(o[~want]).all() and (o[rs[2]] == 0).all()
+    # tokens that a NaN row sees, and no others, get a mass of NaN
+    m = host(mass)
+    seen = 0 if what == "mixed" else ctx[0] + rows // 2 + 1
+    for t in range(ctx[0] + rows):
+        assert np.isnan(m[table[0, t // 64], 0, t % 64]) == (t < seen), t
