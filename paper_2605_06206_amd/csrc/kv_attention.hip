@@ -106,24 +106,14 @@ struct Units {
 };
 
 // How a batch's units are dealt out: to `ranges` workgroups, at least `least` units each;
-// where `round` workgroups would have few enough (see kOneRound), to those.
+// where `round` workgroups would have few enough (see kOneRound in rules.hpp), to those.
 struct Deal {
   int ranges, least, round;
-  // units of a range (a batch's are below 2^39, of tables of up to 2^31 entries, 64 groups
-  // and 2^22 columns: a range of the launches here has fewer than 2^31)
-  __device__ __forceinline__ long long per(long long total) const;
+  // units of a range
+  __device__ __forceinline__ long long per(long long total) const {
+    return range_units(total, ranges, least, round);
+  }
 };
-// Few columns: 1024 ranges are two rounds of the workgroups that fit the chip at a time, the
-// second filling the gaps that the first one's ends leave; while a range has few pages, one
-// round saves more in starting.  us with 1024 and with 512 ranges, 8 groups of two heads,
-// sequences of 1000 to 4000 tokens: 8 of them 23.5 20.5, 16 33.5 27, 32 (20 pages a range
-// of 512) 46.5 42.5; 48 of 100 to 4096, hd 96 (25 pages) 61 65; 64 of 256 to 8192 (66) 113 121.
-constexpr int kOneRound = 22;
-__device__ __forceinline__ long long Deal::per(long long total) const {
-  long long n = (total + ranges - 1) / ranges;
-  if (round > 0 && total <= (long long)kOneRound * round) n = (total + round - 1) / round;
-  return n < least ? least : n;
-}
 
 // Total of the units, count(b) of sequence b, and the sequence that unit range * per falls
 // in (b, or -1 past the end) with its offset there.  Every thread of the workgroup calls
@@ -445,6 +435,8 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_few_kernel(
   locate<kAttThr>(
       bt.B, [&](int i) { return w.group(i) * bt.H; }, deal, blockIdx.x, w.prefix, total, b, off);
   if (b < 0) return;
+  // (at most 2^37 units, of tables of 2^31 entries and 64 groups, in a quarter of them or 1024
+  // ranges)
   const int per = (int)deal.per(total);
   long long unit = (long long)blockIdx.x * per;
   int left = (int)min((long long)per, total - unit);
@@ -506,8 +498,8 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
   locate<kTileThr>(
       bt.B, [&](int i) { return w.group(i) * bt.H; }, deal, range, w.prefix, total, b, off);
   if (b < 0) return;
-  const int per = (int)deal.per(total);
-  int left = (int)min((long long)per, total - (long long)range * per);
+  const long long per = deal.per(total);
+  long long left = min(per, total - range * per);
   int rows = w.rows(b), ctx = bt.context(b), nt = w.tiles(rows), h, t, blk0;
   {
     const long long each = w.group(b);
@@ -535,7 +527,7 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
 
   while (true) {
     const int np = w.pages(ctx, rows, t);
-    const int blk1 = min(np, blk0 + left);
+    const int blk1 = segment_end(np, blk0, left);
     const int row0 = t << w.log2r;
     const int ncol = (min(rows, (t + 1) << w.log2r) - row0) * bt.nq;
     const size_t qrow = ((size_t)h * bt.N + bt.first_row(b) + row0) * bt.nq;

@@ -1,5 +1,5 @@
 // Choices between kernels that depend on sizes alone: plain host code, tested
-// without a GPU.
+// without a GPU (what is constexpr serves the kernels too).
 #pragma once
 
 namespace foe {
@@ -126,6 +126,27 @@ inline bool stream_spreads(int C, int E, int R, int d, int F, int cus) {
   const long long gu = (long long)C * E * ((F + 63) / 64), dn = (long long)C * E * ((d + 127) / 128);
   const int parts = E > 16 ? (E + 7) / 8 : 2;
   return parts * (gu > dn ? gu : dn) <= cus;
+}
+
+// Attention over the cache: units (pages of tiles) of each of `ranges` workgroups, at
+// least `least`; `round` workgroups (0: none) where those would have few enough.
+// Few columns: 1024 ranges are two rounds of the workgroups that fit the chip at a time, the
+// second filling the gaps that the first one's ends leave; while a range has few pages, one
+// round saves more in starting.  us with 1024 and with 512 ranges, 8 groups of two heads,
+// sequences of 1000 to 4000 tokens: 8 of them 23.5 20.5, 16 33.5 27, 32 (20 pages a range
+// of 512) 46.5 42.5; 48 of 100 to 4096, hd 96 (25 pages) 61 65; 64 of 256 to 8192 (66) 113 121.
+constexpr int kOneRound = 22;
+constexpr long long range_units(long long total, int ranges, int least, int round) {
+  long long n = (total + ranges - 1) / ranges;
+  if (round > 0 && total <= (long long)kOneRound * round) n = (total + round - 1) / round;
+  return n < least ? least : n;
+}
+
+// Page before which a range with `left` units to go leaves a tile of np pages that it enters
+// at page blk0.  (A range may have more than 2^31 units: tables of 2^31 entries, 64 groups,
+// and a tile of 4 rows more for every sequence.)
+constexpr int segment_end(int np, int blk0, long long left) {
+  return left < np - blk0 ? blk0 + (int)left : np;
 }
 
 }  // namespace foe
