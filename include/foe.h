@@ -344,9 +344,10 @@ size_t foe_group_attention_workspace_bytes(int H, int S, int d, int nq, int hd);
  *                                   one (when it grows, the codes of all its other slots
  *                                   are rescaled); else slots without a new token are left
  *                                   as they were
- * A token whose key or value holds a non-finite element is stored as a key of
- * NaN codes and a zero value, and has no part in the scales: every query that
- * sees it gives NaN, and no other does.  Rows past the table's end give q_out
+ * A token whose rotated key or value holds an element that is not finite, or of
+ * 1.9375 * 2^127 or more in magnitude (its code would stand for 2^128), is stored
+ * as a key of NaN codes and a zero value, and has no part in the scales: every
+ * query that sees it gives NaN, and no other does.  Rows past the table's end give q_out
  * alone.  Needs no workspace.
  */
 int foe_cache_append(foe_dtype dt, int H, int B, int N, int nq, int hd, int n_pages,

@@ -20,6 +20,7 @@ __all__ = ["PAGE", "VALUES", "encode", "decode", "scale_for", "rotate", "append"
            "evict", "tokens"]
 
 PAGE = 64
+TOO_LARGE = 1.9375 * 2.0 ** 127  # halfway from 240 * 2^120 to 2^128, which fp32 does not hold
 
 
 def _values():
@@ -106,7 +107,7 @@ def append(pool, qkv, table, ctx, row_start, theta, scale, pos=None):
                 rot = rotate(x[:, :nq + 1], p0 + np.arange(n), theta, scale)
             q_out[h, r0:r1] = rot[:, :nq]
             k, v = rot[:, nq], x[:, nq + 1]
-            bad = ~(np.isfinite(k).all(-1) & np.isfinite(v).all(-1))
+            bad = ~((np.abs(k) < TOO_LARGE).all(-1) & (np.abs(v) < TOO_LARGE).all(-1))
             for blk in range(c // PAGE, (c + n - 1) // PAGE + 1):
                 p = _page(pool, table, b, blk)
                 if p < 0:

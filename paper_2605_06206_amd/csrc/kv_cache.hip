@@ -152,23 +152,23 @@ __global__ __launch_bounds__(kAppThr) void cache_append_kernel(
       *reinterpret_cast<bf16x4*>(dst + HD / 2) = bf16x4{y8[it][4], y8[it][5], y8[it][6], y8[it][7]};
     }
   }
-  bool bad[NIT];
+  bool bad[NIT];  // a row that no codes hold
   float2 amax{0.f, 0.f};
 #pragma unroll
   for (int it = 0; it < NIT; ++it) {
-    bool not_finite = false;
+    bool too_large = false;  // or NaN
     float2 m{0.f, 0.f};
     float y[8];
     rotate(it, y);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float k = fabsf(y[e]), w = fabsf((float)v[it][e]);
-      not_finite |= !(k < __builtin_inff()) || !(w < __builtin_inff());
+      too_large |= !(k < kTooLarge) || !(w < kTooLarge);
       m.x = fmaxf(m.x, k);
       m.y = fmaxf(m.y, w);
     }
-    // a row with a non-finite key or value counts for no scale
-    const uint64_t any_bad = __builtin_amdgcn_ballot_w64(not_finite && has(it));
+    // such a row counts for no scale
+    const uint64_t any_bad = __builtin_amdgcn_ballot_w64(too_large && has(it));
     bad[it] = ((any_bad >> (lane_id() & 48)) & 0xffffu) != 0;
     if (!bad[it] && has(it)) amax = float2{fmaxf(amax.x, m.x), fmaxf(amax.y, m.y)};
   }

@@ -7,7 +7,8 @@ namespace foe {
 
 constexpr int kPage = FOE_CACHE_PAGE;      // tokens per page
 constexpr int kSub = 16;                   // tokens per group of the value layout
-constexpr float kMinScale = 0x1p-100f;     // smallest block scale
+// from this magnitude on the code nearest to a value, 256 * 2^120, stands for 2^128
+constexpr float kTooLarge = 0x1.fp127f;
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 

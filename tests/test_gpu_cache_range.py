@@ -6,8 +6,8 @@ import torch
 
 from oracle import cache_oracle as co
 from paper_2605_06206_amd import foe
-from test_gpu_cache import (DEV, SCALE, THETA, attention_bound, batch, bf16, check_evict, host,
-                            ints, mass_bound, random_pool, say, to_dev, to_host)
+from test_gpu_cache import (DEV, SCALE, THETA, attention_bound, batch, bf16, check_append,
+                            check_evict, host, ints, mass_bound, random_pool, say, to_dev, to_host)
 
 pytestmark = pytest.mark.gpu
 
@@ -240,3 +240,43 @@ def test_attention_scores_of_minus_infinity(rows, what):
     seen = 0 if what == "mixed" else ctx[0] + rows // 2 + 1
     for t in range(ctx[0] + rows):
         assert np.isnan(m[table[0, t // 64], 0, t % 64]) == (t < seen), t
+
+
+# ---- magnitudes that no code holds -----------------------------------------------------
+
+@pytest.mark.parametrize("hd", [96, 128])
+def test_append_magnitudes_past_the_codes(hd):
+    """From 1.9375 * 2^127 on a value rounds to 2^128, past fp32, and a rotated key may
+    pass it by itself: such tokens are stored as non-finite ones, the largest below are
+    held."""
+    rng = np.random.default_rng([67, hd])
+    H, nq, most = 2, 1, 1.875 * 2.0 ** 127
+    ctx, rs, table, pages = batch(rng, [(5, 12), (0, 3)])
+    pool = random_pool(rng, pages, H, hd)
+    dev = to_dev(pool)
+    x = rng.normal(size=(H, rs[-1], nq + 2, hd))
+    x[0, 2, 2, 7] = 3.3895e38                   # a value: 1.9921875 * 2^127
+    x[1, 4, 2, 0] = -1.9375 * 2.0 ** 127        # the border itself
+    x[1, 1, 2, 1] = most                        # held
+    x[1, 12, 1, 3] = x[1, 12, 1, 3 + hd // 2] = most   # position 0: held as it is
+    x[1, 12:, 0, 3] = x[1, 12:, 0, 3 + hd // 2] = 0.0  # (a query that it leaves finite)
+    x[0, 8, 1, 0], x[0, 8, 1, hd // 2] = most, -most   # a key whose rotation passes it
+    qkv = bf16(x)
+    bad = np.zeros((rs[-1], H), dtype=bool)
+    bad[2, 0] = bad[4, 1] = bad[8, 0] = True
+    say("append magnitudes", hd)
+    q = foe.cache_append(qkv, dev["k"], dev["v"], dev["kv_scale"], ints(table), ints(ctx),
+                         ints(rs), THETA, SCALE)
+    torch.cuda.synchronize()
+    got = check_append(pool, dev, host(qkv), table, ctx, rs, q)
+    for b, h, i in ((0, 0, 2), (0, 1, 4), (0, 0, 8)):
+        t = ctx[b] + i
+        assert (got["k"][table[b, 0], h, t] == 0x7F).all()
+        assert (got["v"][table[b, 0], h, t // 16, :, t % 16] == 0).all()
+    # the queries that see such a token give NaN, the values of the others are finite
+    o = host(foe.cache_attention(q, dev["k"], dev["v"], dev["kv_scale"], ints(table), ints(ctx),
+                                 ints(rs), 12))
+    want = np.zeros((rs[-1], H), dtype=bool)
+    want[2:12, 0] = want[4:12, 1] = True
+    assert np.array_equal(np.isnan(o).all((2, 3)), want)
+    assert np.isfinite(o[~want]).all()
