@@ -282,7 +282,8 @@ int foe_cluster_block_noalloc(foe_dtype dt, int C, int T, int d, int E, int k, i
  * call's work still follows earlier work on `stream` and precedes later work
  * (also under HIP-graph capture, where the fork and join become edges).  bf16 only
  * and hd = 96 or 128 (else FOE_ERR_UNSUPPORTED); H*S*d and H*S*(nq+2)*hd must stay
- * below 2^30 elements.  S = 0 is a no-op.
+ * below 2^30 elements.  S = 0 is a no-op.  Scores have to stay below 2^29 in magnitude (a
+ * row of larger ones may give NaN; foe_cache_attention takes any).
  */
 int foe_group_attention(foe_dtype dt, int H, int S, int d, int nq, int hd, float theta,
                         float scale, const void* x, const void* w_qkv, const void* w_o,

@@ -28,7 +28,10 @@ namespace {
 constexpr int kHdMax = 128;
 constexpr int kQB = 64;   // rows per workgroup of the preparation pass
 constexpr int kKB = 64;   // keys per block of the V^T layout (its zero padding)
-// floor of the running maximum (log2 units): finite, and far below any score
+// floor of the running maximum (log2 units): finite, and far below any score that the
+// call takes (2^29 in magnitude: past 2^31 the rounding of a maximum, which is a factor of
+// its row's sums, leaves fp32.  A branch for those rows, as in the cache's attention, took
+// 1 to 4% here, 15.0 to 15.6 us for 1000 tokens of 8 groups of one head, hd 96)
 constexpr float kMFloor = -1.0e30f;
 
 // Attention inner step: fragment reads in flight ahead of the score and P V
