@@ -374,7 +374,10 @@ int foe_cache_append(foe_dtype dt, int H, int B, int N, int nq, int hd, int n_pa
  *                          sequences that have rows (0 <= t < ctx_len[b] + rows); other
  *                          entries are not written.  mass_out may be mass_in itself
  *   out       [N, H, nq, hd] dt out   the layout of w_o's columns in foe_group_attention
- *   ws, ws_bytes           workspace of foe_cache_attention_workspace_bytes()
+ *   ws, ws_bytes           workspace of foe_cache_attention_workspace_bytes().  With mass it grows
+ *                          with the table's width (scores of sequences of few columns are
+ *                          kept where all entries' take at most 1 GiB, else formed again):
+ *                          tables need be no wider than the longest sequence
  * bf16: products in bf16 MFMA with fp32 accumulation; softmax statistics, mass and
  * sums in fp32, the probabilities are rounded to bf16 for the product with v.
  * Scores may lie anywhere in fp32's range.  A row with a score of NaN or +inf, or
@@ -400,7 +403,9 @@ size_t foe_cache_attention_workspace_bytes(int H, int B, int N, int nq, int hd, 
  * earlier token; NaN ranks above infinity).  Groups choose for themselves.
  * The kept tokens, in their order, become tokens 0, 1, ... of the pages of
  * dst_table; shorter sequences are moved whole.  Each page's scales follow
- * from the values that it then holds, and mass moves with its token.
+ * from the values that it then holds, and mass moves with its token.  Tokens of
+ * absent pages rank last; one that is kept all the same is stored as a zero key
+ * and value without mass, which later queries see.
  *
  *   keep, recent           0 <= recent <= keep, 1 <= keep <= 2^30
  *   length    [B]          int32  tokens of each sequence
