@@ -358,6 +358,22 @@ int foe_cache_append(foe_dtype dt, int H, int B, int N, int nq, int hd, int n_pa
                      float* kv_scale, void* stream);
 
 /*
+ * foe_cache_append_tree - foe_cache_append for the rows of a tree of drafted tokens
+ * (or any rows whose order in the batch is not their order in the text): row r of
+ * sequence b stands depth[r] places behind its context, so it turns by pos[b] + depth[r].
+ * The rows still become tokens ctx_len[b], ctx_len[b] + 1, ... of the cache, in their
+ * order; foe_cache_attention_ex takes the same depths and each row's ancestors, and
+ * foe_cache_accept keeps the rows of one path.
+ *
+ *   depth     [N]  int32   cut to [0, 2^20]
+ */
+int foe_cache_append_tree(foe_dtype dt, int H, int B, int N, int nq, int hd, int n_pages,
+                          int max_blocks, float theta, float scale, const void* qkv,
+                          const int32_t* row_start, const int32_t* ctx_len, const int32_t* pos,
+                          const int32_t* depth, const int32_t* block_table, void* q_out,
+                          void* k_cache, void* v_cache, float* kv_scale, void* stream);
+
+/*
  * foe_cache_attention - causal attention of the new rows over the cache, after
  * foe_cache_append has stored them (same row_start and ctx_len):
  *   o[r,h,j] = sum_t p_t v_t,  p = softmax over t <= ctx_len[b] + i of q.k_t/sqrt(hd)
@@ -395,6 +411,66 @@ int foe_cache_attention(foe_dtype dt, int H, int B, int N, int nq, int hd, int n
  * for invalid sizes). */
 size_t foe_cache_attention_workspace_bytes(int H, int B, int N, int nq, int hd, int max_blocks,
                                            int max_rows, int with_mass);
+
+/*
+ * foe_cache_attention_ex - foe_cache_attention with other masks and scores (each of the
+ * arguments below may be left out: cap 0, pointers NULL).  With s = q.k_t/sqrt(hd),
+ *   o[r,h,j] = sum_t p_t v_t,  p = softmax over the tokens that row r sees of
+ *              cap * tanh(s / cap) - slope[h,j] * |place(r) - place(t)|
+ *
+ *   cap                    0 (the scores as they are) or in [2^-64, 2^64]
+ *   slope     [H, nq]      fp32   slope of the distance bias of each head
+ *   prefix    [B]  int32   the first prefix[b] tokens are seen by every row of sequence b (those
+ *                          that the cache holds), whatever their order
+ *   tree      [N, tree_words] int32   bit i % 32 of word i / 32 of a row: it sees row i of its
+ *                          sequence.  All rows see the context besides; a row sees itself
+ *                          if its own bit says so.  NULL: itself and the rows before it
+ *   tree_words             at least max_rows / 32, rounded up
+ *   depth     [N]  int32   row r stands at place ctx_len[b] + depth[r], cut as in
+ *                          foe_cache_append_tree.  NULL: row i of its sequence at ctx_len[b] + i.
+ *                          Tokens of the context stand where they are in the cache (also
+ *                          after an eviction).  Only the bias asks for places
+ *   ws, ws_bytes           workspace of foe_cache_attention_ex_workspace_bytes()
+ * A row that sees no token gives zeros.  A mass counts the tokens that the rows see.  Scores
+ * that pass fp32 are capped like any other; a NaN score gives a NaN row.  Capped and biased
+ * scores have to stay within 2^100.
+ */
+int foe_cache_attention_ex(foe_dtype dt, int H, int B, int N, int nq, int hd, int n_pages,
+                           int max_blocks, int max_rows, float cap, const float* slope,
+                           const int32_t* prefix, const int32_t* tree, int tree_words,
+                           const int32_t* depth, const void* q, const int32_t* row_start,
+                           const int32_t* ctx_len, const int32_t* block_table, const void* k_cache,
+                           const void* v_cache, const float* kv_scale, const float* mass_in,
+                           float* mass_out, void* out, void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace bytes of foe_cache_attention_ex, whatever its scores and masks (SIZE_MAX
+ * for invalid sizes). */
+size_t foe_cache_attention_ex_workspace_bytes(int H, int B, int N, int nq, int hd, int max_blocks,
+                                              int max_rows, int with_mass);
+
+/*
+ * foe_cache_accept - keeps the accepted rows of a tree: of the new rows that
+ * foe_cache_append_tree stored behind the context, those that path[b] names become tokens
+ * ctx_len[b], ctx_len[b] + 1, ... of sequence b, in place, and the others are dropped.
+ *
+ *   row_start [B+1], ctx_len [B]  int32   as in foe_cache_append_tree
+ *   path      [B, max_path] int32   rows of the sequence, ascending (every row of a tree stands
+ *                          behind its ancestors); the path ends at the first entry that does
+ *                          not ascend or is no row of the sequence (-1)
+ *   k_cache, v_cache, kv_scale   updated: in the pages from the context's end to the last
+ *                          kept token's, the scales follow from the values that the page then
+ *                          holds (the rule of foe_cache_evict: dropped rows no longer count), and
+ *                          codes are rescaled to them.  Slots past the last kept token are left as
+ *                          they were.  Nothing changes where no row is kept
+ *   mass      [n_pages, H, 64] fp32   moves with its token, or NULL
+ *   new_len   [B]   int32 out   ctx_len[b] and the length of the path (not ctx_len itself)
+ * A row whose page is absent is kept as a zero key and value without mass; rows that fall
+ * into an absent page are lost.  1 <= max_path <= 2^22.  Needs no workspace.
+ */
+int foe_cache_accept(int H, int B, int hd, int n_pages, int max_blocks, int max_path,
+                     const int32_t* row_start, const int32_t* ctx_len, const int32_t* path,
+                     const int32_t* block_table, void* k_cache, void* v_cache, float* kv_scale,
+                     float* mass, int32_t* new_len, void* stream);
 
 /*
  * foe_cache_evict - keeps the tokens that received the most attention.  Of a

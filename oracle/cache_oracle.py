@@ -1,4 +1,5 @@
-"""Plain CPU oracle of the 8-bit key/value cache: append, attention, eviction.
+"""Plain CPU oracle of the 8-bit key/value cache: append, attention, eviction, and of trees
+of drafted tokens: their places, masks and other scores, and keeping an accepted path.
 
 TEST INFRASTRUCTURE ONLY; it shares no code with the HIP library or its Python
 binding.  All arithmetic is fp64; e4m3 codes go through a table of their 256
@@ -17,9 +18,10 @@ import numpy as np
 from oracle.attention_oracle import apply_rope
 
 __all__ = ["PAGE", "VALUES", "encode", "decode", "scale_for", "rotate", "append", "attend",
-           "evict", "tokens"]
+           "accept", "evict", "tokens", "MAX_DEPTH"]
 
 PAGE = 64
+MAX_DEPTH = 1 << 20  # places of a new row behind the context
 TOO_LARGE = 1.9375 * 2.0 ** 127  # halfway from 240 * 2^120 to 2^128, which fp32 does not hold
 
 
@@ -87,8 +89,13 @@ def _page(pool, table, b, blk):
     return p if 0 <= p < len(pool["k"]) else -1
 
 
-def append(pool, qkv, table, ctx, row_start, theta, scale, pos=None):
-    """Stores the new rows in ``pool`` (in place); returns the rotated queries
+def _depth(depth, r0, r1):
+    return np.clip(np.asarray(depth[r0:r1], dtype=np.int64), 0, MAX_DEPTH)
+
+
+def append(pool, qkv, table, ctx, row_start, theta, scale, pos=None, depth=None):
+    """Stores the new rows in ``pool`` (in place), turned by their order or by their places
+    ``depth`` [N] behind the context; returns the rotated queries
     [H, N, nq, hd] and ``raw``, the new keys and values before quantisation
     {(page, h, t): (k, v)}."""
     H, N, n2, hd = qkv.shape
@@ -103,8 +110,9 @@ def append(pool, qkv, table, ctx, row_start, theta, scale, pos=None):
         p0 = c if pos is None else int(pos[b])
         for h in range(H):
             x = np.asarray(qkv[h, r0:r1], dtype=np.float64)
+            at = np.arange(n) if depth is None else _depth(depth, r0, r1)
             with np.errstate(invalid="ignore"):
-                rot = rotate(x[:, :nq + 1], p0 + np.arange(n), theta, scale)
+                rot = rotate(x[:, :nq + 1], p0 + at, theta, scale)
             q_out[h, r0:r1] = rot[:, :nq]
             k, v = rot[:, nq], x[:, nq + 1]
             bad = ~((np.abs(k) < TOO_LARGE).all(-1) & (np.abs(v) < TOO_LARGE).all(-1))
@@ -152,29 +160,51 @@ def tokens(pool, table, b, h, n):
     return k, v, there
 
 
-def attend(pool, q, table, ctx, row_start, rows=None, mass=False):
+def attend(pool, q, table, ctx, row_start, rows=None, mass=False, cap=0.0, slope=None,
+           prefix=None, tree=None, depth=None):
     """Attention of the rows of ``q`` [H, N, nq, hd] (all, or those in ``rows``):
     o [N, H, nq, hd], ``spread`` = sum_t p_t |v_t| of the same shape, the largest
     sum |q_i k_i| / sqrt(hd) of a visible score, and with ``mass`` what the tokens
-    receive, {(b, h): [tokens]}."""
+    receive, {(b, h): [tokens]}.  Scores may be capped, cap * tanh(s / cap), and biased by
+    -slope [H, nq] * |distance| (``depth`` [N]: the rows' places behind the context); a row
+    sees the first ``prefix`` [B] tokens besides, and with ``tree`` (row r sees new row i of
+    its sequence where tree[r][i]) not those before it."""
     H, N, nq, hd = q.shape
     q = np.asarray(q, dtype=np.float64)
     o = np.full((N, H, nq, hd), np.nan)
     spread, got, big = np.full_like(o, np.nan), {}, 0.0
-    cap = table.shape[1] * PAGE
+    top = table.shape[1] * PAGE
     for b in range(len(ctx)):
         r0, r1, c = int(row_start[b]), int(row_start[b + 1]), int(ctx[b])
         mine = [r for r in range(r0, r1) if rows is None or r in rows]
         if not mine:
             continue
-        n = min(c + r1 - r0, cap)
+        n = min(c + r1 - r0, top)
+        place = c + (np.arange(r1 - r0) if depth is None else _depth(depth, r0, r1))
+        spot = np.concatenate([np.arange(min(c, n)), place[:max(n - c, 0)]])
         for h in range(H):
             k, v, there = tokens(pool, table, b, h, n)
             total = np.zeros(n)
             for r in mine:
-                seen = there & (np.arange(n) < min(c + r - r0 + 1, cap))
+                if tree is None:
+                    seen = np.arange(n) < min(c + r - r0 + 1, top)
+                else:
+                    seen = np.arange(n) < c
+                    mask = np.zeros(max(n - c, 0), dtype=bool)
+                    m = np.asarray(tree[r], dtype=bool)[:len(mask)]
+                    mask[:len(m)] = m
+                    seen[c:] = mask
+                if prefix is not None:
+                    seen |= np.arange(n) < int(prefix[b])
+                seen &= there
                 kk, vv = k[seen], v[seen]
-                s = q[h, r] @ kk.T / np.sqrt(hd)
+                with np.errstate(invalid="ignore", over="ignore"):
+                    s = q[h, r] @ kk.T / np.sqrt(hd)
+                    if cap:
+                        s = cap * np.tanh(s / cap)
+                if slope is not None:
+                    far = np.abs(place[r - r0] - spot[seen]).astype(np.float64)
+                    s = s - np.asarray(slope, dtype=np.float64)[h][:, None] * far
                 if s.shape[1] == 0:
                     o[r, h] = spread[r, h] = 0.0
                     continue
@@ -187,6 +217,52 @@ def attend(pool, q, table, ctx, row_start, rows=None, mass=False):
                 total[seen] += p.sum(0)
             got[(b, h)] = total
     return (o, spread, big, got) if mass else (o, spread, big)
+
+
+def accept(pool, table, ctx, row_start, path):
+    """Keeps the rows of each sequence's path, moved together behind its context (in
+    place); new_len.  ``pool["mass"]`` may be None."""
+    H, hd = pool["k"].shape[1], pool["k"].shape[-1]
+    new_len = np.array(ctx, dtype=np.int32)
+    top = table.shape[1] * PAGE
+    for b in range(len(ctx)):
+        c = int(ctx[b])
+        n = min(int(row_start[b + 1]) - int(row_start[b]), top - c)
+        kept, last = [], -1
+        for r in path[b]:
+            if not last < r < n:
+                break
+            kept.append(int(r))
+            last = int(r)
+        new_len[b] = c + len(kept)
+        if not kept:
+            continue
+        lo = c // PAGE * PAGE
+        ids = np.concatenate([np.arange(lo, c), c + np.array(kept)]).astype(int)
+        for h in range(H):
+            k, v, there = tokens(pool, table, b, h, c + n)
+            mass = [0.0 if pool["mass"] is None or not there[t] else
+                    pool["mass"][_page(pool, table, b, t // PAGE), h, t % PAGE] for t in ids]
+            for i in range(0, len(ids), PAGE):
+                p = _page(pool, table, b, (lo + i) // PAGE)
+                if p < 0:
+                    continue
+                t = ids[i:i + PAGE]
+                sk = float(scale_for(np.nanmax(np.abs(k[t]), initial=0.0)))
+                sv = float(scale_for(np.nanmax(np.abs(v[t]), initial=0.0)))
+                # (a page's codes: a NaN code keeps its sign, as everywhere in the cache)
+                old = pool["k"][p, h].copy()
+                codes = encode(k[t] / sk)
+                for j, x in enumerate(t):
+                    src = _page(pool, table, b, x // PAGE)
+                    if np.isnan(k[x]).all():
+                        codes[j] = old[x % PAGE] if src == p else pool["k"][src, h, x % PAGE]
+                pool["kv_scale"][p, h] = sk, sv
+                pool["k"][p, h, :len(t)] = codes
+                _v_put(pool["v"][p, h], encode(v[t] / sv), 0)
+                if pool["mass"] is not None:
+                    pool["mass"][p, h, :len(t)] = mass[i:i + PAGE]
+    return new_len
 
 
 def evict(pool, table, length, keep, recent, dst):

@@ -609,6 +609,106 @@ int entry(F body) {
     return FOE_ERR_HIP;
   }
 }
+
+int cache_append(const char* name, foe_dtype dt, int H, int B, int N, int nq, int hd, int n_pages,
+                 int max_blocks, float theta, float scale, const void* qkv,
+                 const int32_t* row_start, const int32_t* ctx_len, const int32_t* pos,
+                 const int32_t* depth, const int32_t* block_table, void* q_out, void* k_cache,
+                 void* v_cache, float* kv_scale, void* stream) {
+  const std::string at = std::string(name) + ": ";
+  Check c;
+  check_dtype(c, dt);
+  check_cache(c, H, B, n_pages, max_blocks);
+  check_rows(c, N, nq);
+  c.need(theta > 0.f && scale > 0.f, "theta and scale must be > 0");
+  const bool any = N > 0 && B > 0;
+  c.tensor(qkv, any, "qkv");
+  c.small(row_start, any, "row_start");
+  c.small(ctx_len, any, "ctx_len");
+  c.small(pos, false, "pos");
+  c.small(depth, false, "depth");
+  c.small(block_table, any, "block_table");
+  c.tensor(q_out, any, "q_out");
+  c.tensor(k_cache, any, "k_cache");
+  c.tensor(v_cache, any, "v_cache");
+  c.tensor(kv_scale, any, "kv_scale");
+  c.need(!any || qkv != q_out, "q_out must not be qkv");
+  if (!c.err.empty()) return fail(FOE_ERR_INVALID, at + c.err);
+  if (dt != FOE_BF16 || !cache_hd(hd))
+    return fail(FOE_ERR_UNSUPPORTED, at + "bf16 with hd = 96 or 128 only");
+  if (!any) return FOE_OK;
+  const CacheArgs a{H, hd, B, n_pages, max_blocks, static_cast<uint8_t*>(k_cache),
+                    static_cast<uint8_t*>(v_cache), kv_scale, block_table, ctx_len};
+  hipError_t e = launch_cache_append(a, nq, N, qkv, q_out, row_start, pos, depth, theta, scale,
+                                     reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, name);
+  return FOE_OK;
+}
+
+size_t attention_workspace(int H, int B, int N, int nq, int hd, int max_blocks, int max_rows,
+                           int with_mass, bool shaped) {
+  try {
+    Check c;
+    check_cache(c, H, B, 1, max_blocks);
+    check_rows(c, N, nq);
+    c.need(cache_hd(hd), "hd must be 96 or 128");
+    c.need(max_rows >= 1, "max_rows must be >= 1");
+    if (!c.err.empty()) return (g_err = c.err, SIZE_MAX);
+    if (N == 0 || B == 0) return 0;
+    if (max_rows > N) max_rows = N;
+    return cache_attention_scratch_bytes(H, B, N, nq, hd, max_blocks, max_rows, with_mass != 0,
+                                         shaped);
+  } catch (...) {
+    return SIZE_MAX;
+  }
+}
+
+// scores: what foe_cache_attention_ex adds, or null
+int cache_attention(const char* name, foe_dtype dt, int H, int B, int N, int nq, int hd,
+                    int n_pages, int max_blocks, int max_rows, const CacheScores* scores,
+                    const void* q, const int32_t* row_start, const int32_t* ctx_len,
+                    const int32_t* block_table, const void* k_cache, const void* v_cache,
+                    const float* kv_scale, const float* mass_in, float* mass_out, void* out,
+                    void* ws, size_t ws_bytes, void* stream) {
+  const std::string at = std::string(name) + ": ";
+  Check c;
+  check_dtype(c, dt);
+  check_cache(c, H, B, n_pages, max_blocks);
+  check_rows(c, N, nq);
+  const bool any = N > 0 && B > 0;
+  c.need(max_rows >= 1, "max_rows must be >= 1");
+  if (max_rows > N) max_rows = N;
+  c.tensor(q, any, "q");
+  c.small(row_start, any, "row_start");
+  c.small(ctx_len, any, "ctx_len");
+  c.small(block_table, any, "block_table");
+  c.tensor(k_cache, any, "k_cache");
+  c.tensor(v_cache, any, "v_cache");
+  c.tensor(kv_scale, any, "kv_scale");
+  c.tensor(mass_in, false, "mass_in");
+  c.tensor(mass_out, false, "mass_out");
+  c.need((mass_in == nullptr) == (mass_out == nullptr), "mass_in and mass_out go together");
+  c.tensor(out, any, "out");
+  if (!c.err.empty()) return fail(FOE_ERR_INVALID, at + c.err);
+  if (dt != FOE_BF16 || !cache_hd(hd))
+    return fail(FOE_ERR_UNSUPPORTED, at + "bf16 with hd = 96 or 128 only");
+  if (!any) return FOE_OK;
+  const size_t need = cache_attention_scratch_bytes(H, B, N, nq, hd, max_blocks, max_rows,
+                                                    mass_out != nullptr, scores != nullptr);
+  if (need > 0 && (ws == nullptr || !aligned16(ws)))
+    return fail(FOE_ERR_INVALID, at + "ws is NULL or not 16-byte aligned");
+  if (ws_bytes < need)
+    return fail(FOE_ERR_WORKSPACE, at + "workspace needs " + std::to_string(need) +
+                                       " bytes, got " + std::to_string(ws_bytes));
+  const CacheArgs a{H, hd, B, n_pages, max_blocks,
+                    static_cast<uint8_t*>(const_cast<void*>(k_cache)),
+                    static_cast<uint8_t*>(const_cast<void*>(v_cache)),
+                    const_cast<float*>(kv_scale), block_table, ctx_len};
+  hipError_t e = launch_cache_attention(a, nq, N, max_rows, q, row_start, mass_in, mass_out, out,
+                                        ws, reinterpret_cast<hipStream_t>(stream), scores);
+  if (e != hipSuccess) return hip_fail(e, name);
+  return FOE_OK;
+}
 }  // namespace
 }  // namespace foe
 
@@ -619,51 +719,35 @@ int foe_cache_append(foe_dtype dt, int H, int B, int N, int nq, int hd, int n_pa
                      const int32_t* row_start, const int32_t* ctx_len, const int32_t* pos,
                      const int32_t* block_table, void* q_out, void* k_cache, void* v_cache,
                      float* kv_scale, void* stream) {
+  return entry([&] {
+    return cache_append("foe_cache_append", dt, H, B, N, nq, hd, n_pages, max_blocks, theta, scale,
+                        qkv, row_start, ctx_len, pos, nullptr, block_table, q_out, k_cache, v_cache,
+                        kv_scale, stream);
+  });
+}
+
+int foe_cache_append_tree(foe_dtype dt, int H, int B, int N, int nq, int hd, int n_pages,
+                          int max_blocks, float theta, float scale, const void* qkv,
+                          const int32_t* row_start, const int32_t* ctx_len, const int32_t* pos,
+                          const int32_t* depth, const int32_t* block_table, void* q_out,
+                          void* k_cache, void* v_cache, float* kv_scale, void* stream) {
   return entry([&]() -> int {
-    Check c;
-    check_dtype(c, dt);
-    check_cache(c, H, B, n_pages, max_blocks);
-    check_rows(c, N, nq);
-    c.need(theta > 0.f && scale > 0.f, "theta and scale must be > 0");
-    const bool any = N > 0 && B > 0;
-    c.tensor(qkv, any, "qkv");
-    c.small(row_start, any, "row_start");
-    c.small(ctx_len, any, "ctx_len");
-    c.small(pos, false, "pos");
-    c.small(block_table, any, "block_table");
-    c.tensor(q_out, any, "q_out");
-    c.tensor(k_cache, any, "k_cache");
-    c.tensor(v_cache, any, "v_cache");
-    c.tensor(kv_scale, any, "kv_scale");
-    c.need(!any || qkv != q_out, "q_out must not be qkv");
-    if (!c.err.empty()) return fail(FOE_ERR_INVALID, "foe_cache_append: " + c.err);
-    if (dt != FOE_BF16 || !cache_hd(hd))
-      return fail(FOE_ERR_UNSUPPORTED, "foe_cache_append: bf16 with hd = 96 or 128 only");
-    if (!any) return FOE_OK;
-    const CacheArgs a{H, hd, B, n_pages, max_blocks, static_cast<uint8_t*>(k_cache),
-                      static_cast<uint8_t*>(v_cache), kv_scale, block_table, ctx_len};
-    hipError_t e = launch_cache_append(a, nq, N, qkv, q_out, row_start, pos, theta, scale,
-                                       reinterpret_cast<hipStream_t>(stream));
-    if (e != hipSuccess) return hip_fail(e, "foe_cache_append");
-    return FOE_OK;
+    if (N > 0 && B > 0 && depth == nullptr)
+      return fail(FOE_ERR_INVALID, "foe_cache_append_tree: depth is NULL");
+    return cache_append("foe_cache_append_tree", dt, H, B, N, nq, hd, n_pages, max_blocks, theta,
+                        scale, qkv, row_start, ctx_len, pos, depth, block_table, q_out, k_cache,
+                        v_cache, kv_scale, stream);
   });
 }
 
 size_t foe_cache_attention_workspace_bytes(int H, int B, int N, int nq, int hd, int max_blocks,
                                            int max_rows, int with_mass) {
-  try {
-    Check c;
-    check_cache(c, H, B, 1, max_blocks);
-    check_rows(c, N, nq);
-    c.need(cache_hd(hd), "hd must be 96 or 128");
-    c.need(max_rows >= 1, "max_rows must be >= 1");
-    if (!c.err.empty()) return (g_err = c.err, SIZE_MAX);
-    if (N == 0 || B == 0) return 0;
-    if (max_rows > N) max_rows = N;
-    return cache_attention_scratch_bytes(H, B, N, nq, hd, max_blocks, max_rows, with_mass != 0);
-  } catch (...) {
-    return SIZE_MAX;
-  }
+  return attention_workspace(H, B, N, nq, hd, max_blocks, max_rows, with_mass, false);
+}
+
+size_t foe_cache_attention_ex_workspace_bytes(int H, int B, int N, int nq, int hd, int max_blocks,
+                                              int max_rows, int with_mass) {
+  return attention_workspace(H, B, N, nq, hd, max_blocks, max_rows, with_mass, true);
 }
 
 int foe_cache_attention(foe_dtype dt, int H, int B, int N, int nq, int hd, int n_pages,
@@ -671,44 +755,66 @@ int foe_cache_attention(foe_dtype dt, int H, int B, int N, int nq, int hd, int n
                         const int32_t* ctx_len, const int32_t* block_table, const void* k_cache,
                         const void* v_cache, const float* kv_scale, const float* mass_in,
                         float* mass_out, void* out, void* ws, size_t ws_bytes, void* stream) {
+  return entry([&] {
+    return cache_attention("foe_cache_attention", dt, H, B, N, nq, hd, n_pages, max_blocks,
+                           max_rows, nullptr, q, row_start, ctx_len, block_table, k_cache, v_cache,
+                           kv_scale, mass_in, mass_out, out, ws, ws_bytes, stream);
+  });
+}
+
+int foe_cache_attention_ex(foe_dtype dt, int H, int B, int N, int nq, int hd, int n_pages,
+                           int max_blocks, int max_rows, float cap, const float* slope,
+                           const int32_t* prefix, const int32_t* tree, int tree_words,
+                           const int32_t* depth, const void* q, const int32_t* row_start,
+                           const int32_t* ctx_len, const int32_t* block_table, const void* k_cache,
+                           const void* v_cache, const float* kv_scale, const float* mass_in,
+                           float* mass_out, void* out, void* ws, size_t ws_bytes, void* stream) {
   return entry([&]() -> int {
     Check c;
-    check_dtype(c, dt);
+    c.need(cap == 0.f || (cap >= 0x1p-64f && cap <= 0x1p64f), "cap must be 0 or in [2^-64, 2^64]");
+    c.small(slope, false, "slope");
+    c.small(prefix, false, "prefix");
+    c.small(tree, false, "tree");
+    c.small(depth, false, "depth");
+    c.need(tree == nullptr || tree_words >= 1, "tree_words must be >= 1");
+    c.need(tree == nullptr || ((max_rows < N ? max_rows : N) + 31LL) / 32 <= tree_words,
+           "tree_words must be at least max_rows / 32");
+    if (!c.err.empty()) return fail(FOE_ERR_INVALID, "foe_cache_attention_ex: " + c.err);
+    const CacheScores scores{cap, slope, prefix, reinterpret_cast<const uint32_t*>(tree),
+                             tree_words, depth};
+    return cache_attention("foe_cache_attention_ex", dt, H, B, N, nq, hd, n_pages, max_blocks,
+                           max_rows, &scores, q, row_start, ctx_len, block_table, k_cache, v_cache,
+                           kv_scale, mass_in, mass_out, out, ws, ws_bytes, stream);
+  });
+}
+
+int foe_cache_accept(int H, int B, int hd, int n_pages, int max_blocks, int max_path,
+                     const int32_t* row_start, const int32_t* ctx_len, const int32_t* path,
+                     const int32_t* block_table, void* k_cache, void* v_cache, float* kv_scale,
+                     float* mass, int32_t* new_len, void* stream) {
+  return entry([&]() -> int {
+    Check c;
     check_cache(c, H, B, n_pages, max_blocks);
-    check_rows(c, N, nq);
-    const bool any = N > 0 && B > 0;
-    c.need(max_rows >= 1, "max_rows must be >= 1");
-    if (max_rows > N) max_rows = N;
-    c.tensor(q, any, "q");
+    const bool any = B > 0;
+    c.need(max_path >= 1 && max_path <= (1 << 22), "max_path must be in [1, 2^22]");
     c.small(row_start, any, "row_start");
     c.small(ctx_len, any, "ctx_len");
+    c.small(path, any, "path");
     c.small(block_table, any, "block_table");
     c.tensor(k_cache, any, "k_cache");
     c.tensor(v_cache, any, "v_cache");
     c.tensor(kv_scale, any, "kv_scale");
-    c.tensor(mass_in, false, "mass_in");
-    c.tensor(mass_out, false, "mass_out");
-    c.need((mass_in == nullptr) == (mass_out == nullptr), "mass_in and mass_out go together");
-    c.tensor(out, any, "out");
-    if (!c.err.empty()) return fail(FOE_ERR_INVALID, "foe_cache_attention: " + c.err);
-    if (dt != FOE_BF16 || !cache_hd(hd))
-      return fail(FOE_ERR_UNSUPPORTED, "foe_cache_attention: bf16 with hd = 96 or 128 only");
+    c.tensor(mass, false, "mass");
+    c.small(new_len, any, "new_len");
+    c.need(!any || new_len != ctx_len, "new_len must not be ctx_len");
+    if (!c.err.empty()) return fail(FOE_ERR_INVALID, "foe_cache_accept: " + c.err);
+    if (!cache_hd(hd)) return fail(FOE_ERR_UNSUPPORTED, "foe_cache_accept: hd = 96 or 128 only");
     if (!any) return FOE_OK;
-    const size_t need = cache_attention_scratch_bytes(H, B, N, nq, hd, max_blocks, max_rows,
-                                                      mass_out != nullptr);
-    if (need > 0 && (ws == nullptr || !aligned16(ws)))
-      return fail(FOE_ERR_INVALID, "foe_cache_attention: ws is NULL or not 16-byte aligned");
-    if (ws_bytes < need)
-      return fail(FOE_ERR_WORKSPACE, "foe_cache_attention: workspace needs " +
-                                         std::to_string(need) + " bytes, got " +
-                                         std::to_string(ws_bytes));
-    const CacheArgs a{H, hd, B, n_pages, max_blocks,
-                      static_cast<uint8_t*>(const_cast<void*>(k_cache)),
-                      static_cast<uint8_t*>(const_cast<void*>(v_cache)),
-                      const_cast<float*>(kv_scale), block_table, ctx_len};
-    hipError_t e = launch_cache_attention(a, nq, N, max_rows, q, row_start, mass_in, mass_out, out,
-                                          ws, reinterpret_cast<hipStream_t>(stream));
-    if (e != hipSuccess) return hip_fail(e, "foe_cache_attention");
+    const CacheArgs a{H, hd, B, n_pages, max_blocks, static_cast<uint8_t*>(k_cache),
+                      static_cast<uint8_t*>(v_cache), kv_scale, block_table, ctx_len};
+    hipError_t e = launch_cache_accept(a, row_start, path, max_path, mass, new_len,
+                                       reinterpret_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "foe_cache_accept");
     return FOE_OK;
   });
 }

@@ -230,13 +230,28 @@ struct CacheArgs {
   const int32_t *block_table, *length;
 };
 hipError_t launch_cache_append(const CacheArgs& a, int nq, int N, const void* qkv, void* q,
-                               const int32_t* row_start, const int32_t* pos, float theta,
-                               float scale, hipStream_t s);
+                               const int32_t* row_start, const int32_t* pos, const int32_t* depth,
+                               float theta, float scale, hipStream_t s);
+hipError_t launch_cache_accept(const CacheArgs& a, const int32_t* row_start, const int32_t* path,
+                               int max_path, float* mass, int32_t* new_len, hipStream_t s);
+constexpr int kMaxDepth = 1 << 20;  // a new row's places behind its sequence's context
+// What foe_cache_attention_ex's scores and masks have beyond foe_cache_attention's (device
+// pointers, each may be null; cap 0: none).
+struct CacheScores {
+  float cap;
+  const float* slope;      // [H][nq]
+  const int32_t* prefix;   // [B]
+  const uint32_t* tree;    // [N][words]
+  int words;
+  const int32_t* depth;    // [N]
+  __device__ __forceinline__ int depth_of(int row) const { return min(max(depth[row], 0), kMaxDepth); }
+};
 size_t cache_attention_scratch_bytes(int H, int B, int N, int nq, int hd, int max_blocks,
-                                     int max_rows, bool mass);
+                                     int max_rows, bool mass, bool shaped);
 hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_rows, const void* q,
                                   const int32_t* row_start, const float* mass_in, float* mass_out,
-                                  void* out, void* scratch, hipStream_t s);
+                                  void* out, void* scratch, hipStream_t s,
+                                  const CacheScores* scores);
 hipError_t launch_cache_evict(const CacheArgs& a, float* mass, int keep, int recent,
                               const int32_t* dst_table, int dst_blocks, int32_t* kept,
                               int32_t* new_len, void* scratch, hipStream_t s);

@@ -30,6 +30,7 @@ namespace {
 constexpr int kAttThr = 256;          // few columns: four waves, each taking every fourth page
 constexpr int kAttWaves = kAttThr / kWave;
 constexpr int kFewCols = 16;
+constexpr int kShapedCols = 128;      // up to which that form takes shaped calls
 constexpr int kTileThr = 512;         // many columns: eight waves of 32 columns
 constexpr int kTileCols = 256;
 constexpr int kCus = 256;             // compute units of the card; a multiple of the XCDs
@@ -60,7 +61,167 @@ __device__ __forceinline__ float2 column_stat(float m, float inv) {
   return float2{m, far_max(m) ? -inv : inv};
 }
 
+// ---- scores and masks of other shapes ----------------------------------------------
+// foe_cache_attention_ex: a score may be capped, cap * tanh(s / cap), and get a bias of
+// -slope * |distance|; a row may see the new rows that its bits name, and the first tokens
+// whatever its own place.  A lane holds scores of one column at several keys; the scores are
+// transformed where the matrix instructions leave them, before the maximum, so that what
+// follows is the same as without.  With a cap or a bias they are then in units of log2 e (and
+// c_log2 is 1), else as they were.
+struct Shape {
+  CacheScores a;
+  float scale;            // log2 e / sqrt(hd)
+  float cap, x_of;        // cap * log2 e; 1 / (cap * sqrt(hd))
+  float bound, poly[5];   // |s| <= bound: the capped score is s * (poly in s^2)
+
+  __device__ __forceinline__ bool transforms() const { return cap != 0.f || a.slope != nullptr; }
+};
+
+struct NoShape {};  // causal, scores as they are
+template <typename S>
+constexpr bool is_shaped = std::is_same<S, Shape>::value;
+// what the mass needs of a column (see put_stat)
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+template <typename S>
+using Stat = typename std::conditional<is_shaped<S>, f32x4, f32x2>::type;
+
+// Tokens from the first on that row i and those behind it see, whose distances are place - key
+// and not negative.
+__device__ __forceinline__ int plain_tokens(const Shape& sh, int ctx, int i) {
+  return sh.a.tree != nullptr || sh.a.depth != nullptr ? ctx : ctx + i + 1;
+}
+__device__ __forceinline__ int plain_tokens(const NoShape&, int ctx, int i) {
+  return ctx + i + 1;
+}
+
+// tanh(x) / x for |x| <= kTanhBound as a polynomial in x^2: fitted here to the smallest largest
+// relative error, 7.3e-8.
+constexpr float kTanhBound = 0.6f;
+constexpr double kTanhPoly[5] = {0.99999993, -0.33332308, 0.13310172, -0.052101476, 0.015475425};
+
+// What a lane keeps of its column.
+struct Column {
+  float slope;  // times log2 e
+  int place;    // in its sequence
+  int row;      // of the sequence's new rows
+};
+
+// Column c (of ncol; row c / nq, head c % nq) of sequence b, group h.
+__device__ __forceinline__ Column column_of(const Shape& sh, const CacheBatch& bt, int b, int h,
+                                            int ctx, int c, int ncol) {
+  Column k{0.f, ctx, 0};
+  if (c >= ncol) return k;
+  k.row = c / bt.nq;
+  k.place = ctx + (sh.a.depth != nullptr ? sh.a.depth_of(bt.first_row(b) + k.row) : k.row);
+  if (sh.a.slope != nullptr)
+    k.slope = sh.a.slope[h * bt.nq + c - k.row * bt.nq] * 1.4426950408889634f;
+  return k;
+}
+
+// The keys of page blk that the column sees, a bit each.
+__device__ __forceinline__ uint64_t keys_seen(const Shape& sh, const CacheBatch& bt, int b,
+                                              int row, int ctx, int len, int blk) {
+  auto first = [](int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; };
+  const int key0 = blk * kPage;
+  int seen = min(sh.a.tree != nullptr ? ctx : ctx + row + 1, len);
+  if (sh.a.prefix != nullptr) seen = max(seen, min(sh.a.prefix[b], len));
+  uint64_t m = first(seen - key0);
+  if (sh.a.tree != nullptr && key0 + kPage > ctx && key0 < len) {
+    const int i0 = key0 - ctx;  // the new row at the page's first key
+    const uint32_t* bits = sh.a.tree + (size_t)(bt.first_row(b) + row) * sh.a.words;
+    auto word = [&](int w) -> uint64_t { return w < sh.a.words ? bits[w] : 0u; };
+    uint64_t x;
+    if (i0 < 0) {
+      x = (word(0) | word(1) << 32) << -i0;
+    } else {
+      const int w = i0 >> 5, k = i0 & 31;
+      x = (word(w) | word(w + 1) << 32) >> k;
+      if (k != 0) x |= word(w + 2) << (64 - k);
+    }
+    m |= x & first(len - key0);
+  }
+  return m;
+}
+
+// NE scores of a lane (get, set) at keys key0 + off(i), in place.  `all`: the column sees them
+// all and none is a new row; else those outside `sees` (bit of key key0 + off(i): off(i)) are
+// taken out.
+template <int NE, typename Get, typename Set, typename Off>
+__device__ __forceinline__ void shape_scores(const Shape& sh, const CacheBatch& bt, int b, int ctx,
+                                             int rows, const Column& c, int key0, bool all,
+                                             uint64_t sees, Get get, Set set, Off off) {
+  if (sh.cap != 0.f) {
+    float big = 0.f;
+#pragma unroll
+    for (int i = 0; i < NE; ++i) big = fmaxf(big, fabsf(get(i)));
+    // Scores are mostly well below the cap, where the polynomial is 6 operations; the
+    // exponential, which loses the small ones' last digits besides, is taken where a lane
+    // needs it.
+    if (__builtin_amdgcn_ballot_w64(big > sh.bound) == 0) {
+#pragma unroll
+      for (int i = 0; i < NE; ++i) {
+        const float s = get(i), u = s * s;
+        float y = fmaf(sh.poly[4], u, sh.poly[3]);
+        y = fmaf(y, u, sh.poly[2]);
+        y = fmaf(y, u, sh.poly[1]);
+        y = fmaf(y, u, sh.poly[0]);
+        set(i, s * y);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NE; ++i) {
+        if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+        const float x = get(i) * sh.x_of, u = x * x;
+        float y = (float)kTanhPoly[4];
+#pragma unroll
+        for (int k = 3; k >= 0; --k) y = fmaf(y, u, (float)kTanhPoly[k]);
+        const float e = __builtin_amdgcn_exp2f(fabsf(x) * 2.885390081777927f);
+        const float far = copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f), x);
+        set(i, sh.cap * (fabsf(x) > kTanhBound ? far : x * y));
+      }
+    }
+  } else if (sh.a.slope != nullptr) {
+#pragma unroll
+    for (int i = 0; i < NE; ++i) set(i, get(i) * sh.scale);
+  }
+  if (sh.a.slope != nullptr) {
+    if (!all && sh.a.depth != nullptr) {
+      const int row0 = bt.first_row(b);
+#pragma unroll
+      for (int i = 0; i < NE; ++i) {
+        if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);  // (few loads' addresses at a time)
+        const int key = key0 + off(i), r = key - ctx;
+        const int at = r >= 0 && r < rows ? ctx + sh.a.depth_of(row0 + r) : key;
+        set(i, fmaf(-c.slope, fabsf((float)(c.place - at)), get(i)));
+      }
+    } else {
+      const float d = (float)(c.place - key0);
+#pragma unroll
+      for (int i = 0; i < NE; ++i) set(i, fmaf(-c.slope, fabsf(d - (float)off(i)), get(i)));
+    }
+  }
+  if (!all) {
+    const uint32_t lo = (uint32_t)sees, hi = (uint32_t)(sees >> 32);
+#pragma unroll
+    for (int i = 0; i < NE; ++i) {
+      if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+      if (((off(i) < 32 ? lo : hi) >> (off(i) & 31) & 1) == 0) set(i, -__builtin_inff());
+    }
+  }
+}
+
 // ---- dealing out the work -------------------------------------------------------
+
+// What a call's tiles reach beyond their own rows: the prefix, and with a tree every new row.
+struct Reach {
+  const int32_t* prefix;
+  bool tree;
+  __device__ __forceinline__ int pages(const CacheBatch& bt, int b, int ctx, int n) const {
+    if (tree) return (ctx + n + kPage - 1) / kPage;
+    if (prefix == nullptr) return 0;
+    return (min(max(prefix[b], 0), min(ctx + n, bt.cap())) + kPage - 1) / kPage;
+  }
+};
 
 // The units of a batch in a form, numbered by sequence, group, tile and page.  A tile of
 // many columns has 2^log2r rows, tile t reaches page ceil((ctx + last row + 1) / 64), and
@@ -71,6 +232,7 @@ struct Units {
   int max_rows;
   int log2r;   // (many)
   int lo, hi;  // columns that a sequence of this form has: lo < columns <= hi
+  Reach reach;
   long long* prefix;  // [B + 1]: units before each sequence, and in all (for the launches after)
 
   // rows of sequence b in this form
@@ -79,8 +241,20 @@ struct Units {
     return n * bt.nq > lo && n * bt.nq <= hi ? n : 0;
   }
   __device__ __forceinline__ int tiles(int n) const { return (n + (1 << log2r) - 1) >> log2r; }
-  // pages of the tiles before tile t (t < tiles)
-  __device__ __forceinline__ long long before(int ctx, int t) const {
+  // pages that every tile of sequence b reaches, if its rows are not causal alone
+  __device__ __forceinline__ int least(int b, int ctx, int n) const {
+    return FEW ? 0 : reach.pages(bt, b, ctx, n);
+  }
+  // pages of the tiles before tile t (t < tiles), all of them at least `least`
+  __device__ __forceinline__ long long before(int ctx, int t, int least) const {
+    if (least == 0) return causal_before(ctx, t);
+    // the tiles whose own pages are no more than that
+    const long long j = max(((long long)least * kPage - ctx) >> log2r, 0LL);
+    if (t <= j) return (long long)t * least;
+    return j * least + causal_before(ctx, t) - causal_before(ctx, (int)j);
+  }
+  // the same for causal rows
+  __device__ __forceinline__ long long causal_before(int ctx, int t) const {
     const long long c = ctx + kPage - 1;
     if (log2r >= 6) return t * (c / kPage) + ((long long)t * (t + 1) / 2 << (log2r - 6));
     const int m = kPage >> log2r;  // tiles per page
@@ -92,16 +266,16 @@ struct Units {
     return sum(a + t + 1) - sum(a + 1);
   }
   // pages of tile t of a sequence with n rows
-  __device__ __forceinline__ int pages(int ctx, int n, int t) const {
+  __device__ __forceinline__ int pages(int ctx, int n, int t, int least) const {
     if (FEW) return min((ctx + n + kPage - 1) / kPage, bt.max_blocks);
-    return (ctx + min((t + 1) << log2r, n) + kPage - 1) / kPage;
+    return max((ctx + min((t + 1) << log2r, n) + kPage - 1) / kPage, least);
   }
   // units of one group of sequence b
   __device__ __forceinline__ long long group(int b) const {
     const int n = rows(b);
     if (n <= 0) return 0;
-    const int ctx = bt.context(b), t = FEW ? 0 : tiles(n) - 1;
-    return (FEW ? 0 : before(ctx, t)) + pages(ctx, n, t);
+    const int ctx = bt.context(b), t = FEW ? 0 : tiles(n) - 1, more = least(b, ctx, n);
+    return (FEW ? 0 : before(ctx, t, more)) + pages(ctx, n, t, more);
   }
 };
 
@@ -211,6 +385,11 @@ struct PageFrags {
     for (int dt = 0; dt < NDT; ++dt)
       v[dt] = *reinterpret_cast<const u32x4*>(vp + g * (HD * kSub) + (16 * dt + n) * kSub);
   }
+  // key fragment of score tile t and k-step st
+  __device__ __forceinline__ bf16x8 key(int t, int st, float ks) const {
+    const u32x4 w = k[t][st / 2];
+    return codes_to_bf16(w[2 * (st % 2)], w[2 * (st % 2) + 1], ks);
+  }
   // scores of the page: s[t][v] = key 16 g + 4 t + v of column n
   __device__ __forceinline__ void scores(const bf16x8* qf, float ks, f32x4* s) const {
 #pragma unroll
@@ -218,11 +397,8 @@ struct PageFrags {
 #pragma unroll
     for (int st = 0; st < NST; ++st)
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const u32x4 w = k[t][st / 2];
-        const bf16x8 a = codes_to_bf16(w[2 * (st % 2)], w[2 * (st % 2) + 1], ks);
-        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[st], s[t], 0, 0, 0);
-      }
+      for (int t = 0; t < 4; ++t)
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key(t, st, ks), qf[st], s[t], 0, 0, 0);
   }
 };
 
@@ -252,10 +428,25 @@ __host__ __device__ inline size_t part_floats(int cols, int hd) { return (size_t
 
 struct AttnOut {
   bf16* out;
-  float2* stat;      // of each column (see column_stat), or null
+  void* stat;        // of each column (see put_stat), or null
   float* part;
   int part_cols;
 };
+
+// A column's entry for the mass: its maximum and 1 / sum (see column_stat); with a Shape its
+// slope and place besides.  Column c of sequence b, group h is number `at` of the batch.
+__device__ __forceinline__ void put_stat(const NoShape&, const CacheBatch&, int, int, int, int,
+                                         int, size_t at, const AttnOut& o, float m, float inv) {
+  const float2 z = column_stat(m, inv);
+  static_cast<f32x2*>(o.stat)[at] = f32x2{z.x, z.y};
+}
+__device__ __forceinline__ void put_stat(const Shape& sh, const CacheBatch& bt, int b, int h,
+                                         int ctx, int rows, int c, size_t at, const AttnOut& o,
+                                         float m, float inv) {
+  const Column k = column_of(sh, bt, b, h, ctx, c, rows * bt.nq);
+  const float2 z = column_stat(m, inv);
+  static_cast<f32x4*>(o.stat)[at] = f32x4{z.x, z.y, k.slope, __int_as_float(k.place)};
+}
 
 template <int HD>
 struct FewLds {
@@ -415,7 +606,7 @@ __device__ __forceinline__ void few_columns(
       const float inv = inv_sum(m, l);
       const int row = bt.first_row(b) + c / bt.nq;
       o.out[(((size_t)row * bt.H + h) * bt.nq + c % bt.nq) * HD + d] = (bf16)(x * inv);
-      if (d == 0 && o.stat != nullptr) o.stat[qrow + c] = column_stat(m, inv);
+      if (d == 0 && o.stat != nullptr) put_stat(NoShape{}, bt, b, h, ctx, rows, c, qrow + c, o, m, inv);
     } else {
       pt[i] = x;
       if (d == 0) reinterpret_cast<float2*>(pt + o.part_cols * HD)[c] = float2{m, l};
@@ -423,12 +614,10 @@ __device__ __forceinline__ void few_columns(
   }
 }
 
-template <int HD>
-__global__ __launch_bounds__(kAttThr, 2) void cache_attn_few_kernel(
-    const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
-    const float* __restrict__ kv_scale, Units<true> w, Deal deal, float c_log2, AttnOut o,
-    float* __restrict__ score) {
-  __shared__ FewLds<HD> lds;
+// Walks the segments of a range of the few-column form: segment(b, h, rows, ctx, np, blk0,
+// blk1, slot, unit) for each (sequence, group) that the workgroup has pages of.
+template <typename F>
+__device__ __forceinline__ void few_walk(const Units<true>& w, const Deal& deal, F segment) {
   const CacheBatch& bt = w.bt;
   long long total, off;
   int b;
@@ -440,13 +629,12 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_few_kernel(
   const int per = (int)deal.per(total);
   long long unit = (long long)blockIdx.x * per;
   int left = (int)min((long long)per, total - unit);
-  int rows = w.rows(b), ctx = bt.context(b), np = w.pages(ctx, rows, 0);
+  int rows = w.rows(b), ctx = bt.context(b), np = w.pages(ctx, rows, 0, 0);
   int h = (int)(off / np), blk0 = (int)(off % np);
   size_t slot = 2 * (size_t)blockIdx.x;
   while (true) {
     const int blk1 = min(np, blk0 + left);
-    few_columns<HD>(q, kc, vc, kv_scale, bt, b, h, rows, ctx, np, blk0, blk1, c_log2, o, slot,
-                    score != nullptr ? score + unit * o.part_cols * kPage : nullptr, lds);
+    segment(b, h, rows, ctx, np, blk0, blk1, slot, unit);
     left -= blk1 - blk0;
     unit += blk1 - blk0;
     if (left <= 0) return;
@@ -460,9 +648,265 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_few_kernel(
         rows = w.rows(b);
       } while (rows <= 0);
       ctx = bt.context(b);
-      np = w.pages(ctx, rows, 0);
+      np = w.pages(ctx, rows, 0, 0);
     }
   }
+}
+
+template <int HD>
+__global__ __launch_bounds__(kAttThr, 2) void cache_attn_few_kernel(
+    const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
+    const float* __restrict__ kv_scale, Units<true> w, Deal deal, float c_log2, AttnOut o,
+    float* __restrict__ score) {
+  __shared__ FewLds<HD> lds;
+  few_walk(w, deal, [&](int b, int h, int rows, int ctx, int np, int blk0, int blk1, size_t slot,
+                        long long unit) {
+    few_columns<HD>(q, kc, vc, kv_scale, w.bt, b, h, rows, ctx, np, blk0, blk1, c_log2, o, slot,
+                    score != nullptr ? score + unit * o.part_cols * kPage : nullptr, lds);
+  });
+}
+
+// ---- few columns of other shapes -----------------------------------------------------
+// The same products, for up to 128 columns (trees of drafts, and any shaped call of so few).
+// The four waves are G groups of 16 NC columns by 4 / G pages: groups of a workgroup read the
+// same page at about the same time, from L2 but for the first.  The queries are held in LDS, as
+// the waves read them; a page's keys give their registers to the next page's as soon as the
+// scores are formed, and its values after the second product, so that two waves of a SIMD
+// have room for 32 columns each.
+template <int HD, int NC, int G>
+struct ShapedLds {
+  FewLds<HD> few;
+  bf16x8 q[G * NC][HD / 32][kWave];
+};
+
+template <int HD, int NC, int G>
+__device__ __forceinline__ void shaped_columns(
+    const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
+    const float* __restrict__ kv_scale, const CacheBatch& bt, int b, int h, int rows, int ctx,
+    int np, int blk0, int blk1, float c_log2, const Shape& sh, const AttnOut& o, size_t slot,
+    float* __restrict__ score, ShapedLds<HD, NC, G>& lds) {
+  using F = PageFrags<HD>;
+  constexpr int NP = kAttWaves / G;  // pages at a time
+  const int tid = threadIdx.x, lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), cg = wave % G, pl = wave / G;
+  const int n = lane & 15, g = lane >> 4;
+  const int ncol = rows * bt.nq;
+  const size_t qrow = ((size_t)h * bt.N + bt.first_row(b)) * bt.nq;
+  const int col0 = 16 * NC * cg;
+  Column col[NC];
+#pragma unroll
+  for (int j = 0; j < NC; ++j) {
+    const int c = col0 + 16 * j + n;
+    col[j] = column_of(sh, bt, b, h, ctx, c, ncol);
+    if (pl == 0) {
+      bf16x8 qf[F::NST];
+      load_q<HD>(q + qrow * HD, c, ncol, g, qf);
+#pragma unroll
+      for (int st = 0; st < F::NST; ++st) lds.q[NC * cg + j][st][lane] = qf[st];
+    }
+  }
+  const int len = min(ctx + rows, bt.cap());  // tokens the cache holds now
+  const int fewest = min(plain_tokens(sh, ctx, 0), bt.cap());
+  f32x4 oacc[NC][F::NDT];
+  float m_run[NC], l_run[NC];
+  bool saw[NC], far[NC];  // any token; (uniform) a column's maximum is far from 0
+#pragma unroll
+  for (int j = 0; j < NC; ++j) {
+#pragma unroll
+    for (int dt = 0; dt < F::NDT; ++dt) oacc[j][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m_run[j] = kMFloor;
+    l_run[j] = 0.f;
+    saw[j] = far[j] = false;
+  }
+  // page numbers and scales of the wave's next 64 pages, one a lane
+  int pid = -1;
+  float2 psc{0.f, 0.f};
+  const int mine = (blk1 - blk0 - pl + NP - 1) / NP;  // pages of this wave
+  auto pages64 = [&](int i) {
+    const int blk = blk0 + pl + NP * (i + lane);
+    pid = blk < blk1 ? bt.page(b, blk) : -1;
+    if (pid >= 0)
+      psc = *reinterpret_cast<const float2*>(kv_scale + ((size_t)pid * bt.H + h) * 2);
+  };
+  auto at = [&](int i) {  // (an absent page loads page 0)
+    return ((size_t)max(__builtin_amdgcn_readlane(pid, i & 63), 0) * bt.H + h) * (kPage * HD);
+  };
+  F f;
+  if (mine > 0) {
+    pages64(0);
+    f.load_k(kc + at(0), lane);
+    f.load_v(vc + at(0), lane);
+  }
+  __syncthreads();
+  for (int i = 0; i < mine; ++i) {
+    const int blk = blk0 + pl + NP * i;
+    const int page = __builtin_amdgcn_readlane(pid, i & 63);
+    const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(psc.x), i & 63));
+    const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(psc.y), i & 63));
+    f32x4 s[NC][4];
+#pragma unroll
+    for (int j = 0; j < NC; ++j)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) s[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int st = 0; st < F::NST; ++st) {
+      bf16x8 qf[NC];
+#pragma unroll
+      for (int j = 0; j < NC; ++j) qf[j] = lds.q[NC * cg + j][st][lane];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const bf16x8 a = f.key(t, st, ks);
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+          s[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[j], s[j][t], 0, 0, 0);
+      }
+    }
+    const bool more = i + 1 < mine;
+    if (more) {
+      if (((i + 1) & 63) == 0) pages64(i + 1);
+      f.load_k(kc + at(i + 1), lane);
+    }
+    if (page >= 0) {
+      const int k0 = blk * kPage + 16 * g;
+      const bool some = (blk + 1) * kPage > fewest;
+      bf16x8 p[NC][2];
+#pragma unroll
+      for (int j = 0; j < NC; ++j) {
+        __builtin_amdgcn_sched_barrier(0);  // (a tile of columns after another)
+        uint64_t sees = 0;
+        if (some) {
+          if (col0 + 16 * j + n < ncol) sees = keys_seen(sh, bt, b, col[j].row, ctx, len, blk);
+          saw[j] |= sees != 0;
+          sees >>= 16 * g;
+        } else {
+          saw[j] |= col0 + 16 * j + n < ncol;
+        }
+        shape_scores<16>(
+            sh, bt, b, ctx, rows, col[j], k0, !some, sees,
+            [&](int x) { return s[j][x >> 2][x & 3]; },
+            [&](int x, float y) { s[j][x >> 2][x & 3] = y; }, [](int x) { return x; });
+        if (NC == 1 && score != nullptr && n < ncol) {
+          float* to = score + ((size_t)(blk - blk0) * o.part_cols + n) * kPage + 16 * g;
+#pragma unroll
+          for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4*>(to + 4 * t) = s[j][t];
+        }
+        float mx = s[j][0][0];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[j][t][e]);
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        // (the maximum moves only when a page exceeds it by 2^8, as with causal columns)
+        const float mxs = mx * c_log2;
+        const bool need = mxs > m_run[j] + 8.f;
+        if (__builtin_amdgcn_ballot_w64(need)) {
+          const float m_new = need ? mxs : m_run[j];
+          const float a = __builtin_amdgcn_exp2f(m_run[j] - m_new);
+          m_run[j] = m_new;
+          far[j] = __builtin_amdgcn_ballot_w64(far_max(m_run[j])) != 0;
+          l_run[j] *= a;
+#pragma unroll
+          for (int dt = 0; dt < F::NDT; ++dt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) oacc[j][dt][e] *= a;
+        }
+        float c_page = c_log2, m_page = m_run[j];
+        if (far[j]) {
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[j][t][e] = far_exponent(s[j][t][e], c_log2, m_run[j]);
+          c_page = 1.f;
+          m_page = 0.f;
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[j][t][e], c_page, -m_page));
+            l_run[j] += x;
+            p[j][t >> 1][4 * (t & 1) + e] = (bf16)x;
+          }
+      }
+      if (some) {
+        // slots past the last token hold anything: 0 * NaN is NaN
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int in = len - (k0 + 4 * e);
+          const uint32_t m = in >= 4 ? 0xffffffffu : in <= 0 ? 0u : (1u << (8 * in)) - 1;
+#pragma unroll
+          for (int dt = 0; dt < F::NDT; ++dt) f.v[dt][e] &= m;
+        }
+      }
+#pragma unroll
+      for (int dt = 0; dt < F::NDT; ++dt)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const bf16x8 a = codes_to_bf16(f.v[dt][2 * u], f.v[dt][2 * u + 1], vs);
+#pragma unroll
+          for (int j = 0; j < NC; ++j)
+            oacc[j][dt] =
+                __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[j][u], oacc[j][dt], 0, 0, 0);
+        }
+    }
+    if (more) f.load_v(vc + at(i + 1), lane);
+  }
+  const bool whole = blk0 == 0 && blk1 == np;
+  float* pt = o.part + slot * part_floats(o.part_cols, HD);
+  // the states of the waves of a column group, merged in wave order, 16 columns of each group
+  // at a time
+#pragma unroll
+  for (int j = 0; j < NC; ++j) {
+    if (16 * j >= ncol) break;  // (uniform)
+    if (saw[j]) m_run[j] = fmaxf(m_run[j], kMSeen);
+    l_run[j] += __shfl_xor(l_run[j], 16);
+    l_run[j] += __shfl_xor(l_run[j], 32);
+    __syncthreads();  // what was in LDS before has been read
+    const int me = opaque_int(lane), n1 = me & 15, g1 = me >> 4;  // (not held over the pages)
+    if (g1 == 0) lds.few.mm[wave][n1] = m_run[j], lds.few.ll[wave][n1] = l_run[j];
+#pragma unroll
+    for (int dt = 0; dt < F::NDT; ++dt)
+      *reinterpret_cast<f32x4*>(&lds.few.oo[wave][n1][16 * dt + 4 * g1]) = oacc[j][dt];
+    __syncthreads();
+    for (int i = opaque_int(tid); i < G * 16 * HD; i += kAttThr) {
+      const int gr = i / (16 * HD), c = i / HD % 16, d = i % HD;
+      const int cc = 16 * (NC * gr + j) + c;
+      if (cc >= ncol) break;
+      float m = lds.few.mm[gr][c], l = 0.f, x = 0.f;
+#pragma unroll
+      for (int v = 1; v < NP; ++v) m = fmaxf(m, lds.few.mm[v * G + gr][c]);
+#pragma unroll
+      for (int v = 0; v < NP; ++v) {
+        const float a = __builtin_amdgcn_exp2f(lds.few.mm[v * G + gr][c] - m);
+        l += lds.few.ll[v * G + gr][c] * a;
+        x += lds.few.oo[v * G + gr][c][d] * a;
+      }
+      if (whole) {
+        const float inv = inv_sum(m, l);
+        const int row = bt.first_row(b) + cc / bt.nq;
+        o.out[(((size_t)row * bt.H + h) * bt.nq + cc % bt.nq) * HD + d] = (bf16)(x * inv);
+        if (d == 0 && o.stat != nullptr) put_stat(sh, bt, b, h, ctx, rows, cc, qrow + cc, o, m, inv);
+      } else {
+        pt[(size_t)cc * HD + d] = x;
+        if (d == 0) reinterpret_cast<float2*>(pt + o.part_cols * HD)[cc] = float2{m, l};
+      }
+    }
+  }
+}
+
+template <int HD, int NC, int G>
+__global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
+    const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
+    const float* __restrict__ kv_scale, Units<true> w, Deal deal, float c_log2, Shape sh,
+    AttnOut o, float* __restrict__ score) {
+  __shared__ ShapedLds<HD, NC, G> lds;
+  few_walk(w, deal, [&](int b, int h, int rows, int ctx, int np, int blk0, int blk1, size_t slot,
+                        long long unit) {
+    shaped_columns<HD, NC, G>(q, kc, vc, kv_scale, w.bt, b, h, rows, ctx, np, blk0, blk1, c_log2,
+                              sh, o, slot,
+                              score != nullptr ? score + unit * o.part_cols * kPage : nullptr, lds);
+  });
 }
 
 // ---- many columns -----------------------------------------------------------------
@@ -476,19 +920,22 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_few_kernel(
 // 4 (l / 32) + v % 4 of tile t; its 8 scores of 16 keys are the B operand of O^T += V^T
 // P^T in the order that the V^T tile stores.  A page's P V product runs one iteration
 // late, beside the next page's softmax, so K is held for two pages and V^T for three.
-template <int HD>
+template <int HD, typename S>
 __global__ __launch_bounds__(kTileThr) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ kc,
                        const uint8_t* __restrict__ vc, const float* __restrict__ kv_scale,
-                       Units<false> w, Deal deal, float c_log2, AttnOut o) {
+                       Units<false> w, Deal deal, float c_log2, S sh, AttnOut o) {
+  constexpr bool SHAPED = is_shaped<S>;
   constexpr int KT = kPage * 256;       // K tile bytes
   constexpr int VT = HD * kPage * 2;    // V^T tile bytes
   constexpr int NST = HD / 16;          // score k-steps
   constexpr int NDT = HD / 32;          // output tiles
   constexpr int CPR = HD / 16;          // 16-byte pieces of a key row
   __shared__ __align__(1024) unsigned char smem[2 * KT + 3 * VT];
+  __shared__ float2 cols[SHAPED ? kTileCols : 1];  // slope and place of each column
   const CacheBatch& bt = w.bt;
-  const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
+  const int tid = threadIdx.x, lane = lane_id();
+  const int wave = SHAPED ? __builtin_amdgcn_readfirstlane(tid >> 6) : tid >> 6;
   const int qi = lane & 31, hl = lane >> 5;
   // neighbouring ranges, which share a sequence's pages, on one XCD (workgroups go
   // round the eight XCDs; the grid is a multiple of 8)
@@ -501,6 +948,7 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
   const long long per = deal.per(total);
   long long left = min(per, total - range * per);
   int rows = w.rows(b), ctx = bt.context(b), nt = w.tiles(rows), h, t, blk0;
+  int least = SHAPED ? w.least(b, ctx, rows) : 0;
   {
     const long long each = w.group(b);
     h = (int)(off / each);
@@ -508,25 +956,42 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
     int lo = 0, hi = nt - 1;  // the tile: largest t with before(t) <= off
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (w.before(ctx, mid) <= off) lo = mid;
+      if (w.before(ctx, mid, least) <= off) lo = mid;
       else hi = mid - 1;
     }
     t = lo;
-    blk0 = (int)(off - w.before(ctx, t));
+    blk0 = (int)(off - w.before(ctx, t, least));
+    if constexpr (SHAPED) {  // (in scalar registers)
+      b = __builtin_amdgcn_readfirstlane(b);
+      h = __builtin_amdgcn_readfirstlane(h);
+      t = __builtin_amdgcn_readfirstlane(t);
+      blk0 = __builtin_amdgcn_readfirstlane(blk0);
+      left = (long long)__builtin_amdgcn_readfirstlane((int)(left >> 32)) << 32 |
+             (uint32_t)__builtin_amdgcn_readfirstlane((int)left);
+    }
   }
   size_t slot = 2 * (size_t)range;
 
   // staging: thread -> 16 bytes of a key row, and 16 tokens of a value dim
   const bool stages = tid < kPage * CPR;
-  const int krow = tid / CPR, kch = tid % CPR, vg = tid / HD, vd = tid % HD;
-  const uint32_t kdst = krow * 256, vdst = vd * (kPage * 2);
-  const uint32_t ks0 = kdst + (((2 * kch) ^ (krow & 15)) << 4);
-  const uint32_t ks1 = kdst + (((2 * kch + 1) ^ (krow & 15)) << 4);
-  const int vsw = (vd & 7) ^ ((vd >> 3) & 1);
-  const uint32_t vs0 = vdst + (((2 * vg) ^ vsw) << 4), vs1 = vdst + (((2 * vg + 1) ^ vsw) << 4);
+  struct Places {
+    int vg;
+    uint32_t k0, k1, v0, v1;
+  };
+  auto places = [](int i) {
+    const int krow = i / CPR, kch = i % CPR, vg = i / HD, vd = i % HD;
+    const uint32_t kdst = krow * 256, vdst = vd * (kPage * 2);
+    const int vsw = (vd & 7) ^ ((vd >> 3) & 1);
+    return Places{vg, kdst + (((2 * kch) ^ (krow & 15)) << 4),
+                  kdst + (((2 * kch + 1) ^ (krow & 15)) << 4), vdst + (((2 * vg) ^ vsw) << 4),
+                  vdst + (((2 * vg + 1) ^ vsw) << 4)};
+  };
+  const Places mine = places(tid);
+  // (formed again where they are used, if a Shape's values need the registers)
+  auto fresh = [&](int x) { return SHAPED ? opaque_int(x) : x; };
 
   while (true) {
-    const int np = w.pages(ctx, rows, t);
+    const int np = w.pages(ctx, rows, t, least);
     const int blk1 = segment_end(np, blk0, left);
     const int row0 = t << w.log2r;
     const int ncol = (min(rows, (t + 1) << w.log2r) - row0) * bt.nq;
@@ -537,15 +1002,21 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
     for (int st = 0; st < NST; ++st) {
       qf[st] = bf16x8{};
       if (col < ncol)
-        qf[st] = *reinterpret_cast<const bf16x8*>(q + (qrow + col) * HD + st * 16 + hl * 8);
+        qf[st] = *reinterpret_cast<const bf16x8*>(q + (qrow + col) * HD + st * 16 + fresh(hl) * 8);
     }
     const int len = min(ctx + rows, bt.cap());
     const int seen = col < ncol ? min(ctx + row0 + col / bt.nq + 1, bt.cap()) : 0;
     const int c0 = __builtin_amdgcn_readfirstlane(wave * 32);
-    const int fewest = min(ctx + row0 + c0 / bt.nq + 1, bt.cap());
+    const int fewest =  // tokens that every column of this wave sees (see plain_tokens)
+        min(plain_tokens(sh, ctx, row0 + c0 / bt.nq), bt.cap());
+    if constexpr (SHAPED) {  // (read back by its own lanes)
+      const Column cl = column_of(sh, bt, b, h, ctx, row0 * bt.nq + col, row0 * bt.nq + ncol);
+      cols[col] = float2{cl.slope, __int_as_float(cl.place)};
+    }
     // pages that a column of this wave sees some of
-    const int npw = c0 < ncol ? (min(ctx + row0 + min(c0 + 31, ncol - 1) / bt.nq + 1, bt.cap()) +
-                                 kPage - 1) / kPage : 0;
+    int npw = c0 < ncol ? (min(ctx + row0 + min(c0 + 31, ncol - 1) / bt.nq + 1, bt.cap()) +
+                           kPage - 1) / kPage : 0;
+    if (SHAPED && c0 < ncol) npw = max(npw, least);
     f32x16 oacc[NDT];
 #pragma unroll
     for (int i = 0; i < NDT; ++i)
@@ -571,12 +1042,13 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
       const int p = __builtin_amdgcn_readlane(pid, (blk - blk0) & 63);
       kreg = vreg = zero_u32x4();
       if (p >= 0 && stages) {
-        const size_t at = ((size_t)p * bt.H + h) * (kPage * HD) + tid * 16;
+        const size_t at = ((size_t)p * bt.H + h) * (kPage * HD) + fresh(tid) * 16;
         kreg = *reinterpret_cast<const u32x4*>(kc + at);
         vreg = *reinterpret_cast<const u32x4*>(vc + at);
       }
     };
     auto stage = [&](int i, int blk, float ks, float vs) {  // i-th page of the segment
+      const auto [vg, ks0, ks1, vs0, vs1] = SHAPED ? places(opaque_int(tid)) : mine;
       if ((blk + 1) * kPage > len) {  // slots past the last token hold anything
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -596,9 +1068,10 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
       return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), (blk - blk0) & 63));
     };
     auto pv = [&](const unsigned char* vb) {
+      const int r0 = fresh(qi);
 #pragma unroll
       for (int i = 0; i < NDT; ++i) {
-        const int row = i * 32 + qi;
+        const int row = i * 32 + r0;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const bf16x8 vf = *reinterpret_cast<const bf16x8*>(
@@ -642,16 +1115,32 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int v = 0; v < 16; ++v) sacc[i][v] = 0.f;
+        const int r0 = fresh(qi);
 #pragma unroll
         for (int st = 0; st < NST; ++st)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const int row = i * 32 + qi;
+            const int row = i * 32 + r0;
             const bf16x8 kf = *reinterpret_cast<const bf16x8*>(
                 kb + row * 256 + (((st * 2 + hl) ^ (row & 15)) << 4));
             sacc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], sacc[i], 0, 0, 0);
           }
-        if ((blk + 1) * kPage > fewest) {
+        const bool some = (blk + 1) * kPage > fewest;
+        uint64_t sees = 0;  // (SHAPED, some)
+        if constexpr (SHAPED) {
+          __builtin_amdgcn_sched_barrier(0);
+          if (some && fresh(col) < ncol)
+            sees = keys_seen(sh, bt, b, row0 + fresh(col) / bt.nq, ctx, len, blk);
+          const int k4 = 4 * fresh(hl);
+          const float2 sp = cols[fresh(col)];
+          const Column cl{sp.x, __float_as_int(sp.y), 0};
+          shape_scores<32>(
+              sh, bt, b, ctx, rows, cl, blk * kPage + k4, !some, sees >> k4,
+              [&](int x) { return sacc[x >> 4][x & 15]; },
+              [&](int x, float y) { sacc[x >> 4][x & 15] = y; },
+              [](int x) { return 32 * (x >> 4) + 8 * ((x & 15) >> 2) + (x & 3); });
+          __builtin_amdgcn_sched_barrier(0);
+        } else if (some) {
 #pragma unroll
           for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -674,7 +1163,8 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
         const bool need = mxs > m_run + 8.f;
         float m_new = need ? mxs : m_run;
         const float a_new = need ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.f;
-        if (blk * kPage < seen) m_new = fmaxf(m_new, kMSeen);
+        if (SHAPED ? (some ? sees != 0 : col < ncol) : blk * kPage < seen)
+          m_new = fmaxf(m_new, kMSeen);
         m_run = m_new;
         float c_page = c_log2;
         if (__builtin_amdgcn_ballot_w64(far_max(m_new))) {
@@ -709,14 +1199,17 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
     rescale();
     pv(smem + 2 * KT + ((niter + 2) % 3) * VT);
 
-    const float l = l_run + __shfl_xor(l_run, 32);
+    const auto lsw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run),
+                                                      false, false);
+    const float l = __uint_as_float(lsw[0]) + __uint_as_float(lsw[1]);
     const bool whole = blk0 == 0 && blk1 == np;
-    if (col < ncol) {
+    const int ec = fresh(col), eh = fresh(hl);
+    if (ec < ncol) {
       // lane holds dims 32 i + 8 g + 4 hl + [0, 4)
       if (whole) {
         const float inv = inv_sum(m_run, l);
-        const int row = bt.first_row(b) + row0 + col / bt.nq;
-        bf16* dst = o.out + (((size_t)row * bt.H + h) * bt.nq + col % bt.nq) * HD;
+        const int row = bt.first_row(b) + row0 + ec / bt.nq;
+        bf16* dst = o.out + (((size_t)row * bt.H + h) * bt.nq + ec % bt.nq) * HD;
 #pragma unroll
         for (int i = 0; i < NDT; ++i)
 #pragma unroll
@@ -724,18 +1217,19 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
             bf16x4 x;
 #pragma unroll
             for (int v = 0; v < 4; ++v) x[v] = (bf16)(oacc[i][g * 4 + v] * inv);
-            *reinterpret_cast<bf16x4*>(dst + i * 32 + g * 8 + hl * 4) = x;
+            *reinterpret_cast<bf16x4*>(dst + i * 32 + g * 8 + eh * 4) = x;
           }
-        if (o.stat != nullptr && hl == 0) o.stat[qrow + col] = column_stat(m_run, inv);
+        if (o.stat != nullptr && eh == 0)
+          put_stat(sh, bt, b, h, ctx, rows, row0 * bt.nq + ec, qrow + ec, o, m_run, inv);
       } else {
         float* pt = o.part + slot * part_floats(kTileCols, HD);
 #pragma unroll
         for (int i = 0; i < NDT; ++i)
 #pragma unroll
           for (int g = 0; g < 4; ++g)
-            *reinterpret_cast<f32x4*>(pt + ((i * 8 + g * 2 + hl) * kTileCols + col) * 4) =
+            *reinterpret_cast<f32x4*>(pt + ((i * 8 + g * 2 + eh) * kTileCols + ec) * 4) =
                 f32x4{oacc[i][g * 4], oacc[i][g * 4 + 1], oacc[i][g * 4 + 2], oacc[i][g * 4 + 3]};
-        if (hl == 0) reinterpret_cast<float2*>(pt + kTileCols * HD)[col] = float2{m_run, l};
+        if (eh == 0) reinterpret_cast<float2*>(pt + kTileCols * HD)[ec] = float2{m_run, l};
       }
     }
     left -= niter;
@@ -753,6 +1247,7 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
         } while (rows <= 0);
         ctx = bt.context(b);
         nt = w.tiles(rows);
+        if constexpr (SHAPED) least = w.least(b, ctx, rows);
       }
     }
   }
@@ -787,14 +1282,14 @@ __device__ __forceinline__ bool find_parts(const Units<FEW>& w, const Deal& deal
 // lane 4 dims) each sum every eighth part, and are then summed in order.  (A sequence's
 // columns one after another in a workgroup: 13.7 us instead of 4.3 for 16 sequences of 1000 to
 // 4000 tokens, 4 groups of 8 heads.)
-template <int HD>
-__device__ __forceinline__ void join_few(const Units<true>& w, const Deal& deal,
+template <int HD, typename S>
+__device__ __forceinline__ void join_few(const Units<true>& w, const Deal& deal, const S& sh,
                                          const AttnOut& o, int h, int b, int c) {
   __shared__ f32x4 osum[8][32];
   const CacheBatch& bt = w.bt;
   const int rows = w.rows(b);
   if (c >= rows * bt.nq) return;
-  const int np = w.pages(bt.context(b), rows, 0);
+  const int np = w.pages(bt.context(b), rows, 0, 0);
   Parts p{o.part, o.part_cols, HD};
   if (!find_parts(w, deal, w.prefix[b] + (long long)np * h, np, p)) return;
   const int grp = threadIdx.x >> 5, l5 = threadIdx.x & 31, d = 4 * l5;
@@ -836,15 +1331,16 @@ __device__ __forceinline__ void join_few(const Units<true>& w, const Deal& deal,
                                              (bf16)(x[2] * inv), (bf16)(x[3] * inv)};
   }
   if (o.stat != nullptr && l5 == 0)
-    o.stat[((size_t)h * bt.N + bt.first_row(b)) * bt.nq + c] = column_stat(m, inv);
+    put_stat(sh, bt, b, h, bt.context(b), rows, c,
+             ((size_t)h * bt.N + bt.first_row(b)) * bt.nq + c, o, m, inv);
 }
 
 // Many columns: one workgroup per (32 columns of a tile, group h), 8 threads a column; a
 // thread loads its dims of four parts at a time.
 constexpr int kJoinCols = 32;
 
-template <int HD>
-__device__ __forceinline__ void join_tile(const Units<false>& w, const Deal& deal,
+template <int HD, typename S>
+__device__ __forceinline__ void join_tile(const Units<false>& w, const Deal& deal, const S& sh,
                                           const AttnOut& o, int h, int x32) {
   constexpr int CB = kTileCols / kJoinCols, NV = HD / 32, AT_ONCE = 4;
   const CacheBatch& bt = w.bt;
@@ -853,9 +1349,9 @@ __device__ __forceinline__ void join_tile(const Units<false>& w, const Deal& dea
   const int c = x32 % CB * kJoinCols + (threadIdx.x & 31), l3 = threadIdx.x >> 5;
   const int rows = w.rows(b), ctx = bt.context(b), row0 = t << w.log2r;
   const int ncol = (min(rows, (t + 1) << w.log2r) - row0) * bt.nq;
-  const int np = w.pages(ctx, rows, t);
+  const int least = w.least(b, ctx, rows), np = w.pages(ctx, rows, t, least);
   Parts p{o.part, kTileCols, HD};
-  if (!find_parts(w, deal, w.prefix[b] + w.group(b) * h + w.before(ctx, t), np, p) ||
+  if (!find_parts(w, deal, w.prefix[b] + w.group(b) * h + w.before(ctx, t, least), np, p) ||
       c >= ncol)
     return;
   float m = kMFloor, l = 0.f;
@@ -906,7 +1402,8 @@ __device__ __forceinline__ void join_tile(const Units<false>& w, const Deal& dea
         bf16x4{(bf16)(x[k][0] * inv), (bf16)(x[k][1] * inv), (bf16)(x[k][2] * inv),
                (bf16)(x[k][3] * inv)};
   if (o.stat != nullptr && l3 == 0)
-    o.stat[((size_t)h * bt.N + bt.first_row(b) + row0) * bt.nq + c] = column_stat(m, inv);
+    put_stat(sh, bt, b, h, ctx, rows, row0 * bt.nq + c,
+             ((size_t)h * bt.N + bt.first_row(b) + row0) * bt.nq + c, o, m, inv);
 }
 
 // What a form's launches share: its units, how they are dealt out, and where it writes.
@@ -919,12 +1416,12 @@ struct Form {
 
 // One launch joins both forms' parts: `many_blocks` by H workgroups those of tiles, the rest
 // those of few columns.
-template <int HD>
-__global__ __launch_bounds__(256) void cache_join_kernel(Form<true> few, Form<false> many,
+template <int HD, typename S>
+__global__ __launch_bounds__(256) void cache_join_kernel(Form<true> few, Form<false> many, S sh,
                                                          int many_blocks) {
   const int x = blockIdx.x, h = blockIdx.y;
-  if (x < many_blocks) join_tile<HD>(many.w, many.deal, many.o, h, x);
-  else join_few<HD>(few.w, few.deal, few.o, h, (x - many_blocks) / few.o.part_cols,
+  if (x < many_blocks) join_tile<HD>(many.w, many.deal, sh, many.o, h, x);
+  else join_few<HD>(few.w, few.deal, sh, few.o, h, (x - many_blocks) / few.o.part_cols,
                     (x - many_blocks) % few.o.part_cols);
 }
 
@@ -935,9 +1432,10 @@ __global__ __launch_bounds__(256) void cache_join_kernel(Form<true> few, Form<fa
 
 // Few columns: equal ranges of the units again; a wave takes every fourth page, a lane a
 // token.
+template <typename S>
 __device__ __forceinline__ void mass_few(const float* __restrict__ score, const Units<true>& w,
-                                         const Deal& deal, int range, int part_cols,
-                                         float c_log2, const float2* __restrict__ stat,
+                                         const Deal& deal, int range, int part_cols, float c_log2,
+                                         const S& sh, const Stat<S>* __restrict__ stat,
                                          const float* __restrict__ mass_in,
                                          float* __restrict__ mass_out) {
   __shared__ int found;
@@ -951,14 +1449,17 @@ __device__ __forceinline__ void mass_few(const float* __restrict__ score, const 
   __syncthreads();
   int b = found;
   int left = (int)min(per, total - unit);
-  int rows = w.rows(b), ctx = bt.context(b), np = w.pages(ctx, rows, 0);
+  int rows = w.rows(b), ctx = bt.context(b), np = w.pages(ctx, rows, 0, 0);
   const int off = (int)(unit - w.prefix[b]);
   int h = off / np, blk0 = off % np;
   score += unit * part_cols * kPage;
   while (true) {
     const int blk1 = min(np, blk0 + left), ncol = rows * bt.nq;
     float2 z{0.f, 0.f};  // of column `lane`
-    if (lane < ncol) z = stat[((size_t)h * bt.N + bt.first_row(b)) * bt.nq + lane];
+    if (lane < ncol) {
+      const Stat<S> y = stat[((size_t)h * bt.N + bt.first_row(b)) * bt.nq + lane];
+      z = float2{y[0], y[1]};
+    }
     for (int blk = blk0 + wave; blk < blk1; blk += kAttWaves) {
       const int page = bt.page(b, blk), slot = blk * kPage + lane;
       if (page < 0) continue;
@@ -974,7 +1475,14 @@ __device__ __forceinline__ void mass_few(const float* __restrict__ score, const 
         const float x = s[c * kPage];
         const float p = __builtin_amdgcn_exp2f(inv < 0.f ? far_exponent(x, c_log2, m)
                                                          : fmaf(x, c_log2, -m)) * fabsf(inv);
-        y += slot <= last ? p : 0.f;
+        bool sees = slot <= last;
+        if constexpr (is_shaped<S>) {  // (scores of tokens that it does not see are -inf)
+          sees = true;
+          if (inv != inv) {
+            sees = keys_seen(sh, bt, b, c / bt.nq, ctx, min(ctx + rows, bt.cap()), blk) >> lane & 1;
+          }
+        }
+        y += sees ? p : 0.f;
         if (++head == bt.nq) head = 0, ++last;
       }
       if (slot < min(ctx + rows, bt.cap())) mass_out[at] = before + y;
@@ -990,7 +1498,7 @@ __device__ __forceinline__ void mass_few(const float* __restrict__ score, const 
         rows = w.rows(b);
       } while (rows <= 0);
       ctx = bt.context(b);
-      np = w.pages(ctx, rows, 0);
+      np = w.pages(ctx, rows, 0, 0);
     }
   }
 }
@@ -1008,15 +1516,17 @@ __device__ __forceinline__ void mass_few(const float* __restrict__ score, const 
 constexpr int kMassThr = 256, kMassCols = 32;
 constexpr int kMassStages = 4;
 
-template <int HD>
+template <int HD, typename S>
 __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8_t* __restrict__ kc,
                                          const float* __restrict__ kv_scale, const Units<false>& w,
-                                         const Deal& deal, int range, float c_log2,
-                                         const float2* __restrict__ stat,
+                                         const Deal& deal, int range, float c_log2, const S& sh,
+                                         const Stat<S>* __restrict__ stat,
                                          const float* __restrict__ mass_in,
                                          float* __restrict__ mass_out) {
-  constexpr int NST = HD / 16;
-  constexpr int QT = kMassCols * 256, STAGE = QT + 256;  // bytes of a tile, and with its statistics
+  constexpr bool SHAPED = is_shaped<S>;
+  constexpr int NST = HD / 16, ST = sizeof(Stat<S>);
+  // bytes of a tile, and with its statistics
+  constexpr int QT = kMassCols * 256, STAGE = QT + kMassCols * ST;
   constexpr int QI = QT / 1024 / (kMassThr / kWave);     // 1 KB DMA instructions of a wave
   __shared__ __align__(1024) unsigned char smem[kMassStages * STAGE];
   __shared__ float sum[kMassThr / kWave][32];
@@ -1069,11 +1579,13 @@ __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[v] = 0.f;
     // tiles before the first column that sees the pages are left out
-    const long long c_first = (long long)max(blk0 * kPage - ctx, 0) * bt.nq;
+    long long c_first = (long long)max(blk0 * kPage - ctx, 0) * bt.nq;
+    if constexpr (SHAPED)
+      if (blk0 < w.least(b, ctx, rows)) c_first = 0;
     const int t0 = (int)(c_first / kMassCols), t1 = (ncol + kMassCols - 1) / kMassCols;
     // columns past the last read zeros: no query, maximum 0 and 1 / sum 0
     const __amdgpu_buffer_rsrc_t rq = make_rsrc_u(q + qrow * HD, (uint32_t)ncol * (HD * 2));
-    const __amdgpu_buffer_rsrc_t rz = make_rsrc_u(stat + qrow, (uint32_t)ncol * 8u);
+    const __amdgpu_buffer_rsrc_t rz = make_rsrc_u(stat + qrow, (uint32_t)ncol * (uint32_t)ST);
     rsrc_settle(rq, rz);
     uint32_t qoff[QI];
 #pragma unroll
@@ -1089,9 +1601,11 @@ __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8
       for (int i = 0; i < QI; ++i)
         dma16(rq, qoff[i] + step, to + (uint32_t)wave_u * (QI * 1024), i * 1024);
       // (every wave loads the statistics, so that all count the same)
-      dma4(rz, (uint32_t)t * (kMassCols * 8) + lane * 4u, to, QT);
+#pragma unroll
+      for (int i = 0; i < ST / 8; ++i)
+        dma4(rz, (uint32_t)t * (kMassCols * ST) + i * 256u + lane * 4u, to, QT + i * 256);
     };
-    constexpr int OPS = QI + 1;  // DMA instructions of a wave and tile
+    constexpr int OPS = QI + ST / 8;  // DMA instructions of a wave and tile
 #pragma unroll
     for (int i = 0; i < kMassStages - 1; ++i)
       if (t0 + i < t1) issue(t0 + i);
@@ -1103,7 +1617,8 @@ __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8
       if (t + kMassStages - 1 < t1) issue(t + kMassStages - 1);
       const unsigned char* tile = smem + (t & (kMassStages - 1)) * STAGE;
       if (works) {
-        float2 z = *reinterpret_cast<const float2*>(tile + QT + qi * 8);
+        const Stat<S> zs = *reinterpret_cast<const Stat<S>*>(tile + QT + qi * ST);
+        float2 z{zs[0], zs[1]};
         const uint32_t qat = (uint32_t)((t & (kMassStages - 1)) * STAGE + qi * 256 +
                                         (((2 * hl) ^ (qi & 15)) << 4));
         // (formed before the products, so that nothing waits for it behind them)
@@ -1119,9 +1634,21 @@ __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8
               smem + (qat ^ (uint32_t)((4 * (st / 2) + st % 2) << 4)));
           x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[st], qf, x, 0, 0, 0);
         }
-        // (the tile's first column sees the fewest)
-        if (ctx + t * kMassCols / bt.nq + 1 < min(key0 + 32, len + 1)) {
-          const int col = t * kMassCols + qi, seen = col < ncol ? ctx + col / bt.nq + 1 : 0;
+        Column cl{};  // (SHAPED)
+        const int col = t * kMassCols + qi;
+        if constexpr (SHAPED) {
+          const int i0 = t * kMassCols / bt.nq;
+          const bool all = plain_tokens(sh, ctx, i0) >= min(key0 + 32, len + 1);
+          uint64_t sees = 0;
+          cl = Column{zs[2], __float_as_int(zs[3]), col / bt.nq};
+          if (!all && col < ncol)
+            sees = keys_seen(sh, bt, b, cl.row, ctx, len, key0 / kPage) >> ((wave & 1) * 32 + 4 * hl);
+          shape_scores<16>(
+              sh, bt, b, ctx, rows, cl, key0 + 4 * hl, all, sees, [&](int v) { return x[v]; },
+              [&](int v, float y) { x[v] = y; }, [](int v) { return 8 * (v >> 2) + (v & 3); });
+        } else if (ctx + t * kMassCols / bt.nq + 1 < min(key0 + 32, len + 1)) {
+          // (the tile's first column sees the fewest)
+          const int seen = col < ncol ? ctx + col / bt.nq + 1 : 0;
 #pragma unroll
           for (int v = 0; v < 16; ++v)
             if (key0 + 8 * (v >> 2) + 4 * hl + (v & 3) >= seen) x[v] = -__builtin_inff();
@@ -1130,10 +1657,15 @@ __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8
         if (special) {
           // a NaN row counts, as NaN, for the tokens that it sees alone (0 * NaN is NaN)
           if (z.y != z.y) {
-            const int seen = ctx + (t * kMassCols + qi) / bt.nq + 1;
+            const int seen = ctx + col / bt.nq + 1;
+            uint64_t sees = 0;
+            if constexpr (SHAPED)
+              sees = keys_seen(sh, bt, b, cl.row, ctx, len, key0 / kPage) >> ((wave & 1) * 32 + 4 * hl);
 #pragma unroll
             for (int v = 0; v < 16; ++v)
-              if (key0 + 8 * (v >> 2) + 4 * hl + (v & 3) < seen) acc[v] = z.y;
+              if (SHAPED ? (sees >> (8 * (v >> 2) + (v & 3)) & 1) != 0
+                         : key0 + 8 * (v >> 2) + 4 * hl + (v & 3) < seen)
+                acc[v] = z.y;
             z.y = 0.f;
           }
 #pragma unroll
@@ -1171,20 +1703,21 @@ __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8
 
 // One launch for both: `any_ranges` workgroups for the sequences of `any`, the rest for
 // those of few columns, from their scores.
-template <int HD>
-__global__ __launch_bounds__(kMassThr, 4) void cache_mass_kernel(
+template <int HD, typename S>
+__global__ __launch_bounds__(kMassThr, is_shaped<S> ? 3 : 4) void cache_mass_kernel(
     const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const float* __restrict__ kv_scale,
     Units<false> any, int any_ranges, Form<true> few, const float* __restrict__ score, float c_log2,
-    const float2* __restrict__ stat, const float* __restrict__ mass_in,
+    S sh, const Stat<S>* __restrict__ stat, const float* __restrict__ mass_in,
     float* __restrict__ mass_out) {
   static_assert(kMassThr == kAttThr, "one workgroup size");
   const int x = blockIdx.x;
   if (x >= any_ranges) {
     mass_few(score, few.w, Deal{few.deal.ranges, few.deal.least, 0}, x - any_ranges,
-             few.o.part_cols, c_log2, stat, mass_in, mass_out);
+             few.o.part_cols, c_log2, sh, stat, mass_in, mass_out);
     return;
   }
-  mass_any<HD>(q, kc, kv_scale, any, Deal{any_ranges, 1, 0}, x, c_log2, stat, mass_in, mass_out);
+  mass_any<HD>(q, kc, kv_scale, any, Deal{any_ranges, 1, 0}, x, c_log2, sh, stat, mass_in,
+               mass_out);
 }
 
 // Host side of the two forms: ranges (workgroups) and scratch.
@@ -1205,20 +1738,25 @@ struct FormPlan {
 };
 struct AttnPlan {
   FormPlan few, many;
+  int few_cols;  // that the few-column form holds
   bool scores;
   size_t stat, score, total;
 };
 
-AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_rows, bool mass) {
+AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_rows, bool mass,
+                   bool shaped) {
   AttnPlan p{};
   const long long most = (long long)max_rows * nq;
   // Both forms where the sequences beside the longest have few columns on average (us for a
   // 512-row chunk beside 16 decoding sequences, with mass: 85, and 114 in the second form
   // alone); where they are all chunks the first would be a launch for nothing.
-  p.few.on = most <= kFewCols || (B > 1 && (long long)(N - max_rows) * nq <= kFewCols * (B - 1LL));
-  p.many.on = most > kFewCols;
-  p.few.hi = kFewCols;
-  p.many.lo = p.few.on ? kFewCols : 0;
+  p.few_cols = kFewCols;
+  if (shaped && most <= kShapedCols)
+    while (p.few_cols < most) p.few_cols *= 2;
+  p.few.on = most <= p.few_cols || (B > 1 && (long long)(N - max_rows) * nq <= kFewCols * (B - 1LL));
+  p.many.on = most > p.few_cols;
+  p.few.hi = p.few_cols;
+  p.many.lo = p.few.on ? p.few_cols : 0;
   p.many.hi = INT_MAX;
   auto take = [&](size_t& field, size_t bytes) {
     field = p.total;
@@ -1230,8 +1768,9 @@ AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_
     take(f.part, 2 * (size_t)f.ranges * part_floats(f.cols, hd) * 4);
   };
   const long long pages = (long long)B * H * max_blocks;
-  p.few.cols = (int)std::min<long long>(kFewCols, most);
-  p.few.ranges = (int)std::min<long long>(4LL * kCus, (pages + kFewLeast - 1) / kFewLeast);
+  p.few.cols = (int)std::min<long long>(p.few_cols, most);
+  p.few.ranges = (int)std::min<long long>((p.few_cols <= 32 ? 4LL : 2LL) * kCus,
+                                          (pages + kFewLeast - 1) / kFewLeast);
   p.many.cols = kTileCols;
   p.many.ranges = kCus;
   while ((2 << p.many.log2r) * nq <= kTileCols) ++p.many.log2r;
@@ -1240,56 +1779,92 @@ AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_
   scratch(p.few);
   scratch(p.many);
   if (mass) {
-    take(p.stat, (size_t)H * N * nq * sizeof(float2));
+    take(p.stat, (size_t)H * N * nq * (shaped ? sizeof(Stat<Shape>) : sizeof(Stat<NoShape>)));
     const size_t bytes = (size_t)pages * p.few.cols * kPage * 4;
-    p.scores = p.few.on && bytes <= kScoreBytes;
+    p.scores = p.few.on && p.few_cols == kFewCols && bytes <= kScoreBytes;
     if (p.scores) take(p.score, bytes);
   }
   return p;
 }
+
+Shape shape_of(const CacheScores& a, int hd) {
+  constexpr double kLog2e = 1.4426950408889634;
+  Shape sh{};
+  sh.a = a;
+  sh.scale = (float)(kLog2e / sqrt((double)hd));
+  if (a.cap != 0.f) {
+    const double k = 1.0 / (a.cap * sqrt((double)hd));
+    sh.cap = (float)(a.cap * kLog2e);
+    sh.x_of = (float)k;
+    // (beyond, the squares and coefficients could leave fp32)
+    sh.bound = a.cap >= 0x1p-8f && a.cap <= 0x1p10f ? (float)(kTanhBound / k) : -1.f;
+    for (int i = 0; i < 5; ++i)
+      sh.poly[i] = sh.bound > 0.f ? (float)(a.cap * kLog2e * kTanhPoly[i] * pow(k, 2 * i + 1)) : 0.f;
+  }
+  return sh;
+}
 }  // namespace
 
 size_t cache_attention_scratch_bytes(int H, int B, int N, int nq, int hd, int max_blocks,
-                                     int max_rows, bool mass) {
-  return attn_plan(H, B, N, nq, hd, max_blocks, max_rows, mass).total;
+                                     int max_rows, bool mass, bool shaped) {
+  return attn_plan(H, B, N, nq, hd, max_blocks, max_rows, mass, shaped).total;
 }
 
 hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_rows, const void* q,
                                   const int32_t* row_start, const float* mass_in, float* mass_out,
-                                  void* out, void* scratch, hipStream_t s) {
+                                  void* out, void* scratch, hipStream_t s,
+                                  const CacheScores* scores) {
   const CacheBatch bt{a.H, a.B, N, nq, a.n_pages, a.max_blocks, a.block_table, a.length, row_start};
-  const AttnPlan p = attn_plan(a.H, a.B, N, nq, a.hd, a.max_blocks, max_rows, mass_out != nullptr);
+  const AttnPlan p = attn_plan(a.H, a.B, N, nq, a.hd, a.max_blocks, max_rows, mass_out != nullptr,
+                               scores != nullptr);
   unsigned char* base = static_cast<unsigned char*>(scratch);
-  const float c_log2 = 1.4426950408889634f / sqrtf((float)a.hd);
   const bf16* qb = static_cast<const bf16*>(q);
-  float2* stat = mass_out != nullptr ? reinterpret_cast<float2*>(base + p.stat) : nullptr;
+  void* stat = mass_out != nullptr ? base + p.stat : nullptr;
   float* score = p.scores ? reinterpret_cast<float*>(base + p.score) : nullptr;
+  const Reach reach =
+      scores != nullptr ? Reach{scores->prefix, scores->tree != nullptr} : Reach{nullptr, false};
   auto form = [&](const FormPlan& f, int least, int round, auto few) {
     return Form<decltype(few)::value>{
-        {bt, max_rows, f.log2r, f.lo, f.hi, reinterpret_cast<long long*>(base + f.prefix)},
+        {bt, max_rows, f.log2r, f.lo, f.hi, reach, reinterpret_cast<long long*>(base + f.prefix)},
         {f.ranges, least, round},
         {static_cast<bf16*>(out), stat, reinterpret_cast<float*>(base + f.part), f.cols}};
   };
   const Form<true> few = form(p.few, kFewLeast, std::min(p.few.ranges, 2 * kCus), std::true_type{});
   const Form<false> many = form(p.many, kManyLeast, 0, std::false_type{});
-  auto go = [&](auto hdv) {
+  auto go = [&](auto hdv, auto sh) {
     constexpr int HD = decltype(hdv)::value;
+    using S = decltype(sh);
+    float c_log2 = 1.4426950408889634f / sqrtf((float)a.hd);
+    if constexpr (is_shaped<S>)
+      if (sh.a.cap != 0.f || sh.a.slope != nullptr) c_log2 = 1.f;
     if (p.few.on) {
-      ProfileScope ps("cache_attn_few", s);
-      FOE_LAUNCH(cache_attn_few_kernel<HD>, dim3(few.deal.ranges), dim3(kAttThr), 0, s, qb, a.k,
-                 a.v, a.kv_scale, few.w, few.deal, c_log2, few.o, score);
+      if constexpr (is_shaped<S>) {
+        ProfileScope ps("cache_attn_shaped", s);
+        auto launch = [&](auto kernel) {
+          FOE_LAUNCH(kernel, dim3(few.deal.ranges), dim3(kAttThr), 0, s, qb, a.k, a.v, a.kv_scale,
+                     few.w, few.deal, c_log2, sh, few.o, score);
+        };
+        if (p.few_cols == 16) launch(cache_attn_shaped_kernel<HD, 1, 1>);
+        else if (p.few_cols == 32) launch(cache_attn_shaped_kernel<HD, 2, 1>);
+        else if (p.few_cols == 64) launch(cache_attn_shaped_kernel<HD, 2, 2>);
+        else launch(cache_attn_shaped_kernel<HD, 2, 4>);
+      } else {
+        ProfileScope ps("cache_attn_few", s);
+        FOE_LAUNCH(cache_attn_few_kernel<HD>, dim3(few.deal.ranges), dim3(kAttThr), 0, s, qb, a.k,
+                   a.v, a.kv_scale, few.w, few.deal, c_log2, few.o, score);
+      }
     }
     if (p.many.on) {
       ProfileScope ps("cache_attn_tile", s);
-      FOE_LAUNCH(cache_attn_tile_kernel<HD>, dim3(many.deal.ranges), dim3(kTileThr), 0, s, qb, a.k,
-                 a.v, a.kv_scale, many.w, many.deal, c_log2, many.o);
+      FOE_LAUNCH((cache_attn_tile_kernel<HD, S>), dim3(many.deal.ranges), dim3(kTileThr), 0, s, qb,
+                 a.k, a.v, a.kv_scale, many.w, many.deal, c_log2, sh, many.o);
     }
     {
       ProfileScope ps("cache_join", s);
       const int many_blocks = p.many.on ? p.many.tiles * (kTileCols / kJoinCols) : 0;
       const int few_blocks = p.few.on ? a.B * few.o.part_cols : 0;
-      FOE_LAUNCH(cache_join_kernel<HD>, dim3(many_blocks + few_blocks, a.H), dim3(256), 0, s, few,
-                 many, many_blocks);
+      FOE_LAUNCH((cache_join_kernel<HD, S>), dim3(many_blocks + few_blocks, a.H), dim3(256), 0, s,
+                 few, many, sh, many_blocks);
     }
     if (mass_out != nullptr) {
       ProfileScope ps("cache_mass", s);
@@ -1300,13 +1875,18 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
       const long long pairs = (long long)ceil_div(a.max_blocks, 2) * a.H * a.B;
       const int any_ranges =
           p.many.on || score == nullptr ? (int)std::min(16LL * kCus, pairs) : 0;
-      FOE_LAUNCH(cache_mass_kernel<HD>, dim3(any_ranges + (score != nullptr ? few.deal.ranges : 0)),
-                 dim3(kMassThr), 0, s, qb, a.k, a.kv_scale, any, any_ranges, few, score, c_log2,
-                 stat, mass_in, mass_out);
+      FOE_LAUNCH((cache_mass_kernel<HD, S>),
+                 dim3(any_ranges + (score != nullptr ? few.deal.ranges : 0)), dim3(kMassThr), 0, s,
+                 qb, a.k, a.kv_scale, any, any_ranges, few, score, c_log2, sh,
+                 static_cast<const Stat<S>*>(stat), mass_in, mass_out);
     }
   };
-  if (a.hd == 96) go(std::integral_constant<int, 96>{});
-  else go(std::integral_constant<int, 128>{});
+  auto with = [&](auto sh) {
+    if (a.hd == 96) go(std::integral_constant<int, 96>{}, sh);
+    else go(std::integral_constant<int, 128>{}, sh);
+  };
+  if (scores != nullptr) with(shape_of(*scores, a.hd));
+  else with(NoShape{});
   return hipGetLastError();
 }
 

@@ -1,5 +1,7 @@
 // The 8-bit key/value cache: appending new tokens (rotation and quantisation)
 // and evicting the tokens that received the least attention.
+#include <limits.h>
+
 #include <algorithm>
 
 #include "kv_cache.hpp"
@@ -25,11 +27,15 @@ namespace {
 // and a row's heads one after another 22, so 16.
 constexpr int kAppThr = 256;
 
-template <int HD>
+// With row places of their own (depth, a tree of drafts) a page's positions lie between the
+// least and the largest of its rows' depths, which a tree of up to 64 levels keeps within the
+// same two sets of eight; rows further apart form a sine each.
+template <int HD, bool DEPTH>
 __global__ __launch_bounds__(kAppThr) void cache_append_kernel(
     const bf16* __restrict__ qkv, bf16* __restrict__ q_out, uint8_t* __restrict__ kc,
     uint8_t* __restrict__ vc, float* __restrict__ kv_scale, CacheBatch bt,
-    const int32_t* __restrict__ pos, double log2_theta, double rope_scale) {
+    const int32_t* __restrict__ pos, const int32_t* __restrict__ depth, double log2_theta,
+    double rope_scale) {
   constexpr int NIT = kPage * 16 / kAppThr;  // rows of a thread
   constexpr int VROW = kPage + 4;            // bytes of a value dim's row in LDS
   // (cosine, sine) of pair i at positions first + 8 a (rows 0-7) and b (rows 8-15)
@@ -63,6 +69,21 @@ __global__ __launch_bounds__(kAppThr) void cache_append_kernel(
   auto has = [&](int it) { return act && it * (kAppThr / 16) + rr < cnt; };
   auto some = [&](int it) { return it * (kAppThr / 16) < cnt; };  // (uniform)
   const int uc = act ? u : 0;
+  // depths of the thread's rows; the least and the largest of the page (DEPTH)
+  int dep[NIT], dep_min = 0, dep_max = 0;
+  if constexpr (DEPTH) {
+    auto depth_at = [&](int i) { return min(max(depth[r0 + i0 + i], 0), kMaxDepth); };
+    dep_min = dep_max = depth_at(min(lane_id(), cnt - 1));
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+      dep_min = min(dep_min, __shfl_xor(dep_min, o));
+      dep_max = max(dep_max, __shfl_xor(dep_max, o));
+    }
+#pragma unroll
+    for (int it = 0; it < NIT; ++it)
+      dep[it] = depth_at(min(it * (kAppThr / 16) + rr, cnt - 1)) - dep_min;
+  }
+  const bool wide = DEPTH && dep_max - dep_min >= kPage;  // (uniform)
   bf16x8 v[NIT];
   bf16x4 x1[NIT], x2[NIT];
   auto load_head = [&](int j) {
@@ -101,26 +122,36 @@ __global__ __launch_bounds__(kAppThr) void cache_append_kernel(
     if (page >= 0 && t0 < kPage && touched(t0) && !full(t0))
       beside[k] = *reinterpret_cast<const u32x4*>(vp + i * 16);
   }
-  {
-    const long long first = (pos != nullptr ? pos[b] : c0) + (long long)i0;
+  const long long first = (pos != nullptr ? pos[b] : c0) + (long long)(DEPTH ? dep_min : i0);
+  auto turn_of = [&](long long p, int i) {
     constexpr double kTwoPi = 6.283185307179586476925286766559;
-    const int na = (cnt + 7) / 8, nb = min(cnt, 8);
+    double a = (double)p / rope_scale * inv_freq[i];
+    a -= kTwoPi * floor(a / kTwoPi);
+    float2 t;
+    sincosf((float)a, &t.y, &t.x);
+    return t;
+  };
+  if (!wide) {
+    const int n = DEPTH ? dep_max - dep_min + 1 : cnt, na = (n + 7) / 8, nb = min(n, 8);
     for (int e = tid; e < (na + nb) * (HD / 2); e += kAppThr) {
       const int k = e / (HD / 2), i = e % (HD / 2);
-      double a = (double)(k < na ? first + 8 * k : k - na) / rope_scale * inv_freq[i];
-      a -= kTwoPi * floor(a / kTwoPi);
-      float2 t;
-      sincosf((float)a, &t.y, &t.x);
-      turn[k < na ? k : 8 + k - na][i] = t;
+      turn[k < na ? k : 8 + k - na][i] = turn_of(k < na ? first + 8 * k : k - na, i);
     }
   }
   __syncthreads();
   float cs[NIT][4], sn[NIT][4];
 #pragma unroll
   for (int it = 0; it < NIT; ++it) {
-    const int i = min(it * (kAppThr / 16) + rr, cnt - 1);  // position - first
+    // position - first
+    const int i = DEPTH ? dep[it] : min(it * (kAppThr / 16) + rr, cnt - 1);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
+      if (wide) {
+        const float2 t = turn_of(first + i, 4 * uc + e);
+        cs[it][e] = t.x;
+        sn[it][e] = t.y;
+        continue;
+      }
       const float2 a = turn[i >> 3][4 * uc + e], d = turn[8 + (i & 7)][4 * uc + e];
       cs[it][e] = a.x * d.x - a.y * d.y;
       sn[it][e] = a.y * d.x + a.x * d.y;
@@ -237,6 +268,167 @@ __global__ __launch_bounds__(kAppThr) void cache_append_kernel(
       old[e] = (o & ~fresh) | (x[e] & fresh);
     }
     *w = old;
+  }
+}
+
+// ---- keeping an accepted path ------------------------------------------------------
+// One workgroup per (sequence, group), a page of kept tokens after another.  Kept token j comes
+// from row path[j] >= j, so a page's sources lie in it or behind it, and what one page's step
+// writes no later step reads; within a page everything is read before anything is written.
+// (1) The path's length: its first entry that does not ascend.  (2) The page's 64 slots find
+// their source page and its scales; slots before the context's end are their own.  (3) Keys as
+// rows of 16-byte pieces, values as pieces of one dim and 16 tokens, the moved tokens' bytes
+// put in one by one; the page's new scales follow from the largest magnitudes.  (4) Pieces that
+// changed are stored.
+constexpr int kAccThr = 256;
+
+template <int HD>
+__global__ __launch_bounds__(kAccThr) void cache_accept_kernel(
+    uint8_t* kc, uint8_t* vc, float* kv_scale, float* mass, CacheBatch bt,
+    const int32_t* __restrict__ path, int max_path, int32_t* __restrict__ new_len) {
+  constexpr int CPR = HD / 16;                               // 16-byte pieces of a key row
+  constexpr int NK = (kPage * CPR + kAccThr - 1) / kAccThr;  // pieces of a thread
+  constexpr int NV = ((kPage / kSub) * HD + kAccThr - 1) / kAccThr;
+  __shared__ int end;
+  __shared__ int from[kPage];      // source slot in its page (of 64), by slot
+  __shared__ int from_page[kPage]; // its page, -1: not there
+  __shared__ float2 from_scale[kPage];
+  const int tid = threadIdx.x, b = blockIdx.x, h = blockIdx.y;
+  const int c0 = bt.context(b), rows = min(bt.rows(b), bt.cap() - c0);
+  path += (size_t)b * max_path;
+  if (tid == 0) end = max_path;
+  __syncthreads();
+  for (int i = tid; i < max_path; i += kAccThr) {
+    const int p = path[i], before = i > 0 ? path[i - 1] : -1;
+    if (p <= before || p < 0 || p >= rows) {
+      atomicMin(&end, i);
+      break;
+    }
+  }
+  __syncthreads();
+  const int m = end;
+  if (h == 0 && tid == 0) new_len[b] = c0 + m;
+  if (m == 0) return;
+  for (int blk = c0 / kPage; blk <= (c0 + m - 1) / kPage; ++blk) {
+    const int lo = max(c0 - blk * kPage, 0), hi = min(c0 + m - blk * kPage, kPage);
+    const int page = bt.page(b, blk);
+    if (page < 0) continue;  // (uniform) nowhere to keep them
+    __syncthreads();         // the last page's slots have been read
+    if (tid < kPage) {
+      int p = page, t = tid;
+      if (tid >= lo && tid < hi) {
+        const int slot = c0 + path[blk * kPage + tid - c0];
+        p = bt.page(b, slot / kPage);
+        t = slot % kPage;
+      }
+      from[tid] = t;
+      from_page[tid] = p;
+      from_scale[tid] =
+          p >= 0 ? *reinterpret_cast<const float2*>(kv_scale + ((size_t)p * bt.H + h) * 2)
+                 : float2{0.f, 0.f};
+    }
+    __syncthreads();
+    const size_t own = (size_t)page * bt.H + h;
+    auto moved = [&](int t) { return t >= lo && t < hi && (from_page[t] != page || from[t] != t); };
+    u32x4 k[NK], v[NV];
+    float2 amax{0.f, 0.f};
+    auto bigger = [](float a, uint32_t w) {  // (NaN counts for no scale)
+      const float x = fmaxf(fabsf(__builtin_amdgcn_cvt_f32_fp8(w, 0)),
+                            fabsf(__builtin_amdgcn_cvt_f32_fp8(w, 1)));
+      const float y = fmaxf(fabsf(__builtin_amdgcn_cvt_f32_fp8(w, 2)),
+                            fabsf(__builtin_amdgcn_cvt_f32_fp8(w, 3)));
+      return fmaxf(a, fmaxf(x, y));
+    };
+#pragma unroll
+    for (int n = 0; n < NK; ++n) {
+      const int i = n * kAccThr + tid, t = i / CPR;
+      k[n] = zero_u32x4();
+      if (t < hi && from_page[t] >= 0)
+        k[n] = *reinterpret_cast<const u32x4*>(
+            kc + (((size_t)from_page[t] * bt.H + h) * kPage + from[t]) * HD + i % CPR * 16);
+    }
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      const int i = n * kAccThr + tid, d = i % HD, t0 = i / HD * kSub;
+      v[n] = zero_u32x4();
+      if (t0 >= hi) continue;
+      v[n] = *reinterpret_cast<const u32x4*>(vc + own * (kPage * HD) + i * 16);
+#pragma unroll
+      for (int e = 0; e < kSub; ++e) {
+        const int t = t0 + e, p = from_page[t];
+        if (!moved(t)) continue;
+        uint32_t x = 0;
+        if (p >= 0)
+          x = vc[((size_t)p * bt.H + h) * (kPage * HD) + from[t] / kSub * (HD * kSub) + d * kSub +
+                 from[t] % kSub];
+        v[n][e / 4] = (v[n][e / 4] & ~(0xffu << (8 * (e % 4)))) | x << (8 * (e % 4));
+      }
+    }
+    float w = 0.f;
+    if (mass != nullptr && tid < kPage && moved(tid) && from_page[tid] >= 0)
+      w = mass[((size_t)from_page[tid] * bt.H + h) * kPage + from[tid]];
+#pragma unroll
+    for (int n = 0; n < NK; ++n) {
+      const int t = (n * kAccThr + tid) / CPR;
+      if (t >= hi) continue;
+      float x = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x = bigger(x, k[n][e]);
+      amax.x = fmaxf(amax.x, x * from_scale[t].x);
+    }
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      const int t0 = (n * kAccThr + tid) / HD * kSub;
+      if (t0 >= hi) continue;
+#pragma unroll
+      for (int e = 0; e < kSub; ++e) {
+        if (t0 + e >= hi) continue;
+        const float x = fabsf(__builtin_amdgcn_cvt_f32_fp8(v[n][e / 4] >> (8 * (e % 4)), 0));
+        amax.y = fmaxf(amax.y, x * from_scale[t0 + e].y);
+      }
+    }
+    amax = block_max<kAccThr>(amax);  // (and everything has been read)
+    const float ks = block_scale(amax.x), vs = block_scale(amax.y);
+    const float ki = pow2_inv(ks), vi = pow2_inv(vs);
+    if (tid == 0) *reinterpret_cast<float2*>(kv_scale + own * 2) = float2{ks, vs};
+    if (mass != nullptr && tid < kPage && moved(tid)) mass[own * kPage + tid] = w;
+#pragma unroll
+    for (int n = 0; n < NK; ++n) {
+      const int i = n * kAccThr + tid, t = i / CPR;
+      if (t >= hi) continue;
+      const float r = scale_ratio(from_scale[t].x, ki);
+      if (r == 1.f && !moved(t)) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) k[n][e] = rescale4(k[n][e], r);
+      *reinterpret_cast<u32x4*>(kc + own * (kPage * HD) + i * 16) = k[n];
+    }
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      const int i = n * kAccThr + tid, t0 = i / HD * kSub;
+      if (t0 >= hi) continue;
+      bool changed = false;
+#pragma unroll
+      for (int e = 0; e < kSub; e += 4) {
+        uint32_t fresh = 0;
+        float r[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int t = t0 + e + x;
+          const bool in = t < hi;
+          r[x] = in ? scale_ratio(from_scale[t].y, vi) : 1.f;
+          if (in && (r[x] != 1.f || moved(t))) fresh |= 0xffu << (8 * x);
+        }
+        if (fresh == 0) continue;
+        changed = true;
+        const uint32_t o = v[n][e / 4];
+        const uint32_t y = to_codes4(__builtin_amdgcn_cvt_f32_fp8(o, 0) * r[0],
+                                     __builtin_amdgcn_cvt_f32_fp8(o, 1) * r[1],
+                                     __builtin_amdgcn_cvt_f32_fp8(o, 2) * r[2],
+                                     __builtin_amdgcn_cvt_f32_fp8(o, 3) * r[3]);
+        v[n][e / 4] = (o & ~fresh) | (y & fresh);
+      }
+      if (changed) *reinterpret_cast<u32x4*>(vc + own * (kPage * HD) + i * 16) = v[n];
+    }
   }
 }
 
@@ -696,8 +888,8 @@ __global__ __launch_bounds__(kMoveThr, 8) void cache_move_kernel(
 }  // namespace
 
 hipError_t launch_cache_append(const CacheArgs& a, int nq, int N, const void* qkv, void* q,
-                               const int32_t* row_start, const int32_t* pos, float theta,
-                               float scale, hipStream_t s) {
+                               const int32_t* row_start, const int32_t* pos, const int32_t* depth,
+                               float theta, float scale, hipStream_t s) {
   const CacheBatch bt{a.H, a.B, N, nq, a.n_pages, a.max_blocks, a.block_table, a.length, row_start};
   // pages that n rows touch: at most (n + 62) / 64 + 1, and n
   const long long tiles = std::min<long long>(N, ((long long)N + 62LL * a.B) / kPage + a.B);
@@ -705,10 +897,24 @@ hipError_t launch_cache_append(const CacheArgs& a, int nq, int N, const void* qk
   auto go = [&](auto kern) {
     FOE_LAUNCH(kern, dim3((unsigned)tiles, a.H), dim3(kAppThr), 0, s,
                static_cast<const bf16*>(qkv), static_cast<bf16*>(q), a.k, a.v, a.kv_scale, bt, pos,
-               log2((double)theta), (double)scale);
+               depth, log2((double)theta), (double)scale);
   };
-  if (a.hd == 96) go(cache_append_kernel<96>);
-  else go(cache_append_kernel<128>);
+  if (depth != nullptr) go(a.hd == 96 ? cache_append_kernel<96, true> : cache_append_kernel<128, true>);
+  else go(a.hd == 96 ? cache_append_kernel<96, false> : cache_append_kernel<128, false>);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_accept(const CacheArgs& a, const int32_t* row_start, const int32_t* path,
+                               int max_path, float* mass, int32_t* new_len, hipStream_t s) {
+  const CacheBatch bt{a.H, a.B, INT_MAX, 1, a.n_pages, a.max_blocks, a.block_table, a.length,
+                      row_start};
+  ProfileScope ps("cache_accept", s);
+  auto go = [&](auto kern) {
+    FOE_LAUNCH(kern, dim3(a.B, a.H), dim3(kAccThr), 0, s, a.k, a.v, a.kv_scale, mass, bt, path,
+               max_path, new_len);
+  };
+  if (a.hd == 96) go(cache_accept_kernel<96>);
+  else go(cache_accept_kernel<128>);
   return hipGetLastError();
 }
 

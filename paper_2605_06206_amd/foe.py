@@ -53,6 +53,11 @@ _SIGNATURES = {
                                      _c_float, _p, _p, _p, _p, _p, _c_size, _p]),
     "foe_group_attention_workspace_bytes": (_c_size, [_c_int, _c_int, _c_int, _c_int, _c_int]),
     "foe_cache_append": (_c_int, [_c_int] * 8 + [_c_float] * 2 + [_p] * 10),
+    "foe_cache_append_tree": (_c_int, [_c_int] * 8 + [_c_float] * 2 + [_p] * 11),
+    "foe_cache_attention_ex": (_c_int, [_c_int] * 9 + [_c_float] + [_p] * 3 + [_c_int] + [_p] * 11 +
+                               [_p, _c_size, _p]),
+    "foe_cache_attention_ex_workspace_bytes": (_c_size, [_c_int] * 8),
+    "foe_cache_accept": (_c_int, [_c_int] * 6 + [_p] * 10),
     "foe_cache_attention": (_c_int, [_c_int] * 9 + [_p] * 10 + [_p, _c_size, _p]),
     "foe_cache_attention_workspace_bytes": (_c_size, [_c_int] * 8),
     "foe_cache_evict": (_c_int, [_c_int] * 7 + [_p] * 3 + [_c_int] + [_p] * 7 +
@@ -385,69 +390,112 @@ def _size(n, name):
 
 
 def cache_append(qkv, k, v, kv_scale, block_table, ctx_len, row_start, theta, scale=1.0, pos=None,
-                 q=None, stream=None):
-    """foe_cache_append: qkv [H,N,nq+2,hd] into the pages of block_table
-    [B,max_blocks]; returns the rotated queries [H,N,nq,hd]."""
+                 q=None, stream=None, depth=None):
+    """foe_cache_append, or foe_cache_append_tree with ``depth`` [N]: qkv
+    [H,N,nq+2,hd] into the pages of block_table [B,max_blocks]; returns the rotated
+    queries [H,N,nq,hd]."""
     if _elsewhere(qkv, stream):
         with _on(qkv.device, stream):
             return cache_append(qkv, k, v, kv_scale, block_table, ctx_len, row_start, theta, scale,
-                                pos, q)
+                                pos, q, depth=depth)
     n_pages, H, _, hd = k.shape
     N, nq = qkv.shape[1], qkv.shape[2] - 2
     B, max_blocks = block_table.shape
     dev, i32, dt = qkv.get_device(), torch.int32, _dt(qkv)
     if q is None:
         q = torch.empty((H, N, nq, hd), dtype=qkv.dtype, device=qkv.device)
-    rc = lib().foe_cache_append(
-        dt, H, B, N, nq, hd, n_pages, max_blocks, theta, scale,
-        _arg(qkv, "qkv", qkv.dtype, (H, N, nq + 2, hd), dev),
-        _arg(row_start, "row_start", i32, (B + 1,), dev), _arg(ctx_len, "ctx_len", i32, (B,), dev),
-        None if pos is None else _arg(pos, "pos", i32, (B,), dev),
-        _arg(block_table, "block_table", i32, (B, max_blocks), dev),
-        _arg(q, "q", qkv.dtype, (H, N, nq, hd), dev),
-        *_pool_args(k, v, kv_scale, n_pages, H, hd, dev), _stream_of(dev))
-    _check(rc, "foe_cache_append")
+    sizes = (dt, H, B, N, nq, hd, n_pages, max_blocks, theta, scale,
+             _arg(qkv, "qkv", qkv.dtype, (H, N, nq + 2, hd), dev),
+             _arg(row_start, "row_start", i32, (B + 1,), dev),
+             _arg(ctx_len, "ctx_len", i32, (B,), dev),
+             None if pos is None else _arg(pos, "pos", i32, (B,), dev))
+    rest = (_arg(block_table, "block_table", i32, (B, max_blocks), dev),
+            _arg(q, "q", qkv.dtype, (H, N, nq, hd), dev),
+            *_pool_args(k, v, kv_scale, n_pages, H, hd, dev), _stream_of(dev))
+    if depth is None:
+        _check(lib().foe_cache_append(*sizes, *rest), "foe_cache_append")
+    else:
+        depth = _arg(depth, "depth", i32, (N,), dev)
+        _check(lib().foe_cache_append_tree(*sizes, depth, *rest), "foe_cache_append_tree")
     return q
 
 
-def cache_attention_workspace_bytes(q, block_table, max_rows, with_mass=False):
-    """Workspace bytes of cache_attention for these tensors."""
+def cache_attention_workspace_bytes(q, block_table, max_rows, with_mass=False, shaped=False):
+    """Workspace bytes of cache_attention for these tensors (``shaped``: with any of cap,
+    slope, prefix, tree, depth)."""
     H, N, nq, hd = q.shape
     B, max_blocks = block_table.shape
-    return _size(lib().foe_cache_attention_workspace_bytes(H, B, N, nq, hd, max_blocks, max_rows,
-                                                           1 if with_mass else 0),
-                 "foe_cache_attention_workspace_bytes")
+    name = f"foe_cache_attention{'_ex' if shaped else ''}_workspace_bytes"
+    return _size(getattr(lib(), name)(H, B, N, nq, hd, max_blocks, max_rows,
+                                      1 if with_mass else 0), name)
 
 
 def cache_attention(q, k, v, kv_scale, block_table, ctx_len, row_start, max_rows, mass_in=None,
-                    mass_out=None, out=None, ws=None, stream=None):
-    """foe_cache_attention: q [H,N,nq,hd] over the pages of block_table; returns
-    out [N,H,nq,hd]."""
+                    mass_out=None, out=None, ws=None, stream=None, cap=0.0, slope=None,
+                    prefix=None, tree=None, depth=None):
+    """foe_cache_attention, or foe_cache_attention_ex with any of ``cap``, ``slope``
+    [H,nq], ``prefix`` [B], ``tree`` [N,words] and ``depth`` [N]: q [H,N,nq,hd] over the
+    pages of block_table; returns out [N,H,nq,hd]."""
     if _elsewhere(q, stream):
         with _on(q.device, stream):
             return cache_attention(q, k, v, kv_scale, block_table, ctx_len, row_start, max_rows,
-                                   mass_in, mass_out, out, ws)
+                                   mass_in, mass_out, out, ws, None, cap, slope, prefix, tree,
+                                   depth)
     n_pages, H, _, hd = k.shape
     N, nq = q.shape[1], q.shape[2]
     B, max_blocks = block_table.shape
     dev, i32, f32, dt = q.get_device(), torch.int32, torch.float32, _dt(q)
+    shaped = bool(cap) or not (slope is None and prefix is None and tree is None and depth is None)
     mshape = (n_pages, H, CACHE_PAGE)
     if out is None:
         out = torch.empty((N, H, nq, hd), dtype=q.dtype, device=q.device)
     ws, ws_ptr, ws_bytes = _ws_arg(
         ws, lambda: cache_attention_workspace_bytes(q, block_table, max_rows,
-                                                    mass_out is not None), q.device, dev)
-    rc = lib().foe_cache_attention(
-        dt, H, B, N, nq, hd, n_pages, max_blocks, max_rows,
-        _arg(q, "q", q.dtype, (H, N, nq, hd), dev),
+                                                    mass_out is not None, shaped), q.device, dev)
+    sizes = (dt, H, B, N, nq, hd, n_pages, max_blocks, max_rows)
+    rest = (_arg(q, "q", q.dtype, (H, N, nq, hd), dev),
+            _arg(row_start, "row_start", i32, (B + 1,), dev),
+            _arg(ctx_len, "ctx_len", i32, (B,), dev),
+            _arg(block_table, "block_table", i32, (B, max_blocks), dev),
+            *_pool_args(k, v, kv_scale, n_pages, H, hd, dev),
+            None if mass_in is None else _arg(mass_in, "mass_in", f32, mshape, dev),
+            None if mass_out is None else _arg(mass_out, "mass_out", f32, mshape, dev),
+            _arg(out, "out", q.dtype, (N, H, nq, hd), dev), ws_ptr, ws_bytes, _stream_of(dev))
+    if not shaped:
+        _check(lib().foe_cache_attention(*sizes, *rest), "foe_cache_attention")
+        return out
+    words = 0 if tree is None else tree.shape[-1]
+    shape = (cap, None if slope is None else _arg(slope, "slope", f32, (H, nq), dev),
+             None if prefix is None else _arg(prefix, "prefix", i32, (B,), dev),
+             None if tree is None else _arg(tree, "tree", i32, (N, words), dev), words,
+             None if depth is None else _arg(depth, "depth", i32, (N,), dev))
+    _check(lib().foe_cache_attention_ex(*sizes, *shape, *rest), "foe_cache_attention_ex")
+    return out
+
+
+def cache_accept(k, v, kv_scale, block_table, ctx_len, row_start, path, mass=None, new_len=None,
+                 stream=None):
+    """foe_cache_accept: keeps the rows of ``path`` [B,n]; returns new_len [B]."""
+    if _elsewhere(k, stream):
+        with _on(k.device, stream):
+            return cache_accept(k, v, kv_scale, block_table, ctx_len, row_start, path, mass,
+                                new_len)
+    n_pages, H, _, hd = k.shape
+    B, max_blocks = block_table.shape
+    dev, i32 = k.get_device(), torch.int32
+    max_path = path.shape[-1]
+    if new_len is None:
+        new_len = torch.empty((B,), dtype=i32, device=k.device)
+    rc = lib().foe_cache_accept(
+        H, B, hd, n_pages, max_blocks, max_path,
         _arg(row_start, "row_start", i32, (B + 1,), dev), _arg(ctx_len, "ctx_len", i32, (B,), dev),
+        _arg(path, "path", i32, (B, max_path), dev),
         _arg(block_table, "block_table", i32, (B, max_blocks), dev),
         *_pool_args(k, v, kv_scale, n_pages, H, hd, dev),
-        None if mass_in is None else _arg(mass_in, "mass_in", f32, mshape, dev),
-        None if mass_out is None else _arg(mass_out, "mass_out", f32, mshape, dev),
-        _arg(out, "out", q.dtype, (N, H, nq, hd), dev), ws_ptr, ws_bytes, _stream_of(dev))
-    _check(rc, "foe_cache_attention")
-    return out
+        None if mass is None else _arg(mass, "mass", torch.float32, (n_pages, H, CACHE_PAGE), dev),
+        _arg(new_len, "new_len", i32, (B,), dev), _stream_of(dev))
+    _check(rc, "foe_cache_accept")
+    return new_len
 
 
 def cache_evict_workspace_bytes(block_table, H):
