@@ -226,7 +226,8 @@ struct Reach {
 // The units of a batch in a form, numbered by sequence, group, tile and page.  A tile of
 // many columns has 2^log2r rows, tile t reaches page ceil((ctx + last row + 1) / 64), and
 // the sums over tiles are closed forms (which count pages past the table's end too).
-template <bool FEW>
+// (WIDE: rows may see past themselves, see Reach.)
+template <bool FEW, bool WIDE = false>
 struct Units {
   CacheBatch bt;
   int max_rows;
@@ -243,11 +244,11 @@ struct Units {
   __device__ __forceinline__ int tiles(int n) const { return (n + (1 << log2r) - 1) >> log2r; }
   // pages that every tile of sequence b reaches, if its rows are not causal alone
   __device__ __forceinline__ int least(int b, int ctx, int n) const {
-    return FEW ? 0 : reach.pages(bt, b, ctx, n);
+    return WIDE && !FEW ? reach.pages(bt, b, ctx, n) : 0;
   }
   // pages of the tiles before tile t (t < tiles), all of them at least `least`
   __device__ __forceinline__ long long before(int ctx, int t, int least) const {
-    if (least == 0) return causal_before(ctx, t);
+    if (!WIDE || least == 0) return causal_before(ctx, t);
     // the tiles whose own pages are no more than that
     const long long j = max(((long long)least * kPage - ctx) >> log2r, 0LL);
     if (t <= j) return (long long)t * least;
@@ -268,7 +269,8 @@ struct Units {
   // pages of tile t of a sequence with n rows
   __device__ __forceinline__ int pages(int ctx, int n, int t, int least) const {
     if (FEW) return min((ctx + n + kPage - 1) / kPage, bt.max_blocks);
-    return max((ctx + min((t + 1) << log2r, n) + kPage - 1) / kPage, least);
+    const int np = (ctx + min((t + 1) << log2r, n) + kPage - 1) / kPage;
+    return WIDE ? max(np, least) : np;
   }
   // units of one group of sequence b
   __device__ __forceinline__ long long group(int b) const {
@@ -924,7 +926,7 @@ template <int HD, typename S>
 __global__ __launch_bounds__(kTileThr) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ kc,
                        const uint8_t* __restrict__ vc, const float* __restrict__ kv_scale,
-                       Units<false> w, Deal deal, float c_log2, S sh, AttnOut o) {
+                       Units<false, is_shaped<S>> w, Deal deal, float c_log2, S sh, AttnOut o) {
   constexpr bool SHAPED = is_shaped<S>;
   constexpr int KT = kPage * 256;       // K tile bytes
   constexpr int VT = HD * kPage * 2;    // V^T tile bytes
@@ -974,19 +976,19 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
 
   // staging: thread -> 16 bytes of a key row, and 16 tokens of a value dim
   const bool stages = tid < kPage * CPR;
-  struct Places {
-    int vg;
-    uint32_t k0, k1, v0, v1;
-  };
-  auto places = [](int i) {
-    const int krow = i / CPR, kch = i % CPR, vg = i / HD, vd = i % HD;
+  int vg;
+  uint32_t ks0, ks1, vs0, vs1;
+  auto places = [&](int i) {
+    const int krow = i / CPR, kch = i % CPR, vd = i % HD;
+    vg = i / HD;
     const uint32_t kdst = krow * 256, vdst = vd * (kPage * 2);
+    ks0 = kdst + (((2 * kch) ^ (krow & 15)) << 4);
+    ks1 = kdst + (((2 * kch + 1) ^ (krow & 15)) << 4);
     const int vsw = (vd & 7) ^ ((vd >> 3) & 1);
-    return Places{vg, kdst + (((2 * kch) ^ (krow & 15)) << 4),
-                  kdst + (((2 * kch + 1) ^ (krow & 15)) << 4), vdst + (((2 * vg) ^ vsw) << 4),
-                  vdst + (((2 * vg + 1) ^ vsw) << 4)};
+    vs0 = vdst + (((2 * vg) ^ vsw) << 4);
+    vs1 = vdst + (((2 * vg + 1) ^ vsw) << 4);
   };
-  const Places mine = places(tid);
+  places(tid);
   // (formed again where they are used, if a Shape's values need the registers)
   auto fresh = [&](int x) { return SHAPED ? opaque_int(x) : x; };
 
@@ -1048,7 +1050,7 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
       }
     };
     auto stage = [&](int i, int blk, float ks, float vs) {  // i-th page of the segment
-      const auto [vg, ks0, ks1, vs0, vs1] = SHAPED ? places(opaque_int(tid)) : mine;
+      if constexpr (SHAPED) places(opaque_int(tid));
       if ((blk + 1) * kPage > len) {  // slots past the last token hold anything
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -1199,9 +1201,14 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
     rescale();
     pv(smem + 2 * KT + ((niter + 2) % 3) * VT);
 
-    const auto lsw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run),
-                                                      false, false);
-    const float l = __uint_as_float(lsw[0]) + __uint_as_float(lsw[1]);
+    float l;
+    if constexpr (SHAPED) {  // (the lane's number of the shuffle would be held over the pages)
+      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run),
+                                                       __float_as_uint(l_run), false, false);
+      l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    } else {
+      l = l_run + __shfl_xor(l_run, 32);
+    }
     const bool whole = blk0 == 0 && blk1 == np;
     const int ec = fresh(col), eh = fresh(hl);
     if (ec < ncol) {
@@ -1268,8 +1275,8 @@ struct Parts {
   }
 };
 // units u0 .. u0 + np - 1 of the tile; false where one range wrote it whole
-template <bool FEW>
-__device__ __forceinline__ bool find_parts(const Units<FEW>& w, const Deal& deal, long long u0,
+template <bool FEW, bool WIDE>
+__device__ __forceinline__ bool find_parts(const Units<FEW, WIDE>& w, const Deal& deal, long long u0,
                                            int np, Parts& p) {
   const long long per = deal.per(w.prefix[w.bt.B]);
   p.r0 = (int)(u0 / per);
@@ -1340,8 +1347,8 @@ __device__ __forceinline__ void join_few(const Units<true>& w, const Deal& deal,
 constexpr int kJoinCols = 32;
 
 template <int HD, typename S>
-__device__ __forceinline__ void join_tile(const Units<false>& w, const Deal& deal, const S& sh,
-                                          const AttnOut& o, int h, int x32) {
+__device__ __forceinline__ void join_tile(const Units<false, is_shaped<S>>& w, const Deal& deal,
+                                          const S& sh, const AttnOut& o, int h, int x32) {
   constexpr int CB = kTileCols / kJoinCols, NV = HD / 32, AT_ONCE = 4;
   const CacheBatch& bt = w.bt;
   int b, t;
@@ -1407,9 +1414,9 @@ __device__ __forceinline__ void join_tile(const Units<false>& w, const Deal& dea
 }
 
 // What a form's launches share: its units, how they are dealt out, and where it writes.
-template <bool FEW>
+template <bool FEW, bool WIDE = false>
 struct Form {
-  Units<FEW> w;
+  Units<FEW, WIDE> w;
   Deal deal;
   AttnOut o;
 };
@@ -1417,7 +1424,8 @@ struct Form {
 // One launch joins both forms' parts: `many_blocks` by H workgroups those of tiles, the rest
 // those of few columns.
 template <int HD, typename S>
-__global__ __launch_bounds__(256) void cache_join_kernel(Form<true> few, Form<false> many, S sh,
+__global__ __launch_bounds__(256) void cache_join_kernel(Form<true> few,
+                                                         Form<false, is_shaped<S>> many, S sh,
                                                          int many_blocks) {
   const int x = blockIdx.x, h = blockIdx.y;
   if (x < many_blocks) join_tile<HD>(many.w, many.deal, sh, many.o, h, x);
@@ -1518,8 +1526,9 @@ constexpr int kMassStages = 4;
 
 template <int HD, typename S>
 __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8_t* __restrict__ kc,
-                                         const float* __restrict__ kv_scale, const Units<false>& w,
-                                         const Deal& deal, int range, float c_log2, const S& sh,
+                                         const float* __restrict__ kv_scale,
+                                         const Units<false, is_shaped<S>>& w, const Deal& deal,
+                                         int range, float c_log2, const S& sh,
                                          const Stat<S>* __restrict__ stat,
                                          const float* __restrict__ mass_in,
                                          float* __restrict__ mass_out) {
@@ -1706,7 +1715,7 @@ __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8
 template <int HD, typename S>
 __global__ __launch_bounds__(kMassThr, is_shaped<S> ? 3 : 4) void cache_mass_kernel(
     const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const float* __restrict__ kv_scale,
-    Units<false> any, int any_ranges, Form<true> few, const float* __restrict__ score, float c_log2,
+    Units<false, is_shaped<S>> any, int any_ranges, Form<true> few, const float* __restrict__ score, float c_log2,
     S sh, const Stat<S>* __restrict__ stat, const float* __restrict__ mass_in,
     float* __restrict__ mass_out) {
   static_assert(kMassThr == kAttThr, "one workgroup size");
@@ -1823,17 +1832,19 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
   float* score = p.scores ? reinterpret_cast<float*>(base + p.score) : nullptr;
   const Reach reach =
       scores != nullptr ? Reach{scores->prefix, scores->tree != nullptr} : Reach{nullptr, false};
-  auto form = [&](const FormPlan& f, int least, int round, auto few) {
-    return Form<decltype(few)::value>{
+  auto form = [&](const FormPlan& f, int least, int round, auto few, auto wide) {
+    return Form<decltype(few)::value, decltype(wide)::value>{
         {bt, max_rows, f.log2r, f.lo, f.hi, reach, reinterpret_cast<long long*>(base + f.prefix)},
         {f.ranges, least, round},
         {static_cast<bf16*>(out), stat, reinterpret_cast<float*>(base + f.part), f.cols}};
   };
-  const Form<true> few = form(p.few, kFewLeast, std::min(p.few.ranges, 2 * kCus), std::true_type{});
-  const Form<false> many = form(p.many, kManyLeast, 0, std::false_type{});
+  const Form<true> few = form(p.few, kFewLeast, std::min(p.few.ranges, 2 * kCus), std::true_type{},
+                              std::false_type{});
   auto go = [&](auto hdv, auto sh) {
     constexpr int HD = decltype(hdv)::value;
     using S = decltype(sh);
+    const auto many = form(p.many, kManyLeast, 0, std::false_type{},
+                           std::integral_constant<bool, is_shaped<S>>{});
     float c_log2 = 1.4426950408889634f / sqrtf((float)a.hd);
     if constexpr (is_shaped<S>)
       if (sh.a.cap != 0.f || sh.a.slope != nullptr) c_log2 = 1.f;
@@ -1870,7 +1881,7 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
       ProfileScope ps("cache_mass", s);
       // without scores the sequences of both forms; at most 16 workgroups a CU: four rounds,
       // which evens out what pages near a chunk's end have less to do
-      Units<false> any = many.w;
+      auto any = many.w;
       if (score == nullptr) any.lo = 0;
       const long long pairs = (long long)ceil_div(a.max_blocks, 2) * a.H * a.B;
       const int any_ranges =
