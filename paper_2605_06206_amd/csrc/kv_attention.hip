@@ -68,18 +68,21 @@ __device__ __forceinline__ float2 column_stat(float m, float inv) {
 // transformed where the matrix instructions leave them, before the maximum, so that what
 // follows is the same as without.  With a cap or a bias they are then in units of log2 e (and
 // c_log2 is 1), else as they were.
+// (TRANSFORMS: with a cap or a bias; masks alone leave the kernels more registers.)
+template <bool TRANSFORMS>
 struct Shape {
+  static constexpr bool kTransforms = TRANSFORMS;
   CacheScores a;
   float scale;            // log2 e / sqrt(hd)
   float cap, x_of;        // cap * log2 e; 1 / (cap * sqrt(hd))
   float bound, poly[5];   // |s| <= bound: the capped score is s * (poly in s^2)
-
-  __device__ __forceinline__ bool transforms() const { return cap != 0.f || a.slope != nullptr; }
 };
 
-struct NoShape {};  // causal, scores as they are
+struct NoShape {  // causal, scores as they are
+  static constexpr bool kTransforms = false;
+};
 template <typename S>
-constexpr bool is_shaped = std::is_same<S, Shape>::value;
+constexpr bool is_shaped = !std::is_same<S, NoShape>::value;
 // what the mass needs of a column (see put_stat)
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 template <typename S>
@@ -87,8 +90,9 @@ using Stat = typename std::conditional<is_shaped<S>, f32x4, f32x2>::type;
 
 // Tokens from the first on that row i and those behind it see, whose distances are place - key
 // and not negative.
-__device__ __forceinline__ int plain_tokens(const Shape& sh, int ctx, int i) {
-  return sh.a.tree != nullptr || sh.a.depth != nullptr ? ctx : ctx + i + 1;
+template <bool T>
+__device__ __forceinline__ int plain_tokens(const Shape<T>& sh, int ctx, int i) {
+  return sh.a.tree != nullptr || (T && sh.a.depth != nullptr) ? ctx : ctx + i + 1;
 }
 __device__ __forceinline__ int plain_tokens(const NoShape&, int ctx, int i) {
   return ctx + i + 1;
@@ -103,23 +107,24 @@ constexpr double kTanhPoly[5] = {0.99999993, -0.33332308, 0.13310172, -0.0521014
 struct Column {
   float slope;  // times log2 e
   int place;    // in its sequence
-  int row;      // of the sequence's new rows
 };
 
 // Column c (of ncol; row c / nq, head c % nq) of sequence b, group h.
-__device__ __forceinline__ Column column_of(const Shape& sh, const CacheBatch& bt, int b, int h,
+template <bool T>
+__device__ __forceinline__ Column column_of(const Shape<T>& sh, const CacheBatch& bt, int b, int h,
                                             int ctx, int c, int ncol) {
-  Column k{0.f, ctx, 0};
-  if (c >= ncol) return k;
-  k.row = c / bt.nq;
-  k.place = ctx + (sh.a.depth != nullptr ? sh.a.depth_of(bt.first_row(b) + k.row) : k.row);
+  Column k{0.f, ctx};
+  if (!T || c >= ncol) return k;
+  const int row = c / bt.nq;
+  k.place = ctx + (sh.a.depth != nullptr ? sh.a.depth_of(bt.first_row(b) + row) : row);
   if (sh.a.slope != nullptr)
-    k.slope = sh.a.slope[h * bt.nq + c - k.row * bt.nq] * 1.4426950408889634f;
+    k.slope = sh.a.slope[h * bt.nq + c - row * bt.nq] * 1.4426950408889634f;
   return k;
 }
 
 // The keys of page blk that the column sees, a bit each.
-__device__ __forceinline__ uint64_t keys_seen(const Shape& sh, const CacheBatch& bt, int b,
+template <bool T>
+__device__ __forceinline__ uint64_t keys_seen(const Shape<T>& sh, const CacheBatch& bt, int b,
                                               int row, int ctx, int len, int blk) {
   auto first = [](int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; };
   const int key0 = blk * kPage;
@@ -146,11 +151,11 @@ __device__ __forceinline__ uint64_t keys_seen(const Shape& sh, const CacheBatch&
 // NE scores of a lane (get, set) at keys key0 + off(i), in place.  `all`: the column sees them
 // all and none is a new row; else those outside `sees` (bit of key key0 + off(i): off(i)) are
 // taken out.
-template <int NE, typename Get, typename Set, typename Off>
-__device__ __forceinline__ void shape_scores(const Shape& sh, const CacheBatch& bt, int b, int ctx,
+template <int NE, bool T, typename Get, typename Set, typename Off>
+__device__ __forceinline__ void shape_scores(const Shape<T>& sh, const CacheBatch& bt, int b, int ctx,
                                              int rows, const Column& c, int key0, bool all,
                                              uint64_t sees, Get get, Set set, Off off) {
-  if (sh.cap != 0.f) {
+  if (T && sh.cap != 0.f) {
     float big = 0.f;
 #pragma unroll
     for (int i = 0; i < NE; ++i) big = fmaxf(big, fabsf(get(i)));
@@ -180,11 +185,11 @@ __device__ __forceinline__ void shape_scores(const Shape& sh, const CacheBatch& 
         set(i, sh.cap * (fabsf(x) > kTanhBound ? far : x * y));
       }
     }
-  } else if (sh.a.slope != nullptr) {
+  } else if (T && sh.a.slope != nullptr) {
 #pragma unroll
     for (int i = 0; i < NE; ++i) set(i, get(i) * sh.scale);
   }
-  if (sh.a.slope != nullptr) {
+  if (T && sh.a.slope != nullptr) {
     if (!all && sh.a.depth != nullptr) {
       const int row0 = bt.first_row(b);
 #pragma unroll
@@ -442,7 +447,8 @@ __device__ __forceinline__ void put_stat(const NoShape&, const CacheBatch&, int,
   const float2 z = column_stat(m, inv);
   static_cast<f32x2*>(o.stat)[at] = f32x2{z.x, z.y};
 }
-__device__ __forceinline__ void put_stat(const Shape& sh, const CacheBatch& bt, int b, int h,
+template <bool T>
+__device__ __forceinline__ void put_stat(const Shape<T>& sh, const CacheBatch& bt, int b, int h,
                                          int ctx, int rows, int c, size_t at, const AttnOut& o,
                                          float m, float inv) {
   const Column k = column_of(sh, bt, b, h, ctx, c, rows * bt.nq);
@@ -616,44 +622,52 @@ __device__ __forceinline__ void few_columns(
   }
 }
 
-// Walks the segments of a range of the few-column form: segment(b, h, rows, ctx, np, blk0,
-// blk1, slot, unit) for each (sequence, group) that the workgroup has pages of.
-template <typename F>
-__device__ __forceinline__ void few_walk(const Units<true>& w, const Deal& deal, F segment) {
-  const CacheBatch& bt = w.bt;
-  long long total, off;
-  int b;
-  locate<kAttThr>(
-      bt.B, [&](int i) { return w.group(i) * bt.H; }, deal, blockIdx.x, w.prefix, total, b, off);
-  if (b < 0) return;
-  // (at most 2^37 units, of tables of 2^31 entries and 64 groups, in a quarter of them or 1024
-  // ranges)
-  const int per = (int)deal.per(total);
-  long long unit = (long long)blockIdx.x * per;
-  int left = (int)min((long long)per, total - unit);
-  int rows = w.rows(b), ctx = bt.context(b), np = w.pages(ctx, rows, 0, 0);
-  int h = (int)(off / np), blk0 = (int)(off % np);
-  size_t slot = 2 * (size_t)blockIdx.x;
-  while (true) {
-    const int blk1 = min(np, blk0 + left);
-    segment(b, h, rows, ctx, np, blk0, blk1, slot, unit);
+// The segments of a range of the few-column form: pages blk0 .. blk1-1 (of np) of sequence b,
+// group h, numbered from `unit` on; `slot` is where a part goes.
+struct Segment {
+  int b, h, rows, ctx, np, blk0, blk1, left;
+  long long unit;
+  size_t slot;
+
+  // the first one, false where the range is empty; every thread of the workgroup calls it
+  __device__ __forceinline__ bool first(const Units<true>& w, const Deal& deal) {
+    const CacheBatch& bt = w.bt;
+    long long total, off;
+    locate<kAttThr>(
+        bt.B, [&](int i) { return w.group(i) * bt.H; }, deal, blockIdx.x, w.prefix, total, b, off);
+    if (b < 0) return false;
+    // (at most 2^37 units, of tables of 2^31 entries and 64 groups, in a quarter of them or 1024
+    // ranges)
+    const int per = (int)deal.per(total);
+    unit = (long long)blockIdx.x * per;
+    left = (int)min((long long)per, total - unit);
+    rows = w.rows(b), ctx = bt.context(b), np = w.pages(ctx, rows, 0, 0);
+    h = (int)(off / np), blk0 = (int)(off % np);
+    slot = 2 * (size_t)blockIdx.x;
+    blk1 = min(np, blk0 + left);
+    return true;
+  }
+  // the next group, or the next sequence with rows; false past the range's end
+  __device__ __forceinline__ bool next(const Units<true>& w) {
+    const CacheBatch& bt = w.bt;
     left -= blk1 - blk0;
     unit += blk1 - blk0;
-    if (left <= 0) return;
-    // the next group, or the next sequence with rows
+    if (left <= 0) return false;
     slot |= 1;
     blk0 = 0;
     if (++h == bt.H) {
       h = 0;
       do {
-        if (++b >= bt.B) return;
+        if (++b >= bt.B) return false;
         rows = w.rows(b);
       } while (rows <= 0);
       ctx = bt.context(b);
       np = w.pages(ctx, rows, 0, 0);
     }
+    blk1 = min(np, left);
+    return true;
   }
-}
+};
 
 template <int HD>
 __global__ __launch_bounds__(kAttThr, 2) void cache_attn_few_kernel(
@@ -661,11 +675,13 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_few_kernel(
     const float* __restrict__ kv_scale, Units<true> w, Deal deal, float c_log2, AttnOut o,
     float* __restrict__ score) {
   __shared__ FewLds<HD> lds;
-  few_walk(w, deal, [&](int b, int h, int rows, int ctx, int np, int blk0, int blk1, size_t slot,
-                        long long unit) {
-    few_columns<HD>(q, kc, vc, kv_scale, w.bt, b, h, rows, ctx, np, blk0, blk1, c_log2, o, slot,
-                    score != nullptr ? score + unit * o.part_cols * kPage : nullptr, lds);
-  });
+  Segment g;
+  if (!g.first(w, deal)) return;
+  do {
+    few_columns<HD>(q, kc, vc, kv_scale, w.bt, g.b, g.h, g.rows, g.ctx, g.np, g.blk0, g.blk1,
+                    c_log2, o, g.slot,
+                    score != nullptr ? score + g.unit * o.part_cols * kPage : nullptr, lds);
+  } while (g.next(w));
 }
 
 // ---- few columns of other shapes -----------------------------------------------------
@@ -674,241 +690,266 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_few_kernel(
 // same page at about the same time, from L2 but for the first.  The queries are held in LDS, as
 // the waves read them; a page's keys give their registers to the next page's as soon as the
 // scores are formed, and its values after the second product, so that two waves of a SIMD
-// have room for 32 columns each.
+// have room for 32 columns each.  The next segment's page numbers are loaded beside this one's
+// pages, and its first page before this one's states are merged.
 template <int HD, int NC, int G>
 struct ShapedLds {
   FewLds<HD> few;
   bf16x8 q[G * NC][HD / 32][kWave];
 };
 
-template <int HD, int NC, int G>
-__device__ __forceinline__ void shaped_columns(
+template <int HD, int NC, int G, typename S>
+__global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
     const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
-    const float* __restrict__ kv_scale, const CacheBatch& bt, int b, int h, int rows, int ctx,
-    int np, int blk0, int blk1, float c_log2, const Shape& sh, const AttnOut& o, size_t slot,
-    float* __restrict__ score, ShapedLds<HD, NC, G>& lds) {
+    const float* __restrict__ kv_scale, Units<true> w, Deal deal, float c_log2, S sh,
+    AttnOut o, float* __restrict__ score_base) {
   using F = PageFrags<HD>;
   constexpr int NP = kAttWaves / G;  // pages at a time
-  const int tid = threadIdx.x, lane = lane_id();
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), cg = wave % G, pl = wave / G;
+  __shared__ ShapedLds<HD, NC, G> lds;
+  const CacheBatch& bt = w.bt;
+  const int lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), cg = wave % G, pl = wave / G;
   const int n = lane & 15, g = lane >> 4;
-  const int ncol = rows * bt.nq;
-  const size_t qrow = ((size_t)h * bt.N + bt.first_row(b)) * bt.nq;
   const int col0 = 16 * NC * cg;
-  Column col[NC];
-#pragma unroll
-  for (int j = 0; j < NC; ++j) {
-    const int c = col0 + 16 * j + n;
-    col[j] = column_of(sh, bt, b, h, ctx, c, ncol);
-    if (pl == 0) {
-      bf16x8 qf[F::NST];
-      load_q<HD>(q + qrow * HD, c, ncol, g, qf);
-#pragma unroll
-      for (int st = 0; st < F::NST; ++st) lds.q[NC * cg + j][st][lane] = qf[st];
-    }
-  }
-  const int len = min(ctx + rows, bt.cap());  // tokens the cache holds now
-  const int fewest = min(plain_tokens(sh, ctx, 0), bt.cap());
-  f32x4 oacc[NC][F::NDT];
-  float m_run[NC], l_run[NC];
-  bool saw[NC], far[NC];  // any token; (uniform) a column's maximum is far from 0
-#pragma unroll
-  for (int j = 0; j < NC; ++j) {
-#pragma unroll
-    for (int dt = 0; dt < F::NDT; ++dt) oacc[j][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    m_run[j] = kMFloor;
-    l_run[j] = 0.f;
-    saw[j] = far[j] = false;
-  }
-  // page numbers and scales of the wave's next 64 pages, one a lane
-  int pid = -1;
-  float2 psc{0.f, 0.f};
-  const int mine = (blk1 - blk0 - pl + NP - 1) / NP;  // pages of this wave
-  auto pages64 = [&](int i) {
-    const int blk = blk0 + pl + NP * (i + lane);
-    pid = blk < blk1 ? bt.page(b, blk) : -1;
-    if (pid >= 0)
-      psc = *reinterpret_cast<const float2*>(kv_scale + ((size_t)pid * bt.H + h) * 2);
+
+  // the numbers of 64 of the wave's pages from its i-th on, one a lane
+  auto pages64 = [&](const Segment& a, int i) {
+    const int blk = a.blk0 + pl + NP * (i + lane);
+    return blk < a.blk1 ? bt.page(a.b, blk) : -1;
   };
-  auto at = [&](int i) {  // (an absent page loads page 0)
-    return ((size_t)max(__builtin_amdgcn_readlane(pid, i & 63), 0) * bt.H + h) * (kPage * HD);
-  };
+  auto count = [&](const Segment& a) { return (a.blk1 - a.blk0 - pl + NP - 1) / NP; };
+  int pid;
   F f;
-  if (mine > 0) {
-    pages64(0);
-    f.load_k(kc + at(0), lane);
-    f.load_v(vc + at(0), lane);
-  }
-  __syncthreads();
-  for (int i = 0; i < mine; ++i) {
-    const int blk = blk0 + pl + NP * i;
-    const int page = __builtin_amdgcn_readlane(pid, i & 63);
-    const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(psc.x), i & 63));
-    const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(psc.y), i & 63));
-    f32x4 s[NC][4];
+  float2 scale;
+  auto at = [&](int h, int i) {  // (an absent page loads page 0)
+    return (size_t)max(__builtin_amdgcn_readlane(pid, i & 63), 0) * bt.H + h;
+  };
+  auto load_k = [&](int h, int i) {
+    scale = *reinterpret_cast<const float2*>(kv_scale + at(h, i) * 2);
+    f.load_k(kc + at(h, i) * (kPage * HD), lane);
+  };
+  auto load_v = [&](int h, int i) { f.load_v(vc + at(h, i) * (kPage * HD), lane); };
+
+  Segment a;
+  if (!a.first(w, deal)) return;
+  pid = pages64(a, 0);
+  if (count(a) > 0) load_k(a.h, 0), load_v(a.h, 0);
+  while (true) {
+    Segment ahead = a;
+    const bool another = ahead.next(w);
+    const int b = a.b, h = a.h, rows = a.rows, ctx = a.ctx, ncol = rows * bt.nq;
+    const size_t qrow = ((size_t)h * bt.N + bt.first_row(b)) * bt.nq;
+    int pid_ahead = -1;
+    if (another) pid_ahead = pages64(ahead, 0);
+    Column col[NC];
 #pragma unroll
-    for (int j = 0; j < NC; ++j)
+    for (int j = 0; j < NC; ++j) {
+      const int c = col0 + 16 * j + n;
+      col[j] = column_of(sh, bt, b, h, ctx, c, ncol);
+      if (pl == 0) {
+        bf16x8 qf[F::NST];
+        load_q<HD>(q + qrow * HD, c, ncol, g, qf);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) s[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int st = 0; st < F::NST; ++st) {
-      bf16x8 qf[NC];
-#pragma unroll
-      for (int j = 0; j < NC; ++j) qf[j] = lds.q[NC * cg + j][st][lane];
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const bf16x8 a = f.key(t, st, ks);
-#pragma unroll
-        for (int j = 0; j < NC; ++j)
-          s[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[j], s[j][t], 0, 0, 0);
+        for (int st = 0; st < F::NST; ++st) lds.q[NC * cg + j][st][lane] = qf[st];
       }
     }
-    const bool more = i + 1 < mine;
-    if (more) {
-      if (((i + 1) & 63) == 0) pages64(i + 1);
-      f.load_k(kc + at(i + 1), lane);
+    const int len = min(ctx + rows, bt.cap());  // tokens the cache holds now
+    const int fewest = min(plain_tokens(sh, ctx, 0), bt.cap());
+    float* score =
+        NC == 1 && score_base != nullptr ? score_base + a.unit * o.part_cols * kPage : nullptr;
+    f32x4 oacc[NC][F::NDT];
+    float m_run[NC], l_run[NC];
+    bool saw[NC], far[NC];  // any token; (uniform) a column's maximum is far from 0
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+#pragma unroll
+      for (int dt = 0; dt < F::NDT; ++dt) oacc[j][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      m_run[j] = kMFloor;
+      l_run[j] = 0.f;
+      saw[j] = far[j] = false;
     }
-    if (page >= 0) {
-      const int k0 = blk * kPage + 16 * g;
-      const bool some = (blk + 1) * kPage > fewest;
-      bf16x8 p[NC][2];
+    const int mine = count(a);
+    __syncthreads();
+    for (int i = 0; i < mine; ++i) {
+      const int blk = a.blk0 + pl + NP * i;
+      const int page = __builtin_amdgcn_readlane(pid, i & 63);
+      const float ks = scale.x, vs = scale.y;
+      f32x4 s[NC][4];
 #pragma unroll
-      for (int j = 0; j < NC; ++j) {
-        __builtin_amdgcn_sched_barrier(0);  // (a tile of columns after another)
-        uint64_t sees = 0;
-        if (some) {
-          if (col0 + 16 * j + n < ncol) sees = keys_seen(sh, bt, b, col[j].row, ctx, len, blk);
-          saw[j] |= sees != 0;
-          sees >>= 16 * g;
-        } else {
-          saw[j] |= col0 + 16 * j + n < ncol;
+      for (int j = 0; j < NC; ++j)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) s[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int st = 0; st < F::NST; ++st) {
+        bf16x8 qf[NC];
+#pragma unroll
+        for (int j = 0; j < NC; ++j) qf[j] = lds.q[NC * cg + j][st][lane];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const bf16x8 kf = f.key(t, st, ks);
+#pragma unroll
+          for (int j = 0; j < NC; ++j)
+            s[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[j], s[j][t], 0, 0, 0);
         }
-        shape_scores<16>(
-            sh, bt, b, ctx, rows, col[j], k0, !some, sees,
-            [&](int x) { return s[j][x >> 2][x & 3]; },
-            [&](int x, float y) { s[j][x >> 2][x & 3] = y; }, [](int x) { return x; });
-        if (NC == 1 && score != nullptr && n < ncol) {
-          float* to = score + ((size_t)(blk - blk0) * o.part_cols + n) * kPage + 16 * g;
+      }
+      const bool more = i + 1 < mine;
+      if (more) {
+        if (((i + 1) & 63) == 0) pid = pages64(a, i + 1);
+        load_k(h, i + 1);
+      }
+      if (page >= 0) {
+        const int k0 = blk * kPage + 16 * g;
+        const bool some = (blk + 1) * kPage > fewest;
+        bf16x8 p[NC][2];
 #pragma unroll
-          for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4*>(to + 4 * t) = s[j][t];
-        }
-        float mx = s[j][0][0];
+        for (int j = 0; j < NC; ++j) {
+          __builtin_amdgcn_sched_barrier(0);  // (a tile of columns after another)
+          uint64_t sees = 0;
+          if (some) {
+            const int c = col0 + 16 * j + opaque_int(n);  // (its row is not held)
+            if (c < ncol) sees = keys_seen(sh, bt, b, c / bt.nq, ctx, len, blk);
+            saw[j] |= sees != 0;
+            sees >>= 16 * g;
+          } else {
+            saw[j] |= col0 + 16 * j + n < ncol;
+          }
+          shape_scores<16>(
+              sh, bt, b, ctx, rows, col[j], k0, !some, sees,
+              [&](int x) { return s[j][x >> 2][x & 3]; },
+              [&](int x, float y) { s[j][x >> 2][x & 3] = y; }, [](int x) { return x; });
+          if (NC == 1 && score != nullptr && n < ncol) {
+            float* to = score + ((size_t)(blk - a.blk0) * o.part_cols + n) * kPage + 16 * g;
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[j][t][e]);
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        // (the maximum moves only when a page exceeds it by 2^8, as with causal columns)
-        const float mxs = mx * c_log2;
-        const bool need = mxs > m_run[j] + 8.f;
-        if (__builtin_amdgcn_ballot_w64(need)) {
-          const float m_new = need ? mxs : m_run[j];
-          const float a = __builtin_amdgcn_exp2f(m_run[j] - m_new);
-          m_run[j] = m_new;
-          far[j] = __builtin_amdgcn_ballot_w64(far_max(m_run[j])) != 0;
-          l_run[j] *= a;
-#pragma unroll
-          for (int dt = 0; dt < F::NDT; ++dt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) oacc[j][dt][e] *= a;
-        }
-        float c_page = c_log2, m_page = m_run[j];
-        if (far[j]) {
+            for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4*>(to + 4 * t) = s[j][t];
+          }
+          float mx = s[j][0][0];
 #pragma unroll
           for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[j][t][e] = far_exponent(s[j][t][e], c_log2, m_run[j]);
-          c_page = 1.f;
-          m_page = 0.f;
-        }
+            for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[j][t][e]);
+          mx = fmaxf(mx, __shfl_xor(mx, 16));
+          mx = fmaxf(mx, __shfl_xor(mx, 32));
+          // (the maximum moves only when a page exceeds it by 2^8, as with causal columns)
+          const float mxs = mx * c_log2;
+          const bool need = mxs > m_run[j] + 8.f;
+          if (__builtin_amdgcn_ballot_w64(need)) {
+            const float m_new = need ? mxs : m_run[j];
+            const float x = __builtin_amdgcn_exp2f(m_run[j] - m_new);
+            m_run[j] = m_new;
+            far[j] = __builtin_amdgcn_ballot_w64(far_max(m_run[j])) != 0;
+            l_run[j] *= x;
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+            for (int dt = 0; dt < F::NDT; ++dt)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) oacc[j][dt][e] *= x;
+          }
+          float c_page = c_log2, m_page = m_run[j];
+          if (far[j]) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) s[j][t][e] = far_exponent(s[j][t][e], c_log2, m_run[j]);
+            c_page = 1.f;
+            m_page = 0.f;
+          }
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float x = __builtin_amdgcn_exp2f(fmaf(s[j][t][e], c_page, -m_page));
+              l_run[j] += x;
+              p[j][t >> 1][4 * (t & 1) + e] = (bf16)x;
+            }
+        }
+        if (some) {
+          // slots past the last token hold anything: 0 * NaN is NaN
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float x = __builtin_amdgcn_exp2f(fmaf(s[j][t][e], c_page, -m_page));
-            l_run[j] += x;
-            p[j][t >> 1][4 * (t & 1) + e] = (bf16)x;
+            const int in = len - (k0 + 4 * e);
+            const uint32_t m = in >= 4 ? 0xffffffffu : in <= 0 ? 0u : (1u << (8 * in)) - 1;
+#pragma unroll
+            for (int dt = 0; dt < F::NDT; ++dt) f.v[dt][e] &= m;
+          }
+        }
+#pragma unroll
+        for (int dt = 0; dt < F::NDT; ++dt)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const bf16x8 vf = codes_to_bf16(f.v[dt][2 * u], f.v[dt][2 * u + 1], vs);
+#pragma unroll
+            for (int j = 0; j < NC; ++j)
+              oacc[j][dt] =
+                  __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[j][u], oacc[j][dt], 0, 0, 0);
           }
       }
-      if (some) {
-        // slots past the last token hold anything: 0 * NaN is NaN
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int in = len - (k0 + 4 * e);
-          const uint32_t m = in >= 4 ? 0xffffffffu : in <= 0 ? 0u : (1u << (8 * in)) - 1;
-#pragma unroll
-          for (int dt = 0; dt < F::NDT; ++dt) f.v[dt][e] &= m;
-        }
-      }
-#pragma unroll
-      for (int dt = 0; dt < F::NDT; ++dt)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const bf16x8 a = codes_to_bf16(f.v[dt][2 * u], f.v[dt][2 * u + 1], vs);
-#pragma unroll
-          for (int j = 0; j < NC; ++j)
-            oacc[j][dt] =
-                __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[j][u], oacc[j][dt], 0, 0, 0);
-        }
+      if (more) load_v(h, i + 1);
     }
-    if (more) f.load_v(vc + at(i + 1), lane);
-  }
-  const bool whole = blk0 == 0 && blk1 == np;
-  float* pt = o.part + slot * part_floats(o.part_cols, HD);
-  // the states of the waves of a column group, merged in wave order, 16 columns of each group
-  // at a time
-#pragma unroll
-  for (int j = 0; j < NC; ++j) {
-    if (16 * j >= ncol) break;  // (uniform)
-    if (saw[j]) m_run[j] = fmaxf(m_run[j], kMSeen);
-    l_run[j] += __shfl_xor(l_run[j], 16);
-    l_run[j] += __shfl_xor(l_run[j], 32);
-    __syncthreads();  // what was in LDS before has been read
+    if (another) {
+      pid = pid_ahead;
+      if (count(ahead) > 0) load_k(ahead.h, 0), load_v(ahead.h, 0);
+    }
+    const bool whole = a.blk0 == 0 && a.blk1 == a.np;
+    float* pt = o.part + a.slot * part_floats(o.part_cols, HD);
     const int me = opaque_int(lane), n1 = me & 15, g1 = me >> 4;  // (not held over the pages)
-    if (g1 == 0) lds.few.mm[wave][n1] = m_run[j], lds.few.ll[wave][n1] = l_run[j];
-#pragma unroll
-    for (int dt = 0; dt < F::NDT; ++dt)
-      *reinterpret_cast<f32x4*>(&lds.few.oo[wave][n1][16 * dt + 4 * g1]) = oacc[j][dt];
-    __syncthreads();
-    for (int i = opaque_int(tid); i < G * 16 * HD; i += kAttThr) {
-      const int gr = i / (16 * HD), c = i / HD % 16, d = i % HD;
-      const int cc = 16 * (NC * gr + j) + c;
-      if (cc >= ncol) break;
-      float m = lds.few.mm[gr][c], l = 0.f, x = 0.f;
-#pragma unroll
-      for (int v = 1; v < NP; ++v) m = fmaxf(m, lds.few.mm[v * G + gr][c]);
-#pragma unroll
-      for (int v = 0; v < NP; ++v) {
-        const float a = __builtin_amdgcn_exp2f(lds.few.mm[v * G + gr][c] - m);
-        l += lds.few.ll[v * G + gr][c] * a;
-        x += lds.few.oo[v * G + gr][c][d] * a;
-      }
+    // four dims from d on of column c
+    auto put = [&](int c, int d, const f32x4& x, float m, float l) {
       if (whole) {
         const float inv = inv_sum(m, l);
-        const int row = bt.first_row(b) + cc / bt.nq;
-        o.out[(((size_t)row * bt.H + h) * bt.nq + cc % bt.nq) * HD + d] = (bf16)(x * inv);
-        if (d == 0 && o.stat != nullptr) put_stat(sh, bt, b, h, ctx, rows, cc, qrow + cc, o, m, inv);
+        const int row = c / bt.nq;
+        bf16* to = o.out + (((size_t)(bt.first_row(b) + row) * bt.H + h) * bt.nq + c - row * bt.nq) * HD;
+        *reinterpret_cast<bf16x4*>(to + d) = bf16x4{(bf16)(x[0] * inv), (bf16)(x[1] * inv),
+                                                    (bf16)(x[2] * inv), (bf16)(x[3] * inv)};
+        if (d == 0 && o.stat != nullptr) put_stat(sh, bt, b, h, ctx, rows, c, qrow + c, o, m, inv);
       } else {
-        pt[(size_t)cc * HD + d] = x;
-        if (d == 0) reinterpret_cast<float2*>(pt + o.part_cols * HD)[cc] = float2{m, l};
+        *reinterpret_cast<f32x4*>(pt + (size_t)c * HD + d) = x;
+        if (d == 0) reinterpret_cast<float2*>(pt + o.part_cols * HD)[c] = float2{m, l};
+      }
+    };
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      if (saw[j]) m_run[j] = fmaxf(m_run[j], kMSeen);
+      l_run[j] += __shfl_xor(l_run[j], 16);
+      l_run[j] += __shfl_xor(l_run[j], 32);
+      if constexpr (NP == 1) {  // the wave has all of its columns' pages
+        const int c = col0 + 16 * j + n1;
+        if (c < ncol) {
+#pragma unroll
+          for (int dt = 0; dt < F::NDT; ++dt) put(c, 16 * dt + 4 * g1, oacc[j][dt], m_run[j], l_run[j]);
+        }
+      } else {
+        // the states of the waves of a column group, merged in wave order, 16 columns of each
+        // group at a time
+        if (16 * j >= ncol) break;  // (uniform)
+        __syncthreads();  // what was in LDS before has been read
+        if (g1 == 0) lds.few.mm[wave][n1] = m_run[j], lds.few.ll[wave][n1] = l_run[j];
+#pragma unroll
+        for (int dt = 0; dt < F::NDT; ++dt)
+          *reinterpret_cast<f32x4*>(&lds.few.oo[wave][n1][16 * dt + 4 * g1]) = oacc[j][dt];
+        __syncthreads();
+        for (int i = opaque_int(threadIdx.x); i < G * 16 * (HD / 4); i += kAttThr) {
+          const int gr = i / (16 * (HD / 4)), c = i / (HD / 4) % 16, d = i % (HD / 4) * 4;
+          const int cc = 16 * (NC * gr + j) + c;
+          if (cc >= ncol) break;
+          float m = lds.few.mm[gr][c], l = 0.f;
+          f32x4 x{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int v = 1; v < NP; ++v) m = fmaxf(m, lds.few.mm[v * G + gr][c]);
+#pragma unroll
+          for (int v = 0; v < NP; ++v) {
+            const float y = __builtin_amdgcn_exp2f(lds.few.mm[v * G + gr][c] - m);
+            const f32x4 z = *reinterpret_cast<const f32x4*>(&lds.few.oo[v * G + gr][c][d]);
+            l += lds.few.ll[v * G + gr][c] * y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] += z[e] * y;
+          }
+          put(cc, d, x, m, l);
+        }
       }
     }
+    if (!another) return;
+    a = ahead;
+    if constexpr (NP == 1) __syncthreads();  // the queries have been read
   }
-}
-
-template <int HD, int NC, int G>
-__global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
-    const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
-    const float* __restrict__ kv_scale, Units<true> w, Deal deal, float c_log2, Shape sh,
-    AttnOut o, float* __restrict__ score) {
-  __shared__ ShapedLds<HD, NC, G> lds;
-  few_walk(w, deal, [&](int b, int h, int rows, int ctx, int np, int blk0, int blk1, size_t slot,
-                        long long unit) {
-    shaped_columns<HD, NC, G>(q, kc, vc, kv_scale, w.bt, b, h, rows, ctx, np, blk0, blk1, c_log2,
-                              sh, o, slot,
-                              score != nullptr ? score + unit * o.part_cols * kPage : nullptr, lds);
-  });
 }
 
 // ---- many columns -----------------------------------------------------------------
@@ -1135,7 +1176,7 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
             sees = keys_seen(sh, bt, b, row0 + fresh(col) / bt.nq, ctx, len, blk);
           const int k4 = 4 * fresh(hl);
           const float2 sp = cols[fresh(col)];
-          const Column cl{sp.x, __float_as_int(sp.y), 0};
+          const Column cl{sp.x, __float_as_int(sp.y)};
           shape_scores<32>(
               sh, bt, b, ctx, rows, cl, blk * kPage + k4, !some, sees >> k4,
               [&](int x) { return sacc[x >> 4][x & 15]; },
@@ -1342,6 +1383,63 @@ __device__ __forceinline__ void join_few(const Units<true>& w, const Deal& deal,
              ((size_t)h * bt.N + bt.first_row(b)) * bt.nq + c, o, m, inv);
 }
 
+// The same for a workgroup's eight columns from c0 on, 32 lanes each, where the sequences have
+// many columns and few parts: their sums need no second step, and what finds the parts is shared.
+// us for 64 sequences of 32 columns, 2 or 3 parts each, 8 groups: a workgroup a column 39.
+template <int HD, typename S>
+__device__ __forceinline__ void join_few8(const Units<true>& w, const Deal& deal, const S& sh,
+                                          const AttnOut& o, int h, int b, int c0) {
+  const CacheBatch& bt = w.bt;
+  const int rows = w.rows(b), ncol = rows * bt.nq;
+  if (c0 >= ncol) return;
+  const int np = w.pages(bt.context(b), rows, 0, 0);
+  Parts p{o.part, o.part_cols, HD};
+  if (!find_parts(w, deal, w.prefix[b] + (long long)np * h, np, p)) return;
+  const int l5 = threadIdx.x & 31, c = c0 + (threadIdx.x >> 5), d = 4 * l5;
+  if (c >= ncol) return;
+  float m = kMFloor, l = 0.f;
+  f32x4 x{0.f, 0.f, 0.f, 0.f};
+  constexpr int AT_ONCE = 4;
+  for (int r0 = p.r0; r0 <= p.r1; r0 += AT_ONCE) {
+    float2 z[AT_ONCE];
+    f32x4 y[AT_ONCE];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      z[i] = float2{kMFloor, 0.f};
+      y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (r0 + i > p.r1) continue;
+      z[i] = p.stats(r0 + i)[c];
+      if (d < HD) y[i] = *reinterpret_cast<const f32x4*>(p.at(r0 + i) + (size_t)c * HD + d);
+    }
+    float mn = m;
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) mn = fmaxf(mn, z[i].x);
+    const float a0 = __builtin_amdgcn_exp2f(m - mn);
+    m = mn;
+    l *= a0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] *= a0;
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const float a = __builtin_amdgcn_exp2f(z[i].x - m);
+      l += z[i].y * a;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += y[i][e] * a;
+    }
+  }
+  const float inv = inv_sum(m, l);
+  if (d < HD) {
+    const int row = c / bt.nq;
+    bf16* dst =
+        o.out + (((size_t)(bt.first_row(b) + row) * bt.H + h) * bt.nq + c - row * bt.nq) * HD + d;
+    *reinterpret_cast<bf16x4*>(dst) = bf16x4{(bf16)(x[0] * inv), (bf16)(x[1] * inv),
+                                             (bf16)(x[2] * inv), (bf16)(x[3] * inv)};
+  }
+  if (o.stat != nullptr && l5 == 0)
+    put_stat(sh, bt, b, h, bt.context(b), rows, c,
+             ((size_t)h * bt.N + bt.first_row(b)) * bt.nq + c, o, m, inv);
+}
+
 // Many columns: one workgroup per (32 columns of a tile, group h), 8 threads a column; a
 // thread loads its dims of four parts at a time.
 constexpr int kJoinCols = 32;
@@ -1426,11 +1524,22 @@ struct Form {
 template <int HD, typename S>
 __global__ __launch_bounds__(256) void cache_join_kernel(Form<true> few,
                                                          Form<false, is_shaped<S>> many, S sh,
-                                                         int many_blocks) {
-  const int x = blockIdx.x, h = blockIdx.y;
-  if (x < many_blocks) join_tile<HD>(many.w, many.deal, sh, many.o, h, x);
-  else join_few<HD>(few.w, few.deal, sh, few.o, h, (x - many_blocks) / few.o.part_cols,
-                    (x - many_blocks) % few.o.part_cols);
+                                                         int many_blocks, int few_each) {
+  int x = blockIdx.x;
+  const int h = blockIdx.y;
+  if (x < many_blocks) {
+    join_tile<HD>(many.w, many.deal, sh, many.o, h, x);
+    return;
+  }
+  x -= many_blocks;
+  if constexpr (is_shaped<S>) {
+    if (few_each == 8) {
+      const int each = (few.o.part_cols + 7) / 8;
+      join_few8<HD>(few.w, few.deal, sh, few.o, h, x / each, x % each * 8);
+      return;
+    }
+  }
+  join_few<HD>(few.w, few.deal, sh, few.o, h, x / few.o.part_cols, x % few.o.part_cols);
 }
 
 // ---- mass ---------------------------------------------------------------------------
@@ -1649,9 +1758,9 @@ __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8
           const int i0 = t * kMassCols / bt.nq;
           const bool all = plain_tokens(sh, ctx, i0) >= min(key0 + 32, len + 1);
           uint64_t sees = 0;
-          cl = Column{zs[2], __float_as_int(zs[3]), col / bt.nq};
+          cl = Column{zs[2], __float_as_int(zs[3])};
           if (!all && col < ncol)
-            sees = keys_seen(sh, bt, b, cl.row, ctx, len, key0 / kPage) >> ((wave & 1) * 32 + 4 * hl);
+            sees = keys_seen(sh, bt, b, col / bt.nq, ctx, len, key0 / kPage) >> ((wave & 1) * 32 + 4 * hl);
           shape_scores<16>(
               sh, bt, b, ctx, rows, cl, key0 + 4 * hl, all, sees, [&](int v) { return x[v]; },
               [&](int v, float y) { x[v] = y; }, [](int v) { return 8 * (v >> 2) + (v & 3); });
@@ -1669,7 +1778,7 @@ __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8
             const int seen = ctx + col / bt.nq + 1;
             uint64_t sees = 0;
             if constexpr (SHAPED)
-              sees = keys_seen(sh, bt, b, cl.row, ctx, len, key0 / kPage) >> ((wave & 1) * 32 + 4 * hl);
+              sees = keys_seen(sh, bt, b, col / bt.nq, ctx, len, key0 / kPage) >> ((wave & 1) * 32 + 4 * hl);
 #pragma unroll
             for (int v = 0; v < 16; ++v)
               if (SHAPED ? (sees >> (8 * (v >> 2) + (v & 3)) & 1) != 0
@@ -1713,7 +1822,7 @@ __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8
 // One launch for both: `any_ranges` workgroups for the sequences of `any`, the rest for
 // those of few columns, from their scores.
 template <int HD, typename S>
-__global__ __launch_bounds__(kMassThr, is_shaped<S> ? 3 : 4) void cache_mass_kernel(
+__global__ __launch_bounds__(kMassThr, S::kTransforms ? 3 : 4) void cache_mass_kernel(
     const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const float* __restrict__ kv_scale,
     Units<false, is_shaped<S>> any, int any_ranges, Form<true> few, const float* __restrict__ score, float c_log2,
     S sh, const Stat<S>* __restrict__ stat, const float* __restrict__ mass_in,
@@ -1732,6 +1841,7 @@ __global__ __launch_bounds__(kMassThr, is_shaped<S> ? 3 : 4) void cache_mass_ker
 // Host side of the two forms: ranges (workgroups) and scratch.
 constexpr int kFewLeast = 4;   // pages of a range at least: one for each wave
 constexpr int kManyLeast = 2;
+constexpr int kJoinParts = 24;  // parts up to which eight columns are joined by a workgroup
 // The scores of few columns are kept for the mass where the tables' room for them is up to
 // this many bytes of workspace; beyond, they are formed again.  us kept and formed again, 8
 // groups of two heads: 16 sequences of 1000 to 4000 tokens 35 53, 64 of 1000 to 8000 155 264,
@@ -1788,7 +1898,7 @@ AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_
   scratch(p.few);
   scratch(p.many);
   if (mass) {
-    take(p.stat, (size_t)H * N * nq * (shaped ? sizeof(Stat<Shape>) : sizeof(Stat<NoShape>)));
+    take(p.stat, (size_t)H * N * nq * (shaped ? sizeof(Stat<Shape<true>>) : sizeof(Stat<NoShape>)));
     const size_t bytes = (size_t)pages * p.few.cols * kPage * 4;
     p.scores = p.few.on && p.few_cols == kFewCols && bytes <= kScoreBytes;
     if (p.scores) take(p.score, bytes);
@@ -1796,9 +1906,10 @@ AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_
   return p;
 }
 
-Shape shape_of(const CacheScores& a, int hd) {
+template <bool T>
+Shape<T> shape_of(const CacheScores& a, int hd) {
   constexpr double kLog2e = 1.4426950408889634;
-  Shape sh{};
+  Shape<T> sh{};
   sh.a = a;
   sh.scale = (float)(kLog2e / sqrt((double)hd));
   if (a.cap != 0.f) {
@@ -1847,7 +1958,7 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
                            std::integral_constant<bool, is_shaped<S>>{});
     float c_log2 = 1.4426950408889634f / sqrtf((float)a.hd);
     if constexpr (is_shaped<S>)
-      if (sh.a.cap != 0.f || sh.a.slope != nullptr) c_log2 = 1.f;
+      if (S::kTransforms) c_log2 = 1.f;
     if (p.few.on) {
       if constexpr (is_shaped<S>) {
         ProfileScope ps("cache_attn_shaped", s);
@@ -1855,10 +1966,10 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
           FOE_LAUNCH(kernel, dim3(few.deal.ranges), dim3(kAttThr), 0, s, qb, a.k, a.v, a.kv_scale,
                      few.w, few.deal, c_log2, sh, few.o, score);
         };
-        if (p.few_cols == 16) launch(cache_attn_shaped_kernel<HD, 1, 1>);
-        else if (p.few_cols == 32) launch(cache_attn_shaped_kernel<HD, 2, 1>);
-        else if (p.few_cols == 64) launch(cache_attn_shaped_kernel<HD, 2, 2>);
-        else launch(cache_attn_shaped_kernel<HD, 2, 4>);
+        if (p.few_cols == 16) launch(cache_attn_shaped_kernel<HD, 1, 1, S>);
+        else if (p.few_cols == 32) launch(cache_attn_shaped_kernel<HD, 2, 1, S>);
+        else if (p.few_cols == 64) launch(cache_attn_shaped_kernel<HD, 2, 2, S>);
+        else launch(cache_attn_shaped_kernel<HD, 2, 4, S>);
       } else {
         ProfileScope ps("cache_attn_few", s);
         FOE_LAUNCH(cache_attn_few_kernel<HD>, dim3(few.deal.ranges), dim3(kAttThr), 0, s, qb, a.k,
@@ -1873,9 +1984,14 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
     {
       ProfileScope ps("cache_join", s);
       const int many_blocks = p.many.on ? p.many.tiles * (kTileCols / kJoinCols) : 0;
-      const int few_blocks = p.few.on ? a.B * few.o.part_cols : 0;
+      // with many parts of a (sequence, group) a column's are shared by a workgroup
+      const int few_each = is_shaped<S> && p.few_cols > kFewCols &&
+                                   few.deal.ranges <= (long long)kJoinParts * a.B * a.H
+                               ? 8
+                               : 1;
+      const int few_blocks = p.few.on ? a.B * ceil_div(few.o.part_cols, few_each) : 0;
       FOE_LAUNCH((cache_join_kernel<HD, S>), dim3(many_blocks + few_blocks, a.H), dim3(256), 0, s,
-                 few, many, sh, many_blocks);
+                 few, many, sh, many_blocks, few_each);
     }
     if (mass_out != nullptr) {
       ProfileScope ps("cache_mass", s);
@@ -1896,8 +2012,9 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
     if (a.hd == 96) go(std::integral_constant<int, 96>{}, sh);
     else go(std::integral_constant<int, 128>{}, sh);
   };
-  if (scores != nullptr) with(shape_of(*scores, a.hd));
-  else with(NoShape{});
+  if (scores == nullptr) with(NoShape{});
+  else if (scores->cap != 0.f || scores->slope != nullptr) with(shape_of<true>(*scores, a.hd));
+  else with(shape_of<false>(*scores, a.hd));
   return hipGetLastError();
 }
 
