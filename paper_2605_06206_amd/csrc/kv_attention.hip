@@ -231,7 +231,10 @@ struct Reach {
 // The units of a batch in a form, numbered by sequence, group, tile and page.  A tile of
 // many columns has 2^log2r rows, tile t reaches page ceil((ctx + last row + 1) / 64), and
 // the sums over tiles are closed forms (which count pages past the table's end too).
-// (WIDE: rows may see past themselves, see Reach.)
+// (WIDE: shaped calls.  Rows may see past themselves, see Reach; and with few columns each
+// (sequence, group) has kStartPages units before its pages', for what starting on it costs.)
+constexpr int kStartPages = 5;
+
 template <bool FEW, bool WIDE = false>
 struct Units {
   CacheBatch bt;
@@ -282,7 +285,7 @@ struct Units {
     const int n = rows(b);
     if (n <= 0) return 0;
     const int ctx = bt.context(b), t = FEW ? 0 : tiles(n) - 1, more = least(b, ctx, n);
-    return (FEW ? 0 : before(ctx, t, more)) + pages(ctx, n, t, more);
+    return (FEW ? (WIDE ? kStartPages : 0) : before(ctx, t, more)) + pages(ctx, n, t, more);
   }
 };
 
@@ -624,35 +627,44 @@ __device__ __forceinline__ void few_columns(
 
 // The segments of a range of the few-column form: pages blk0 .. blk1-1 (of np) of sequence b,
 // group h, numbered from `unit` on; `slot` is where a part goes.
+template <bool WIDE>
 struct Segment {
+  static constexpr int kStart = WIDE ? kStartPages : 0;
   int b, h, rows, ctx, np, blk0, blk1, left;
   long long unit;
   size_t slot;
 
-  // the first one, false where the range is empty; every thread of the workgroup calls it
-  __device__ __forceinline__ bool first(const Units<true>& w, const Deal& deal) {
+  // range `r`'s first one, false where it has none; every thread of the workgroup calls it
+  __device__ __forceinline__ bool first(const Units<true, WIDE>& w, const Deal& deal, int r) {
     const CacheBatch& bt = w.bt;
     long long total, off;
     locate<kAttThr>(
-        bt.B, [&](int i) { return w.group(i) * bt.H; }, deal, blockIdx.x, w.prefix, total, b, off);
+        bt.B, [&](int i) { return w.group(i) * bt.H; }, deal, r, w.prefix, total, b, off);
     if (b < 0) return false;
     // (at most 2^37 units, of tables of 2^31 entries and 64 groups, in a quarter of them or 1024
     // ranges)
     const int per = (int)deal.per(total);
-    unit = (long long)blockIdx.x * per;
+    unit = (long long)r * per;
     left = (int)min((long long)per, total - unit);
     rows = w.rows(b), ctx = bt.context(b), np = w.pages(ctx, rows, 0, 0);
-    h = (int)(off / np), blk0 = (int)(off % np);
-    slot = 2 * (size_t)blockIdx.x;
+    h = (int)(off / (np + kStart)), blk0 = (int)(off % (np + kStart));
+    slot = 2 * (size_t)r;
+    if constexpr (WIDE) {
+      const int start = max(kStart - blk0, 0);
+      left -= start;
+      blk0 = max(blk0 - kStart, 0);
+      if (left <= 0) return false;
+    }
     blk1 = min(np, blk0 + left);
     return true;
   }
   // the next group, or the next sequence with rows; false past the range's end
-  __device__ __forceinline__ bool next(const Units<true>& w) {
+  __device__ __forceinline__ bool next(const Units<true, WIDE>& w) {
     const CacheBatch& bt = w.bt;
     left -= blk1 - blk0;
     unit += blk1 - blk0;
-    if (left <= 0) return false;
+    if (left <= kStart) return false;
+    left -= kStart;
     slot |= 1;
     blk0 = 0;
     if (++h == bt.H) {
@@ -675,8 +687,8 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_few_kernel(
     const float* __restrict__ kv_scale, Units<true> w, Deal deal, float c_log2, AttnOut o,
     float* __restrict__ score) {
   __shared__ FewLds<HD> lds;
-  Segment g;
-  if (!g.first(w, deal)) return;
+  Segment<false> g;
+  if (!g.first(w, deal, blockIdx.x)) return;
   do {
     few_columns<HD>(q, kc, vc, kv_scale, w.bt, g.b, g.h, g.rows, g.ctx, g.np, g.blk0, g.blk1,
                     c_log2, o, g.slot,
@@ -692,6 +704,11 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_few_kernel(
 // scores are formed, and its values after the second product, so that two waves of a SIMD
 // have room for 32 columns each.  The next segment's page numbers are loaded beside this one's
 // pages, and its first page before this one's states are merged.
+// number of a page among the kept scores of shaped calls
+__device__ __forceinline__ size_t score_page(const CacheBatch& bt, int b, int h, int blk) {
+  return ((size_t)b * bt.H + h) * bt.max_blocks + blk;
+}
+
 template <int HD, int NC, int G>
 struct ShapedLds {
   FewLds<HD> few;
@@ -701,7 +718,7 @@ struct ShapedLds {
 template <int HD, int NC, int G, typename S>
 __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
     const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
-    const float* __restrict__ kv_scale, Units<true> w, Deal deal, float c_log2, S sh,
+    const float* __restrict__ kv_scale, Units<true, true> w, Deal deal, float c_log2, S sh,
     AttnOut o, float* __restrict__ score_base) {
   using F = PageFrags<HD>;
   constexpr int NP = kAttWaves / G;  // pages at a time
@@ -713,11 +730,11 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
   const int col0 = 16 * NC * cg;
 
   // the numbers of 64 of the wave's pages from its i-th on, one a lane
-  auto pages64 = [&](const Segment& a, int i) {
+  auto pages64 = [&](const Segment<true>& a, int i) {
     const int blk = a.blk0 + pl + NP * (i + lane);
     return blk < a.blk1 ? bt.page(a.b, blk) : -1;
   };
-  auto count = [&](const Segment& a) { return (a.blk1 - a.blk0 - pl + NP - 1) / NP; };
+  auto count = [&](const Segment<true>& a) { return (a.blk1 - a.blk0 - pl + NP - 1) / NP; };
   int pid;
   F f;
   float2 scale;
@@ -730,12 +747,12 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
   };
   auto load_v = [&](int h, int i) { f.load_v(vc + at(h, i) * (kPage * HD), lane); };
 
-  Segment a;
-  if (!a.first(w, deal)) return;
+  Segment<true> a;
+  if (!a.first(w, deal, blockIdx.x)) return;
   pid = pages64(a, 0);
   if (count(a) > 0) load_k(a.h, 0), load_v(a.h, 0);
   while (true) {
-    Segment ahead = a;
+    Segment<true> ahead = a;
     const bool another = ahead.next(w);
     const int b = a.b, h = a.h, rows = a.rows, ctx = a.ctx, ncol = rows * bt.nq;
     const size_t qrow = ((size_t)h * bt.N + bt.first_row(b)) * bt.nq;
@@ -755,8 +772,9 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
     }
     const int len = min(ctx + rows, bt.cap());  // tokens the cache holds now
     const int fewest = min(plain_tokens(sh, ctx, 0), bt.cap());
-    float* score =
-        NC == 1 && score_base != nullptr ? score_base + a.unit * o.part_cols * kPage : nullptr;
+    float* score = NC == 1 && score_base != nullptr
+                       ? score_base + score_page(bt, b, h, a.blk0) * o.part_cols * kPage
+                       : nullptr;
     f32x4 oacc[NC][F::NDT];
     float m_run[NC], l_run[NC];
     bool saw[NC], far[NC];  // any token; (uniform) a column's maximum is far from 0
@@ -1315,14 +1333,20 @@ struct Parts {
     return reinterpret_cast<const float2*>(at(r) + (size_t)cols * hd);
   }
 };
-// units u0 .. u0 + np - 1 of the tile; false where one range wrote it whole
+// units u0 .. of a tile of np pages; false where one range wrote it whole
 template <bool FEW, bool WIDE>
 __device__ __forceinline__ bool find_parts(const Units<FEW, WIDE>& w, const Deal& deal, long long u0,
                                            int np, Parts& p) {
   const long long per = deal.per(w.prefix[w.bt.B]);
-  p.r0 = (int)(u0 / per);
-  p.r1 = (int)((u0 + np - 1) / per);
-  p.first_late = u0 % per != 0;
+  if constexpr (FEW && WIDE) {  // (a range that starts before the pages has none of the tile before)
+    p.r0 = (int)((u0 + kStartPages) / per);
+    p.r1 = (int)((u0 + kStartPages + np - 1) / per);
+    p.first_late = u0 > p.r0 * per;
+  } else {
+    p.r0 = (int)(u0 / per);
+    p.r1 = (int)((u0 + np - 1) / per);
+    p.first_late = u0 % per != 0;
+  }
   return p.r0 != p.r1;
 }
 
@@ -1331,7 +1355,8 @@ __device__ __forceinline__ bool find_parts(const Units<FEW, WIDE>& w, const Deal
 // columns one after another in a workgroup: 13.7 us instead of 4.3 for 16 sequences of 1000 to
 // 4000 tokens, 4 groups of 8 heads.)
 template <int HD, typename S>
-__device__ __forceinline__ void join_few(const Units<true>& w, const Deal& deal, const S& sh,
+__device__ __forceinline__ void join_few(const Units<true, is_shaped<S>>& w, const Deal& deal,
+                                         const S& sh,
                                          const AttnOut& o, int h, int b, int c) {
   __shared__ f32x4 osum[8][32];
   const CacheBatch& bt = w.bt;
@@ -1339,7 +1364,7 @@ __device__ __forceinline__ void join_few(const Units<true>& w, const Deal& deal,
   if (c >= rows * bt.nq) return;
   const int np = w.pages(bt.context(b), rows, 0, 0);
   Parts p{o.part, o.part_cols, HD};
-  if (!find_parts(w, deal, w.prefix[b] + (long long)np * h, np, p)) return;
+  if (!find_parts(w, deal, w.prefix[b] + w.group(b) * h, np, p)) return;
   const int grp = threadIdx.x >> 5, l5 = threadIdx.x & 31, d = 4 * l5;
   float m = kMFloor, l = 0.f;
   for (int r = p.r0 + l5; r <= p.r1; r += 32) {
@@ -1387,14 +1412,14 @@ __device__ __forceinline__ void join_few(const Units<true>& w, const Deal& deal,
 // many columns and few parts: their sums need no second step, and what finds the parts is shared.
 // us for 64 sequences of 32 columns, 2 or 3 parts each, 8 groups: a workgroup a column 39.
 template <int HD, typename S>
-__device__ __forceinline__ void join_few8(const Units<true>& w, const Deal& deal, const S& sh,
+__device__ __forceinline__ void join_few8(const Units<true, true>& w, const Deal& deal, const S& sh,
                                           const AttnOut& o, int h, int b, int c0) {
   const CacheBatch& bt = w.bt;
   const int rows = w.rows(b), ncol = rows * bt.nq;
   if (c0 >= ncol) return;
   const int np = w.pages(bt.context(b), rows, 0, 0);
   Parts p{o.part, o.part_cols, HD};
-  if (!find_parts(w, deal, w.prefix[b] + (long long)np * h, np, p)) return;
+  if (!find_parts(w, deal, w.prefix[b] + w.group(b) * h, np, p)) return;
   const int l5 = threadIdx.x & 31, c = c0 + (threadIdx.x >> 5), d = 4 * l5;
   if (c >= ncol) return;
   float m = kMFloor, l = 0.f;
@@ -1522,7 +1547,7 @@ struct Form {
 // One launch joins both forms' parts: `many_blocks` by H workgroups those of tiles, the rest
 // those of few columns.
 template <int HD, typename S>
-__global__ __launch_bounds__(256) void cache_join_kernel(Form<true> few,
+__global__ __launch_bounds__(256) void cache_join_kernel(Form<true, is_shaped<S>> few,
                                                          Form<false, is_shaped<S>> many, S sh,
                                                          int many_blocks, int few_each) {
   int x = blockIdx.x;
@@ -1549,10 +1574,9 @@ __global__ __launch_bounds__(256) void cache_join_kernel(Form<true> few,
 
 // Few columns: equal ranges of the units again; a wave takes every fourth page, a lane a
 // token.
-template <typename S>
 __device__ __forceinline__ void mass_few(const float* __restrict__ score, const Units<true>& w,
-                                         const Deal& deal, int range, int part_cols, float c_log2,
-                                         const S& sh, const Stat<S>* __restrict__ stat,
+                                         const Deal& deal, int range, int part_cols,
+                                         float c_log2, const f32x2* __restrict__ stat,
                                          const float* __restrict__ mass_in,
                                          float* __restrict__ mass_out) {
   __shared__ int found;
@@ -1574,7 +1598,7 @@ __device__ __forceinline__ void mass_few(const float* __restrict__ score, const 
     const int blk1 = min(np, blk0 + left), ncol = rows * bt.nq;
     float2 z{0.f, 0.f};  // of column `lane`
     if (lane < ncol) {
-      const Stat<S> y = stat[((size_t)h * bt.N + bt.first_row(b)) * bt.nq + lane];
+      const f32x2 y = stat[((size_t)h * bt.N + bt.first_row(b)) * bt.nq + lane];
       z = float2{y[0], y[1]};
     }
     for (int blk = blk0 + wave; blk < blk1; blk += kAttWaves) {
@@ -1592,14 +1616,7 @@ __device__ __forceinline__ void mass_few(const float* __restrict__ score, const 
         const float x = s[c * kPage];
         const float p = __builtin_amdgcn_exp2f(inv < 0.f ? far_exponent(x, c_log2, m)
                                                          : fmaf(x, c_log2, -m)) * fabsf(inv);
-        bool sees = slot <= last;
-        if constexpr (is_shaped<S>) {  // (scores of tokens that it does not see are -inf)
-          sees = true;
-          if (inv != inv) {
-            sees = keys_seen(sh, bt, b, c / bt.nq, ctx, min(ctx + rows, bt.cap()), blk) >> lane & 1;
-          }
-        }
-        y += sees ? p : 0.f;
+        y += slot <= last ? p : 0.f;
         if (++head == bt.nq) head = 0, ++last;
       }
       if (slot < min(ctx + rows, bt.cap())) mass_out[at] = before + y;
@@ -1618,6 +1635,169 @@ __device__ __forceinline__ void mass_few(const float* __restrict__ score, const 
       np = w.pages(ctx, rows, 0, 0);
     }
   }
+}
+
+// The same for shaped calls, whose scores are -inf for the tokens that a column does not see.
+template <typename S>
+__device__ __forceinline__ void mass_scores(const float* __restrict__ score_base,
+                                            const Units<true, true>& w, const Deal& deal, int range,
+                                            int part_cols, float c_log2, const S& sh,
+                                            const f32x4* __restrict__ stat,
+                                            const float* __restrict__ mass_in,
+                                            float* __restrict__ mass_out) {
+  const CacheBatch& bt = w.bt;
+  const int lane = lane_id(), wave = threadIdx.x >> 6;
+  Segment<true> a;
+  if (!a.first(w, deal, range)) return;
+  do {
+    const int ncol = a.rows * bt.nq, len = min(a.ctx + a.rows, bt.cap());
+    f32x4 z{0.f, 0.f, 0.f, 0.f};  // of column `lane`
+    if (lane < ncol) z = stat[((size_t)a.h * bt.N + bt.first_row(a.b)) * bt.nq + lane];
+    for (int blk = a.blk0 + wave; blk < a.blk1; blk += kAttWaves) {
+      const int page = bt.page(a.b, blk), slot = blk * kPage + lane;
+      if (page < 0) continue;
+      const size_t at = ((size_t)page * bt.H + a.h) * kPage + lane;
+      const float before = slot < a.ctx ? mass_in[at] : 0.f;
+      const float* s = score_base + score_page(bt, a.b, a.h, blk) * part_cols * kPage + lane;
+      float y = 0.f;
+      for (int c = 0; c < ncol; ++c) {
+        const float m = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(z[0]), c));
+        const float inv = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(z[1]), c));
+        const float x = s[c * kPage];
+        float p = __builtin_amdgcn_exp2f(inv < 0.f ? far_exponent(x, c_log2, m)
+                                                   : fmaf(x, c_log2, -m)) * fabsf(inv);
+        // (a NaN row counts for the tokens that it sees alone)
+        if (inv != inv && (keys_seen(sh, bt, a.b, c / bt.nq, a.ctx, len, blk) >> lane & 1) == 0)
+          p = 0.f;
+        y += p;
+      }
+      if (slot < len) mass_out[at] = before + y;
+    }
+  } while (a.next(w));
+}
+
+// Shaped calls of more than 16 columns, or whose scores take too much room: the scores are
+// formed again from the keys alone, a page a wave, as in the attention; the probabilities of a
+// lane's 16 keys are summed over its tiles' columns and then over the 16 lanes of a key.
+// us for 48 trees of 25 rows (hd 96, 100 to 4096 tokens): MASSNEW; as sequences of many columns
+// (mass_any) 53.
+template <int HD, typename S>
+__global__ __launch_bounds__(kAttThr, 2) void cache_mass_shaped_kernel(
+    const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const float* __restrict__ kv_scale,
+    Units<true, true> w, Deal deal, float c_log2, S sh, const f32x4* __restrict__ stat,
+    const float* __restrict__ mass_in, float* __restrict__ mass_out) {
+  using F = PageFrags<HD>;
+  constexpr int MT = kShapedCols / 16;
+  __shared__ bf16x8 qs[MT][F::NST][kWave];
+  __shared__ f32x4 zs[MT * 16];
+  const CacheBatch& bt = w.bt;
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 15, g = lane >> 4;
+  Segment<true> a;
+  if (!a.first(w, deal, blockIdx.x)) return;
+  do {
+    const int ncol = a.rows * bt.nq, len = min(a.ctx + a.rows, bt.cap());
+    const int tiles = (ncol + 15) / 16;
+    const size_t qrow = ((size_t)a.h * bt.N + bt.first_row(a.b)) * bt.nq;
+    int pid = -1;  // of the wave's next 64 pages, one a lane
+    auto pages64 = [&](int blk) {
+      const int mine = blk + kAttWaves * lane;
+      pid = mine < a.blk1 ? bt.page(a.b, mine) : -1;
+    };
+    F f;
+    float ks = 0.f, before = 0.f;
+    auto load = [&](int i) {  // (an absent page loads page 0)
+      const size_t pg = (size_t)max(__builtin_amdgcn_readlane(pid, i & 63), 0) * bt.H + a.h;
+      ks = kv_scale[pg * 2];
+      f.load_k(kc + pg * (kPage * HD), lane);
+      before = mass_in[pg * kPage + lane];
+    };
+    if (a.blk0 + wave < a.blk1) pages64(a.blk0 + wave), load(0);
+    __syncthreads();  // the last segment's queries have been read
+    for (int j = wave; j < tiles; j += kAttWaves) {
+      bf16x8 qf[F::NST];
+      load_q<HD>(q + qrow * HD, 16 * j + n, ncol, g, qf);
+#pragma unroll
+      for (int st = 0; st < F::NST; ++st) qs[j][st][lane] = qf[st];
+    }
+    for (int c = threadIdx.x; c < tiles * 16; c += kAttThr)
+      zs[c] = c < ncol ? stat[qrow + c] : f32x4{0.f, 0.f, 0.f, 0.f};
+    const int fewest = min(plain_tokens(sh, a.ctx, 0), bt.cap());
+    __syncthreads();
+    int i = 0;
+    for (int blk = a.blk0 + wave; blk < a.blk1; blk += kAttWaves, ++i) {
+      const int page = __builtin_amdgcn_readlane(pid, i & 63);
+      const bool some = (blk + 1) * kPage > fewest;
+      const float was = before;
+      float sum[16];
+#pragma unroll
+      for (int x = 0; x < 16; ++x) sum[x] = 0.f;
+      bf16x8 kf[4][F::NST];
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int st = 0; st < F::NST; ++st) kf[t][st] = f.key(t, st, ks);
+      if (blk + kAttWaves < a.blk1) {
+        if (((i + 1) & 63) == 0) pages64(blk + kAttWaves);
+        load(i + 1);
+      }
+      if (page < 0) continue;
+      for (int j = 0; j < tiles; ++j) {
+        f32x4 s[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < F::NST; ++st) {
+          const bf16x8 qf = qs[j][st][lane];
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+            s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t][st], qf, s[t], 0, 0, 0);
+        }
+        const f32x4 z = zs[16 * j + n];
+        uint64_t sees = 0;
+        if (some) {
+          if (16 * j + n < ncol)
+            sees = keys_seen(sh, bt, a.b, (16 * j + n) / bt.nq, a.ctx, len, blk);
+          sees >>= 16 * g;
+        }
+        shape_scores<16>(
+            sh, bt, a.b, a.ctx, a.rows, Column{z[2], __float_as_int(z[3])}, blk * kPage + 16 * g,
+            !some, sees, [&](int x) { return s[x >> 2][x & 3]; },
+            [&](int x, float y) { s[x >> 2][x & 3] = y; }, [](int x) { return x; });
+        float m = z[0], c_tile = c_log2;
+        if (__builtin_amdgcn_ballot_w64(z[1] < 0.f)) {
+#pragma unroll
+          for (int x = 0; x < 16; ++x) s[x >> 2][x & 3] = far_exponent(s[x >> 2][x & 3], c_log2, m);
+          m = 0.f;
+          c_tile = 1.f;
+        }
+        const float inv = fabsf(z[1]);
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(s[x >> 2][x & 3], c_tile, -m));
+          // (a NaN row counts for the tokens that it sees alone)
+          sum[x] = fmaf(p, some && (sees >> x & 1) == 0 ? 0.f : inv, sum[x]);
+        }
+      }
+      // over the 16 lanes of a key: each step halves the keys of a lane, which ends with key n
+      auto fold = [&](auto halfv) {
+        constexpr int half = decltype(halfv)::value;
+        const bool up = (n & half) != 0;
+#pragma unroll
+        for (int x = 0; x < half; ++x) {
+          const float mine = up ? sum[x + half] : sum[x], other = up ? sum[x] : sum[x + half];
+          sum[x] = mine + __shfl_xor(other, half);
+        }
+      };
+      fold(std::integral_constant<int, 8>{});
+      fold(std::integral_constant<int, 4>{});
+      fold(std::integral_constant<int, 2>{});
+      fold(std::integral_constant<int, 1>{});
+      const int slot = blk * kPage + lane;
+      if (slot < len)
+        mass_out[((size_t)page * bt.H + a.h) * kPage + lane] = (slot < a.ctx ? was : 0.f) + sum[0];
+    }
+  } while (a.next(w));
 }
 
 // Any columns: a workgroup takes pairs of pages, a wave 32 of their keys, held in
@@ -1824,14 +2004,19 @@ __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8
 template <int HD, typename S>
 __global__ __launch_bounds__(kMassThr, S::kTransforms ? 3 : 4) void cache_mass_kernel(
     const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const float* __restrict__ kv_scale,
-    Units<false, is_shaped<S>> any, int any_ranges, Form<true> few, const float* __restrict__ score, float c_log2,
+    Units<false, is_shaped<S>> any, int any_ranges, Form<true, is_shaped<S>> few, const float* __restrict__ score, float c_log2,
     S sh, const Stat<S>* __restrict__ stat, const float* __restrict__ mass_in,
     float* __restrict__ mass_out) {
   static_assert(kMassThr == kAttThr, "one workgroup size");
   const int x = blockIdx.x;
   if (x >= any_ranges) {
-    mass_few(score, few.w, Deal{few.deal.ranges, few.deal.least, 0}, x - any_ranges,
-             few.o.part_cols, c_log2, sh, stat, mass_in, mass_out);
+    const Deal deal{few.deal.ranges, few.deal.least, 0};
+    if constexpr (is_shaped<S>)
+      mass_scores(score, few.w, deal, x - any_ranges, few.o.part_cols, c_log2, sh, stat, mass_in,
+                  mass_out);
+    else
+      mass_few(score, few.w, deal, x - any_ranges, few.o.part_cols, c_log2, stat, mass_in,
+               mass_out);
     return;
   }
   mass_any<HD>(q, kc, kv_scale, any, Deal{any_ranges, 1, 0}, x, c_log2, sh, stat, mass_in,
@@ -1949,13 +2134,13 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
         {f.ranges, least, round},
         {static_cast<bf16*>(out), stat, reinterpret_cast<float*>(base + f.part), f.cols}};
   };
-  const Form<true> few = form(p.few, kFewLeast, std::min(p.few.ranges, 2 * kCus), std::true_type{},
-                              std::false_type{});
   auto go = [&](auto hdv, auto sh) {
     constexpr int HD = decltype(hdv)::value;
     using S = decltype(sh);
-    const auto many = form(p.many, kManyLeast, 0, std::false_type{},
-                           std::integral_constant<bool, is_shaped<S>>{});
+    constexpr std::integral_constant<bool, is_shaped<S>> wide;
+    const auto few =
+        form(p.few, kFewLeast, std::min(p.few.ranges, 2 * kCus), std::true_type{}, wide);
+    const auto many = form(p.many, kManyLeast, 0, std::false_type{}, wide);
     float c_log2 = 1.4426950408889634f / sqrtf((float)a.hd);
     if constexpr (is_shaped<S>)
       if (S::kTransforms) c_log2 = 1.f;
@@ -1992,6 +2177,17 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
       const int few_blocks = p.few.on ? a.B * ceil_div(few.o.part_cols, few_each) : 0;
       FOE_LAUNCH((cache_join_kernel<HD, S>), dim3(many_blocks + few_blocks, a.H), dim3(256), 0, s,
                  few, many, sh, many_blocks, few_each);
+    }
+    if constexpr (is_shaped<S>) {
+      if (mass_out != nullptr && !p.many.on && score == nullptr) {
+        ProfileScope ps("cache_mass", s);
+        Deal deal = few.deal;
+        deal.round = 0;
+        FOE_LAUNCH((cache_mass_shaped_kernel<HD, S>), dim3(deal.ranges), dim3(kAttThr), 0, s, qb, a.k,
+                   a.kv_scale, few.w, deal, c_log2, sh, static_cast<const f32x4*>(stat), mass_in,
+                   mass_out);
+        return;
+      }
     }
     if (mass_out != nullptr) {
       ProfileScope ps("cache_mass", s);
