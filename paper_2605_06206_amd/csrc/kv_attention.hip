@@ -736,16 +736,17 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
   };
   auto count = [&](const Segment<true>& a) { return (a.blk1 - a.blk0 - pl + NP - 1) / NP; };
   int pid;
-  F f;
+  F f, next;  // (NC == 1: the page in flight has registers of its own)
+  F& to = NC == 1 ? next : f;
   float2 scale;
   auto at = [&](int h, int i) {  // (an absent page loads page 0)
     return (size_t)max(__builtin_amdgcn_readlane(pid, i & 63), 0) * bt.H + h;
   };
   auto load_k = [&](int h, int i) {
     scale = *reinterpret_cast<const float2*>(kv_scale + at(h, i) * 2);
-    f.load_k(kc + at(h, i) * (kPage * HD), lane);
+    to.load_k(kc + at(h, i) * (kPage * HD), lane);
   };
-  auto load_v = [&](int h, int i) { f.load_v(vc + at(h, i) * (kPage * HD), lane); };
+  auto load_v = [&](int h, int i) { to.load_v(vc + at(h, i) * (kPage * HD), lane); };
 
   Segment<true> a;
   if (!a.first(w, deal, blockIdx.x)) return;
@@ -792,6 +793,15 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
       const int blk = a.blk0 + pl + NP * i;
       const int page = __builtin_amdgcn_readlane(pid, i & 63);
       const float ks = scale.x, vs = scale.y;
+      const bool more = i + 1 < mine;
+      if constexpr (NC == 1) {
+        f = next;
+        if (more) {
+          if (((i + 1) & 63) == 0) pid = pages64(a, i + 1);
+          load_k(h, i + 1);
+          load_v(h, i + 1);
+        }
+      }
       f32x4 s[NC][4];
 #pragma unroll
       for (int j = 0; j < NC; ++j)
@@ -810,8 +820,7 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
             s[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[j], s[j][t], 0, 0, 0);
         }
       }
-      const bool more = i + 1 < mine;
-      if (more) {
+      if (NC > 1 && more) {
         if (((i + 1) & 63) == 0) pid = pages64(a, i + 1);
         load_k(h, i + 1);
       }
@@ -900,7 +909,7 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
                   __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[j][u], oacc[j][dt], 0, 0, 0);
           }
       }
-      if (more) load_v(h, i + 1);
+      if (NC > 1 && more) load_v(h, i + 1);
     }
     if (another) {
       pid = pid_ahead;
@@ -2170,7 +2179,7 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
       ProfileScope ps("cache_join", s);
       const int many_blocks = p.many.on ? p.many.tiles * (kTileCols / kJoinCols) : 0;
       // with many parts of a (sequence, group) a column's are shared by a workgroup
-      const int few_each = is_shaped<S> && p.few_cols > kFewCols &&
+      const int few_each = is_shaped<S> && p.few.cols >= 8 &&
                                    few.deal.ranges <= (long long)kJoinParts * a.B * a.H
                                ? 8
                                : 1;
