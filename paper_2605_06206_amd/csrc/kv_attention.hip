@@ -149,63 +149,80 @@ __device__ __forceinline__ uint64_t keys_seen(const Shape<T>& sh, const CacheBat
 }
 
 // NE scores of a lane (get, set) at keys key0 + off(i), in place.  `all`: the column sees them
-// all and none is a new row; else those outside `sees` (bit of key key0 + off(i): off(i)) are
-// taken out.
+// all, at distances place - key >= 0, and none is a new row of a depth of its own.  `masked`: some
+// column does not, and those outside `sees` (bit of key key0 + off(i): off(i)) are taken out.
 template <int NE, bool T, typename Get, typename Set, typename Off>
 __device__ __forceinline__ void shape_scores(const Shape<T>& sh, const CacheBatch& bt, int b, int ctx,
                                              int rows, const Column& c, int key0, bool all,
-                                             uint64_t sees, Get get, Set set, Off off) {
-  if (T && sh.cap != 0.f) {
-    float big = 0.f;
-#pragma unroll
-    for (int i = 0; i < NE; ++i) big = fmaxf(big, fabsf(get(i)));
-    // Scores are mostly well below the cap, where the polynomial is 6 operations; the
-    // exponential, which loses the small ones' last digits besides, is taken where a lane
-    // needs it.
-    if (__builtin_amdgcn_ballot_w64(big > sh.bound) == 0) {
+                                             bool masked, uint64_t sees, Get get, Set set,
+                                             Off off) {
+  if constexpr (T) {
+    const bool biased = sh.a.slope != nullptr;
+    const float d = (float)(c.place - key0);
+    // the bias of a page that is seen whole, linear in the key, joins the score's last product:
+    // slope * key - slope * place (of the page's start, so what is rounded is small where it counts)
+    const bool linear = biased && all;
+    const float base = -c.slope * d;
+    auto each = [&](auto with, auto factor) {
 #pragma unroll
       for (int i = 0; i < NE; ++i) {
-        const float s = get(i), u = s * s;
-        float y = fmaf(sh.poly[4], u, sh.poly[3]);
-        y = fmaf(y, u, sh.poly[2]);
-        y = fmaf(y, u, sh.poly[1]);
-        y = fmaf(y, u, sh.poly[0]);
-        set(i, s * y);
+        const float s = get(i), y = factor(s);
+        set(i, decltype(with)::value ? fmaf(s, y, fmaf(c.slope, (float)off(i), base)) : s * y);
+      }
+    };
+    auto scaled = [&](auto factor) {
+      if (linear) each(std::true_type{}, factor);
+      else each(std::false_type{}, factor);
+    };
+    if (sh.cap != 0.f) {
+      float big = 0.f;
+#pragma unroll
+      for (int i = 0; i < NE; ++i) big = fmaxf(big, fabsf(get(i)));
+      // Scores are mostly well below the cap, where the polynomial is 6 operations; the
+      // exponential, which loses the small ones' last digits besides, is taken where a lane
+      // needs it.
+      if (__builtin_amdgcn_ballot_w64(big > sh.bound) == 0) {
+        scaled([&](float s) {
+          const float u = s * s;
+          float y = fmaf(sh.poly[4], u, sh.poly[3]);
+          y = fmaf(y, u, sh.poly[2]);
+          y = fmaf(y, u, sh.poly[1]);
+          return fmaf(y, u, sh.poly[0]);
+        });
+      } else {
+#pragma unroll
+        for (int i = 0; i < NE; ++i) {
+          if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+          const float x = get(i) * sh.x_of, u = x * x;
+          float y = (float)kTanhPoly[4];
+#pragma unroll
+          for (int k = 3; k >= 0; --k) y = fmaf(y, u, (float)kTanhPoly[k]);
+          const float e = __builtin_amdgcn_exp2f(fabsf(x) * 2.885390081777927f);
+          const float far = copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f), x);
+          const float add = linear ? fmaf(c.slope, (float)off(i), base) : 0.f;
+          set(i, fmaf(sh.cap, fabsf(x) > kTanhBound ? far : x * y, add));
+        }
       }
     } else {
+      scaled([&](float) { return sh.scale; });
+    }
+    if (biased && !all) {
+      if (sh.a.depth != nullptr) {
+        const int row0 = bt.first_row(b);
 #pragma unroll
-      for (int i = 0; i < NE; ++i) {
-        if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
-        const float x = get(i) * sh.x_of, u = x * x;
-        float y = (float)kTanhPoly[4];
+        for (int i = 0; i < NE; ++i) {
+          if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);  // (few loads' addresses at a time)
+          const int key = key0 + off(i), r = key - ctx;
+          const int at = r >= 0 && r < rows ? ctx + sh.a.depth_of(row0 + r) : key;
+          set(i, fmaf(-c.slope, fabsf((float)(c.place - at)), get(i)));
+        }
+      } else {
 #pragma unroll
-        for (int k = 3; k >= 0; --k) y = fmaf(y, u, (float)kTanhPoly[k]);
-        const float e = __builtin_amdgcn_exp2f(fabsf(x) * 2.885390081777927f);
-        const float far = copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f), x);
-        set(i, sh.cap * (fabsf(x) > kTanhBound ? far : x * y));
+        for (int i = 0; i < NE; ++i) set(i, fmaf(-c.slope, fabsf(d - (float)off(i)), get(i)));
       }
     }
-  } else if (T && sh.a.slope != nullptr) {
-#pragma unroll
-    for (int i = 0; i < NE; ++i) set(i, get(i) * sh.scale);
   }
-  if (T && sh.a.slope != nullptr) {
-    if (!all && sh.a.depth != nullptr) {
-      const int row0 = bt.first_row(b);
-#pragma unroll
-      for (int i = 0; i < NE; ++i) {
-        if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);  // (few loads' addresses at a time)
-        const int key = key0 + off(i), r = key - ctx;
-        const int at = r >= 0 && r < rows ? ctx + sh.a.depth_of(row0 + r) : key;
-        set(i, fmaf(-c.slope, fabsf((float)(c.place - at)), get(i)));
-      }
-    } else {
-      const float d = (float)(c.place - key0);
-#pragma unroll
-      for (int i = 0; i < NE; ++i) set(i, fmaf(-c.slope, fabsf(d - (float)off(i)), get(i)));
-    }
-  }
-  if (!all) {
+  if (masked) {
     const uint32_t lo = (uint32_t)sees, hi = (uint32_t)(sees >> 32);
 #pragma unroll
     for (int i = 0; i < NE; ++i) {
@@ -709,10 +726,11 @@ __device__ __forceinline__ size_t score_page(const CacheBatch& bt, int b, int h,
   return ((size_t)b * bt.H + h) * bt.max_blocks + blk;
 }
 
-template <int HD, int NC, int G>
+template <int HD, int NC, int G, bool T>
 struct ShapedLds {
   FewLds<HD> few;
   bf16x8 q[G * NC][HD / 32][kWave];
+  Column cols[T ? 16 * NC * G : 1];
 };
 
 template <int HD, int NC, int G, typename S>
@@ -722,7 +740,7 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
     AttnOut o, float* __restrict__ score_base) {
   using F = PageFrags<HD>;
   constexpr int NP = kAttWaves / G;  // pages at a time
-  __shared__ ShapedLds<HD, NC, G> lds;
+  __shared__ ShapedLds<HD, NC, G, S::kTransforms> lds;
   const CacheBatch& bt = w.bt;
   const int lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), cg = wave % G, pl = wave / G;
@@ -742,11 +760,13 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
   auto at = [&](int h, int i) {  // (an absent page loads page 0)
     return (size_t)max(__builtin_amdgcn_readlane(pid, i & 63), 0) * bt.H + h;
   };
+  // (the lane's addresses in a page are not held where registers are short)
+  auto place = [&]() { return NC == 1 ? lane : opaque_int(lane); };
   auto load_k = [&](int h, int i) {
     scale = *reinterpret_cast<const float2*>(kv_scale + at(h, i) * 2);
-    to.load_k(kc + at(h, i) * (kPage * HD), lane);
+    to.load_k(kc + at(h, i) * (kPage * HD), place());
   };
-  auto load_v = [&](int h, int i) { to.load_v(vc + at(h, i) * (kPage * HD), lane); };
+  auto load_v = [&](int h, int i) { to.load_v(vc + at(h, i) * (kPage * HD), place()); };
 
   Segment<true> a;
   if (!a.first(w, deal, blockIdx.x)) return;
@@ -759,12 +779,11 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
     const size_t qrow = ((size_t)h * bt.N + bt.first_row(b)) * bt.nq;
     int pid_ahead = -1;
     if (another) pid_ahead = pages64(ahead, 0);
-    Column col[NC];
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
       const int c = col0 + 16 * j + n;
-      col[j] = column_of(sh, bt, b, h, ctx, c, ncol);
       if (pl == 0) {
+        if constexpr (S::kTransforms) lds.cols[c] = column_of(sh, bt, b, h, ctx, c, ncol);
         bf16x8 qf[F::NST];
         load_q<HD>(q + qrow * HD, c, ncol, g, qf);
 #pragma unroll
@@ -831,17 +850,21 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
           __builtin_amdgcn_sched_barrier(0);  // (a tile of columns after another)
+          const int c = col0 + 16 * j + opaque_int(n);  // (not held, nor its slope and place)
           uint64_t sees = 0;
+          bool masked = false;
           if (some) {
-            const int c = col0 + 16 * j + opaque_int(n);  // (its row is not held)
             if (c < ncol) sees = keys_seen(sh, bt, b, c / bt.nq, ctx, len, blk);
             saw[j] |= sees != 0;
+            masked = __builtin_amdgcn_ballot_w64(c < ncol && ~sees != 0) != 0;
             sees >>= 16 * g;
           } else {
-            saw[j] |= col0 + 16 * j + n < ncol;
+            saw[j] |= c < ncol;
           }
+          Column col{};
+          if constexpr (S::kTransforms) col = lds.cols[c];
           shape_scores<16>(
-              sh, bt, b, ctx, rows, col[j], k0, !some, sees,
+              sh, bt, b, ctx, rows, col, k0, !some, masked, sees,
               [&](int x) { return s[j][x >> 2][x & 3]; },
               [&](int x, float y) { s[j][x >> 2][x & 3] = y; }, [](int x) { return x; });
           if (NC == 1 && score != nullptr && n < ncol) {
@@ -1205,7 +1228,8 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
           const float2 sp = cols[fresh(col)];
           const Column cl{sp.x, __float_as_int(sp.y)};
           shape_scores<32>(
-              sh, bt, b, ctx, rows, cl, blk * kPage + k4, !some, sees >> k4,
+              sh, bt, b, ctx, rows, cl, blk * kPage + k4, !some,
+              some && __builtin_amdgcn_ballot_w64(fresh(col) < ncol && ~sees != 0) != 0, sees >> k4,
               [&](int x) { return sacc[x >> 4][x & 15]; },
               [&](int x, float y) { sacc[x >> 4][x & 15] = y; },
               [](int x) { return 32 * (x >> 4) + 8 * ((x & 15) >> 2) + (x & 3); });
@@ -1764,14 +1788,16 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_mass_shaped_kernel(
         }
         const f32x4 z = zs[16 * j + n];
         uint64_t sees = 0;
+        bool masked = false;
         if (some) {
           if (16 * j + n < ncol)
             sees = keys_seen(sh, bt, a.b, (16 * j + n) / bt.nq, a.ctx, len, blk);
+          masked = __builtin_amdgcn_ballot_w64(~sees != 0) != 0;
           sees >>= 16 * g;
         }
         shape_scores<16>(
             sh, bt, a.b, a.ctx, a.rows, Column{z[2], __float_as_int(z[3])}, blk * kPage + 16 * g,
-            !some, sees, [&](int x) { return s[x >> 2][x & 3]; },
+            !some, masked, sees, [&](int x) { return s[x >> 2][x & 3]; },
             [&](int x, float y) { s[x >> 2][x & 3] = y; }, [](int x) { return x; });
         float m = z[0], c_tile = c_log2;
         if (__builtin_amdgcn_ballot_w64(z[1] < 0.f)) {
@@ -1785,7 +1811,7 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_mass_shaped_kernel(
         for (int x = 0; x < 16; ++x) {
           const float p = __builtin_amdgcn_exp2f(fmaf(s[x >> 2][x & 3], c_tile, -m));
           // (a NaN row counts for the tokens that it sees alone)
-          sum[x] = fmaf(p, some && (sees >> x & 1) == 0 ? 0.f : inv, sum[x]);
+          sum[x] = fmaf(p, masked && (sees >> x & 1) == 0 ? 0.f : inv, sum[x]);
         }
       }
       // over the 16 lanes of a key: each step halves the keys of a lane, which ends with key n
@@ -1941,18 +1967,21 @@ __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8
               smem + (qat ^ (uint32_t)((4 * (st / 2) + st % 2) << 4)));
           x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[st], qf, x, 0, 0, 0);
         }
-        Column cl{};  // (SHAPED)
         const int col = t * kMassCols + qi;
         if constexpr (SHAPED) {
           const int i0 = t * kMassCols / bt.nq;
           const bool all = plain_tokens(sh, ctx, i0) >= min(key0 + 32, len + 1);
           uint64_t sees = 0;
-          cl = Column{zs[2], __float_as_int(zs[3])};
-          if (!all && col < ncol)
-            sees = keys_seen(sh, bt, b, col / bt.nq, ctx, len, key0 / kPage) >> ((wave & 1) * 32 + 4 * hl);
+          bool masked = false;
+          if (!all) {
+            if (col < ncol) sees = keys_seen(sh, bt, b, col / bt.nq, ctx, len, key0 / kPage);
+            masked = __builtin_amdgcn_ballot_w64(~sees != 0) != 0;
+            sees >>= (wave & 1) * 32 + 4 * hl;
+          }
           shape_scores<16>(
-              sh, bt, b, ctx, rows, cl, key0 + 4 * hl, all, sees, [&](int v) { return x[v]; },
-              [&](int v, float y) { x[v] = y; }, [](int v) { return 8 * (v >> 2) + (v & 3); });
+              sh, bt, b, ctx, rows, Column{zs[2], __float_as_int(zs[3])}, key0 + 4 * hl, all,
+              masked, sees, [&](int v) { return x[v]; }, [&](int v, float y) { x[v] = y; },
+              [](int v) { return 8 * (v >> 2) + (v & 3); });
         } else if (ctx + t * kMassCols / bt.nq + 1 < min(key0 + 32, len + 1)) {
           // (the tile's first column sees the fewest)
           const int seen = col < ncol ? ctx + col / bt.nq + 1 : 0;

@@ -27,9 +27,12 @@ namespace {
 // and a row's heads one after another 22, so 16.
 constexpr int kAppThr = 256;
 
-// With row places of their own (depth, a tree of drafts) a page's positions lie between the
+// With row places of their own (DEPTH, a tree of drafts) a page's positions lie between the
 // least and the largest of its rows' depths, which a tree of up to 64 levels keeps within the
-// same two sets of eight; rows further apart form a sine each.
+// same two sets of eight; rows further apart form a sine each.  us for 128 trees of 32 to 64 rows,
+// 8 groups, two query heads, hd 128 (89 MB in 1800 workgroups of 27 rows on average, a chain of
+// loads each): 32; in registers for four workgroups a CU instead of three, some of them
+// spilled, 36.
 template <int HD, bool DEPTH>
 __global__ __launch_bounds__(kAppThr) void cache_append_kernel(
     const bf16* __restrict__ qkv, bf16* __restrict__ q_out, uint8_t* __restrict__ kc,
@@ -38,9 +41,12 @@ __global__ __launch_bounds__(kAppThr) void cache_append_kernel(
     double rope_scale) {
   constexpr int NIT = kPage * 16 / kAppThr;  // rows of a thread
   constexpr int VROW = kPage + 4;            // bytes of a value dim's row in LDS
-  // (cosine, sine) of pair i at positions first + 8 a (rows 0-7) and b (rows 8-15)
-  __shared__ float2 turn[16][HD / 2];
-  __shared__ __align__(16) uint8_t vt[HD * VROW];
+  // (cosine, sine) of pair i at positions first + 8 a (rows 0-7) and b (rows 8-15), or (DEPTH)
+  // of each of the page's rows; the values take their place (DEPTH)
+  __shared__ __align__(16) float2 turn[DEPTH ? kPage : 16][HD / 2];
+  __shared__ __align__(16) uint8_t vt_own[DEPTH ? 16 : HD * VROW];
+  uint8_t* vt = DEPTH ? reinterpret_cast<uint8_t*>(turn) : vt_own;
+  static_assert(!DEPTH || sizeof(turn) >= HD * VROW, "room for the values");
   __shared__ double inv_freq[HD / 2];
   const int tid = threadIdx.x, h = blockIdx.y;
   // (the first frequency is 1 for an infinite base too, where 0 * log2 is NaN)
@@ -69,21 +75,9 @@ __global__ __launch_bounds__(kAppThr) void cache_append_kernel(
   auto has = [&](int it) { return act && it * (kAppThr / 16) + rr < cnt; };
   auto some = [&](int it) { return it * (kAppThr / 16) < cnt; };  // (uniform)
   const int uc = act ? u : 0;
-  // depths of the thread's rows; the least and the largest of the page (DEPTH)
-  int dep[NIT], dep_min = 0, dep_max = 0;
-  if constexpr (DEPTH) {
-    auto depth_at = [&](int i) { return min(max(depth[r0 + i0 + i], 0), kMaxDepth); };
-    dep_min = dep_max = depth_at(min(lane_id(), cnt - 1));
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-      dep_min = min(dep_min, __shfl_xor(dep_min, o));
-      dep_max = max(dep_max, __shfl_xor(dep_max, o));
-    }
-#pragma unroll
-    for (int it = 0; it < NIT; ++it)
-      dep[it] = depth_at(min(it * (kAppThr / 16) + rr, cnt - 1)) - dep_min;
-  }
-  const bool wide = DEPTH && dep_max - dep_min >= kPage;  // (uniform)
+  auto depth_at = [&](int i) { return min(max(depth[r0 + i0 + min(i, cnt - 1)], 0), kMaxDepth); };
+  int dep_lane = 0;  // (DEPTH) depth of row `lane`, on its way beside the rows
+  if constexpr (DEPTH) dep_lane = depth_at(lane_id());
   bf16x8 v[NIT];
   bf16x4 x1[NIT], x2[NIT];
   auto load_head = [&](int j) {
@@ -122,37 +116,50 @@ __global__ __launch_bounds__(kAppThr) void cache_append_kernel(
     if (page >= 0 && t0 < kPage && touched(t0) && !full(t0))
       beside[k] = *reinterpret_cast<const u32x4*>(vp + i * 16);
   }
+  // (DEPTH) the least and the largest depth of the page's rows, and those of the thread's rows
+  // past the least, a byte each where they fit
+  int dep_min = 0, dep_max = 0;
+  uint32_t dep = 0;
+  if constexpr (DEPTH) {
+    dep_min = dep_max = dep_lane;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+      dep_min = min(dep_min, __shfl_xor(dep_min, o));
+      dep_max = max(dep_max, __shfl_xor(dep_max, o));
+    }
+#pragma unroll
+    for (int it = 0; it < NIT; ++it) {
+      const int d = __shfl(dep_lane, it * (kAppThr / 16) + rr) - dep_min;
+      dep |= (uint32_t)(d & 255) << (8 * it);
+    }
+  }
+  const bool wide = DEPTH && dep_max - dep_min >= kPage;  // (uniform)
   const long long first = (pos != nullptr ? pos[b] : c0) + (long long)(DEPTH ? dep_min : i0);
-  auto turn_of = [&](long long p, int i) {
+  const int n_pos = DEPTH ? dep_max - dep_min + 1 : cnt;
+  const int na = wide ? cnt : (n_pos + 7) / 8, nb = wide ? 0 : min(n_pos, 8);
+  {
     constexpr double kTwoPi = 6.283185307179586476925286766559;
-    double a = (double)p / rope_scale * inv_freq[i];
-    a -= kTwoPi * floor(a / kTwoPi);
-    float2 t;
-    sincosf((float)a, &t.y, &t.x);
-    return t;
-  };
-  if (!wide) {
-    const int n = DEPTH ? dep_max - dep_min + 1 : cnt, na = (n + 7) / 8, nb = min(n, 8);
     for (int e = tid; e < (na + nb) * (HD / 2); e += kAppThr) {
       const int k = e / (HD / 2), i = e % (HD / 2);
-      turn[k < na ? k : 8 + k - na][i] = turn_of(k < na ? first + 8 * k : k - na, i);
+      long long at = k < na ? first + 8 * k : k - na;
+      if (DEPTH && wide) at = first - dep_min + depth_at(k);
+      double a = (double)at / rope_scale * inv_freq[i];
+      a -= kTwoPi * floor(a / kTwoPi);
+      float2 t;
+      sincosf((float)a, &t.y, &t.x);
+      turn[k < na ? k : 8 + k - na][i] = t;
     }
   }
   __syncthreads();
   float cs[NIT][4], sn[NIT][4];
 #pragma unroll
   for (int it = 0; it < NIT; ++it) {
-    // position - first
-    const int i = DEPTH ? dep[it] : min(it * (kAppThr / 16) + rr, cnt - 1);
+    const int row = min(it * (kAppThr / 16) + rr, cnt - 1);
+    const int i = DEPTH ? (int)(dep >> (8 * it) & 255) : row;  // position - first
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      if (wide) {
-        const float2 t = turn_of(first + i, 4 * uc + e);
-        cs[it][e] = t.x;
-        sn[it][e] = t.y;
-        continue;
-      }
-      const float2 a = turn[i >> 3][4 * uc + e], d = turn[8 + (i & 7)][4 * uc + e];
+      const float2 a = turn[DEPTH && wide ? row : i >> 3][4 * uc + e];
+      const float2 d = DEPTH && wide ? float2{1.f, 0.f} : turn[8 + (i & 7)][4 * uc + e];
       cs[it][e] = a.x * d.x - a.y * d.y;
       sn[it][e] = a.y * d.x + a.x * d.y;
     }
@@ -275,11 +282,13 @@ __global__ __launch_bounds__(kAppThr) void cache_append_kernel(
 // One workgroup per (sequence, group), a page of kept tokens after another.  Kept token j comes
 // from row path[j] >= j, so a page's sources lie in it or behind it, and what one page's step
 // writes no later step reads; within a page everything is read before anything is written.
-// (1) The path's length: its first entry that does not ascend.  (2) The page's 64 slots find
-// their source page and its scales; slots before the context's end are their own.  (3) Keys as
-// rows of 16-byte pieces, values as pieces of one dim and 16 tokens, the moved tokens' bytes
-// put in one by one; the page's new scales follow from the largest magnitudes.  (4) Pieces that
-// changed are stored.
+// (1) What the first page holds before the context's end is on its way while the path's length
+// is found: its first entry that does not ascend.  (2) The kept slots find their source page and
+// its scales.  (3) Keys as rows of 16-byte pieces, values as pieces of one dim and 16 tokens, a
+// moved token's bytes put in one by one; the page's new scales follow from the largest
+// magnitudes.  (4) Pieces that changed are stored.
+// us for 128 sequences, 0 to 12 kept tokens, 8 groups, hd 128 (10 MB; bound by the chain of
+// dependent loads): ACCEPTUS; every token's source looked up in LDS for each of its dims 20.
 constexpr int kAccThr = 256;
 
 template <int HD>
@@ -290,12 +299,35 @@ __global__ __launch_bounds__(kAccThr) void cache_accept_kernel(
   constexpr int NK = (kPage * CPR + kAccThr - 1) / kAccThr;  // pieces of a thread
   constexpr int NV = ((kPage / kSub) * HD + kAccThr - 1) / kAccThr;
   __shared__ int end;
-  __shared__ int from[kPage];      // source slot in its page (of 64), by slot
-  __shared__ int from_page[kPage]; // its page, -1: not there
+  __shared__ int from[kPage];       // source slot in its page (of 64), by slot
+  __shared__ int from_page[kPage];  // its page, -1: not there
   __shared__ float2 from_scale[kPage];
   const int tid = threadIdx.x, b = blockIdx.x, h = blockIdx.y;
   const int c0 = bt.context(b), rows = min(bt.rows(b), bt.cap() - c0);
   path += (size_t)b * max_path;
+  u32x4 k[NK], v[NV];
+  float2 own_scale;
+  auto slot_of = [&](int n) { return (n * kAccThr + tid) / CPR; };           // of a key piece
+  auto first_of = [&](int n) { return (n * kAccThr + tid) / HD * kSub; };    // of a value piece
+  // keys of the slots before lo, and all values, of a page as it is
+  auto load_own = [&](int page, int lo) {
+    const size_t own = ((size_t)max(page, 0) * bt.H + h) * (kPage * HD);
+    own_scale = *reinterpret_cast<const float2*>(kv_scale + ((size_t)max(page, 0) * bt.H + h) * 2);
+#pragma unroll
+    for (int n = 0; n < NK; ++n) {
+      k[n] = zero_u32x4();
+      if (slot_of(n) < lo)
+        k[n] = *reinterpret_cast<const u32x4*>(kc + own + (n * kAccThr + tid) * 16);
+    }
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      v[n] = zero_u32x4();
+      if (first_of(n) < kPage)
+        v[n] = *reinterpret_cast<const u32x4*>(vc + own + (n * kAccThr + tid) * 16);
+    }
+  };
+  int page = bt.page(b, c0 / kPage);
+  load_own(page, c0 % kPage);
   if (tid == 0) end = max_path;
   __syncthreads();
   for (int i = tid; i < max_path; i += kAccThr) {
@@ -311,9 +343,12 @@ __global__ __launch_bounds__(kAccThr) void cache_accept_kernel(
   if (m == 0) return;
   for (int blk = c0 / kPage; blk <= (c0 + m - 1) / kPage; ++blk) {
     const int lo = max(c0 - blk * kPage, 0), hi = min(c0 + m - blk * kPage, kPage);
-    const int page = bt.page(b, blk);
+    if (blk > c0 / kPage) {
+      __syncthreads();  // the last page's slots have been read
+      page = bt.page(b, blk);
+      load_own(page, 0);
+    }
     if (page < 0) continue;  // (uniform) nowhere to keep them
-    __syncthreads();         // the last page's slots have been read
     if (tid < kPage) {
       int p = page, t = tid;
       if (tid >= lo && tid < hi) {
@@ -329,9 +364,14 @@ __global__ __launch_bounds__(kAccThr) void cache_accept_kernel(
     }
     __syncthreads();
     const size_t own = (size_t)page * bt.H + h;
-    auto moved = [&](int t) { return t >= lo && t < hi && (from_page[t] != page || from[t] != t); };
-    u32x4 k[NK], v[NV];
-    float2 amax{0.f, 0.f};
+    // the kept slots (those that stay in place among them), of 16 tokens from t0 on
+    auto kept = [&](int t0) {
+      const uint64_t below = hi < 64 ? (1ull << hi) - 1 : ~0ull;
+      return (uint32_t)((below & ~((1ull << lo) - 1)) >> t0) & 0xffffu;
+    };
+    auto bytes = [](uint32_t bits) {  // 0xff where one of four bits is set
+      return ((bits & 15u) * 0x00204081u & 0x01010101u) * 0xffu;
+    };
     auto bigger = [](float a, uint32_t w) {  // (NaN counts for no scale)
       const float x = fmaxf(fabsf(__builtin_amdgcn_cvt_f32_fp8(w, 0)),
                             fabsf(__builtin_amdgcn_cvt_f32_fp8(w, 1)));
@@ -339,95 +379,91 @@ __global__ __launch_bounds__(kAccThr) void cache_accept_kernel(
                             fabsf(__builtin_amdgcn_cvt_f32_fp8(w, 3)));
       return fmaxf(a, fmaxf(x, y));
     };
+    float2 amax{0.f, 0.f};
 #pragma unroll
     for (int n = 0; n < NK; ++n) {
-      const int i = n * kAccThr + tid, t = i / CPR;
-      k[n] = zero_u32x4();
-      if (t < hi && from_page[t] >= 0)
+      const int t = slot_of(n);
+      if (t >= lo && t < hi && from_page[t] >= 0)
         k[n] = *reinterpret_cast<const u32x4*>(
-            kc + (((size_t)from_page[t] * bt.H + h) * kPage + from[t]) * HD + i % CPR * 16);
-    }
-#pragma unroll
-    for (int n = 0; n < NV; ++n) {
-      const int i = n * kAccThr + tid, d = i % HD, t0 = i / HD * kSub;
-      v[n] = zero_u32x4();
-      if (t0 >= hi) continue;
-      v[n] = *reinterpret_cast<const u32x4*>(vc + own * (kPage * HD) + i * 16);
-#pragma unroll
-      for (int e = 0; e < kSub; ++e) {
-        const int t = t0 + e, p = from_page[t];
-        if (!moved(t)) continue;
-        uint32_t x = 0;
-        if (p >= 0)
-          x = vc[((size_t)p * bt.H + h) * (kPage * HD) + from[t] / kSub * (HD * kSub) + d * kSub +
-                 from[t] % kSub];
-        v[n][e / 4] = (v[n][e / 4] & ~(0xffu << (8 * (e % 4)))) | x << (8 * (e % 4));
-      }
+            kc + (((size_t)from_page[t] * bt.H + h) * kPage + from[t]) * HD +
+            (n * kAccThr + tid) % CPR * 16);
     }
     float w = 0.f;
-    if (mass != nullptr && tid < kPage && moved(tid) && from_page[tid] >= 0)
+    if (mass != nullptr && tid >= lo && tid < hi && from_page[tid] >= 0)
       w = mass[((size_t)from_page[tid] * bt.H + h) * kPage + from[tid]];
 #pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      const int t0 = first_of(n), d = (n * kAccThr + tid) % HD;
+      if (t0 >= hi) continue;
+      const uint32_t bits = kept(t0), below = lo > t0 ? (1u << min(lo - t0, 16)) - 1 : 0u;
+      float x = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x = bigger(x, v[n][e] & bytes(below >> (4 * e)));
+      amax.y = fmaxf(amax.y, x * own_scale.y);
+      uint32_t fresh[kSub];
+#pragma unroll
+      for (int e = 0; e < kSub; ++e) {
+        fresh[e] = 0;
+        const int t = t0 + e, p = bits >> e & 1 ? from_page[t] : -1;
+        if (p >= 0)
+          fresh[e] = vc[((size_t)p * bt.H + h) * (kPage * HD) + from[t] / kSub * (HD * kSub) +
+                        d * kSub + from[t] % kSub];
+      }
+#pragma unroll
+      for (int e = 0; e < kSub; ++e) {
+        if ((bits >> e & 1) == 0) continue;
+        amax.y = fmaxf(amax.y, fabsf(__builtin_amdgcn_cvt_f32_fp8(fresh[e], 0)) * from_scale[t0 + e].y);
+        v[n][e / 4] = (v[n][e / 4] & ~(0xffu << (8 * (e % 4)))) | fresh[e] << (8 * (e % 4));
+      }
+    }
+#pragma unroll
     for (int n = 0; n < NK; ++n) {
-      const int t = (n * kAccThr + tid) / CPR;
+      const int t = slot_of(n);
       if (t >= hi) continue;
       float x = 0.f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) x = bigger(x, k[n][e]);
       amax.x = fmaxf(amax.x, x * from_scale[t].x);
     }
-#pragma unroll
-    for (int n = 0; n < NV; ++n) {
-      const int t0 = (n * kAccThr + tid) / HD * kSub;
-      if (t0 >= hi) continue;
-#pragma unroll
-      for (int e = 0; e < kSub; ++e) {
-        if (t0 + e >= hi) continue;
-        const float x = fabsf(__builtin_amdgcn_cvt_f32_fp8(v[n][e / 4] >> (8 * (e % 4)), 0));
-        amax.y = fmaxf(amax.y, x * from_scale[t0 + e].y);
-      }
-    }
     amax = block_max<kAccThr>(amax);  // (and everything has been read)
     const float ks = block_scale(amax.x), vs = block_scale(amax.y);
     const float ki = pow2_inv(ks), vi = pow2_inv(vs);
     if (tid == 0) *reinterpret_cast<float2*>(kv_scale + own * 2) = float2{ks, vs};
-    if (mass != nullptr && tid < kPage && moved(tid)) mass[own * kPage + tid] = w;
+    if (mass != nullptr && tid >= lo && tid < hi) mass[own * kPage + tid] = w;
 #pragma unroll
     for (int n = 0; n < NK; ++n) {
-      const int i = n * kAccThr + tid, t = i / CPR;
+      const int t = slot_of(n);
       if (t >= hi) continue;
       const float r = scale_ratio(from_scale[t].x, ki);
-      if (r == 1.f && !moved(t)) continue;
+      if (r == 1.f && t < lo) continue;
 #pragma unroll
       for (int e = 0; e < 4; ++e) k[n][e] = rescale4(k[n][e], r);
-      *reinterpret_cast<u32x4*>(kc + own * (kPage * HD) + i * 16) = k[n];
+      *reinterpret_cast<u32x4*>(kc + own * (kPage * HD) + (n * kAccThr + tid) * 16) = k[n];
     }
+    const float r_own = scale_ratio(own_scale.y, vi);
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
-      const int i = n * kAccThr + tid, t0 = i / HD * kSub;
+      const int t0 = first_of(n);
       if (t0 >= hi) continue;
-      bool changed = false;
+      const uint32_t bits = kept(t0), below = lo > t0 ? (1u << min(lo - t0, 16)) - 1 : 0u;
+      if (bits == 0 && r_own == 1.f) continue;
+      if (r_own != 1.f) {
 #pragma unroll
-      for (int e = 0; e < kSub; e += 4) {
-        uint32_t fresh = 0;
-        float r[4];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const int t = t0 + e + x;
-          const bool in = t < hi;
-          r[x] = in ? scale_ratio(from_scale[t].y, vi) : 1.f;
-          if (in && (r[x] != 1.f || moved(t))) fresh |= 0xffu << (8 * x);
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t m4 = bytes(below >> (4 * e));
+          if (m4 != 0) v[n][e] = (v[n][e] & ~m4) | (rescale4(v[n][e], r_own) & m4);
         }
-        if (fresh == 0) continue;
-        changed = true;
-        const uint32_t o = v[n][e / 4];
-        const uint32_t y = to_codes4(__builtin_amdgcn_cvt_f32_fp8(o, 0) * r[0],
-                                     __builtin_amdgcn_cvt_f32_fp8(o, 1) * r[1],
-                                     __builtin_amdgcn_cvt_f32_fp8(o, 2) * r[2],
-                                     __builtin_amdgcn_cvt_f32_fp8(o, 3) * r[3]);
-        v[n][e / 4] = (o & ~fresh) | (y & fresh);
       }
-      if (changed) *reinterpret_cast<u32x4*>(vc + own * (kPage * HD) + i * 16) = v[n];
+#pragma unroll
+      for (int e = 0; e < kSub; ++e) {
+        if ((bits >> e & 1) == 0) continue;
+        const float r = scale_ratio(from_scale[t0 + e].y, vi);
+        const int sh = 8 * (e % 4);
+        const float x = __builtin_amdgcn_cvt_f32_fp8(v[n][e / 4] >> sh, 0) * r;
+        const uint32_t c = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false) & 255u;
+        v[n][e / 4] = (v[n][e / 4] & ~(255u << sh)) | c << sh;
+      }
+      *reinterpret_cast<u32x4*>(vc + own * (kPage * HD) + (n * kAccThr + tid) * 16) = v[n];
     }
   }
 }
