@@ -224,10 +224,12 @@ __device__ __forceinline__ void shape_scores(const Shape<T>& sh, const CacheBatc
   }
   if (masked) {
     const uint32_t lo = (uint32_t)sees, hi = (uint32_t)(sees >> 32);
+    // (through the bit spread over a word: a comparison each would hold a scalar pair each)
 #pragma unroll
     for (int i = 0; i < NE; ++i) {
-      if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
-      if (((off(i) < 32 ? lo : hi) >> (off(i) & 31) & 1) == 0) set(i, -__builtin_inff());
+      const uint32_t keep =
+          (uint32_t)__builtin_amdgcn_sbfe((int)(off(i) < 32 ? lo : hi), off(i) & 31, 1);
+      set(i, __uint_as_float((keep & __float_as_uint(get(i))) | (~keep & 0xff800000u)));
     }
   }
 }
@@ -642,6 +644,11 @@ __device__ __forceinline__ void few_columns(
   }
 }
 
+__device__ __forceinline__ long long uniform64(long long x) {
+  return (long long)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 |
+         (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+}
+
 // The segments of a range of the few-column form: pages blk0 .. blk1-1 (of np) of sequence b,
 // group h, numbered from `unit` on; `slot` is where a part goes.
 template <bool WIDE>
@@ -658,6 +665,11 @@ struct Segment {
     locate<kAttThr>(
         bt.B, [&](int i) { return w.group(i) * bt.H; }, deal, r, w.prefix, total, b, off);
     if (b < 0) return false;
+    if constexpr (WIDE) {  // (in scalar registers, and all that follows)
+      b = __builtin_amdgcn_readfirstlane(b);
+      total = uniform64(total);
+      off = uniform64(off);
+    }
     // (at most 2^37 units, of tables of 2^31 entries and 64 groups, in a quarter of them or 1024
     // ranges)
     const int per = (int)deal.per(total);
@@ -719,11 +731,154 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_few_kernel(
 // same page at about the same time, from L2 but for the first.  The queries are held in LDS, as
 // the waves read them; a page's keys give their registers to the next page's as soon as the
 // scores are formed, and its values after the second product, so that two waves of a SIMD
-// have room for 32 columns each.  The next segment's page numbers are loaded beside this one's
+// have room for 32 columns each.  (Pages through a ring of LDS-DMA stages, loaded once for the
+// four waves of 128 columns: 460 us for four sequences of 131072 tokens, 64 rows of two heads, 8
+// groups, and so 380: the waves wait for one another at each page.)  The next segment's page numbers are loaded beside this one's
 // pages, and its first page before this one's states are merged.
 // number of a page among the kept scores of shaped calls
 __device__ __forceinline__ size_t score_page(const CacheBatch& bt, int b, int h, int blk) {
   return ((size_t)b * bt.H + h) * bt.max_blocks + blk;
+}
+
+// Where a page lies: sequence, context, new rows, columns and tokens, number; `some`: not every
+// column sees it whole (see plain_tokens).
+struct PageOf {
+  int b, ctx, rows, ncol, len, blk;
+  bool some;
+};
+
+// A wave's 16 NC columns: sums, running maxima and sums of probabilities.
+template <int NC, int NDT>
+struct ShapedState {
+  f32x4 oacc[NC][NDT];
+  float m_run[NC], l_run[NC];
+  bool saw[NC], far[NC];  // any token; (uniform) a column's maximum is far from 0
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) oacc[j][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      m_run[j] = kMFloor;
+      l_run[j] = 0.f;
+      saw[j] = far[j] = false;
+    }
+  }
+  // the page's scores s into probabilities p, in bf16 for the product with the values; columns
+  // col0 on; `score`: where column 0's scores are kept, or null
+  template <typename S>
+  __device__ __forceinline__ void softmax(const S& sh, const CacheBatch& bt, const PageOf& at,
+                                          int col0, int lane, const Column* cols, float c_log2,
+                                          f32x4 (*s)[4], bf16x8 (*p)[2], float* score) {
+    const int n = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      __builtin_amdgcn_sched_barrier(0);  // (a tile of columns after another)
+      const int c = col0 + 16 * j + opaque_int(n);  // (not held, nor its slope and place)
+      uint64_t sees = 0;
+      bool masked = false;
+      if (at.some) {
+        if (c < at.ncol) sees = keys_seen(sh, bt, at.b, c / bt.nq, at.ctx, at.len, at.blk);
+        saw[j] |= sees != 0;
+        masked = __builtin_amdgcn_ballot_w64(c < at.ncol && ~sees != 0) != 0;
+        sees >>= 16 * g;
+      } else {
+        saw[j] |= c < at.ncol;
+      }
+      Column col{};
+      if constexpr (S::kTransforms) col = cols[c];
+      shape_scores<16>(
+          sh, bt, at.b, at.ctx, at.rows, col, at.blk * kPage + 16 * g, !at.some, masked, sees,
+          [&](int x) { return s[j][x >> 2][x & 3]; },
+          [&](int x, float y) { s[j][x >> 2][x & 3] = y; }, [](int x) { return x; });
+      if (NC == 1 && score != nullptr && n < at.ncol) {
+        float* to = score + n * kPage + 16 * g;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4*>(to + 4 * t) = s[j][t];
+      }
+      float mx = s[j][0][0];
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[j][t][e]);
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      // (the maximum moves only when a page exceeds it by 2^8, as with causal columns)
+      const float mxs = mx * c_log2;
+      const bool need = mxs > m_run[j] + 8.f;
+      if (__builtin_amdgcn_ballot_w64(need)) {
+        const float m_new = need ? mxs : m_run[j];
+        const float x = __builtin_amdgcn_exp2f(m_run[j] - m_new);
+        m_run[j] = m_new;
+        far[j] = __builtin_amdgcn_ballot_w64(far_max(m_run[j])) != 0;
+        l_run[j] *= x;
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) oacc[j][dt][e] *= x;
+      }
+      float c_page = c_log2, m_page = m_run[j];
+      if (far[j]) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[j][t][e] = far_exponent(s[j][t][e], c_log2, m_run[j]);
+        c_page = 1.f;
+        m_page = 0.f;
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x = __builtin_amdgcn_exp2f(fmaf(s[j][t][e], c_page, -m_page));
+          l_run[j] += x;
+          p[j][t >> 1][4 * (t & 1) + e] = (bf16)x;
+        }
+      // (formed here, so that the next tile has the scores' registers)
+      asm volatile("" : "+v"(p[j][0]), "+v"(p[j][1]));
+    }
+  }
+  // the sums over a column's lanes
+  __device__ __forceinline__ void finish(int j) {
+    if (saw[j]) m_run[j] = fmaxf(m_run[j], kMSeen);
+    l_run[j] += __shfl_xor(l_run[j], 16);
+    l_run[j] += __shfl_xor(l_run[j], 32);
+  }
+};
+
+// Slots past the last token hold anything, and 0 * NaN is NaN: their bytes of values of 16
+// tokens from key k0 on are cleared.
+template <int NDT>
+__device__ __forceinline__ void clear_past(u32x4 (&v)[NDT], int k0, int len) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int in = len - (k0 + 4 * e);
+    const uint32_t m = in >= 4 ? 0xffffffffu : in <= 0 ? 0u : (1u << (8 * in)) - 1;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) v[dt][e] &= m;
+  }
+}
+
+// Writes four dims from d on of column c of a segment: the result where it is a whole tile, else
+// the part.
+template <int HD, typename S>
+__device__ __forceinline__ void put_columns(const S& sh, const CacheBatch& bt, const Segment<true>& a,
+                                            const AttnOut& o, size_t qrow, int c, int d,
+                                            const f32x4& x, float m, float l) {
+  if (a.blk0 == 0 && a.blk1 == a.np) {
+    const float inv = inv_sum(m, l);
+    const int row = c / bt.nq;
+    bf16* to = o.out +
+               (((size_t)(bt.first_row(a.b) + row) * bt.H + a.h) * bt.nq + c - row * bt.nq) * HD;
+    *reinterpret_cast<bf16x4*>(to + d) = bf16x4{(bf16)(x[0] * inv), (bf16)(x[1] * inv),
+                                                (bf16)(x[2] * inv), (bf16)(x[3] * inv)};
+    if (d == 0 && o.stat != nullptr)
+      put_stat(sh, bt, a.b, a.h, a.ctx, a.rows, c, qrow + c, o, m, inv);
+  } else {
+    float* pt = o.part + a.slot * part_floats(o.part_cols, HD);
+    *reinterpret_cast<f32x4*>(pt + (size_t)c * HD + d) = x;
+    if (d == 0) reinterpret_cast<float2*>(pt + o.part_cols * HD)[c] = float2{m, l};
+  }
 }
 
 template <int HD, int NC, int G, bool T>
@@ -787,7 +942,7 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
         bf16x8 qf[F::NST];
         load_q<HD>(q + qrow * HD, c, ncol, g, qf);
 #pragma unroll
-        for (int st = 0; st < F::NST; ++st) lds.q[NC * cg + j][st][lane] = qf[st];
+        for (int ks = 0; ks < F::NST; ++ks) lds.q[NC * cg + j][ks][lane] = qf[ks];
       }
     }
     const int len = min(ctx + rows, bt.cap());  // tokens the cache holds now
@@ -795,17 +950,8 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
     float* score = NC == 1 && score_base != nullptr
                        ? score_base + score_page(bt, b, h, a.blk0) * o.part_cols * kPage
                        : nullptr;
-    f32x4 oacc[NC][F::NDT];
-    float m_run[NC], l_run[NC];
-    bool saw[NC], far[NC];  // any token; (uniform) a column's maximum is far from 0
-#pragma unroll
-    for (int j = 0; j < NC; ++j) {
-#pragma unroll
-      for (int dt = 0; dt < F::NDT; ++dt) oacc[j][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-      m_run[j] = kMFloor;
-      l_run[j] = 0.f;
-      saw[j] = far[j] = false;
-    }
+    ShapedState<NC, F::NDT> st;
+    st.clear();
     const int mine = count(a);
     __syncthreads();
     for (int i = 0; i < mine; ++i) {
@@ -827,13 +973,13 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
 #pragma unroll
         for (int t = 0; t < 4; ++t) s[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int st = 0; st < F::NST; ++st) {
+      for (int step = 0; step < F::NST; ++step) {
         bf16x8 qf[NC];
 #pragma unroll
-        for (int j = 0; j < NC; ++j) qf[j] = lds.q[NC * cg + j][st][lane];
+        for (int j = 0; j < NC; ++j) qf[j] = lds.q[NC * cg + j][step][lane];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-          const bf16x8 kf = f.key(t, st, ks);
+          const bf16x8 kf = f.key(t, step, ks);
 #pragma unroll
           for (int j = 0; j < NC; ++j)
             s[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[j], s[j][t], 0, 0, 0);
@@ -847,80 +993,12 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
         const int k0 = blk * kPage + 16 * g;
         const bool some = (blk + 1) * kPage > fewest;
         bf16x8 p[NC][2];
-#pragma unroll
-        for (int j = 0; j < NC; ++j) {
-          __builtin_amdgcn_sched_barrier(0);  // (a tile of columns after another)
-          const int c = col0 + 16 * j + opaque_int(n);  // (not held, nor its slope and place)
-          uint64_t sees = 0;
-          bool masked = false;
-          if (some) {
-            if (c < ncol) sees = keys_seen(sh, bt, b, c / bt.nq, ctx, len, blk);
-            saw[j] |= sees != 0;
-            masked = __builtin_amdgcn_ballot_w64(c < ncol && ~sees != 0) != 0;
-            sees >>= 16 * g;
-          } else {
-            saw[j] |= c < ncol;
-          }
-          Column col{};
-          if constexpr (S::kTransforms) col = lds.cols[c];
-          shape_scores<16>(
-              sh, bt, b, ctx, rows, col, k0, !some, masked, sees,
-              [&](int x) { return s[j][x >> 2][x & 3]; },
-              [&](int x, float y) { s[j][x >> 2][x & 3] = y; }, [](int x) { return x; });
-          if (NC == 1 && score != nullptr && n < ncol) {
-            float* to = score + ((size_t)(blk - a.blk0) * o.part_cols + n) * kPage + 16 * g;
-#pragma unroll
-            for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4*>(to + 4 * t) = s[j][t];
-          }
-          float mx = s[j][0][0];
-#pragma unroll
-          for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[j][t][e]);
-          mx = fmaxf(mx, __shfl_xor(mx, 16));
-          mx = fmaxf(mx, __shfl_xor(mx, 32));
-          // (the maximum moves only when a page exceeds it by 2^8, as with causal columns)
-          const float mxs = mx * c_log2;
-          const bool need = mxs > m_run[j] + 8.f;
-          if (__builtin_amdgcn_ballot_w64(need)) {
-            const float m_new = need ? mxs : m_run[j];
-            const float x = __builtin_amdgcn_exp2f(m_run[j] - m_new);
-            m_run[j] = m_new;
-            far[j] = __builtin_amdgcn_ballot_w64(far_max(m_run[j])) != 0;
-            l_run[j] *= x;
-#pragma unroll
-            for (int dt = 0; dt < F::NDT; ++dt)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) oacc[j][dt][e] *= x;
-          }
-          float c_page = c_log2, m_page = m_run[j];
-          if (far[j]) {
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) s[j][t][e] = far_exponent(s[j][t][e], c_log2, m_run[j]);
-            c_page = 1.f;
-            m_page = 0.f;
-          }
-#pragma unroll
-          for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float x = __builtin_amdgcn_exp2f(fmaf(s[j][t][e], c_page, -m_page));
-              l_run[j] += x;
-              p[j][t >> 1][4 * (t & 1) + e] = (bf16)x;
-            }
-        }
-        if (some) {
-          // slots past the last token hold anything: 0 * NaN is NaN
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int in = len - (k0 + 4 * e);
-            const uint32_t m = in >= 4 ? 0xffffffffu : in <= 0 ? 0u : (1u << (8 * in)) - 1;
-#pragma unroll
-            for (int dt = 0; dt < F::NDT; ++dt) f.v[dt][e] &= m;
-          }
-        }
+        const PageOf at_page{b, ctx, rows, ncol, len, blk, some};
+        st.softmax(sh, bt, at_page, col0, lane, lds.cols, c_log2, s, p,
+                   NC == 1 && score != nullptr
+                       ? score + (size_t)(blk - a.blk0) * o.part_cols * kPage
+                       : nullptr);
+        if (some) clear_past(f.v, k0, len);
 #pragma unroll
         for (int dt = 0; dt < F::NDT; ++dt)
 #pragma unroll
@@ -928,8 +1006,8 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
             const bf16x8 vf = codes_to_bf16(f.v[dt][2 * u], f.v[dt][2 * u + 1], vs);
 #pragma unroll
             for (int j = 0; j < NC; ++j)
-              oacc[j][dt] =
-                  __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[j][u], oacc[j][dt], 0, 0, 0);
+              st.oacc[j][dt] =
+                  __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[j][u], st.oacc[j][dt], 0, 0, 0);
           }
       }
       if (NC > 1 && more) load_v(h, i + 1);
@@ -938,43 +1016,29 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
       pid = pid_ahead;
       if (count(ahead) > 0) load_k(ahead.h, 0), load_v(ahead.h, 0);
     }
-    const bool whole = a.blk0 == 0 && a.blk1 == a.np;
-    float* pt = o.part + a.slot * part_floats(o.part_cols, HD);
     const int me = opaque_int(lane), n1 = me & 15, g1 = me >> 4;  // (not held over the pages)
-    // four dims from d on of column c
-    auto put = [&](int c, int d, const f32x4& x, float m, float l) {
-      if (whole) {
-        const float inv = inv_sum(m, l);
-        const int row = c / bt.nq;
-        bf16* to = o.out + (((size_t)(bt.first_row(b) + row) * bt.H + h) * bt.nq + c - row * bt.nq) * HD;
-        *reinterpret_cast<bf16x4*>(to + d) = bf16x4{(bf16)(x[0] * inv), (bf16)(x[1] * inv),
-                                                    (bf16)(x[2] * inv), (bf16)(x[3] * inv)};
-        if (d == 0 && o.stat != nullptr) put_stat(sh, bt, b, h, ctx, rows, c, qrow + c, o, m, inv);
-      } else {
-        *reinterpret_cast<f32x4*>(pt + (size_t)c * HD + d) = x;
-        if (d == 0) reinterpret_cast<float2*>(pt + o.part_cols * HD)[c] = float2{m, l};
-      }
+    const auto put = [&](int c, int d, const f32x4& x, float m, float l) {
+      put_columns<HD>(sh, bt, a, o, qrow, c, d, x, m, l);
     };
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
-      if (saw[j]) m_run[j] = fmaxf(m_run[j], kMSeen);
-      l_run[j] += __shfl_xor(l_run[j], 16);
-      l_run[j] += __shfl_xor(l_run[j], 32);
+      st.finish(j);
       if constexpr (NP == 1) {  // the wave has all of its columns' pages
         const int c = col0 + 16 * j + n1;
         if (c < ncol) {
 #pragma unroll
-          for (int dt = 0; dt < F::NDT; ++dt) put(c, 16 * dt + 4 * g1, oacc[j][dt], m_run[j], l_run[j]);
+          for (int dt = 0; dt < F::NDT; ++dt)
+            put(c, 16 * dt + 4 * g1, st.oacc[j][dt], st.m_run[j], st.l_run[j]);
         }
       } else {
         // the states of the waves of a column group, merged in wave order, 16 columns of each
         // group at a time
         if (16 * j >= ncol) break;  // (uniform)
         __syncthreads();  // what was in LDS before has been read
-        if (g1 == 0) lds.few.mm[wave][n1] = m_run[j], lds.few.ll[wave][n1] = l_run[j];
+        if (g1 == 0) lds.few.mm[wave][n1] = st.m_run[j], lds.few.ll[wave][n1] = st.l_run[j];
 #pragma unroll
         for (int dt = 0; dt < F::NDT; ++dt)
-          *reinterpret_cast<f32x4*>(&lds.few.oo[wave][n1][16 * dt + 4 * g1]) = oacc[j][dt];
+          *reinterpret_cast<f32x4*>(&lds.few.oo[wave][n1][16 * dt + 4 * g1]) = st.oacc[j][dt];
         __syncthreads();
         for (int i = opaque_int(threadIdx.x); i < G * 16 * (HD / 4); i += kAttThr) {
           const int gr = i / (16 * (HD / 4)), c = i / (HD / 4) % 16, d = i % (HD / 4) * 4;
@@ -1059,8 +1123,7 @@ cache_attn_tile_kernel(const bf16* __restrict__ q, const uint8_t* __restrict__ k
       h = __builtin_amdgcn_readfirstlane(h);
       t = __builtin_amdgcn_readfirstlane(t);
       blk0 = __builtin_amdgcn_readfirstlane(blk0);
-      left = (long long)__builtin_amdgcn_readfirstlane((int)(left >> 32)) << 32 |
-             (uint32_t)__builtin_amdgcn_readfirstlane((int)left);
+      left = uniform64(left);
     }
   }
   size_t slot = 2 * (size_t)range;
