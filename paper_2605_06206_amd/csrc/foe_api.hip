@@ -615,7 +615,7 @@ int cache_append(const char* name, foe_dtype dt, int H, int B, int N, int nq, in
                  const int32_t* row_start, const int32_t* ctx_len, const int32_t* pos,
                  const int32_t* depth, const int32_t* block_table, void* q_out, void* k_cache,
                  void* v_cache, float* kv_scale, void* stream) {
-  const std::string at = std::string(name) + ": ";
+  const auto at = [name] { return std::string(name) + ": "; };
   Check c;
   check_dtype(c, dt);
   check_cache(c, H, B, n_pages, max_blocks);
@@ -633,9 +633,9 @@ int cache_append(const char* name, foe_dtype dt, int H, int B, int N, int nq, in
   c.tensor(v_cache, any, "v_cache");
   c.tensor(kv_scale, any, "kv_scale");
   c.need(!any || qkv != q_out, "q_out must not be qkv");
-  if (!c.err.empty()) return fail(FOE_ERR_INVALID, at + c.err);
+  if (!c.err.empty()) return fail(FOE_ERR_INVALID, at() + c.err);
   if (dt != FOE_BF16 || !cache_hd(hd))
-    return fail(FOE_ERR_UNSUPPORTED, at + "bf16 with hd = 96 or 128 only");
+    return fail(FOE_ERR_UNSUPPORTED, at() + "bf16 with hd = 96 or 128 only");
   if (!any) return FOE_OK;
   const CacheArgs a{H, hd, B, n_pages, max_blocks, static_cast<uint8_t*>(k_cache),
                     static_cast<uint8_t*>(v_cache), kv_scale, block_table, ctx_len};
@@ -670,7 +670,7 @@ int cache_attention(const char* name, foe_dtype dt, int H, int B, int N, int nq,
                     const int32_t* block_table, const void* k_cache, const void* v_cache,
                     const float* kv_scale, const float* mass_in, float* mass_out, void* out,
                     void* ws, size_t ws_bytes, void* stream) {
-  const std::string at = std::string(name) + ": ";
+  const auto at = [name] { return std::string(name) + ": "; };
   Check c;
   check_dtype(c, dt);
   check_cache(c, H, B, n_pages, max_blocks);
@@ -689,16 +689,16 @@ int cache_attention(const char* name, foe_dtype dt, int H, int B, int N, int nq,
   c.tensor(mass_out, false, "mass_out");
   c.need((mass_in == nullptr) == (mass_out == nullptr), "mass_in and mass_out go together");
   c.tensor(out, any, "out");
-  if (!c.err.empty()) return fail(FOE_ERR_INVALID, at + c.err);
+  if (!c.err.empty()) return fail(FOE_ERR_INVALID, at() + c.err);
   if (dt != FOE_BF16 || !cache_hd(hd))
-    return fail(FOE_ERR_UNSUPPORTED, at + "bf16 with hd = 96 or 128 only");
+    return fail(FOE_ERR_UNSUPPORTED, at() + "bf16 with hd = 96 or 128 only");
   if (!any) return FOE_OK;
   const size_t need = cache_attention_scratch_bytes(H, B, N, nq, hd, max_blocks, max_rows,
                                                     mass_out != nullptr, scores != nullptr);
   if (need > 0 && (ws == nullptr || !aligned16(ws)))
-    return fail(FOE_ERR_INVALID, at + "ws is NULL or not 16-byte aligned");
+    return fail(FOE_ERR_INVALID, at() + "ws is NULL or not 16-byte aligned");
   if (ws_bytes < need)
-    return fail(FOE_ERR_WORKSPACE, at + "workspace needs " + std::to_string(need) +
+    return fail(FOE_ERR_WORKSPACE, at() + "workspace needs " + std::to_string(need) +
                                        " bytes, got " + std::to_string(ws_bytes));
   const CacheArgs a{H, hd, B, n_pages, max_blocks,
                     static_cast<uint8_t*>(const_cast<void*>(k_cache)),

@@ -244,7 +244,9 @@ struct CacheScores {
   const uint32_t* tree;    // [N][words]
   int words;
   const int32_t* depth;    // [N]
-  __device__ __forceinline__ int depth_of(int row) const { return min(max(depth[row], 0), kMaxDepth); }
+  __device__ __forceinline__ int depth_of(int row) const {
+    return min(max(depth[row], 0), kMaxDepth);
+  }
 };
 size_t cache_attention_scratch_bytes(int H, int B, int N, int nq, int hd, int max_blocks,
                                      int max_rows, bool mass, bool shaped);

@@ -152,15 +152,15 @@ __device__ __forceinline__ uint64_t keys_seen(const Shape<T>& sh, const CacheBat
 // all, at distances place - key >= 0, and none is a new row of a depth of its own.  `masked`: some
 // column does not, and those outside `sees` (bit of key key0 + off(i): off(i)) are taken out.
 template <int NE, bool T, typename Get, typename Set, typename Off>
-__device__ __forceinline__ void shape_scores(const Shape<T>& sh, const CacheBatch& bt, int b, int ctx,
-                                             int rows, const Column& c, int key0, bool all,
+__device__ __forceinline__ void shape_scores(const Shape<T>& sh, const CacheBatch& bt, int b,
+                                             int ctx, int rows, const Column& c, int key0, bool all,
                                              bool masked, uint64_t sees, Get get, Set set,
                                              Off off) {
   if constexpr (T) {
     const bool biased = sh.a.slope != nullptr;
     const float d = (float)(c.place - key0);
     // the bias of a page that is seen whole, linear in the key, joins the score's last product:
-    // slope * key - slope * place (of the page's start, so what is rounded is small where it counts)
+    // slope * key - slope * place (of the page's start: what is rounded is small where it counts)
     const bool linear = biased && all;
     const float base = -c.slope * d;
     auto each = [&](auto with, auto factor) {
@@ -636,7 +636,8 @@ __device__ __forceinline__ void few_columns(
       const float inv = inv_sum(m, l);
       const int row = bt.first_row(b) + c / bt.nq;
       o.out[(((size_t)row * bt.H + h) * bt.nq + c % bt.nq) * HD + d] = (bf16)(x * inv);
-      if (d == 0 && o.stat != nullptr) put_stat(NoShape{}, bt, b, h, ctx, rows, c, qrow + c, o, m, inv);
+      if (d == 0 && o.stat != nullptr)
+        put_stat(NoShape{}, bt, b, h, ctx, rows, c, qrow + c, o, m, inv);
     } else {
       pt[i] = x;
       if (d == 0) reinterpret_cast<float2*>(pt + o.part_cols * HD)[c] = float2{m, l};
@@ -733,8 +734,9 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_few_kernel(
 // scores are formed, and its values after the second product, so that two waves of a SIMD
 // have room for 32 columns each.  (Pages through a ring of LDS-DMA stages, loaded once for the
 // four waves of 128 columns: 460 us for four sequences of 131072 tokens, 64 rows of two heads, 8
-// groups, and so 380: the waves wait for one another at each page.)  The next segment's page numbers are loaded beside this one's
-// pages, and its first page before this one's states are merged.
+// groups, and so 380: the waves wait for one another at each page.)  The next segment's page
+// numbers are loaded beside this one's pages, and its first page before this one's states are
+// merged.
 // number of a page among the kept scores of shaped calls
 __device__ __forceinline__ size_t score_page(const CacheBatch& bt, int b, int h, int blk) {
   return ((size_t)b * bt.H + h) * bt.max_blocks + blk;
@@ -862,9 +864,9 @@ __device__ __forceinline__ void clear_past(u32x4 (&v)[NDT], int k0, int len) {
 // Writes four dims from d on of column c of a segment: the result where it is a whole tile, else
 // the part.
 template <int HD, typename S>
-__device__ __forceinline__ void put_columns(const S& sh, const CacheBatch& bt, const Segment<true>& a,
-                                            const AttnOut& o, size_t qrow, int c, int d,
-                                            const f32x4& x, float m, float l) {
+__device__ __forceinline__ void put_columns(const S& sh, const CacheBatch& bt,
+                                            const Segment<true>& a, const AttnOut& o, size_t qrow,
+                                            int c, int d, const f32x4& x, float m, float l) {
   if (a.blk0 == 0 && a.blk1 == a.np) {
     const float inv = inv_sum(m, l);
     const int row = c / bt.nq;
@@ -1431,10 +1433,10 @@ struct Parts {
 };
 // units u0 .. of a tile of np pages; false where one range wrote it whole
 template <bool FEW, bool WIDE>
-__device__ __forceinline__ bool find_parts(const Units<FEW, WIDE>& w, const Deal& deal, long long u0,
-                                           int np, Parts& p) {
+__device__ __forceinline__ bool find_parts(const Units<FEW, WIDE>& w, const Deal& deal,
+                                           long long u0, int np, Parts& p) {
   const long long per = deal.per(w.prefix[w.bt.B]);
-  if constexpr (FEW && WIDE) {  // (a range that starts before the pages has none of the tile before)
+  if constexpr (FEW && WIDE) {  // (a range that starts before the pages has none of a tile's)
     p.r0 = (int)((u0 + kStartPages) / per);
     p.r1 = (int)((u0 + kStartPages + np - 1) / per);
     p.first_late = u0 > p.r0 * per;
@@ -1775,7 +1777,7 @@ __device__ __forceinline__ void mass_scores(const float* __restrict__ score_base
 // Shaped calls of more than 16 columns, or whose scores take too much room: the scores are
 // formed again from the keys alone, a page a wave, as in the attention; the probabilities of a
 // lane's 16 keys are summed over its tiles' columns and then over the 16 lanes of a key.
-// us for 48 trees of 25 rows (hd 96, 100 to 4096 tokens): MASSNEW; as sequences of many columns
+// us for 48 trees of 25 rows (hd 96, 100 to 4096 tokens): 30; as sequences of many columns
 // (mass_any) 53.
 template <int HD, typename S>
 __global__ __launch_bounds__(kAttThr, 2) void cache_mass_shaped_kernel(
@@ -2059,7 +2061,8 @@ __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8
             const int seen = ctx + col / bt.nq + 1;
             uint64_t sees = 0;
             if constexpr (SHAPED)
-              sees = keys_seen(sh, bt, b, col / bt.nq, ctx, len, key0 / kPage) >> ((wave & 1) * 32 + 4 * hl);
+              sees = keys_seen(sh, bt, b, col / bt.nq, ctx, len, key0 / kPage) >>
+                     ((wave & 1) * 32 + 4 * hl);
 #pragma unroll
             for (int v = 0; v < 16; ++v)
               if (SHAPED ? (sees >> (8 * (v >> 2) + (v & 3)) & 1) != 0
@@ -2105,9 +2108,9 @@ __device__ __forceinline__ void mass_any(const bf16* __restrict__ q, const uint8
 template <int HD, typename S>
 __global__ __launch_bounds__(kMassThr, S::kTransforms ? 3 : 4) void cache_mass_kernel(
     const bf16* __restrict__ q, const uint8_t* __restrict__ kc, const float* __restrict__ kv_scale,
-    Units<false, is_shaped<S>> any, int any_ranges, Form<true, is_shaped<S>> few, const float* __restrict__ score, float c_log2,
-    S sh, const Stat<S>* __restrict__ stat, const float* __restrict__ mass_in,
-    float* __restrict__ mass_out) {
+    Units<false, is_shaped<S>> any, int any_ranges, Form<true, is_shaped<S>> few,
+    const float* __restrict__ score, float c_log2, S sh, const Stat<S>* __restrict__ stat,
+    const float* __restrict__ mass_in, float* __restrict__ mass_out) {
   static_assert(kMassThr == kAttThr, "one workgroup size");
   const int x = blockIdx.x;
   if (x >= any_ranges) {
@@ -2158,7 +2161,8 @@ AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_
   p.few_cols = kFewCols;
   if (shaped && most <= kShapedCols)
     while (p.few_cols < most) p.few_cols *= 2;
-  p.few.on = most <= p.few_cols || (B > 1 && (long long)(N - max_rows) * nq <= kFewCols * (B - 1LL));
+  p.few.on =
+      most <= p.few_cols || (B > 1 && (long long)(N - max_rows) * nq <= kFewCols * (B - 1LL));
   p.many.on = most > p.few_cols;
   p.few.hi = p.few_cols;
   p.many.lo = p.few.on ? p.few_cols : 0;
@@ -2205,7 +2209,8 @@ Shape<T> shape_of(const CacheScores& a, int hd) {
     // (beyond, the squares and coefficients could leave fp32)
     sh.bound = a.cap >= 0x1p-8f && a.cap <= 0x1p10f ? (float)(kTanhBound / k) : -1.f;
     for (int i = 0; i < 5; ++i)
-      sh.poly[i] = sh.bound > 0.f ? (float)(a.cap * kLog2e * kTanhPoly[i] * pow(k, 2 * i + 1)) : 0.f;
+      sh.poly[i] =
+          sh.bound > 0.f ? (float)(a.cap * kLog2e * kTanhPoly[i] * pow(k, 2 * i + 1)) : 0.f;
   }
   return sh;
 }
@@ -2284,9 +2289,9 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
         ProfileScope ps("cache_mass", s);
         Deal deal = few.deal;
         deal.round = 0;
-        FOE_LAUNCH((cache_mass_shaped_kernel<HD, S>), dim3(deal.ranges), dim3(kAttThr), 0, s, qb, a.k,
-                   a.kv_scale, few.w, deal, c_log2, sh, static_cast<const f32x4*>(stat), mass_in,
-                   mass_out);
+        FOE_LAUNCH((cache_mass_shaped_kernel<HD, S>), dim3(deal.ranges), dim3(kAttThr), 0, s, qb,
+                   a.k, a.kv_scale, few.w, deal, c_log2, sh, static_cast<const f32x4*>(stat),
+                   mass_in, mass_out);
         return;
       }
     }

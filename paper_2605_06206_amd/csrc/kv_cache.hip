@@ -288,7 +288,7 @@ __global__ __launch_bounds__(kAppThr) void cache_append_kernel(
 // moved token's bytes put in one by one; the page's new scales follow from the largest
 // magnitudes.  (4) Pieces that changed are stored.
 // us for 128 sequences, 0 to 12 kept tokens, 8 groups, hd 128 (10 MB; bound by the chain of
-// dependent loads): ACCEPTUS; every token's source looked up in LDS for each of its dims 20.
+// dependent loads): 16; every token's source looked up in LDS for each of its dims 20.
 constexpr int kAccThr = 256;
 
 template <int HD>
@@ -412,7 +412,8 @@ __global__ __launch_bounds__(kAccThr) void cache_accept_kernel(
 #pragma unroll
       for (int e = 0; e < kSub; ++e) {
         if ((bits >> e & 1) == 0) continue;
-        amax.y = fmaxf(amax.y, fabsf(__builtin_amdgcn_cvt_f32_fp8(fresh[e], 0)) * from_scale[t0 + e].y);
+        amax.y = fmaxf(amax.y, fabsf(__builtin_amdgcn_cvt_f32_fp8(fresh[e], 0)) *
+                                   from_scale[t0 + e].y);
         v[n][e / 4] = (v[n][e / 4] & ~(0xffu << (8 * (e % 4)))) | fresh[e] << (8 * (e % 4));
       }
     }
@@ -935,8 +936,11 @@ hipError_t launch_cache_append(const CacheArgs& a, int nq, int N, const void* qk
                static_cast<const bf16*>(qkv), static_cast<bf16*>(q), a.k, a.v, a.kv_scale, bt, pos,
                depth, log2((double)theta), (double)scale);
   };
-  if (depth != nullptr) go(a.hd == 96 ? cache_append_kernel<96, true> : cache_append_kernel<128, true>);
-  else go(a.hd == 96 ? cache_append_kernel<96, false> : cache_append_kernel<128, false>);
+  if (depth != nullptr) {
+    go(a.hd == 96 ? cache_append_kernel<96, true> : cache_append_kernel<128, true>);
+  } else {
+    go(a.hd == 96 ? cache_append_kernel<96, false> : cache_append_kernel<128, false>);
+  }
   return hipGetLastError();
 }
 

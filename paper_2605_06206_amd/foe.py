@@ -404,19 +404,17 @@ def cache_append(qkv, k, v, kv_scale, block_table, ctx_len, row_start, theta, sc
     dev, i32, dt = qkv.get_device(), torch.int32, _dt(qkv)
     if q is None:
         q = torch.empty((H, N, nq, hd), dtype=qkv.dtype, device=qkv.device)
-    sizes = (dt, H, B, N, nq, hd, n_pages, max_blocks, theta, scale,
-             _arg(qkv, "qkv", qkv.dtype, (H, N, nq + 2, hd), dev),
-             _arg(row_start, "row_start", i32, (B + 1,), dev),
-             _arg(ctx_len, "ctx_len", i32, (B,), dev),
-             None if pos is None else _arg(pos, "pos", i32, (B,), dev))
-    rest = (_arg(block_table, "block_table", i32, (B, max_blocks), dev),
-            _arg(q, "q", qkv.dtype, (H, N, nq, hd), dev),
-            *_pool_args(k, v, kv_scale, n_pages, H, hd, dev), _stream_of(dev))
-    if depth is None:
-        _check(lib().foe_cache_append(*sizes, *rest), "foe_cache_append")
-    else:
-        depth = _arg(depth, "depth", i32, (N,), dev)
-        _check(lib().foe_cache_append_tree(*sizes, depth, *rest), "foe_cache_append_tree")
+    name = "foe_cache_append" if depth is None else "foe_cache_append_tree"
+    rc = getattr(lib(), name)(
+        dt, H, B, N, nq, hd, n_pages, max_blocks, theta, scale,
+        _arg(qkv, "qkv", qkv.dtype, (H, N, nq + 2, hd), dev),
+        _arg(row_start, "row_start", i32, (B + 1,), dev), _arg(ctx_len, "ctx_len", i32, (B,), dev),
+        None if pos is None else _arg(pos, "pos", i32, (B,), dev),
+        *(() if depth is None else (_arg(depth, "depth", i32, (N,), dev),)),
+        _arg(block_table, "block_table", i32, (B, max_blocks), dev),
+        _arg(q, "q", qkv.dtype, (H, N, nq, hd), dev),
+        *_pool_args(k, v, kv_scale, n_pages, H, hd, dev), _stream_of(dev))
+    _check(rc, name)
     return q
 
 
@@ -452,24 +450,23 @@ def cache_attention(q, k, v, kv_scale, block_table, ctx_len, row_start, max_rows
     ws, ws_ptr, ws_bytes = _ws_arg(
         ws, lambda: cache_attention_workspace_bytes(q, block_table, max_rows,
                                                     mass_out is not None, shaped), q.device, dev)
-    sizes = (dt, H, B, N, nq, hd, n_pages, max_blocks, max_rows)
-    rest = (_arg(q, "q", q.dtype, (H, N, nq, hd), dev),
-            _arg(row_start, "row_start", i32, (B + 1,), dev),
-            _arg(ctx_len, "ctx_len", i32, (B,), dev),
-            _arg(block_table, "block_table", i32, (B, max_blocks), dev),
-            *_pool_args(k, v, kv_scale, n_pages, H, hd, dev),
-            None if mass_in is None else _arg(mass_in, "mass_in", f32, mshape, dev),
-            None if mass_out is None else _arg(mass_out, "mass_out", f32, mshape, dev),
-            _arg(out, "out", q.dtype, (N, H, nq, hd), dev), ws_ptr, ws_bytes, _stream_of(dev))
-    if not shaped:
-        _check(lib().foe_cache_attention(*sizes, *rest), "foe_cache_attention")
-        return out
-    words = 0 if tree is None else tree.shape[-1]
-    shape = (cap, None if slope is None else _arg(slope, "slope", f32, (H, nq), dev),
-             None if prefix is None else _arg(prefix, "prefix", i32, (B,), dev),
-             None if tree is None else _arg(tree, "tree", i32, (N, words), dev), words,
-             None if depth is None else _arg(depth, "depth", i32, (N,), dev))
-    _check(lib().foe_cache_attention_ex(*sizes, *shape, *rest), "foe_cache_attention_ex")
+    name, scores = "foe_cache_attention", ()
+    if shaped:
+        name, words = "foe_cache_attention_ex", 0 if tree is None else tree.shape[-1]
+        scores = (cap, None if slope is None else _arg(slope, "slope", f32, (H, nq), dev),
+                  None if prefix is None else _arg(prefix, "prefix", i32, (B,), dev),
+                  None if tree is None else _arg(tree, "tree", i32, (N, words), dev), words,
+                  None if depth is None else _arg(depth, "depth", i32, (N,), dev))
+    rc = getattr(lib(), name)(
+        dt, H, B, N, nq, hd, n_pages, max_blocks, max_rows, *scores,
+        _arg(q, "q", q.dtype, (H, N, nq, hd), dev),
+        _arg(row_start, "row_start", i32, (B + 1,), dev), _arg(ctx_len, "ctx_len", i32, (B,), dev),
+        _arg(block_table, "block_table", i32, (B, max_blocks), dev),
+        *_pool_args(k, v, kv_scale, n_pages, H, hd, dev),
+        None if mass_in is None else _arg(mass_in, "mass_in", f32, mshape, dev),
+        None if mass_out is None else _arg(mass_out, "mass_out", f32, mshape, dev),
+        _arg(out, "out", q.dtype, (N, H, nq, hd), dev), ws_ptr, ws_bytes, _stream_of(dev))
+    _check(rc, name)
     return out
 
 

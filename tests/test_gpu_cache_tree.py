@@ -42,7 +42,8 @@ def pack(rows, words):
     out = np.zeros((len(rows), words * 32), dtype=np.uint8)
     for i, r in enumerate(rows):
         out[i, :len(r)] = r
-    return torch.from_numpy(np.packbits(out, axis=1, bitorder="little").view(np.int32).copy()).to(DEV)
+    bits = np.packbits(out, axis=1, bitorder="little").view(np.int32)
+    return torch.from_numpy(bits.copy()).to(DEV)
 
 
 # ---- append -----------------------------------------------------------------------
