@@ -421,7 +421,7 @@ size_t foe_cache_attention_workspace_bytes(int H, int B, int N, int nq, int hd, 
  *   cap                    0 (the scores as they are) or in [2^-64, 2^64]
  *   slope     [H, nq]      fp32   slope of the distance bias of each head
  *   prefix    [B]  int32   the first prefix[b] tokens are seen by every row of sequence b (those
- *                          that the cache holds), whatever their order
+ *                          of its context and its rows up to max_rows), whatever their order
  *   tree      [N, tree_words] int32   bit i % 32 of word i / 32 of a row: it sees row i of its
  *                          sequence.  All rows see the context besides; a row sees itself
  *                          if its own bit says so.  NULL: itself and the rows before it
@@ -463,7 +463,7 @@ size_t foe_cache_attention_ex_workspace_bytes(int H, int B, int N, int nq, int h
  *                          codes are rescaled to them.  Slots past the last kept token are left as
  *                          they were.  Nothing changes where no row is kept
  *   mass      [n_pages, H, 64] fp32   moves with its token, or NULL
- *   new_len   [B]   int32 out   ctx_len[b] and the length of the path (not ctx_len itself)
+ *   new_len   [B]   int32 out   ctx_len[b] and the length of the path (a buffer of its own)
  * A row whose page is absent is kept as a zero key and value without mass; rows that fall
  * into an absent page are lost.  1 <= max_path <= 2^22.  Needs no workspace.
  */

@@ -806,7 +806,8 @@ int foe_cache_accept(int H, int B, int hd, int n_pages, int max_blocks, int max_
     c.tensor(kv_scale, any, "kv_scale");
     c.tensor(mass, false, "mass");
     c.small(new_len, any, "new_len");
-    c.need(!any || new_len != ctx_len, "new_len must not be ctx_len");
+    c.need(!any || (new_len != ctx_len && new_len != path && new_len != row_start),
+           "new_len must not be ctx_len, path or row_start");
     if (!c.err.empty()) return fail(FOE_ERR_INVALID, "foe_cache_accept: " + c.err);
     if (!cache_hd(hd)) return fail(FOE_ERR_UNSUPPORTED, "foe_cache_accept: hd = 96 or 128 only");
     if (!any) return FOE_OK;

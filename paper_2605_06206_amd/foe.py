@@ -452,6 +452,8 @@ def cache_attention(q, k, v, kv_scale, block_table, ctx_len, row_start, max_rows
                                                     mass_out is not None, shaped), q.device, dev)
     name, scores = "foe_cache_attention", ()
     if shaped:
+        if cap != 0 and not abs(cap) >= 2.0 ** -64:  # (a float may round what is less to 0)
+            raise FoeError(FOE_ERR_INVALID, f"{name}: cap must be 0 or in [2^-64, 2^64]")
         name, words = "foe_cache_attention_ex", 0 if tree is None else tree.shape[-1]
         scores = (cap, None if slope is None else _arg(slope, "slope", f32, (H, nq), dev),
                   None if prefix is None else _arg(prefix, "prefix", i32, (B,), dev),

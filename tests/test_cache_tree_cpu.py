@@ -84,6 +84,7 @@ ACCEPT = [8, 4, 128, 100, 16, 6, P, P, P, P, P, P, P, P, P2, None]
     (8, None, INV, "path"), (8, P + 2, INV, "path"), (9, None, INV, "block_table"),
     (10, None, INV, "k_cache"), (11, P + 4, INV, "v_cache"), (12, None, INV, "kv_scale"),
     (13, P + 4, INV, "mass"), (14, None, INV, "new_len"), (14, P, INV, "new_len must not"),
+    (8, P2, INV, "path or row_start"), (6, P2, INV, "path or row_start"),
 ])
 def test_accept_rejects(L, at, value, rc, msg):
     assert L.foe_cache_accept(*changed(ACCEPT, at, value)) == rc

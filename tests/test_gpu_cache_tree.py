@@ -854,3 +854,13 @@ def test_binding_refuses():
     x = ints([3])
     with pytest.raises(foe.FoeError):
         foe.cache_accept(*kv, ints([[0, 1]]), x, ints([0, 40]), ints([[0]]), new_len=x)
+
+
+@pytest.mark.parametrize("cap", [1e-50, -1e-50, 1e-20])
+def test_binding_refuses_caps_below_range(cap):
+    """A cap that fp32 would round to 0, no cap, is refused like the others below 2^-64."""
+    dev = foe.cache_empty(1, 1, 96, DEV)
+    q = torch.zeros((1, 1, 1, 96), dtype=torch.bfloat16, device=DEV)
+    with pytest.raises(foe.FoeError):
+        foe.cache_attention(q, dev["k"], dev["v"], dev["kv_scale"], ints([[0]]), ints([0]),
+                            ints([0, 1]), 1, cap=cap)
