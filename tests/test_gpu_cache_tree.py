@@ -826,6 +826,42 @@ def test_empty_batches():
     assert int(n) == 3
 
 
+@pytest.mark.parametrize("nq,top", [(1, 2), (2, 12), (2, 40)])
+def test_batches_of_more_sequences_than_threads(nq, top):
+    """600 sequences, many without rows: more than any workgroup has threads to look them up."""
+    rng = np.random.default_rng([41, nq, top])
+    seqs = [(int(rng.integers(0, 70)), int(rng.integers(0, top + 1)) * int(rng.random() < 0.3))
+            for _ in range(600)]
+    seqs[577] = (65, top)
+    say("many sequences", nq, top)
+    ctx, rs, table, pages = batch(rng, seqs)
+    pool = random_pool(rng, pages, 1, 96)
+    depth, sees = trees(rng, seqs)
+    a = dict(cap=20.0, sees=sees, depth=depth)
+    q = bf16(rng.normal(size=(1, rs[-1], nq, 96)))
+    out, m = run_shaped(pool, table, ctx, rs, q, top, True, **a)
+    check_shaped(pool, table, ctx, rs, q, out, m, **a)
+
+
+@pytest.mark.parametrize("rows", [1, 9, 30, 120, 300])
+def test_mass_in_place(rows):
+    """A mass that is added to in place is the one that is written elsewhere."""
+    rng = np.random.default_rng([42, rows])
+    seqs = [(1900, rows), (333, max(rows // 2, 1)), (0, 0)]
+    say("mass in place", rows)
+    ctx, rs, table, pages = batch(rng, seqs)
+    pool = random_pool(rng, pages, 2, 128)
+    depth, sees = trees(rng, seqs)
+    q = bf16(rng.normal(size=(2, rs[-1], 2, 128)))
+    dev = to_dev(pool)
+    kw = dict(cap=15.0, tree=pack(sees, -(-rows // 32)), depth=ints(depth))
+    args = (q, dev["k"], dev["v"], dev["kv_scale"], ints(table), ints(ctx), ints(rs), rows)
+    apart, mine = dev["mass"].clone(), dev["mass"].clone()
+    want = foe.cache_attention(*args, mass_in=dev["mass"], mass_out=apart, **kw)
+    got = foe.cache_attention(*args, mass_in=mine, mass_out=mine, **kw)
+    assert torch.equal(want, got) and torch.equal(apart, mine)
+
+
 def test_binding_refuses():
     dev = foe.cache_empty(2, 1, 96, DEV)
     kv = (dev["k"], dev["v"], dev["kv_scale"])
