@@ -76,6 +76,7 @@ struct Shape {
   float scale;            // log2 e / sqrt(hd)
   float cap, x_of;        // cap * log2 e; 1 / (cap * sqrt(hd))
   float bound, poly[5];   // |s| <= bound: the capped score is s * (poly in s^2)
+  float near, low[3];     // and the same for |s| <= near
 };
 
 struct NoShape {  // causal, scores as they are
@@ -102,6 +103,9 @@ __device__ __forceinline__ int plain_tokens(const NoShape&, int ctx, int i) {
 // relative error, 7.3e-8.
 constexpr float kTanhBound = 0.6f;
 constexpr double kTanhPoly[5] = {0.99999993, -0.33332308, 0.13310172, -0.052101476, 0.015475425};
+// And for |x| <= kTanhNear, 7.4e-8.
+constexpr float kTanhNear = 0.1875f;
+constexpr double kTanhLow[3] = {0.99999993, -0.33329659, 0.13053289};
 
 // What a lane keeps of its column.
 struct Column {
@@ -181,7 +185,12 @@ __device__ __forceinline__ void shape_scores(const Shape<T>& sh, const CacheBatc
       // Scores are mostly well below the cap, where the polynomial is 6 operations; the
       // exponential, which loses the small ones' last digits besides, is taken where a lane
       // needs it.
-      if (__builtin_amdgcn_ballot_w64(big > sh.bound) == 0) {
+      if (__builtin_amdgcn_ballot_w64(big > sh.near) == 0) {
+        scaled([&](float s) {
+          const float u = s * s;
+          return fmaf(fmaf(sh.low[2], u, sh.low[1]), u, sh.low[0]);
+        });
+      } else if (__builtin_amdgcn_ballot_w64(big > sh.bound) == 0) {
         scaled([&](float s) {
           const float u = s * s;
           float y = fmaf(sh.poly[4], u, sh.poly[3]);
@@ -2207,10 +2216,14 @@ Shape<T> shape_of(const CacheScores& a, int hd) {
     sh.cap = (float)(a.cap * kLog2e);
     sh.x_of = (float)k;
     // (beyond, the squares and coefficients could leave fp32)
-    sh.bound = a.cap >= 0x1p-8f && a.cap <= 0x1p10f ? (float)(kTanhBound / k) : -1.f;
-    for (int i = 0; i < 5; ++i)
-      sh.poly[i] =
-          sh.bound > 0.f ? (float)(a.cap * kLog2e * kTanhPoly[i] * pow(k, 2 * i + 1)) : 0.f;
+    const bool fits = a.cap >= 0x1p-8f && a.cap <= 0x1p10f;
+    sh.bound = fits ? (float)(kTanhBound / k) : -1.f;
+    sh.near = fits ? (float)(kTanhNear / k) : -1.f;
+    auto factor = [&](double c, int i) {
+      return fits ? (float)(a.cap * kLog2e * c * pow(k, 2 * i + 1)) : 0.f;
+    };
+    for (int i = 0; i < 5; ++i) sh.poly[i] = factor(kTanhPoly[i], i);
+    for (int i = 0; i < 3; ++i) sh.low[i] = factor(kTanhLow[i], i);
   }
   return sh;
 }
