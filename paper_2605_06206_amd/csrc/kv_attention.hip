@@ -2138,6 +2138,9 @@ __global__ __launch_bounds__(kMassThr, S::kTransforms ? 3 : 4) void cache_mass_k
 
 // Host side of the two forms: ranges (workgroups) and scratch.
 constexpr int kFewLeast = 4;   // pages of a range at least: one for each wave
+// With 128 columns every wave takes every page.  us for 64 rows of two heads over 300, 1500 and
+// 5000 tokens, 8 groups: 22 22 26, with four 28 24 28.
+constexpr int kFullLeast = 2;
 constexpr int kManyLeast = 2;
 constexpr int kJoinParts = 24;  // parts up to which eight columns are joined by a workgroup
 // The scores of few columns are kept for the mass where the tables' room for them is up to
@@ -2150,7 +2153,7 @@ constexpr size_t kScoreBytes = (size_t)1 << 30;
 struct FormPlan {
   bool on;
   int lo, hi;                 // columns of its sequences
-  int ranges, cols, log2r, tiles;
+  int ranges, least, cols, log2r, tiles;
   size_t prefix, part;
 };
 struct AttnPlan {
@@ -2187,10 +2190,12 @@ AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_
   };
   const long long pages = (long long)B * H * max_blocks;
   p.few.cols = (int)std::min<long long>(p.few_cols, most);
+  p.few.least = p.few_cols == kShapedCols ? kFullLeast : kFewLeast;
   p.few.ranges = (int)std::min<long long>((p.few_cols <= 32 ? 4LL : 2LL) * kCus,
-                                          (pages + kFewLeast - 1) / kFewLeast);
+                                          (pages + p.few.least - 1) / p.few.least);
   p.many.cols = kTileCols;
   p.many.ranges = kCus;
+  p.many.least = kManyLeast;
   while ((2 << p.many.log2r) * nq <= kTileCols) ++p.many.log2r;
   // tiles of the batch: at most n / 2^log2r, rounded up, of each sequence
   p.many.tiles = (int)std::min<long long>(N, ((long long)N >> p.many.log2r) + B);
@@ -2247,19 +2252,18 @@ hipError_t launch_cache_attention(const CacheArgs& a, int nq, int N, int max_row
   float* score = p.scores ? reinterpret_cast<float*>(base + p.score) : nullptr;
   const Reach reach =
       scores != nullptr ? Reach{scores->prefix, scores->tree != nullptr} : Reach{nullptr, false};
-  auto form = [&](const FormPlan& f, int least, int round, auto few, auto wide) {
+  auto form = [&](const FormPlan& f, int round, auto few, auto wide) {
     return Form<decltype(few)::value, decltype(wide)::value>{
         {bt, max_rows, f.log2r, f.lo, f.hi, reach, reinterpret_cast<long long*>(base + f.prefix)},
-        {f.ranges, least, round},
+        {f.ranges, f.least, round},
         {static_cast<bf16*>(out), stat, reinterpret_cast<float*>(base + f.part), f.cols}};
   };
   auto go = [&](auto hdv, auto sh) {
     constexpr int HD = decltype(hdv)::value;
     using S = decltype(sh);
     constexpr std::integral_constant<bool, is_shaped<S>> wide;
-    const auto few =
-        form(p.few, kFewLeast, std::min(p.few.ranges, 2 * kCus), std::true_type{}, wide);
-    const auto many = form(p.many, kManyLeast, 0, std::false_type{}, wide);
+    const auto few = form(p.few, std::min(p.few.ranges, 2 * kCus), std::true_type{}, wide);
+    const auto many = form(p.many, 0, std::false_type{}, wide);
     float c_log2 = 1.4426950408889634f / sqrtf((float)a.hd);
     if constexpr (is_shaped<S>)
       if (S::kTransforms) c_log2 = 1.f;
