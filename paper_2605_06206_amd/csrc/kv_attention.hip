@@ -744,8 +744,8 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_few_kernel(
 // have room for 32 columns each.  (Pages through a ring of LDS-DMA stages, loaded once for the
 // four waves of 128 columns: 460 us for four sequences of 131072 tokens, 64 rows of two heads, 8
 // groups, and so 380: the waves wait for one another at each page.)  The next segment's page
-// numbers are loaded beside this one's pages, and its first page before this one's states are
-// merged.
+// numbers are loaded beside this one's pages, and its first page (of more than 16 columns the keys)
+// before this one's states are merged.
 // number of a page among the kept scores of shaped calls
 __device__ __forceinline__ size_t score_page(const CacheBatch& bt, int b, int h, int blk) {
   return ((size_t)b * bt.H + h) * bt.max_blocks + blk;
@@ -757,6 +757,17 @@ struct PageOf {
   int b, ctx, rows, ncol, len, blk;
   bool some;
 };
+
+// The maximum over a column's four lanes, by register swaps: through LDS, as a shuffle goes, its
+// latency stands between a page's scores and their exponentials.
+__device__ __forceinline__ float column_max(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
 
 // A wave's 16 NC columns: sums, running maxima and sums of probabilities.
 template <int NC, int NDT>
@@ -812,8 +823,7 @@ struct ShapedState {
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[j][t][e]);
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      mx = column_max(mx);
       // (the maximum moves only when a page exceeds it by 2^8, as with causal columns)
       const float mxs = mx * c_log2;
       const bool need = mxs > m_run[j] + 8.f;
@@ -937,7 +947,10 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
   Segment<true> a;
   if (!a.first(w, deal, blockIdx.x)) return;
   pid = pages64(a, 0);
-  if (count(a) > 0) load_k(a.h, 0), load_v(a.h, 0);
+  if (count(a) > 0) {
+    load_k(a.h, 0);
+    if (NC == 1) load_v(a.h, 0);
+  }
   while (true) {
     Segment<true> ahead = a;
     const bool another = ahead.next(w);
@@ -977,6 +990,13 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
           load_k(h, i + 1);
           load_v(h, i + 1);
         }
+      } else {
+        // (here and not behind the last page's product, the same moment, and the next page's keys
+        // below even if there is none: in one block and always as many, so that a wait for keys
+        // leaves the values on their way and the other way round.  48 trees of 25 rows, hd 96, 100
+        // to 4096 tokens: 44 us, and 46 with a wait for both)
+        load_v(h, i);
+        __builtin_amdgcn_sched_barrier(0);
       }
       f32x4 s[NC][4];
 #pragma unroll
@@ -996,8 +1016,8 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
             s[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[j], s[j][t], 0, 0, 0);
         }
       }
-      if (NC > 1 && more) {
-        if (((i + 1) & 63) == 0) pid = pages64(a, i + 1);
+      if constexpr (NC > 1) {
+        if (more && ((i + 1) & 63) == 0) pid = pages64(a, i + 1);
         load_k(h, i + 1);
       }
       if (page >= 0) {
@@ -1021,11 +1041,13 @@ __global__ __launch_bounds__(kAttThr, 2) void cache_attn_shaped_kernel(
                   __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[j][u], st.oacc[j][dt], 0, 0, 0);
           }
       }
-      if (NC > 1 && more) load_v(h, i + 1);
     }
     if (another) {
       pid = pid_ahead;
-      if (count(ahead) > 0) load_k(ahead.h, 0), load_v(ahead.h, 0);
+      if (count(ahead) > 0) {
+        load_k(ahead.h, 0);
+        if (NC == 1) load_v(ahead.h, 0);
+      }
     }
     const int me = opaque_int(lane), n1 = me & 15, g1 = me >> 4;  // (not held over the pages)
     const auto put = [&](int c, int d, const f32x4& x, float m, float l) {
