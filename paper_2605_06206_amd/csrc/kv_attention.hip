@@ -136,17 +136,18 @@ __device__ __forceinline__ uint64_t keys_seen(const Shape<T>& sh, const CacheBat
   if (sh.a.prefix != nullptr) seen = max(seen, min(sh.a.prefix[b], len));
   uint64_t m = first(seen - key0);
   if (sh.a.tree != nullptr && key0 + kPage > ctx && key0 < len) {
-    const int i0 = key0 - ctx;  // the new row at the page's first key
+    // the new row at the page's first key, in bit k of word w, or the first row in bit `up`
+    const int i0 = max(key0 - ctx, 0), up = max(ctx - key0, 0), w = i0 >> 5, k = i0 & 31;
     const uint32_t* bits = sh.a.tree + (size_t)(bt.first_row(b) + row) * sh.a.words;
-    auto word = [&](int w) -> uint64_t { return w < sh.a.words ? bits[w] : 0u; };
-    uint64_t x;
-    if (i0 < 0) {
-      x = (word(0) | word(1) << 32) << -i0;
-    } else {
-      const int w = i0 >> 5, k = i0 & 31;
-      x = (word(w) | word(w + 1) << 32) >> k;
-      if (k != 0) x |= word(w + 2) << (64 - k);
-    }
+    const int last = sh.a.words - 1;
+    uint32_t lo = bits[min(w, last)], mid = bits[min(w + 1, last)], hi = bits[min(w + 2, last)];
+    asm volatile("" : "+v"(lo), "+v"(mid), "+v"(hi));  // (on their way together)
+    if (w > last) lo = 0;
+    if (w + 1 > last) mid = 0;
+    if (w + 2 > last) hi = 0;
+    lo = __builtin_amdgcn_alignbit(mid, lo, k);
+    mid = __builtin_amdgcn_alignbit(hi, mid, k);
+    const uint64_t x = (lo | (uint64_t)mid << 32) << up;
     m |= x & first(len - key0);
   }
   return m;
