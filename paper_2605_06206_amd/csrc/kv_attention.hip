@@ -261,8 +261,10 @@ struct Reach {
 // many columns has 2^log2r rows, tile t reaches page ceil((ctx + last row + 1) / 64), and
 // the sums over tiles are closed forms (which count pages past the table's end too).
 // (WIDE: shaped calls.  Rows may see past themselves, see Reach; and with few columns each
-// (sequence, group) has kStartPages units before its pages', for what starting on it costs.)
-constexpr int kStartPages = 5;
+// (sequence, group) has kStartPages units before its pages', for what starting on it costs.  us
+// with 2, 5, 7 and 12, calls of 48 trees of 25 rows (hd 96, 100 to 4096 tokens, mass) 87 84 82 85,
+// of 64 trees of 16 (256 to 8192) 142 135 134 133, of 64 capped and biased rows 121 122 124 128.)
+constexpr int kStartPages = 7;
 
 template <bool FEW, bool WIDE = false>
 struct Units {
