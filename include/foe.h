@@ -390,10 +390,13 @@ int foe_cache_append_tree(foe_dtype dt, int H, int B, int N, int nq, int hd, int
  *                          sequences that have rows (0 <= t < ctx_len[b] + rows); other
  *                          entries are not written.  mass_out may be mass_in itself
  *   out       [N, H, nq, hd] dt out   the layout of w_o's columns in foe_group_attention
- *   ws, ws_bytes           workspace of foe_cache_attention_workspace_bytes().  With mass it grows
- *                          with the table's width (scores of sequences of few columns are
- *                          kept where all entries' take at most 1 GiB, else formed again):
- *                          tables need be no wider than the longest sequence
+ *   ws, ws_bytes           workspace of foe_cache_attention_workspace_bytes(), which no smaller
+ *                          size takes more of: one for the largest H, B, N, nq, max_blocks and
+ *                          max_rows of a caller's calls, with mass if any has it, serves them
+ *                          all, one after another.  With mass it grows with the table's width
+ *                          (scores of sequences of few columns are kept where all entries'
+ *                          take at most 1 GiB, else formed again): tables need be no wider
+ *                          than the longest sequence
  * bf16: products in bf16 MFMA with fp32 accumulation; softmax statistics, mass and
  * sums in fp32, the probabilities are rounded to bf16 for the product with v.
  * Scores may lie anywhere in fp32's range.  A row with a score of NaN or +inf, or
@@ -444,7 +447,7 @@ int foe_cache_attention_ex(foe_dtype dt, int H, int B, int N, int nq, int hd, in
                            float* mass_out, void* out, void* ws, size_t ws_bytes, void* stream);
 
 /* Workspace bytes of foe_cache_attention_ex, whatever its scores and masks (SIZE_MAX
- * for invalid sizes). */
+ * for invalid sizes); as with foe_cache_attention_workspace_bytes, smaller sizes take no more. */
 size_t foe_cache_attention_ex_workspace_bytes(int H, int B, int N, int nq, int hd, int max_blocks,
                                               int max_rows, int with_mass);
 

@@ -2208,29 +2208,41 @@ AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_
     field = p.total;
     p.total = align_up(p.total + bytes, 256);
   };
-  auto scratch = [&](FormPlan& f) {
-    if (!f.on) return;
+  auto scratch = [&](FormPlan& f, size_t part_bytes) {
     take(f.prefix, (size_t)(B + 1) * 8);
-    take(f.part, 2 * (size_t)f.ranges * part_floats(f.cols, hd) * 4);
+    take(f.part, part_bytes);
   };
   const long long pages = (long long)B * H * max_blocks;
+  auto least_of = [](int few_cols) { return few_cols == kShapedCols ? kFullLeast : kFewLeast; };
+  auto ranges_of = [&](int few_cols) {
+    return (int)std::min<long long>((few_cols <= 32 ? 4LL : 2LL) * kCus,
+                                    (pages + least_of(few_cols) - 1) / least_of(few_cols));
+  };
+  auto parts_of = [&](int ranges, int cols) { return 2 * (size_t)ranges * part_floats(cols, hd) * 4; };
   p.few.cols = (int)std::min<long long>(p.few_cols, most);
-  p.few.least = p.few_cols == kShapedCols ? kFullLeast : kFewLeast;
-  p.few.ranges = (int)std::min<long long>((p.few_cols <= 32 ? 4LL : 2LL) * kCus,
-                                          (pages + p.few.least - 1) / p.few.least);
+  p.few.least = least_of(p.few_cols);
+  p.few.ranges = ranges_of(p.few_cols);
   p.many.cols = kTileCols;
   p.many.ranges = kCus;
   p.many.least = kManyLeast;
   while ((2 << p.many.log2r) * nq <= kTileCols) ++p.many.log2r;
   // tiles of the batch: at most n / 2^log2r, rounded up, of each sequence
   p.many.tiles = (int)std::min<long long>(N, ((long long)N >> p.many.log2r) + B);
-  scratch(p.few);
-  scratch(p.many);
+  // Every region has room for any call of no larger sizes, whichever forms and widths that takes,
+  // so that a caller's one workspace for its largest batch serves the smaller ones: the parts of
+  // each width that so many columns or fewer take, the scores of the first 16 columns.
+  size_t few_parts = 0;
+  for (int w = kFewCols; w <= (shaped ? kShapedCols : kFewCols); w *= 2)
+    if (w == kFewCols || most > w / 2)
+      few_parts = std::max(few_parts,
+                           parts_of(ranges_of(w), (int)std::min<long long>(w, most)));
+  scratch(p.few, few_parts);
+  if (p.many.on) scratch(p.many, parts_of(p.many.ranges, p.many.cols));
   if (mass) {
     take(p.stat, (size_t)H * N * nq * (shaped ? sizeof(Stat<Shape<true>>) : sizeof(Stat<NoShape>)));
-    const size_t bytes = (size_t)pages * p.few.cols * kPage * 4;
+    const size_t bytes = (size_t)pages * std::min<long long>(kFewCols, most) * kPage * 4;
     p.scores = p.few.on && p.few_cols == kFewCols && bytes <= kScoreBytes;
-    if (p.scores) take(p.score, bytes);
+    take(p.score, std::min(bytes, kScoreBytes));
   }
   return p;
 }

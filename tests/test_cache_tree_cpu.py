@@ -74,6 +74,34 @@ def test_attention_ex_workspace(L):
         assert L.foe_cache_attention_ex(*call) == WS
 
 
+@pytest.mark.parametrize("name", ["", "_ex"])
+@pytest.mark.parametrize("hd", [96, 128])
+def test_workspace_of_the_largest_call_serves_smaller_ones(L, name, hd):
+    """A server's one workspace, sized for its largest batch: no smaller number of rows, of
+    sequences, of pages, of heads or of groups takes more, with and without the mass, whatever
+    form and width it takes."""
+    f = getattr(L, f"foe_cache_attention{name}_workspace_bytes")
+    rng = np.random.default_rng([11, hd])
+    assert f(8, 64, 64 * 64, 2, hd, 128, 8, 1) <= f(8, 64, 64 * 64, 2, hd, 128, 64, 1)
+    assert f(8, 64, 64 * 64, 1, hd, 128, 32, 0) <= f(8, 64, 64 * 64, 1, hd, 128, 33, 0)
+    assert f(1, 1, 2, 2, hd, 1 << 17, 1, 1) <= f(1, 1, 2, 2, hd, 1 << 18, 1, 1)
+    for _ in range(300):
+        H, nq, B = int(rng.integers(1, 9)), int(rng.integers(1, 9)), int(rng.integers(1, 100))
+        blocks = int(2 ** rng.uniform(0, 12))
+        N = B * int(2 ** rng.uniform(0, 8))
+        top = int(2 ** rng.uniform(0, 8))
+        mass = int(rng.integers(2))
+        most = f(H, B, N, nq, hd, blocks, top, mass)
+        assert 0 < most < SIZE_MAX
+        for rows in {1, 2, 3, 16 // nq, 17 // nq, 32 // nq, 64 // nq, 128 // nq, top - 1}:
+            if 0 < rows <= top:
+                less = [H, B, N, nq, hd, blocks, rows, mass]
+                assert f(*less) <= most, (less, top)
+                for at, value in ((0, 1), (1, max(1, B // 2)), (2, max(1, N // 3)), (3, 1),
+                                  (5, max(1, blocks // 2)), (7, 0)):
+                    assert f(*changed(less, at, value)) <= most, (less, at, top)
+
+
 ACCEPT = [8, 4, 128, 100, 16, 6, P, P, P, P, P, P, P, P, P2, None]
 
 
