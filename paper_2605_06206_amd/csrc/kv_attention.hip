@@ -99,11 +99,11 @@ __device__ __forceinline__ int plain_tokens(const NoShape&, int ctx, int i) {
   return ctx + i + 1;
 }
 
-// tanh(x) / x for |x| <= kTanhBound as a polynomial in x^2: fitted here to the smallest largest
-// relative error, 7.3e-8.
+// tanh(x) / x for |x| <= kTanhBound as a polynomial in x^2, fitted here for a small largest relative
+// error: 8.2e-8 (at 0.6), and 8.9e-8 with the coefficients in fp32.
 constexpr float kTanhBound = 0.6f;
 constexpr double kTanhPoly[5] = {0.99999993, -0.33332308, 0.13310172, -0.052101476, 0.015475425};
-// And for |x| <= kTanhNear, 7.4e-8.
+// And for |x| <= kTanhNear, 7.4e-8, in fp32 8.4e-8.
 constexpr float kTanhNear = 0.1875f;
 constexpr double kTanhLow[3] = {0.99999993, -0.33329659, 0.13053289};
 

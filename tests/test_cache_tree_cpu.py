@@ -2,11 +2,14 @@
 reaches a launch, the addresses are never dereferenced) and pins of the oracle."""
 
 import ctypes
+import os
+import re
 
 import numpy as np
 import pytest
 
 from oracle import cache_oracle as co
+from paper_2605_06206_amd import build as build_mod
 from paper_2605_06206_amd import foe
 
 P, P2 = 0x10000, 0x20000
@@ -214,3 +217,22 @@ def test_oracle_accept_by_hand():
     np.testing.assert_array_equal(co.decode(pool["v"][0, 0, 0, 0, :4]) * -0.5, want)
     np.testing.assert_array_equal(pool["mass"][0, 0, :4], mass[0, 0, [0, 1, 3, 5]])
     np.testing.assert_array_equal(pool["k"][0, 0, 4:6], co.encode(x[4:, None] * np.ones(16)))
+
+
+def test_tanh_polynomials_are_as_exact_as_they_say():
+    """The cap's polynomials (csrc/kv_attention.hip): the relative errors that stand at their
+    coefficients, as written and in fp32, up to the last digit that is given."""
+    with open(os.path.join(build_mod.CSRC, "kv_attention.hip")) as f:
+        src = f.read()
+    for poly, bound, exact, single in (("kTanhPoly", "kTanhBound", 8.2e-8, 8.9e-8),
+                                       ("kTanhLow", "kTanhNear", 7.4e-8, 8.4e-8)):
+        end = float(re.search(rf"float {bound} = ([0-9.]+)f;", src)[1])
+        said = src[:src.index(f"double {poly}[")].rsplit(f"|x| <= {bound}", 1)[1]
+        assert all(f"{e:.1e}".replace("e-0", "e-") in said for e in (exact, single))
+        c = np.array([float(x) for x in
+                      re.search(rf"double {poly}\[\d\] = {{([^}}]+)}}", src)[1].split(",")])
+        x = np.linspace(1e-4, end, 400001)
+        for k, want in ((c, exact), (c.astype(np.float32).astype(float), single)):
+            y = np.polynomial.polynomial.polyval(x * x, k)
+            worst = np.abs(y * x / np.tanh(x) - 1).max()
+            assert want - 1e-9 < worst < want + 1e-9, (poly, worst)
