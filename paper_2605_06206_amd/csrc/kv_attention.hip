@@ -683,8 +683,9 @@ struct Segment {
       total = uniform64(total);
       off = uniform64(off);
     }
-    // (at most 2^37 units, of tables of 2^31 entries and 64 groups, in a quarter of them or 1024
-    // ranges)
+    // (fits: at most 2^37 pages, of tables of 2^31 entries and 64 groups, and kStartPages for each of
+    // 65535 sequences' groups, in 512 ranges or more; fewer ranges have at most kFewLeast pages
+    // of the tables each, whose groups are no more than the pages)
     const int per = (int)deal.per(total);
     unit = (long long)r * per;
     left = (int)min((long long)per, total - unit);

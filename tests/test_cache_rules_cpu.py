@@ -1,6 +1,8 @@
 """How the cache's attention deals out its work (csrc/rules.hpp), compiled for the host."""
 
 import ctypes
+import os
+import re
 import shutil
 import subprocess
 
@@ -73,3 +75,19 @@ def test_ranges_of_the_largest_batch(rules):
 @pytest.mark.parametrize("np_,blk0,left", [(1, 0, 1), (7, 3, 2), (7, 3, 4), (7, 3, 5), (7, 6, 100)])
 def test_a_range_ends_inside_a_tile(rules, np_, blk0, left):
     assert rules.walk(np_, blk0, left) == left
+
+
+def test_ranges_of_few_columns_fit_an_int(rules):
+    """The few-column form counts the units of a range in 32 bits: the largest tables and batch, in
+    the fewest ranges of a full grid, and grids that small tables cut (a range has at least 2 or 4
+    pages), where every (sequence, group) adds its start units to a page."""
+    src = open(os.path.join(build_mod.CSRC, "kv_attention.hip")).read()
+    start = int(re.search(r"constexpr int kStartPages = (\d+);", src)[1])
+    pages, groups = (1 << 31) * 64, 65535 * 64
+    for ranges, least in ((512, 2), (512, 4), (1024, 4)):
+        for total in (pages, pages + start * groups):
+            per = rules.per(total, ranges, least, 512)
+            assert per * ranges >= total and per < 1 << 29
+        for n in (1, least, ranges // 2 * least, (ranges - 1) * least):
+            cut = min(ranges, -(-n // least))
+            assert rules.per(n + start * n, cut, least, min(cut, 512)) <= least * (start + 2)
