@@ -1,13 +1,13 @@
 """Trees and other scores over the 8-bit cache at the borders of their forms: one workspace for
-batches of all widths."""
+batches of all widths, and tables too wide for the scores to be kept for the mass."""
 
 import numpy as np
 import pytest
 import torch
 
 from paper_2605_06206_amd import foe
-from test_gpu_cache import DEV, batch, bf16, ints, random_pool, say, to_dev
-from test_gpu_cache_tree import check_shaped, pack, trees
+from test_gpu_cache import DEV, batch, bf16, host, ints, random_pool, say, to_dev
+from test_gpu_cache_tree import check_shaped, pack, run_shaped, slopes, trees
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +53,81 @@ def test_one_workspace_serves_batches_of_all_widths(nq, hd, shaped):
             torch.cuda.synchronize()
             assert (ws[size(b, int(rs[-1]), rows, mass):] == 0xA5).all()
             check_shaped(pool, table[:b], ctx, rs, q, out, m, **a)
+
+
+def wide(table):
+    """The same pages in a table of the most entries: the scores of 16 columns of two groups, or of
+    one of 64 sequences' groups, pass 1 GiB."""
+    out = np.full((len(table), 1 << 18), -1, dtype=np.int32)
+    out[:, :table.shape[1]] = table
+    return out
+
+
+@pytest.mark.parametrize("H,nq,hd,seqs,what", [
+    (2, 2, 128, [(700, 8), (64, 5), (0, 8), (63, 1)], "tree"),
+    (2, 1, 96, [(300, 16)], "tree"),
+    (3, 4, 96, [(1000, 4), (127, 3), (0, 0), (5, 1)], "tree cap bias"),
+    (2, 2, 128, [(90, 8), (1500, 3)], "cap"),
+    (2, 16, 96, [(130, 1), (64, 1), (0, 1)], "cap bias"),
+    (2, 1, 128, [(200, 16), (10, 9)], "bias prefix"),
+    (8, 1, 128, [(40 * b, 1) for b in range(16)], "cap"),
+    (4, 1, 96, [(50 * b, 1 + b % 2) for b in range(16)], "tree"),
+    # sequences of few columns beside those of more than any few-column form holds
+    (2, 2, 128, [(100, 150), (300, 2), (64, 8), (0, 1), (500, 1)], "tree"),
+    (2, 1, 96, [(0, 200), (700, 16), (63, 3), (1, 1), (90, 2), (400, 1)], "tree cap bias"),
+    (2, 2, 96, [(65, 140), (128, 1), (30, 2), (250, 5)], "cap prefix"),
+])
+def test_mass_where_scores_are_formed_again(H, nq, hd, seqs, what):
+    say("formed again", H, nq, hd, seqs, what)
+    rng = np.random.default_rng([52, H, nq, hd, len(seqs), len(what)])
+    ctx, rs, table, pages = batch(rng, seqs)
+    pool = random_pool(rng, pages, H, hd)
+    depth, sees = trees(rng, seqs)
+    a = {}
+    if "cap" in what:
+        a["cap"] = 8.0
+    if "bias" in what:
+        a["slope"] = slopes(rng, H, nq)
+    if "prefix" in what:
+        a["prefix"] = [int(rng.integers(0, c + n + 30)) for c, n in seqs]
+    if "tree" in what:
+        a.update(sees=sees, depth=depth)
+    q = bf16(2.0 * rng.normal(size=(H, rs[-1], nq, hd)))
+    top = max(n for _, n in seqs)
+    # (what the call takes without the mass, the statistics, and all that scores may take: they
+    # are past it, and not kept)
+    assert len(seqs) * H * (1 << 18) * min(16, top * nq) * 64 * 4 > 1 << 30
+    out, m = run_shaped(pool, wide(table), ctx, rs, q, top, True, **a)
+    check_shaped(pool, table, ctx, rs, q, out, m, **a)
+
+
+@pytest.mark.parametrize("rows,more", [(16, 0), (10, 0), (3, 150)])
+def test_nan_rows_where_scores_are_formed_again(rows, more):
+    """A row of a NaN key counts, as NaN, for the tokens that it sees alone."""
+    rng = np.random.default_rng([53, rows, more])
+    H, nq, hd, seqs = 2, 1, 128, [(100, rows), (130, 2)] + ([(20, more)] if more else [])
+    ctx, rs, table, pages = batch(rng, seqs)
+    pool = random_pool(rng, pages, H, hd)
+    _, sees = trees(rng, seqs)
+    bad = rows // 2  # a row that no other sees
+    for r in range(rows):
+        if r != bad:
+            sees[r][bad] = False
+    t = 100 + bad
+    p = table[0, t // 64]
+    pool["k"][p, :, t % 64] = 0x7F
+    pool["v"][p, :, (t % 64) // 16, :, t % 16] = 0
+    q = bf16(rng.normal(size=(H, rs[-1], nq, hd)))
+    say("NaN rows, formed again", rows, more)
+    out, m = run_shaped(pool, wide(table), ctx, rs, q, max(rows, more), True, sees=sees, cap=9.0)
+    g, m = host(out), host(m)
+    good = [r for r in range(rs[-1]) if r != bad]
+    assert np.isfinite(g[good]).all() and np.isnan(g[bad]).all()
+    for t in range(100 + rows):
+        seen = t < 100 or sees[bad][t - 100]
+        assert np.isnan(m[table[0, t // 64], :, t % 64]).all() == seen, t
+    for t in range(132):
+        assert np.isfinite(m[table[1, t // 64], :, t % 64]).all(), t
+    sees[bad][:] = False
+    pool["k"][p, :, (100 + bad) % 64] = 0
+    check_shaped(pool, table, ctx, rs, q, out, None, rows=good, sees=sees, cap=9.0)
