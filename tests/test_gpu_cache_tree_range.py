@@ -1,10 +1,12 @@
 """Trees and other scores over the 8-bit cache at the borders of their forms: one workspace for
-batches of all widths, and tables too wide for the scores to be kept for the mass."""
+batches of all widths, tables too wide for the scores to be kept for the mass, and biases over long
+contexts by bounds that weigh each token."""
 
 import numpy as np
 import pytest
 import torch
 
+from oracle import cache_oracle as co
 from paper_2605_06206_amd import foe
 from test_gpu_cache import DEV, batch, bf16, host, ints, random_pool, say, to_dev
 from test_gpu_cache_tree import check_shaped, pack, run_shaped, slopes, trees
@@ -131,3 +133,85 @@ def test_nan_rows_where_scores_are_formed_again(rows, more):
     sees[bad][:] = False
     pool["k"][p, :, (100 + bad) % 64] = 0
     check_shaped(pool, table, ctx, rs, q, out, None, rows=good, sees=sees, cap=9.0)
+
+
+def weighed(pool, table, ctx, q, slope, cap=0.0, depth=None, sees=None):
+    """One sequence's outputs and masses in fp64, and bounds of their errors that weigh each token
+    by its probability.  A score may be off by e_t: its sum of hd products of magnitude a_t in all,
+    scaling and cap (hd + 24 roundings of a_t), and the bias: the slope in units of log2 e (two),
+    its product with the distance from the page's first token, up to 63 more than the token's own,
+    that with the rest, the sum with the score and what is left of the maximum (6 roundings).  A
+    probability is then off by e_t and, through the sum, by the mean of all e_t, relatively; by
+    2^-16 for the exponential and the sum's additions (a lane's chain has at most 16 for each of
+    15 pages).  One below 2^-126 may be lost."""
+    H, n, nq, hd = q.shape
+    L = ctx + n
+    q = host(q)
+    slope = np.asarray(slope, dtype=np.float32).astype(np.float64)
+    step = np.arange(n) if depth is None else np.clip(depth, 0, co.MAX_DEPTH)
+    place, spot = ctx + step, np.concatenate([np.arange(ctx), ctx + step])
+    seen = np.arange(L) <= ctx + np.arange(n)[:, None]
+    if sees is not None:
+        seen = np.ones((n, L), dtype=bool)
+        seen[:, ctx:] = np.array([r[:n] for r in sees])
+    o, o_lim = np.zeros((n, H, nq, hd)), np.zeros((n, H, nq, hd))
+    mass, m_lim = np.zeros((H, L)), np.zeros((H, L))
+    far = np.abs(place[:, None] - spot).astype(np.float64)
+    for h in range(H):
+        k, v, _ = co.tokens(pool, table, 0, h, L)
+        for j in range(nq):
+            s = q[h, :, j] @ k.T / np.sqrt(hd)
+            if cap:
+                s = cap * np.tanh(s / cap)
+            s = np.where(seen, s - slope[h, j] * far, -np.inf)
+            p = np.exp(s - s.max(1, keepdims=True))
+            p /= p.sum(1, keepdims=True)
+            e = np.abs(q[h, :, j]) @ np.abs(k).T / np.sqrt(hd) * (hd + 24)
+            e = 1.45 * 2.0 ** -24 * (e + 6 * abs(slope[h, j]) * (far + 63))
+            pe = p * (e + (p * e).sum(1, keepdims=True) + 2.0 ** -16)
+            o[:, h, j] = p @ v
+            # (bf16 for the product with the values and for the output, 2^-12 for its fp32 sums)
+            o_lim[:, h, j] = (pe + (2.0 ** -8 + 2.0 ** -12) * p) @ np.abs(v) + \
+                2.0 ** -8 * np.abs(o[:, h, j]) + 2.0 ** -124 * L
+            mass[h] += p.sum(0)
+            m_lim[h] += (pe + n * nq * 2.0 ** -24 * p + 2.0 ** -126).sum(0)
+    return o, o_lim, mass, m_lim
+
+
+@pytest.mark.parametrize("H,nq,hd,ctx,rows,what", [
+    (1, 2, 128, 131071, 1, "cap"),
+    (1, 4, 96, 130990, 1, ""),
+    (1, 2, 128, 131071, 16, "tree"),
+    (1, 1, 96, 65000, 64, "tree cap"),
+    (2, 2, 128, 20000, 30, "tree"),
+    (1, 3, 128, 9001, 90, "cap"),
+    (1, 2, 128, 3000, 40, "tree far"),
+    (2, 1, 96, 777, 12, "far"),
+    (1, 2, 96, 500, 200, "tree far"),
+])
+def test_bias_by_the_weight_of_each_token(H, nq, hd, ctx, rows, what):
+    """Biases over contexts up to the longest, from those that reach a few tokens to those that
+    reach all of them, outputs and masses (`far`: some rows stand 2^18 to 2^20 places behind)."""
+    rng = np.random.default_rng([54, H, nq, hd, ctx, rows])
+    _, rs, table, pages = batch(rng, [(ctx, rows)])
+    pool = random_pool(rng, pages, H, hd)
+    pool["mass"][:] = 0.0  # (the sum with what was there would hide more)
+    depth, sees = trees(rng, [(ctx, rows)])
+    q = bf16(1.5 * rng.normal(size=(H, rows, nq, hd)))
+    a = {"cap": 20.0 if "cap" in what else 0.0}
+    if "tree" in what:
+        a.update(sees=sees, depth=depth)
+    if "far" in what:
+        depth[rows // 2:] += rng.integers(1 << 18, 1 << 20, rows - rows // 2)
+        a["depth"] = depth
+    for near, end in ((0.9, 0.1), (2.0 ** -5, 2.0 ** -9), (2.0 ** -14, 2.0 ** -18)):
+        slope = np.exp(rng.uniform(np.log(end), np.log(near), (H, nq)))
+        say("weighed bias", H, nq, hd, ctx, rows, what, near)
+        out, m = run_shaped(pool, table, [ctx], rs, q, rows, True, slope=slope, **a)
+        o, o_lim, mass, m_lim = weighed(pool, table, ctx, q, slope, **a)
+        err = np.abs(host(out) - o)
+        say(f"outputs {float((err / o_lim).max()):.3f} of the bound")
+        got = host(m).transpose(1, 0, 2)[:, table[0]].reshape(H, -1)[:, :ctx + rows]
+        off = np.abs(got - mass)
+        say(f"masses {float((off / m_lim).max()):.3f} of the bound")
+        assert (err <= o_lim).all() and (off <= m_lim).all()
