@@ -431,12 +431,15 @@ size_t foe_cache_attention_workspace_bytes(int H, int B, int N, int nq, int hd, 
  *   tree_words             at least max_rows / 32, rounded up
  *   depth     [N]  int32   row r stands at place ctx_len[b] + depth[r], cut as in
  *                          foe_cache_append_tree.  NULL: row i of its sequence at ctx_len[b] + i.
- *                          Tokens of the context stand where they are in the cache (also
- *                          after an eviction).  Only the bias asks for places
+ *                          Tokens of the context stand where they are in the cache: after
+ *                          an eviction distances count the tokens that were kept, not those
+ *                          of the text (each group keeps others).  Only the bias asks for
+ *                          places
  *   ws, ws_bytes           workspace of foe_cache_attention_ex_workspace_bytes()
- * A row that sees no token gives zeros.  A mass counts the tokens that the rows see.  Scores
- * that pass fp32 are capped like any other; a NaN score gives a NaN row.  Capped and biased
- * scores have to stay within 2^100.
+ * A row that sees no token gives zeros.  A mass counts the tokens that the rows see, and every
+ * row, also those that foe_cache_accept then drops (see there for masses of the text alone).
+ * Scores that pass fp32 are capped like any other; a NaN score gives a NaN row.  Capped and
+ * biased scores have to stay within 2^100.
  */
 int foe_cache_attention_ex(foe_dtype dt, int H, int B, int N, int nq, int hd, int n_pages,
                            int max_blocks, int max_rows, float cap, const float* slope,
@@ -469,6 +472,11 @@ size_t foe_cache_attention_ex_workspace_bytes(int H, int B, int N, int nq, int h
  *   new_len   [B]   int32 out   ctx_len[b] and the length of the path (a buffer of its own)
  * A row whose page is absent is kept as a zero key and value without mass; rows that fall
  * into an absent page are lost.  1 <= max_path <= 2^22.  Needs no workspace.
+ * A mass that was written with the whole tree holds the dropped rows' weights too, and
+ * foe_cache_evict would rank the context by drafts that are no part of the text.  Where that
+ * counts, verify the tree without a mass, accept the path, and add the kept rows' weights by
+ * a causal call with the mass: foe_cache_attention (or _ex with the same cap and slope) of
+ * their queries alone, with this call's ctx_len and the row_start of the paths.
  */
 int foe_cache_accept(int H, int B, int hd, int n_pages, int max_blocks, int max_path,
                      const int32_t* row_start, const int32_t* ctx_len, const int32_t* path,

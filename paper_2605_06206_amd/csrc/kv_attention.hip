@@ -99,8 +99,8 @@ __device__ __forceinline__ int plain_tokens(const NoShape&, int ctx, int i) {
   return ctx + i + 1;
 }
 
-// tanh(x) / x for |x| <= kTanhBound as a polynomial in x^2, fitted here for a small largest relative
-// error: 8.2e-8 (at 0.6), and 8.9e-8 with the coefficients in fp32.
+// tanh(x) / x for |x| <= kTanhBound as a polynomial in x^2, fitted here for a small largest
+// relative error: 8.2e-8 (at 0.6), and 8.9e-8 with the coefficients in fp32.
 constexpr float kTanhBound = 0.6f;
 constexpr double kTanhPoly[5] = {0.99999993, -0.33332308, 0.13310172, -0.052101476, 0.015475425};
 // And for |x| <= kTanhNear, 7.4e-8, in fp32 8.4e-8.
@@ -683,8 +683,8 @@ struct Segment {
       total = uniform64(total);
       off = uniform64(off);
     }
-    // (fits: at most 2^37 pages, of tables of 2^31 entries and 64 groups, and kStartPages for each of
-    // 65535 sequences' groups, in 512 ranges or more; fewer ranges have at most kFewLeast pages
+    // (fits: at most 2^37 pages, of tables of 2^31 entries and 64 groups, and kStartPages for each
+    // of 65535 sequences' groups, in 512 ranges or more; fewer ranges have at most kFewLeast pages
     // of the tables each, whose groups are no more than the pages)
     const int per = (int)deal.per(total);
     unit = (long long)r * per;
@@ -2219,7 +2219,9 @@ AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_
     return (int)std::min<long long>((few_cols <= 32 ? 4LL : 2LL) * kCus,
                                     (pages + least_of(few_cols) - 1) / least_of(few_cols));
   };
-  auto parts_of = [&](int ranges, int cols) { return 2 * (size_t)ranges * part_floats(cols, hd) * 4; };
+  auto parts_of = [&](int ranges, int cols) {
+    return 2 * (size_t)ranges * part_floats(cols, hd) * 4;
+  };
   p.few.cols = (int)std::min<long long>(p.few_cols, most);
   p.few.least = least_of(p.few_cols);
   p.few.ranges = ranges_of(p.few_cols);

@@ -1,6 +1,6 @@
 """Trees and other scores over the 8-bit cache at the borders of their forms: one workspace for
-batches of all widths, tables too wide for the scores to be kept for the mass, and biases over long
-contexts by bounds that weigh each token."""
+batches of all widths, tables too wide for the scores to be kept for the mass, biases over long
+contexts by bounds that weigh each token, and the masses of accepted paths alone."""
 
 import numpy as np
 import pytest
@@ -8,7 +8,7 @@ import torch
 
 from oracle import cache_oracle as co
 from paper_2605_06206_amd import foe
-from test_gpu_cache import DEV, batch, bf16, host, ints, random_pool, say, to_dev
+from test_gpu_cache import DEV, SCALE, THETA, batch, bf16, host, ints, random_pool, say, to_dev
 from test_gpu_cache_tree import check_shaped, pack, run_shaped, slopes, trees
 
 pytestmark = pytest.mark.gpu
@@ -215,3 +215,69 @@ def test_bias_by_the_weight_of_each_token(H, nq, hd, ctx, rows, what):
         off = np.abs(got - mass)
         say(f"masses {float((off / m_lim).max()):.3f} of the bound")
         assert (err <= o_lim).all() and (off <= m_lim).all()
+
+
+@pytest.mark.parametrize("nq,hd,back", [(2, 128, 4), (1, 96, 2)])
+def test_masses_of_accepted_paths_alone(nq, hd, back):
+    """Trees verified without the mass, and the weights of the kept rows added once a path is
+    accepted, by a causal call of those rows: bit for bit the masses, and what is then evicted, of a
+    cache that never held a rejected draft.  (Every token's largest key and value are the same, so
+    that neither cache's pages ever have another scale, and no tree crosses a page, so that both
+    form the same sines.)"""
+    rng = np.random.default_rng([55, nq, hd])
+    H, B, blocks = 2, 3, 6
+    perm = rng.permutation(3 * B * blocks).astype(np.int32)
+    t1, t2, fresh = (perm[i * B * blocks:(i + 1) * B * blocks].reshape(B, blocks) for i in range(3))
+    dev = foe.cache_empty(3 * B * blocks, H, hd, DEV)
+    kv, mass = (dev["k"], dev["v"], dev["kv_scale"]), dev["mass"]
+
+    def rows_of(n):
+        x = np.clip(rng.normal(size=(H, n, nq + 2, hd)), -4, 4)
+        x[..., hd // 2 - 1] = 6.0   # (of the pair that hardly turns)
+        return bf16(x)
+
+    ln = np.array([3, 65, 130])
+    rs = np.concatenate([[0], np.cumsum(ln)])
+    qkv = rows_of(rs[-1])
+    for t in (t1, t2):
+        q = foe.cache_append(qkv, *kv, ints(t), ints(np.zeros(B)), ints(rs), THETA, SCALE)
+        foe.cache_attention(q, *kv, ints(t), ints(np.zeros(B)), ints(rs), 130, mass_in=mass,
+                            mass_out=mass)
+    for step in range(5):
+        n = rng.integers(2, 13, B)
+        rs = np.concatenate([[0], np.cumsum(n)])
+        depth, sees = trees(rng, list(zip(ln, n)), back=back)
+        qkv, top = rows_of(rs[-1]), int(n.max())
+        say("masses of paths", step, ln, n)
+        q = foe.cache_append(qkv, *kv, ints(t1), ints(ln), ints(rs), THETA, SCALE,
+                             depth=ints(depth))
+        foe.cache_attention(q, *kv, ints(t1), ints(ln), ints(rs), top, depth=ints(depth),
+                            tree=pack(sees, 1))
+        path, keep = np.full((B, 25), -1), []
+        for b in range(B):
+            keep.append(np.nonzero(sees[rs[b] + int(rng.integers(n[b]))][:n[b]])[0])
+            if b == step % 4:       # (nothing is accepted)
+                keep[b] = keep[b][:0]
+            path[b, :len(keep[b])] = keep[b]
+        new = foe.cache_accept(*kv, ints(t1), ints(ln), ints(rs), ints(path))
+        m = [len(x) for x in keep]
+        rs2 = np.concatenate([[0], np.cumsum(m)])
+        rows = torch.from_numpy(np.concatenate([rs[b] + keep[b] for b in range(B)])).to(DEV)
+        foe.cache_attention(q[:, rows].contiguous(), *kv, ints(t1), ints(ln), ints(rs2), max(m),
+                            mass_in=mass, mass_out=mass)
+        q2 = foe.cache_append(qkv[:, rows].contiguous(), *kv, ints(t2), ints(ln), ints(rs2), THETA,
+                              SCALE)
+        foe.cache_attention(q2, *kv, ints(t2), ints(ln), ints(rs2), max(m), mass_in=mass,
+                            mass_out=mass)
+        torch.cuda.synchronize()
+        ln = host(new).astype(int)
+        both = [mass.cpu().numpy()[t].transpose(0, 2, 1, 3).reshape(B, H, -1) for t in (t1, t2)]
+        for b in range(B):
+            assert np.array_equal(both[0][b, :, :ln[b]], both[1][b, :, :ln[b]]), (step, b)
+            assert (both[0][b, :, :ln[b]] > 0).all()
+    kept = []
+    for t in (t1, t2):
+        got, _ = foe.cache_evict(*kv, mass.clone(), ints(t), ints(ln), 40, 8, dst_table=ints(fresh))
+        kept.append(got)
+    torch.cuda.synchronize()
+    assert torch.equal(kept[0], kept[1])
