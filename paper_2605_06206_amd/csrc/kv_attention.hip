@@ -2168,6 +2168,13 @@ constexpr int kFewLeast = 4;   // pages of a range at least: one for each wave
 // 5000 tokens, 8 groups: 22 22 26, with four 28 24 28.
 constexpr int kFullLeast = 2;
 constexpr int kManyLeast = 2;
+// Pages of the tables from which a shaped call of 65 to 128 columns whose other sequences have few
+// takes both forms: in the 128-column one each wave would form 128 columns of every sequence.  us
+// for one tree of 64 rows of two heads beside single rows, 8 groups, the 128-column form and both,
+// in brackets with the mass: 15 rows over 256 to 2000 tokens (4096 pages) 35 39 (55 52), over 256
+// to 8192 (16384) 63 62 (102 81), 63 rows over 256 to 2000 84 61 (133 82), over 256 to 8192 224 150
+// (354 202).  Of 32 rows (64 columns, with the 64-column form) 63 rows 144 147, 15 rows 40 59.
+constexpr long long kMixedPages = 16384;
 constexpr int kJoinParts = 24;  // parts up to which eight columns are joined by a workgroup
 // The scores of few columns are kept for the mass where the tables' room for them is up to
 // this many bytes of workspace; beyond, they are formed again.  us kept and formed again, 8
@@ -2193,14 +2200,16 @@ AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_
                    bool shaped) {
   AttnPlan p{};
   const long long most = (long long)max_rows * nq;
+  const long long pages = (long long)B * H * max_blocks;
   // Both forms where the sequences beside the longest have few columns on average (us for a
   // 512-row chunk beside 16 decoding sequences, with mass: 85, and 114 in the second form
   // alone); where they are all chunks the first would be a launch for nothing.
+  const bool mixed = B > 1 && (long long)(N - max_rows) * nq <= kFewCols * (B - 1LL);
   p.few_cols = kFewCols;
-  if (shaped && most <= kShapedCols)
+  if (shaped && most <= kShapedCols &&
+      !(mixed && most > kShapedCols / 2 && pages >= kMixedPages))
     while (p.few_cols < most) p.few_cols *= 2;
-  p.few.on =
-      most <= p.few_cols || (B > 1 && (long long)(N - max_rows) * nq <= kFewCols * (B - 1LL));
+  p.few.on = most <= p.few_cols || mixed;
   p.many.on = most > p.few_cols;
   p.few.hi = p.few_cols;
   p.many.lo = p.few.on ? p.few_cols : 0;
@@ -2213,7 +2222,6 @@ AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_
     take(f.prefix, (size_t)(B + 1) * 8);
     take(f.part, part_bytes);
   };
-  const long long pages = (long long)B * H * max_blocks;
   auto least_of = [](int few_cols) { return few_cols == kShapedCols ? kFullLeast : kFewLeast; };
   auto ranges_of = [&](int few_cols) {
     return (int)std::min<long long>((few_cols <= 32 ? 4LL : 2LL) * kCus,
@@ -2240,7 +2248,8 @@ AttnPlan attn_plan(int H, int B, int N, int nq, int hd, int max_blocks, int max_
       few_parts = std::max(few_parts,
                            parts_of(ranges_of(w), (int)std::min<long long>(w, most)));
   scratch(p.few, few_parts);
-  if (p.many.on) scratch(p.many, parts_of(p.many.ranges, p.many.cols));
+  if (most > (shaped ? kShapedCols / 2 : kFewCols))
+    scratch(p.many, parts_of(p.many.ranges, p.many.cols));
   if (mass) {
     take(p.stat, (size_t)H * N * nq * (shaped ? sizeof(Stat<Shape<true>>) : sizeof(Stat<NoShape>)));
     const size_t bytes = (size_t)pages * std::min<long long>(kFewCols, most) * kPage * 4;

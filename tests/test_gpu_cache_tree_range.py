@@ -1,6 +1,7 @@
 """Trees and other scores over the 8-bit cache at the borders of their forms: one workspace for
-batches of all widths, tables too wide for the scores to be kept for the mass, biases over long
-contexts by bounds that weigh each token, and the masses of accepted paths alone."""
+batches of all widths, tables too wide for the scores to be kept for the mass, one wide tree beside
+single rows, biases over long contexts by bounds that weigh each token, and the masses of accepted
+paths alone."""
 
 import numpy as np
 import pytest
@@ -133,6 +134,40 @@ def test_nan_rows_where_scores_are_formed_again(rows, more):
     sees[bad][:] = False
     pool["k"][p, :, (100 + bad) % 64] = 0
     check_shaped(pool, table, ctx, rs, q, out, None, rows=good, sees=sees, cap=9.0)
+
+
+@pytest.mark.parametrize("blocks", [1 << 13, 1 << 18])
+@pytest.mark.parametrize("H,nq,hd,seqs,what", [
+    (2, 2, 128, [(300, 1), (100, 64), (64, 1), (0, 8), (500, 1)], "tree"),
+    (2, 1, 96, [(0, 100), (700, 16), (63, 17), (1, 1), (90, 2), (400, 1)], "tree cap bias"),
+    (2, 2, 96, [(65, 33), (128, 1), (30, 2), (250, 5)], "cap prefix"),
+    (1, 9, 128, [(10, 1), (0, 0), (200, 14), (1500, 2)], "bias"),
+    (1, 64, 128, [(10, 2), (200, 0), (99, 0), (1500, 0), (3, 0)], "tree"),
+])
+def test_a_wide_tree_beside_few_columns(H, nq, hd, seqs, what, blocks):
+    """Calls of 65 to 128 columns whose other sequences have few, in tables that hold the pages
+    from which both forms are taken."""
+    say("wide beside few", H, nq, hd, seqs, what, blocks)
+    rng = np.random.default_rng([56, H, nq, hd, len(seqs), len(what)])
+    ctx, rs, table, pages = batch(rng, seqs)
+    pool = random_pool(rng, pages, H, hd)
+    depth, sees = trees(rng, seqs)
+    a = {}
+    if "cap" in what:
+        a["cap"] = 8.0
+    if "bias" in what:
+        a["slope"] = slopes(rng, H, nq)
+    if "prefix" in what:
+        a["prefix"] = [int(rng.integers(0, c + n + 30)) for c, n in seqs]
+    if "tree" in what:
+        a.update(sees=sees, depth=depth)
+    q = bf16(1.5 * rng.normal(size=(H, rs[-1], nq, hd)))
+    top = max(n for _, n in seqs)
+    assert 64 < top * nq <= 128 and (rs[-1] - top) * nq <= 16 * (len(seqs) - 1)
+    assert len(seqs) * H * blocks >= 16384
+    for mass in (False, True):
+        out, m = run_shaped(pool, wide(table)[:, :blocks].copy(), ctx, rs, q, top, mass, **a)
+        check_shaped(pool, table, ctx, rs, q, out, m, **a)
 
 
 def weighed(pool, table, ctx, q, slope, cap=0.0, depth=None, sees=None):
